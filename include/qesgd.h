@@ -81,7 +81,11 @@ enum {
     QESGD_ERR_BITS = -11,      /* b not in {2,4,8,16}                                  */
     QESGD_ERR_DELTA = -12,     /* delta not a positive finite number                   */
     QESGD_ERR_ROUNDS = -13,    /* rounds == 0                                          */
-    QESGD_ERR_SCRATCH = -14    /* the shape needs more than QESGD_NOALLOC_SCRATCH_BYTES */
+    QESGD_ERR_SCRATCH = -14,   /* the shape needs more than QESGD_NOALLOC_SCRATCH_BYTES */
+    QESGD_ERR_DTYPE = -15,     /* dtype not QESGD_F32, QESGD_BF16 or QESGD_F16         */
+    QESGD_ERR_MODE = -16,      /* mode not QESGD_MX4_NEAREST or QESGD_MX4_STOCHASTIC   */
+    QESGD_ERR_STEPS = -17,     /* steps == 0 or steps > QESGD_MAX_STEPS                */
+    QESGD_ERR_COEFF = -18      /* a coefficient, eps, alpha or mu not finite, eps < 0  */
 };
 
 enum { QESGD_NORM_L2 = 0, QESGD_NORM_MAX = 1 };
@@ -222,6 +226,90 @@ int qesgd_dequantize_fixed_update(const void* codes, uint64_t d, float delta, ui
 /* End of an epoch (Alg. 3, last step; equal to Alg. 2's mean of the iterates u_{t,k}):
  * w_i += zsum_i / rounds, then zsum_i = 0 for the next epoch (z starts again at 0). */
 int qesgd_epoch_commit(float* w_inout, float* zsum_inout, uint32_t rounds, uint64_t d, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Parameters that are matrices: 4-bit microscaled codes, the product of two packed matrices, and
+ * the orthogonalised update.  A round of a matrix parameter: the workers run their layer on packed
+ * operands (qesgd_mx4_product), send packed gradients (qesgd_mx4_quantize_pack), the server takes
+ * their mean (qesgd_mx4_unpack_aggregate_update) and orthogonalises it (qesgd_orthogonal_update).
+ * ------------------------------------------------------------------------- */
+
+enum { QESGD_F32 = 0, QESGD_BF16 = 1, QESGD_F16 = 2 };              /* element types */
+enum { QESGD_MX4_NEAREST = 0, QESGD_MX4_STOCHASTIC = 1 };
+#define QESGD_MAX_STEPS 32u
+
+/* Packed 4-bit form of a matrix [rows, cols].  A row is padded with zeros to `wide`, the next
+ * multiple of 128 columns, and cut into blocks of 32.  Block: one byte e + 127 (e = -127 .. 125) and 32
+ * elements of 4 bits, sign and magnitude 0 .5 1 1.5 2 3 4 6 (codes 0..7); element value =
+ * +-magnitude * 2^e.  Byte 255 marks a block that holds a NaN or an infinity: all of it reads as NaN.
+ * Two elements a byte, the even column in the low half.
+ *     uint8_t codes [rows][wide/2]      at codes_off (= 0)
+ *     uint8_t scales[rows][wide/32]     at scales_off (a multiple of 256)
+ * A vector is a matrix of one row. */
+typedef struct qesgd_mx4_layout {
+    uint64_t rows, cols;
+    uint64_t row_codes;        /* wide/2: bytes of a row of codes                       */
+    uint64_t row_scales;       /* wide/32: bytes of a row of scales                     */
+    uint64_t codes_off;
+    uint64_t scales_off;
+    uint64_t bytes;            /* of the packed block, a multiple of 256                */
+    uint64_t payload_bytes;    /* rows * (row_codes + row_scales)                       */
+} qesgd_mx4_layout;
+
+/* Host only.  QESGD_ERR_DIM: a side is 0, or rows * wide > 2^38. */
+int qesgd_mx4_layout_query(uint64_t rows, uint64_t cols, qesgd_mx4_layout* out);
+
+/* Quantises K workers' matrices, worker k's at x + k*x_stride, rows ld apart (both in elements; any ld >= cols,
+ * x aligned to its element).  ld matters from two rows on, the strides from two workers on.
+ *   mode  QESGD_MX4_NEAREST: e = floor(log2(max|v|)) - 2, elements to nearest even, |v| > 6 * 2^e to 6.
+ *         QESGD_MX4_STOCHASTIC: the smallest e with max|v| <= 6 * 2^e (at most 125), elements to one of
+ *         the two neighbours as qesgd_quantize_pack rounds: up iff r + trunc(f * 2^16) >= 2^16, f the
+ *         fraction of the way and r the variate of coordinate row*wide + column for (seed, round,
+ *         worker + k); unbiased to 2^-16 of a step.
+ *   packed    nullable: K blocks of qesgd_mx4_layout_query(rows, cols), packed_stride bytes apart (a multiple of 256).
+ *   packed_t  nullable: the same of the transposed matrices, layout (cols, rows), blocks along the
+ *         columns of x; equal to quantising a transposed copy.  Both come from one read of x: a
+ *         layer's gradients need its operands along either side.  One of the two must be given. */
+int qesgd_mx4_quantize_pack(const void* x, uint32_t dtype, uint64_t ld, uint64_t x_stride, uint64_t rows, uint64_t cols,
+                            uint32_t K, uint32_t mode, uint64_t seed, uint32_t round, uint32_t worker,
+                            void* packed, uint64_t packed_stride, void* packed_t, uint64_t packed_t_stride, void* stream);
+
+/* Server side: zbar = (sum_k q_k) / K, workers added in order from +0; u = w + zbar; zsum += zbar.  The vectors are
+ * [rows*cols] without padding.  zbar_out, (w_snap, u_out) and zsum_inout are each optional, at least
+ * one output must be given; K = 1 with zbar_out alone decodes.  u_out may alias w_snap. */
+int qesgd_mx4_unpack_aggregate_update(const void* packed_slab, uint64_t packed_stride, uint32_t K, uint64_t rows, uint64_t cols,
+                                      const float* w_snap, float* zbar_out, float* u_out, float* zsum_inout, void* stream);
+
+/* C[i, j] = sum_k A[i, k] B[j, k] of two packed matrices, layouts (M, K) and (N, K); products are exact, sums
+ * in fp32, C [M, N] in dtype with rows ldc elements apart, rounded once.  M, N, K in [1, 2^20].  A block that
+ * reads as NaN makes its row (column) of C NaN.  Forward pass of a layer: A = activations [tokens, in], B = weights
+ * [out, in]; gradients: A = dy, B = the weights' transposed form; A = dy's transposed form, B = the activations'.
+ * workspace: qesgd_mx4_product_workspace_bytes(M, N, K), 16-byte aligned; may be NULL when that is 0. */
+size_t qesgd_mx4_product_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
+int qesgd_mx4_product(const void* a_packed, const void* b_packed, uint64_t M, uint64_t N, uint64_t K, void* c, uint32_t dtype,
+                      uint64_t ldc, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Orthogonalises n matrices x [n, rows, cols] by `steps` odd polynomials of degree five: X = x / (||x||_F + eps),
+ * then X = (a I + b G + c G^2) X with G = X X^T (X^T X on the longer side), (a, b, c) = coeffs[3*i .. 3*i+2] (host
+ * memory, read during the call); out = X.  Singular values s become p_steps(.. p_1(s)), p(s) = a s + b s^3 + c s^5;
+ * singular vectors stay.  Norms in fp64, products of fp32 accuracy (each operand as the sum of two fp16
+ * numbers, sums in fp32).  |coefficients| must keep every iterate's and polynomial's entries below 16
+ * (singular values that stay near 1 do); beyond that the result is infinite or NaN.  A matrix of zeros gives zeros.
+ *   out  same type and shape as x, may be x itself.
+ *   workspace  qesgd_orthogonalize_workspace_bytes(rows, cols, n), 256-byte aligned.  rows, cols <= 2^20, n <= 65535. */
+size_t qesgd_orthogonalize_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n);
+int qesgd_orthogonalize(const void* x, uint32_t dtype, uint64_t rows, uint64_t cols, uint32_t n, const float* coeffs, uint32_t steps,
+                        float eps, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The server's step on n matrix parameters of one shape, all fp32 [n, rows, cols]:
+ *   m = mu*m + g;  x = nesterov ? g + mu*m : m   (momentum_inout NULL: x = g)
+ *   step = alpha * orthogonalised x;  z += step;  u = w + z;  zsum += z
+ * as the update of qesgd_gradient_round.  step_out, z_inout, (w_snap, u_out) and zsum_inout are each optional; one of
+ * step_out and z_inout must be given, and u_out and zsum_inout need z_inout.  g may not alias an output; u_out may alias w_snap. */
+int qesgd_orthogonal_update(const float* g, uint64_t rows, uint64_t cols, uint32_t n, float* momentum_inout, float mu, uint32_t nesterov,
+                            const float* coeffs, uint32_t steps, float eps, float alpha, float* step_out, float* z_inout,
+                            const float* w_snap, float* u_out, float* zsum_inout, void* workspace, size_t workspace_bytes,
+                            void* stream);
 
 const char* qesgd_strerror(int code);
 /* hipError_t (as int) of the last failed launch on the calling thread, 0 if none. */

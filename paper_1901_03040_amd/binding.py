@@ -24,7 +24,11 @@ OK = 0
 ERR_NULL, ERR_DIM, ERR_LEVELS, ERR_BUCKET, ERR_WORKERS = -1, -2, -3, -4, -5
 ERR_NORM_KIND, ERR_ALIGN, ERR_STRIDE, ERR_WORKSPACE, ERR_HIP = -6, -7, -8, -9, -10
 ERR_BITS, ERR_DELTA, ERR_ROUNDS, ERR_SCRATCH = -11, -12, -13, -14
+ERR_DTYPE, ERR_MODE, ERR_STEPS, ERR_COEFF = -15, -16, -17, -18
 NOALLOC_SCRATCH_BYTES = 4 << 20
+MX4_NEAREST, MX4_STOCHASTIC = 0, 1
+MAX_STEPS = 32
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 class QesgdError(RuntimeError):
@@ -50,6 +54,23 @@ class Layout:
     signs_off: int
     levels_off: int
     bytes_per_worker: int
+    payload_bytes: int
+
+
+class _Mx4Layout(C.Structure):
+    _fields_ = [(n, C.c_uint64) for n in ("rows", "cols", "row_codes", "row_scales", "codes_off", "scales_off", "bytes",
+                                          "payload_bytes")]
+
+
+@dataclass(frozen=True)
+class Mx4Layout:
+    rows: int
+    cols: int
+    row_codes: int
+    row_scales: int
+    codes_off: int
+    scales_off: int
+    bytes: int
     payload_bytes: int
 
 
@@ -93,6 +114,23 @@ def lib():
         L.qesgd_dequantize_fixed_update.restype = C.c_int
         L.qesgd_epoch_commit.argtypes = [vp, vp, u32, u64, vp]
         L.qesgd_epoch_commit.restype = C.c_int
+        f32 = C.c_float
+        L.qesgd_mx4_layout_query.argtypes = [u64, u64, C.POINTER(_Mx4Layout)]
+        L.qesgd_mx4_layout_query.restype = C.c_int
+        L.qesgd_mx4_quantize_pack.argtypes = [vp, u32, u64, u64, u64, u64, u32, u32, u64, u32, u32, vp, u64, vp, u64, vp]
+        L.qesgd_mx4_quantize_pack.restype = C.c_int
+        L.qesgd_mx4_unpack_aggregate_update.argtypes = [vp, u64, u32, u64, u64, vp, vp, vp, vp, vp]
+        L.qesgd_mx4_unpack_aggregate_update.restype = C.c_int
+        L.qesgd_mx4_product_workspace_bytes.argtypes = [u64, u64, u64]
+        L.qesgd_mx4_product_workspace_bytes.restype = sz
+        L.qesgd_mx4_product.argtypes = [vp, vp, u64, u64, u64, vp, u32, u64, vp, sz, vp]
+        L.qesgd_mx4_product.restype = C.c_int
+        L.qesgd_orthogonalize_workspace_bytes.argtypes = [u64, u64, u32]
+        L.qesgd_orthogonalize_workspace_bytes.restype = sz
+        L.qesgd_orthogonalize.argtypes = [vp, u32, u64, u64, u32, vp, u32, f32, vp, vp, sz, vp]
+        L.qesgd_orthogonalize.restype = C.c_int
+        L.qesgd_orthogonal_update.argtypes = [vp, u64, u64, u32, vp, f32, u32, vp, u32, f32, f32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.qesgd_orthogonal_update.restype = C.c_int
         L.qesgd_strerror.argtypes = [C.c_int]
         L.qesgd_strerror.restype = C.c_char_p
         L.qesgd_last_hip_error.argtypes = []
@@ -216,6 +254,77 @@ def qesgd_epoch_commit(w_inout, zsum_inout, rounds, d, stream=None):
            "qesgd_epoch_commit")
 
 
+# ---- matrix parameters ------------------------------------------------------
+
+def _dtype(t: torch.Tensor, where: str) -> int:
+    code = DTYPES.get(t.dtype)
+    if code is None:
+        raise QesgdError(ERR_DTYPE, where)
+    return code
+
+
+def _ws(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def qesgd_mx4_layout_query(rows: int, cols: int) -> Mx4Layout:
+    out = _Mx4Layout()
+    _check(lib().qesgd_mx4_layout_query(int(rows), int(cols), C.byref(out)), "qesgd_mx4_layout_query")
+    return Mx4Layout(*(getattr(out, n) for n, _ in _Mx4Layout._fields_))
+
+
+def qesgd_mx4_quantize_pack(x, ld, x_stride, rows, cols, K, mode, seed, rnd, packed, packed_stride, packed_t=None,
+                            packed_t_stride=0, worker=0, stream=None):
+    _check(lib().qesgd_mx4_quantize_pack(_ptr(x), _dtype(x, "qesgd_mx4_quantize_pack"), int(ld), int(x_stride), int(rows), int(cols),
+                                         int(K), int(mode), int(seed), int(rnd), int(worker), _ptr(packed), int(packed_stride),
+                                         _ptr(packed_t), int(packed_t_stride), _stream(stream)), "qesgd_mx4_quantize_pack")
+
+
+def qesgd_mx4_unpack_aggregate_update(packed_slab, packed_stride, K, rows, cols, w_snap, zbar_out, u_out, zsum_inout,
+                                      stream=None):
+    _check(lib().qesgd_mx4_unpack_aggregate_update(_ptr(packed_slab), int(packed_stride), int(K), int(rows), int(cols),
+                                                   _ptr(w_snap), _ptr(zbar_out), _ptr(u_out), _ptr(zsum_inout),
+                                                   _stream(stream)), "qesgd_mx4_unpack_aggregate_update")
+
+
+def qesgd_mx4_product_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib().qesgd_mx4_product_workspace_bytes(int(M), int(N), int(K)))
+
+
+def qesgd_mx4_product(a_packed, b_packed, M, N, K, c, ldc, workspace=None, stream=None):
+    _check(lib().qesgd_mx4_product(_ptr(a_packed), _ptr(b_packed), int(M), int(N), int(K), _ptr(c),
+                                   _dtype(c, "qesgd_mx4_product"), int(ldc), *_ws(workspace), _stream(stream)),
+           "qesgd_mx4_product")
+
+
+def _coeffs(coeffs):
+    """(a, b, c) of every step as a C array."""
+    flat = [float(v) for step in coeffs for v in step]
+    if len(flat) != 3 * len(coeffs):
+        raise ValueError("coeffs: three numbers for each step")
+    return (C.c_float * len(flat))(*flat)
+
+
+def qesgd_orthogonalize_workspace_bytes(rows: int, cols: int, n: int) -> int:
+    return int(lib().qesgd_orthogonalize_workspace_bytes(int(rows), int(cols), int(n)))
+
+
+def qesgd_orthogonalize(x, rows, cols, n, coeffs, eps, out, workspace, stream=None):
+    if out.dtype != x.dtype:
+        raise QesgdError(ERR_DTYPE, "qesgd_orthogonalize")
+    _check(lib().qesgd_orthogonalize(_ptr(x), _dtype(x, "qesgd_orthogonalize"), int(rows), int(cols), int(n), _coeffs(coeffs),
+                                     len(coeffs), float(eps), _ptr(out), *_ws(workspace), _stream(stream)),
+           "qesgd_orthogonalize")
+
+
+def qesgd_orthogonal_update(g, rows, cols, n, momentum_inout, mu, nesterov, coeffs, eps, alpha, step_out, z_inout, w_snap,
+                            u_out, zsum_inout, workspace, stream=None):
+    _check(lib().qesgd_orthogonal_update(_ptr(g), int(rows), int(cols), int(n), _ptr(momentum_inout), float(mu),
+                                         int(bool(nesterov)), _coeffs(coeffs), len(coeffs), float(eps), float(alpha),
+                                         _ptr(step_out), _ptr(z_inout), _ptr(w_snap), _ptr(u_out), _ptr(zsum_inout),
+                                         *_ws(workspace), _stream(stream)), "qesgd_orthogonal_update")
+
+
 def qesgd_abi_version() -> int:
     return int(lib().qesgd_abi_version())
 
@@ -239,3 +348,15 @@ def planes(packed_row: torch.Tensor, lay: Layout):
     signs = packed_row[lay.signs_off: lay.signs_off + 4 * lay.sign_words].view(torch.int32)
     levels = packed_row[lay.levels_off: lay.levels_off + 4 * lay.level_words].view(torch.int32)
     return norms, signs, levels
+
+
+def alloc_mx4(lay: Mx4Layout, K: Optional[int] = None, device="cuda") -> torch.Tensor:
+    """[bytes] or [K, bytes] uint8 for the packed 4-bit form, 256-byte aligned."""
+    t = torch.empty((lay.bytes,) if K is None else (K, lay.bytes), dtype=torch.uint8, device=device)
+    assert t.data_ptr() % 256 == 0
+    return t
+
+
+def alloc_workspace(n_bytes: int, device="cuda") -> Optional[torch.Tensor]:
+    """Device scratch of that many bytes, None for none."""
+    return torch.empty(n_bytes, dtype=torch.uint8, device=device) if n_bytes else None

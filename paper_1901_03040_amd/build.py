@@ -14,7 +14,8 @@ LIB = os.path.join(HERE, "libqesgd.so")
 OBJDIR = os.path.join(HERE, "_build")
 SOURCES = ["qesgd_api.cpp", "qesgd_quantize.hip", "qesgd_aggregate.hip", "qesgd_fixed.hip", "qesgd_round.hip",
            "qesgd_round_1_2.hip", "qesgd_round_3_5.hip", "qesgd_round_6_7.hip",
-           "qesgd_round_4.hip", "qesgd_round_8.hip", "qesgd_round_16.hip"]
+           "qesgd_round_4.hip", "qesgd_round_8.hip", "qesgd_round_16.hip",
+           "qesgd_matrix_api.cpp", "qesgd_mx4.hip", "qesgd_mx4_product.hip", "qesgd_orthogonalize.hip"]
 PROBE_SRC = "bench_probe.hip"
 PROBE_LIB = os.path.join(HERE, "libqesgd_bench_probe.so")
 

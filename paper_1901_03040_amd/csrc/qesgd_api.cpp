@@ -314,6 +314,10 @@ const char* qesgd_strerror(int code) {
         case QESGD_ERR_DELTA: return "delta must be a positive finite number";
         case QESGD_ERR_ROUNDS: return "rounds must be at least 1";
         case QESGD_ERR_SCRATCH: return "shape needs more scratch than the no-allocation entry point holds (4 MiB)";
+        case QESGD_ERR_DTYPE: return "dtype must be 0 (f32), 1 (bf16) or 2 (f16)";
+        case QESGD_ERR_MODE: return "mode must be 0 (nearest) or 1 (stochastic)";
+        case QESGD_ERR_STEPS: return "steps must be in [1, 32]";
+        case QESGD_ERR_COEFF: return "coefficients, eps, alpha and mu must be finite, eps not negative";
         default: return "unknown error code";
     }
 }

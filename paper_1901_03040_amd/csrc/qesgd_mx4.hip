@@ -1,0 +1,450 @@
+// The microscaled 4-bit form of matrices: quantisation along the rows, along the columns or both from one read,
+// and its inverse fused with the mean over the workers and the update.
+//
+// Block of 32 coordinates with largest magnitude m: scale 2^e, element q of {0, .5, 1, 1.5, 2, 3, 4, 6} with a sign.
+//   nearest     e = floor(log2 m) - 2, q = |v| / 2^e to nearest even, at most 6
+//   stochastic  e = the smallest with m <= 6 * 2^e, q one of the two neighbours of a = |v| / 2^e: up iff r + T >= 2^16,
+//               T = trunc(f * 2^16), f the fraction of the way; E[q] = a to 2^-16 of a step
+// a is exact (a power of two only moves the exponent; what falls below fp32's range is far below the grid).
+#include <type_traits>
+
+#include "qesgd_device.h"
+#include "qesgd_matrix.h"
+
+namespace qesgd {
+namespace {
+
+typedef uint32_t uvec4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uvec2 __attribute__((ext_vector_type(2)));
+typedef float fvec2 __attribute__((ext_vector_type(2)));
+// 128-bit accesses at any element's address: the rows of a matrix start where they start
+typedef uvec4 uvec4_any __attribute__((aligned(2)));
+typedef vec4 vec4_any __attribute__((aligned(4)));
+
+// Byte e + 127 of a block from the bits of its largest magnitude; 255 where that is infinite or a NaN.  The exponent field
+// less 2 is floor(log2 m) - 2 + 127; adding 0x3FFFFF first carries into it iff the significand is over 1.5, i.e. m > 6 * 2^e.
+// Subnormal m, and zero, end at e = -127; e = 126 (m > 1.5 * 2^127, stochastic) is held at 125, where 6 is the end of the range.
+template <bool STOCHASTIC>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+    const int32_t e = (int32_t)((top + (STOCHASTIC ? 0x3FFFFFu : 0u)) >> 23) - 2;
+    const uint32_t b = (uint32_t)(e < 0 ? 0 : e > 252 ? 252 : e);
+    return top >= 0x7F800000u ? 255u : b;
+}
+
+// Codes of eight coordinates that share the scale byte sb, as one word.  `group`: number of their Philox call.
+template <bool STOCHASTIC>
+__device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t sb, uint64_t group, uint32_t worker, uint32_t round,
+                                            uint32_t key0, uint32_t key1) {
+    uint32_t word = 0;
+    if (!STOCHASTIC) {
+        // the conversion divides by the power of two in its scale's exponent field, rounds to nearest even and ends at 6
+        const float scale = __uint_as_float(sb << 23);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[0], v[1], scale, 0);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[2], v[3], scale, 1);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[4], v[5], scale, 2);
+        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[6], v[7], scale, 3);
+    } else {
+        uint32_t rnd[4];
+        philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), worker, round, key0, key1, rnd);
+        const float inv = __uint_as_float((254u - sb) << 23);              // 2^-e
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t r = variate16(rnd, i);
+            const float a = __builtin_fabsf(v[i]) * inv;
+            // from 1 on the code is the exponent and the first bit of the significand, and T its next 16 bits: adding r there
+            // carries into the code iff r + T >= 2^16; below, the grid is a multiple of 1/2
+            const uint32_t high = ((__float_as_uint(a) + (r << 6)) >> 22) - 252u;
+            const uint32_t low = ((uint32_t)(a * 131072.0f) + r) >> 16;
+            const uint32_t q = min(a < 1.0f ? low : high, 7u);
+            word |= (q | (__float_as_uint(v[i]) >> 31 << 3)) << (4 * i);
+        }
+    }
+    return sb == 255u ? 0u : word;
+}
+
+template <uint32_t DT>
+__device__ __forceinline__ float widen(uint32_t half) {
+    if (DT == QESGD_BF16) return __uint_as_float(half << 16);
+    return (float)__builtin_bit_cast(_Float16, (unsigned short)half);
+}
+
+template <uint32_t DT>
+__device__ __forceinline__ void widen8(uvec4 w, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = DT == QESGD_BF16 ? __uint_as_float(w[i] << 16) : widen<DT>(w[i] & 0xFFFFu);
+        v[2 * i + 1] = DT == QESGD_BF16 ? __uint_as_float(w[i] & 0xFFFF0000u) : widen<DT>(w[i] >> 16);
+    }
+}
+
+// Eight consecutive elements from element `at` on, of which the first n (0..8) exist; the others are 0.
+template <uint32_t DT>
+__device__ __forceinline__ void load8(const void* x, uint64_t at, uint32_t n, float (&v)[8]) {
+    if (DT == QESGD_F32) {
+        const float* p = (const float*)x + at;
+        if (n == 8) {
+            const vec4 a = *(const vec4_any*)p, b = *(const vec4_any*)(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+        }
+    } else {
+        const unsigned short* p = (const unsigned short*)x + at;
+        if (n == 8) {
+            const uvec4 w = *(const uvec4_any*)p;
+            widen8<DT>(w, v);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) v[i] = i < n ? widen<DT>(p[i]) : 0.0f;
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t top8(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);    // as integers: a NaN counts as the largest
+    return m;
+}
+// Over the four lanes of a quad, which share a block.
+__device__ __forceinline__ uint32_t quad_max(uint32_t m) {
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, false));
+    return max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, false));
+}
+// The four quads of a row of 16 lanes: their bytes as one word, in every lane.
+__device__ __forceinline__ uint32_t row_bytes(uint32_t byte, uint32_t lane) {
+    uint32_t w = byte << (8u * ((lane >> 2) & 3u));
+    w |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x124, 0xF, 0xF, false);   // row_ror:4
+    w |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x128, 0xF, 0xF, false);   // row_ror:8
+    return w;
+}
+
+struct QParams {
+    const void* x;
+    uint64_t ld, x_stride, rows, cols;
+    uint64_t slots;                   // rows * wide
+    uint32_t groups;                  // wide / 128
+    uint32_t groups_t;                // the same of the transposed form
+    unsigned char* packed;
+    uint64_t packed_stride, scales_off;
+    unsigned char* packed_t;
+    uint64_t packed_t_stride, scales_t_off;
+    uint32_t key0, key1, round, worker0;
+    uint32_t xcd_group;
+};
+
+// Slots: the padded matrix, row after row.  A lane owns 8 consecutive ones (one Philox call, one word of codes), a quad a block,
+// a wave 512.  FLAT: the matrix is one row (a vector, or rows that need no padding and follow one another).
+constexpr uint32_t kQWaves = 4;
+
+template <uint32_t DT, bool STOCHASTIC, bool FLAT>
+__global__ void __launch_bounds__(kQWaves * 64) k_mx4_quantize(const QParams p) {
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint64_t slot0 = ((uint64_t)xcd_tile(blockIdx.x, gridDim.x, p.xcd_group) * kQWaves + (threadIdx.x >> 6)) * kChunk;
+    const uint64_t slot = slot0 + lane * kLaneElems;
+    if (slot0 >= p.slots) return;
+    const uint32_t k = blockIdx.y;
+    const uint64_t x0 = (uint64_t)k * p.x_stride;
+    float v[8];
+    if (FLAT && slot0 + kChunk <= p.cols) {
+        if (DT == QESGD_F32 && (((uintptr_t)p.x | (p.x_stride << 2)) & 15u) == 0) {
+            vec4 a[1], b[1];
+            load_halves_as<1, false>((const float*)p.x + x0 + slot0 + half_offset(lane), a, b);
+            halves_to_lane(a[0], b[0], v);
+        } else {
+            load8<DT>(p.x, x0 + slot, 8u, v);
+        }
+    } else {
+        uint64_t row = 0, col = slot;
+        if (!FLAT) {
+            const uint32_t g = (uint32_t)(slot >> 7);
+            row = g / p.groups;
+            col = (uint64_t)(g - (uint32_t)row * p.groups) * 128u + (slot & 127u);
+        }
+        const uint32_t n = slot >= p.slots || col >= p.cols ? 0u : p.cols - col < 8 ? (uint32_t)(p.cols - col) : 8u;
+        load8<DT>(p.x, x0 + row * p.ld + col, n, v);
+    }
+    const uint32_t sb = scale_byte<STOCHASTIC>(quad_max(top8(v)));
+    const uint32_t word = encode8<STOCHASTIC>(v, sb, slot >> 3, p.worker0 + k, p.round, p.key0, p.key1);
+    const uint32_t scales = row_bytes(sb, lane);
+    if (slot < p.slots) {                                      // slots come in 128s: a row of lanes is in or out
+        unsigned char* out = p.packed + (uint64_t)k * p.packed_stride;
+        *(uint32_t*)(out + (slot >> 1)) = word;
+        if ((lane & 15u) == 0) *(uint32_t*)(out + p.scales_off + (slot >> 5)) = scales;
+    }
+}
+
+// Both forms, or the transposed one alone, of a 128 x 128 tile.  The rows' form is made while the tile is read (a wave takes four
+// rows at a time, a quad a block); the raw elements go to LDS, and then a lane takes 32 rows of one column.
+constexpr uint32_t kTile = 128;
+
+template <uint32_t DT, bool STOCHASTIC>
+__global__ void __launch_bounds__(256) k_mx4_quantize_both(const QParams p) {
+    typedef typename std::conditional<DT == QESGD_F32, float, unsigned short>::type elem;
+    // 32 rows, then 64 bytes of room: the four blocks of a column that a quad reads at once lie in different banks
+    constexpr uint32_t kRoom = 64 / sizeof(elem);
+    __shared__ __attribute__((aligned(16))) elem tile[kTile * kTile + 4 * kRoom];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, k = blockIdx.y;
+    const uint32_t tr = blockIdx.x / p.groups, tc = blockIdx.x - tr * p.groups;
+    const uint64_t r0 = (uint64_t)tr * kTile, c0 = (uint64_t)tc * kTile;
+    const uint64_t x0 = (uint64_t)k * p.x_stride;
+    const uint32_t col = (lane & 15u) * 8u;
+    const uint32_t n = c0 + col >= p.cols ? 0u : p.cols - c0 - col < 8 ? (uint32_t)(p.cols - c0 - col) : 8u;
+#pragma unroll 4
+    for (uint32_t i = 0; i < 8; ++i) {
+        const uint32_t r = i * 16u + wave * 4u + (lane >> 4);
+        const uint64_t row = r0 + r;
+        float v[8];
+        load8<DT>(p.x, x0 + row * p.ld + c0 + col, row < p.rows ? n : 0u, v);
+        elem* to = tile + r * kTile + (r >> 5) * kRoom + col;
+        if constexpr (DT == QESGD_F32) {
+            *(vec4*)to = vec4{v[0], v[1], v[2], v[3]};
+            *(vec4*)(to + 4) = vec4{v[4], v[5], v[6], v[7]};
+        } else {
+            uvec4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (DT == QESGD_BF16) w[j] = (__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xFFFF0000u);
+                else w[j] = (uint32_t)__builtin_bit_cast(unsigned short, (_Float16)v[2 * j]) |
+                            ((uint32_t)__builtin_bit_cast(unsigned short, (_Float16)v[2 * j + 1]) << 16);
+            }
+            *(uvec4*)to = w;
+        }
+        if (p.packed) {
+            const uint64_t slot = row * ((uint64_t)p.groups * 128u) + c0 + col;
+            const uint32_t sb = scale_byte<STOCHASTIC>(quad_max(top8(v)));
+            const uint32_t word = encode8<STOCHASTIC>(v, sb, slot >> 3, p.worker0 + k, p.round, p.key0, p.key1);
+            const uint32_t scales = row_bytes(sb, lane);
+            if (row < p.rows) {
+                unsigned char* out = p.packed + (uint64_t)k * p.packed_stride;
+                *(uint32_t*)(out + (slot >> 1)) = word;
+                if ((lane & 15u) == 0) *(uint32_t*)(out + p.scales_off + (slot >> 5)) = scales;
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t block = lane & 3u;
+#pragma unroll 1
+    for (uint32_t i = 0; i < 2; ++i) {
+        const uint32_t c = i * 64u + wave * 16u + (lane >> 2);
+        const elem* from = tile + block * (32u * kTile + kRoom) + c;
+        float v[4][8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (DT == QESGD_F32) v[j][e] = from[(j * 8 + e) * kTile];
+                else v[j][e] = widen<DT>(from[(j * 8 + e) * kTile]);
+            }
+            top = max(top, top8(v[j]));
+        }
+        const uint32_t sb = scale_byte<STOCHASTIC>(top);
+        const uint64_t slot = (c0 + c) * ((uint64_t)p.groups_t * 128u) + r0 + block * 32u;
+        uvec4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            w[j] = encode8<STOCHASTIC>(v[j], sb, (slot >> 3) + j, p.worker0 + k, p.round, p.key0, p.key1);
+        uint32_t scales = sb << (8u * block);
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0xB1, 0xF, 0xF, false);
+        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x4E, 0xF, 0xF, false);
+        if (c0 + c < p.cols) {
+            unsigned char* out = p.packed_t + (uint64_t)k * p.packed_t_stride;
+            *(uvec4*)(out + (slot >> 1)) = w;
+            if (block == 0) *(uint32_t*)(out + p.scales_t_off + (slot >> 5)) = scales;
+        }
+    }
+}
+
+struct AParams {
+    const unsigned char* packed;
+    uint64_t packed_stride, scales_off;
+    uint64_t slots, cols;
+    uint32_t groups, K;
+    const float* w;
+    float* zbar;
+    float* u;
+    float* zsum;
+    float inv_k, k;
+    bool pow2;
+    uint32_t xcd_group;
+};
+
+// A lane owns 8 slots again: a word of codes and a scale byte per worker, decoded by the conversion that multiplies by a power of
+// two (exact); workers are added in order from +0.
+template <bool FLAT>
+__global__ void __launch_bounds__(256) k_mx4_aggregate_update(const AParams p) {
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint64_t slot0 = ((uint64_t)xcd_tile(blockIdx.x, gridDim.x, p.xcd_group) * 4u + (threadIdx.x >> 6)) * kChunk;
+    const uint64_t slot = slot0 + lane * kLaneElems;
+    if (slot >= p.slots) return;
+    uint64_t at = slot;
+    uint32_t n = 8;
+    const bool whole = FLAT && slot0 + kChunk <= p.cols;       // uniform
+    if (!whole) {
+        uint64_t row = 0, col = slot;
+        if (!FLAT) {
+            const uint32_t g = (uint32_t)(slot >> 7);
+            row = g / p.groups;
+            col = (uint64_t)(g - (uint32_t)row * p.groups) * 128u + (slot & 127u);
+        }
+        n = col >= p.cols ? 0u : p.cols - col < 8 ? (uint32_t)(p.cols - col) : 8u;
+        at = row * p.cols + col;
+    }
+    const unsigned char* codes = p.packed + (slot >> 1);
+    const unsigned char* scales = p.packed + p.scales_off + (slot >> 5);
+    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    uint32_t k = 0;
+    auto add = [&](uint32_t word, uint32_t byte) {
+        const float s = __uint_as_float(byte << 23);            // the conversion reads the exponent field; 255 gives NaN
+        const fvec2 q0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 0), q1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 1);
+        const fvec2 q2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 2), q3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, s, 3);
+        acc[0] += q0[0]; acc[1] += q0[1]; acc[2] += q1[0]; acc[3] += q1[1];
+        acc[4] += q2[0]; acc[5] += q2[1]; acc[6] += q3[0]; acc[7] += q3[1];
+    };
+    for (; k + 4 <= p.K; k += 4) {
+        uint32_t word[4], byte[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            word[j] = *(const uint32_t*)(codes + (k + j) * p.packed_stride);
+            byte[j] = scales[(k + j) * p.packed_stride];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) add(word[j], byte[j]);
+    }
+    for (; k < p.K; ++k) add(*(const uint32_t*)(codes + k * p.packed_stride), scales[k * p.packed_stride]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = p.pow2 ? acc[i] * p.inv_k : acc[i] / p.k;
+
+    if (whole) {
+        const uint64_t h = slot0 + half_offset(lane);
+        vec4 za, zb;
+        lane_to_halves(acc, za, zb);
+        if (p.zbar) { store_stream(p.zbar + h, za); store_stream(p.zbar + h + kChunk / 2, zb); }
+        if (p.u) {
+            store_stream(p.u + h, load_stream(p.w + h) + za);
+            store_stream(p.u + h + kChunk / 2, load_stream(p.w + h + kChunk / 2) + zb);
+        }
+        if (p.zsum) {
+            store_stream(p.zsum + h, load_stream(p.zsum + h) + za);
+            store_stream(p.zsum + h + kChunk / 2, load_stream(p.zsum + h + kChunk / 2) + zb);
+        }
+    } else if (n == 8) {
+        const vec4 za = {acc[0], acc[1], acc[2], acc[3]}, zb = {acc[4], acc[5], acc[6], acc[7]};
+        if (p.zbar) { *(vec4_any*)(p.zbar + at) = za; *(vec4_any*)(p.zbar + at + 4) = zb; }
+        if (p.u) {
+            const vec4 a = *(const vec4_any*)(p.w + at) + za, b = *(const vec4_any*)(p.w + at + 4) + zb;
+            *(vec4_any*)(p.u + at) = a;
+            *(vec4_any*)(p.u + at + 4) = b;
+        }
+        if (p.zsum) {
+            const vec4 a = *(const vec4_any*)(p.zsum + at) + za, b = *(const vec4_any*)(p.zsum + at + 4) + zb;
+            *(vec4_any*)(p.zsum + at) = a;
+            *(vec4_any*)(p.zsum + at + 4) = b;
+        }
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 7; ++i) {
+            if (i >= n) break;
+            if (p.zbar) p.zbar[at + i] = acc[i];
+            if (p.u) p.u[at + i] = p.w[at + i] + acc[i];
+            if (p.zsum) p.zsum[at + i] += acc[i];
+        }
+    }
+}
+
+int finish_launch() {
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return QESGD_OK;
+    set_last_hip_error((int)e);
+    return QESGD_ERR_HIP;
+}
+
+template <uint32_t DT, bool STOCHASTIC>
+int launch_quantize_as(const Mx4Quantize& a, QParams& p, bool flat) {
+    if (p.packed_t) {
+        const uint64_t tiles = ((a.rows + kTile - 1) / kTile) * p.groups;
+        if (tiles >= (1ull << 31)) return QESGD_ERR_DIM;
+        k_mx4_quantize_both<DT, STOCHASTIC><<<dim3((uint32_t)tiles, a.K), 256, 0, a.stream>>>(p);
+        return finish_launch();
+    }
+    const uint64_t tiles = (p.slots + kQWaves * kChunk - 1) / (kQWaves * kChunk);
+    if (tiles >= (1ull << 31)) return QESGD_ERR_DIM;
+    p.xcd_group = xcd_group_log2(kQWaves * kChunk);
+    const dim3 grid((uint32_t)tiles, a.K);
+    if (flat) k_mx4_quantize<DT, STOCHASTIC, true><<<grid, kQWaves * 64, 0, a.stream>>>(p);
+    else k_mx4_quantize<DT, STOCHASTIC, false><<<grid, kQWaves * 64, 0, a.stream>>>(p);
+    return finish_launch();
+}
+
+template <uint32_t DT>
+int launch_quantize_type(const Mx4Quantize& a, QParams& p, bool flat) {
+    return a.stochastic ? launch_quantize_as<DT, true>(a, p, flat) : launch_quantize_as<DT, false>(a, p, flat);
+}
+
+}  // namespace
+
+int launch_mx4_quantize(const Mx4Quantize& a) {
+    qesgd_mx4_layout L{}, T{};
+    int rc = make_mx4_layout(a.rows, a.cols, &L);
+    if (rc == QESGD_OK && a.packed_t) rc = make_mx4_layout(a.cols, a.rows, &T);
+    if (rc != QESGD_OK) return rc;
+    QParams p{};
+    p.x = a.x;
+    p.ld = a.ld;
+    p.x_stride = a.x_stride;
+    p.rows = a.rows;
+    p.cols = a.cols;
+    p.groups = (uint32_t)(L.row_codes / 64);
+    p.groups_t = (uint32_t)(T.row_codes / 64);
+    p.slots = a.rows * L.row_codes * 2;
+    p.packed = a.packed;
+    p.packed_stride = a.packed_stride;
+    p.scales_off = L.scales_off;
+    p.packed_t = a.packed_t;
+    p.packed_t_stride = a.packed_t_stride;
+    p.scales_t_off = T.scales_off;
+    p.key0 = (uint32_t)a.seed;
+    p.key1 = (uint32_t)(a.seed >> 32);
+    p.round = a.round;
+    p.worker0 = a.worker0;
+    const bool flat = !a.packed_t && (a.rows == 1 || (a.cols % kMx4Pad == 0 && a.ld == a.cols));
+    if (flat) p.cols = a.rows * a.cols;
+    switch (a.dtype) {
+        case QESGD_F32: return launch_quantize_type<QESGD_F32>(a, p, flat);
+        case QESGD_BF16: return launch_quantize_type<QESGD_BF16>(a, p, flat);
+        default: return launch_quantize_type<QESGD_F16>(a, p, flat);
+    }
+}
+
+int launch_mx4_aggregate(const Mx4Aggregate& a) {
+    qesgd_mx4_layout L;
+    const int rc = make_mx4_layout(a.rows, a.cols, &L);
+    if (rc != QESGD_OK) return rc;
+    AParams p{};
+    p.packed = a.packed;
+    p.packed_stride = a.packed_stride;
+    p.scales_off = L.scales_off;
+    p.slots = a.rows * L.row_codes * 2;
+    p.groups = (uint32_t)(L.row_codes / 64);
+    p.K = a.K;
+    p.w = a.w;
+    p.zbar = a.zbar;
+    p.u = a.u;
+    p.zsum = a.zsum;
+    p.pow2 = (a.K & (a.K - 1)) == 0;
+    p.k = (float)a.K;
+    p.inv_k = 1.0f / (float)a.K;
+    const bool flat = a.rows == 1 || a.cols % kMx4Pad == 0;
+    p.cols = flat ? a.rows * a.cols : a.cols;
+    const uint64_t tiles = (p.slots + 4 * kChunk - 1) / (4 * kChunk);
+    if (tiles >= (1ull << 31)) return QESGD_ERR_DIM;
+    p.xcd_group = xcd_group_log2(4 * kChunk);
+    if (flat) k_mx4_aggregate_update<true><<<(uint32_t)tiles, 256, 0, a.stream>>>(p);
+    else k_mx4_aggregate_update<false><<<(uint32_t)tiles, 256, 0, a.stream>>>(p);
+    return finish_launch();
+}
+
+}  // namespace qesgd
