@@ -319,6 +319,8 @@ def qesgd_orthogonalize(x, rows, cols, n, coeffs, eps, out, workspace, stream=No
 
 def qesgd_orthogonal_update(g, rows, cols, n, momentum_inout, mu, nesterov, coeffs, eps, alpha, step_out, z_inout, w_snap,
                             u_out, zsum_inout, workspace, stream=None):
+    if g.dtype != torch.float32:
+        raise QesgdError(ERR_DTYPE, "qesgd_orthogonal_update")
     _check(lib().qesgd_orthogonal_update(_ptr(g), int(rows), int(cols), int(n), _ptr(momentum_inout), float(mu),
                                          int(bool(nesterov)), _coeffs(coeffs), len(coeffs), float(eps), float(alpha),
                                          _ptr(step_out), _ptr(z_inout), _ptr(w_snap), _ptr(u_out), _ptr(zsum_inout),

@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(256) k_orthogonal_split(const SParams p) {
     __syncthreads();
     sum = (part[0] + part[1]) + (part[2] + part[3]);
     const double norm = sqrt(sum) + (double)p.eps;
-    const float scale = norm > 0.0 ? (float)(1.0 / norm) : 0.0f;
+    const double scale = norm > 0.0 ? (double)kScaleX / norm : 0.0;     // beyond fp32 where x is subnormal
 
     const uint32_t r0 = blockIdx.y * 64u, c0 = blockIdx.x * 64u;
     const uint64_t base = (uint64_t)blockIdx.z * p.d;
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(256) k_orthogonal_split(const SParams p) {
             v = fetch<DT>(p.x, at);
             if (p.momentum) v = p.nesterov ? v + p.mu * p.momentum[at] : p.momentum[at];
         }
-        tile[i][tx] = v * scale * kScaleX;
+        tile[i][tx] = (float)((double)v * scale);
     }
     __syncthreads();
     // rows of x: those of X where rows <= cols, of its transpose otherwise

@@ -1,0 +1,87 @@
+"""The operators for matrix parameters together, as the epoch loop runs them: layer, gradients, codes, mean, orthogonalised step."""
+import numpy as np
+import pytest
+import torch
+
+import matrix_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def loop_class():
+    from paper_1901_03040_amd.epoch_loop import QesgdMatrixLoop
+    assert torch.cuda.is_available()
+    return QesgdMatrixLoop
+
+
+def q(x, stochastic=False, seed=0, rnd=0, worker=0):
+    return R.values(*R.quantize(x, stochastic, seed, rnd, worker), x.shape[1])
+
+
+def close(got, want, terms, magnitudes, half_step):
+    got = got.double().cpu().numpy()
+    assert (np.abs(got - want) <= terms * 2.0 ** -24 * magnitudes + half_step * np.abs(want) * 1.001).all()
+
+
+@pytest.mark.parametrize("out,inn,tokens,dtype", [(40, 72, 17, torch.float32), (130, 64, 50, torch.bfloat16), (33, 257, 1, torch.float32)])
+def test_layer_and_round(loop_class, out, inn, tokens, dtype):
+    K, seed = 3, 1234567
+    g = torch.Generator().manual_seed(out)
+    w0 = torch.randn(out, inn, generator=g) / inn ** 0.5
+    loop = loop_class(w0.cuda(), K, seed)
+    half_step = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8
+    w, z, zsum, m = w0.double().numpy(), np.zeros((out, inn), np.float32), np.zeros((out, inn), np.float32), np.zeros((out, inn), np.float32)
+    for epoch in range(2):
+        for rnd in range(3):
+            u = loop.u.double().cpu().numpy()
+            grads = torch.empty(K, out, inn, device="cuda")
+            for k in range(K):
+                x, dy = torch.randn(tokens, inn, generator=g).to(dtype), (torch.randn(tokens, out, generator=g) * 1e-2).to(dtype)
+                y, saved = loop.forward(x.cuda())
+                dx, dw = loop.backward(dy.cuda(), saved)
+                assert y.dtype == dtype and dx.dtype == dtype and dw.dtype == torch.float32
+                x64, dy64 = x.double().numpy(), dy.double().numpy()
+                a, b = q(x64), q(u)
+                close(y, a @ b.T, inn, np.abs(a) @ np.abs(b).T, half_step)
+                a, b = q(dy64, True, seed, loop.round_id), q(u.T)
+                close(dx, a @ b.T, out, np.abs(a) @ np.abs(b).T, half_step)
+                a, b = q(dy64.T, True, seed, loop.round_id), q(x64.T)
+                close(dw, a @ b.T, tokens, np.abs(a) @ np.abs(b).T, 2.0 ** -24)
+                grads[k] = dw
+            acc = np.zeros((out, inn), np.float32)
+            for k in range(K):
+                acc = acc + q(grads[k].double().cpu().numpy(), True, seed, loop.round_id, k).astype(np.float32)
+            mean = acc / np.float32(K)
+            before = loop.z.cpu().numpy().copy()
+            loop.orthogonal_round(grads, 0.02, last=rnd == 2)
+            assert np.array_equal(loop.mean.cpu().numpy(), mean)
+            m = np.float32(0.95) * m + mean
+            assert np.array_equal(loop.momentum.cpu().numpy(), m)
+            look = (mean + np.float32(0.95) * m).astype(np.float64)
+            want = -0.02 * R.newton_schulz(look)
+            moved = R.newton_schulz(look, noise=2.0 ** -22 / np.sqrt(max(look.shape)), rng=np.random.default_rng(0)) * -0.02
+            z = loop.z.cpu().numpy()
+            limit = 8 * (np.linalg.norm(moved - want) + 2.0 ** -22 * np.linalg.norm(want)) + 2.0 ** -23 * (np.linalg.norm(z) + np.linalg.norm(before))
+            assert np.linalg.norm(z.astype(np.float64) - before - want) <= limit
+            w32 = loop.w.cpu().numpy()
+            assert np.array_equal(loop.u.cpu().numpy(), w32 + z)
+            if rnd < 2:
+                zsum = zsum + z
+            assert np.array_equal(loop.zsum.cpu().numpy(), zsum)
+        w32 = loop.w.cpu().numpy()
+        loop.end_epoch()
+        assert np.array_equal(loop.w.cpu().numpy(), w32 + zsum / np.float32(3))
+        loop.begin_epoch()
+        zsum = np.zeros((out, inn), np.float32)
+        assert torch.equal(loop.u, loop.w) and not loop.z.any()
+
+
+def test_operands_that_are_not_contiguous(loop_class):
+    g = torch.Generator().manual_seed(0)
+    loop = loop_class(torch.randn(48, 80, generator=g).cuda(), 1, 5)
+    wide = torch.randn(20, 200, generator=g).cuda()
+    y, _ = loop.forward(wide[:, 7:87])                          # rows apart
+    assert torch.equal(y, loop.forward(wide[:, 7:87].contiguous())[0])
+    turned = torch.randn(80, 20, generator=g).cuda().t()        # columns together
+    assert torch.equal(loop.forward(turned)[0], loop.forward(turned.contiguous())[0])
