@@ -296,7 +296,8 @@ int qesgd_mx4_product(const void* a_packed, const void* b_packed, uint64_t M, ui
  * numbers, sums in fp32).  |coefficients| must keep every iterate's and polynomial's entries below 16
  * (singular values that stay near 1 do); beyond that the result is infinite or NaN.  A matrix of zeros gives zeros.
  *   out  same type and shape as x, may be x itself.
- *   workspace  qesgd_orthogonalize_workspace_bytes(rows, cols, n), 256-byte aligned.  rows, cols <= 2^20, n <= 65535. */
+ *   workspace  qesgd_orthogonalize_workspace_bytes(rows, cols, n), 256-byte aligned; may be NULL when that is 0 (matrices that fit
+ *        the shared memory of a CU).  rows, cols <= 2^20, n <= 65535. */
 size_t qesgd_orthogonalize_workspace_bytes(uint64_t rows, uint64_t cols, uint32_t n);
 int qesgd_orthogonalize(const void* x, uint32_t dtype, uint64_t rows, uint64_t cols, uint32_t n, const float* coeffs, uint32_t steps,
                         float eps, void* out, void* workspace, size_t workspace_bytes, void* stream);

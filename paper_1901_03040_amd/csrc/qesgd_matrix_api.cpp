@@ -47,7 +47,8 @@ static int orthogonal_check(const Orthogonalize& a, size_t workspace_bytes) {
     if (!aligned(a.x, 16) || !aligned(a.momentum, 16) || !aligned(a.out, 16) || !aligned(a.z, 16) || !aligned(a.w, 16) ||
         !aligned(a.u, 16) || !aligned(a.zsum, 16) || !aligned(a.workspace, 256))
         return QESGD_ERR_ALIGN;
-    if (!a.workspace || workspace_bytes < orthogonalize_workspace(a.rows, a.cols, a.n)) return QESGD_ERR_WORKSPACE;
+    const size_t need = orthogonalize_workspace(a.rows, a.cols, a.n);
+    if (need > 0 && (!a.workspace || workspace_bytes < need)) return QESGD_ERR_WORKSPACE;
     return QESGD_OK;
 }
 

@@ -1,5 +1,6 @@
 // C = A B^T of two packed 4-bit matrices on the scaled matrix instruction: a lane's operand is 32 elements of one row, which is one
 // block of the format, next to its scale byte, so nothing is unpacked.  Element products are exact, sums are fp32.
+#include <stdlib.h>
 #include <type_traits>
 
 #include "qesgd_internal.h"
@@ -28,101 +29,124 @@ __device__ __forceinline__ void put(void* c, uint64_t at, float v) {
     else ((__bf16*)c)[at] = (__bf16)v;
 }
 
+template <class S>
+struct Mx4Ops {
+    static constexpr int PARTS = 4;                            // 64 columns each: one matrix instruction deep
+    static constexpr int LOADS = (S::BM + S::BN) * 8 / S::threads;
+    struct Frag { int4v a[S::FM], b[S::FN]; };
+    // Scales of two steps: 16 bytes of every row of the tile, four words a row.  A load from memory for each fragment instead touches 32
+    // lines for 128 bytes, 96 times a step, and held the kernel at a quarter of the matrix rate.
+    static constexpr int NA = S::BM * 4 / S::threads, NB = S::BN * 4 / S::threads;
+    static constexpr int scale_bytes = (S::BM + S::BN) * 16;
+    TileLoader<S::BM, S::threads> la;
+    TileLoader<S::BN, S::threads> lb;
+    const unsigned char *a, *b;
+    const unsigned char *sa, *sb;                              // scales of the tile's first rows
+    unsigned char* scales;                                     // in LDS, two buffers
+    uint32_t off_a[NA], off_b[NB];                             // rows of the words that the lane moves
+    uint32_t row_scales, scale_at, scale_at_a, scale_at_b;
+    uint32_t ya[S::FM][2], yb[S::FN][2], xa[S::FM][2], xb[S::FN][2];            // of the next step, and of this one
+    uint32_t at_a, at_b, steps, h, second;
+    bool half;
+    acc16 acc[S::FM][S::FN];
+
+    __device__ __forceinline__ void init_scales(const PParams& p, uint32_t m0, uint32_t n0, uint32_t wm, uint32_t wn) {
+        row_scales = p.row_scales;
+        sa = p.a_scales + (uint64_t)m0 * row_scales;
+        sb = p.b_scales + (uint64_t)n0 * row_scales;
+#pragma unroll
+        for (int i = 0; i < NA; ++i) off_a[i] = min((i * S::threads + threadIdx.x) >> 2, p.M - m0 - 1u) * row_scales;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) off_b[i] = min((i * S::threads + threadIdx.x) >> 2, p.N - n0 - 1u) * row_scales;
+        scale_at = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * 256u);
+        scale_at_a = (wm * S::FM * 32u + (threadIdx.x & 31u)) * 16u;
+        scale_at_b = (S::BM + wn * S::FN * 32u + (threadIdx.x & 31u)) * 16u;
+    }
+    __device__ __forceinline__ void fetch_pair(uint32_t step) {
+        // a row ends with a whole word; what would lie behind it takes that one again
+        const uint32_t word = min(step * 8u + (threadIdx.x & 3u) * 4u, row_scales - 4u);
+        const uint32_t to = lds_number(scales) + ((step >> 1) & 1u) * scale_bytes + scale_at;
+#pragma unroll
+        for (int i = 0; i < NA; ++i) load_to_lds_4(sa, off_a[i] + word, to + i * S::threads * 4);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) load_to_lds_4(sb, off_b[i] + word, to + S::BM * 16 + i * S::threads * 4);
+    }
+    __device__ __forceinline__ void fetch(uint32_t step, unsigned char* to) {
+        const bool short_step = half && step + 1 == steps;
+        la.load(a + (uint64_t)step * kStepBytes, to, short_step);
+        lb.load(b + (uint64_t)step * kStepBytes, to + S::BM * kStepBytes, short_step);
+    }
+    __device__ __forceinline__ void arrive(uint32_t step) {
+        const unsigned char* from = scales + ((step >> 1) & 1u) * scale_bytes + (step & 1u) * 8u;
+#pragma unroll
+        for (int f = 0; f < S::FM; ++f) { const uint2 v = *(const uint2*)(from + scale_at_a + f * 512); ya[f][0] = v.x; ya[f][1] = v.y; }
+#pragma unroll
+        for (int f = 0; f < S::FN; ++f) { const uint2 v = *(const uint2*)(from + scale_at_b + f * 512); yb[f][0] = v.x; yb[f][1] = v.y; }
+        // The second half of a half step repeats the first half's codes and takes 2^-127 on either side: those products, at most
+        // 36 * 2^-254, are zero in fp32.
+        second = half && step + 1 >= steps ? 0u : 0xFFFFFFFFu;
+    }
+    // A lane's blocks of a step are scale bytes 2 s + h of its row: a shift by 8 h brings them to bytes 0 and 2 of the two words.
+    __device__ __forceinline__ void next() {
+#pragma unroll
+        for (int f = 0; f < S::FM; ++f) { xa[f][0] = ya[f][0] >> (8u * h); xa[f][1] = (ya[f][1] & second) >> (8u * h); }
+#pragma unroll
+        for (int f = 0; f < S::FN; ++f) { xb[f][0] = yb[f][0] >> (8u * h); xb[f][1] = (yb[f][1] & second) >> (8u * h); }
+    }
+    __device__ __forceinline__ void read(Frag& f, const unsigned char* from, int part) {
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) f.a[i] = *(const int4v*)(from + (at_a ^ (part * 32u)) + i * 4096);
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) f.b[j] = *(const int4v*)(from + (at_b ^ (part * 32u)) + j * 4096);
+    }
+    __device__ __forceinline__ static int8v wide(const int4v& v) { return int8v{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }
+    template <int PART>
+    __device__ __forceinline__ void multiply_part(const Frag& f) {
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(f.a[i]), wide(f.b[j]), acc[i][j], 4, 4, (PART & 1) * 2,
+                                                                           (int)xa[i][PART >> 1], (PART & 1) * 2, (int)xb[j][PART >> 1]);
+    }
+    __device__ __forceinline__ void multiply(const Frag& f, int part) {
+        switch (part) {
+            case 0: multiply_part<0>(f); break;
+            case 1: multiply_part<1>(f); break;
+            case 2: multiply_part<2>(f); break;
+            default: multiply_part<3>(f); break;
+        }
+    }
+};
+
 template <class S, uint32_t DT>
 __global__ void __launch_bounds__(S::threads) k_mx4_product(const PParams p) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds0[(S::BM + S::BN) * kStepBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char lds1[(S::BM + S::BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char scales[2 * Mx4Ops<S>::scale_bytes];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
     const uint32_t wm = wave / S::WN, wn = wave % S::WN;
-    const uint32_t t = tile_of_workgroup(blockIdx.x, gridDim.x);
-    const uint32_t tm = t % p.tiles_m, tn = t / p.tiles_m;
+    uint32_t tm, tn;
+    banded_tile(tile_of_workgroup(blockIdx.x, gridDim.x), p.tiles_m, p.tiles_n, tm, tn);
     const uint32_t m0 = tm * S::BM, n0 = tn * S::BN;
-    const unsigned char* a = p.a + (uint64_t)m0 * p.row_codes;
-    const unsigned char* b = p.b + (uint64_t)n0 * p.row_codes;
-    TileLoader<S::BM, S::threads> la;
-    TileLoader<S::BN, S::threads> lb;
-    la.init(p.row_codes, p.M - m0);
-    lb.init(p.row_codes, p.N - n0);
-    const uint32_t steps = (p.row_codes + 127u) / 128u;
-    const bool ragged = (p.row_codes & 127u) != 0;
-
-    const unsigned char* sa[S::FM];
-    const unsigned char* sb[S::FN];
+    Mx4Ops<S> ops;
+    ops.a = p.a + (uint64_t)m0 * p.row_codes;
+    ops.b = p.b + (uint64_t)n0 * p.row_codes;
+    ops.la.init(p.row_codes, p.M - m0);
+    ops.lb.init(p.row_codes, p.N - n0);
+    ops.scales = scales;
+    ops.init_scales(p, m0, n0, wm, wn);
+    ops.at_a = wm * S::FM * 32 * kStepBytes + lane_place(lane);
+    ops.at_b = (S::BM + wn * S::FN * 32) * kStepBytes + lane_place(lane);
+    ops.steps = (p.row_codes + kStepBytes - 1u) / kStepBytes;
+    ops.half = p.row_codes % kStepBytes != 0;
+    ops.h = h;
 #pragma unroll
-    for (int f = 0; f < S::FM; ++f) sa[f] = p.a_scales + (uint64_t)min(m0 + (wm * S::FM + f) * 32u + (lane & 31u), p.M - 1u) * p.row_scales;
+    for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-    for (int f = 0; f < S::FN; ++f) sb[f] = p.b_scales + (uint64_t)min(n0 + (wn * S::FN + f) * 32u + (lane & 31u), p.N - 1u) * p.row_scales;
-
-    acc16 acc[S::FM][S::FN] = {};
-    uint32_t at[4];                               // a lane's four chunks of a row
-#pragma unroll
-    for (uint32_t s = 0; s < 4; ++s) at[s] = (lane & 31u) * 128u + (((2u * s + h) ^ (lane & 7u)) * 16u);
-
-    uint32_t ra[S::FM][2], rb[S::FN][2], xa[S::FM][2], xb[S::FN][2];      // scales: on their way, and of this step
-    auto fetch = [&](uint32_t step, unsigned char* to) {
-        const bool half = ragged && step + 1 == steps;
-        // 256 columns have 8 scale bytes a row; the half step at the end has 4 and takes them twice
-        const uint32_t o0 = step * 8u, o1 = o0 + (half ? 0u : 4u);
-#pragma unroll
-        for (int f = 0; f < S::FM; ++f) { ra[f][0] = *(const uint32_t*)(sa[f] + o0); ra[f][1] = *(const uint32_t*)(sa[f] + o1); }
-#pragma unroll
-        for (int f = 0; f < S::FN; ++f) { rb[f][0] = *(const uint32_t*)(sb[f] + o0); rb[f][1] = *(const uint32_t*)(sb[f] + o1); }
-        la.load(a + (uint64_t)step * 128u, to, half);
-        lb.load(b + (uint64_t)step * 128u, to + S::BM * kStepBytes, half);
-    };
-    // A lane's blocks of a step are scale bytes 2 s + h of its row: a shift by 8 h brings them to bytes 0 and 2 of the two words.
-    auto scales = [&]() {
-#pragma unroll
-        for (int f = 0; f < S::FM; ++f) { xa[f][0] = ra[f][0] >> (8u * h); xa[f][1] = ra[f][1] >> (8u * h); }
-#pragma unroll
-        for (int f = 0; f < S::FN; ++f) { xb[f][0] = rb[f][0] >> (8u * h); xb[f][1] = rb[f][1] >> (8u * h); }
-    };
-    auto compute = [&](uint32_t step, const unsigned char* from) {
-        const bool half = ragged && step + 1 == steps;
-        const unsigned char* fa = from + wm * S::FM * 32 * kStepBytes;
-        const unsigned char* fb = from + (S::BM + wn * S::FN * 32) * kStepBytes;
-        auto part = [&](auto s_) {
-            constexpr int s = decltype(s_)::value;
-            int8v va[S::FM], vb[S::FN];
-#pragma unroll
-            for (int f = 0; f < S::FM; ++f) {
-                const int4v v = *(const int4v*)(fa + f * 4096 + at[s]);
-                va[f] = int8v{v[0], v[1], v[2], v[3], 0, 0, 0, 0};
-            }
-#pragma unroll
-            for (int f = 0; f < S::FN; ++f) {
-                const int4v v = *(const int4v*)(fb + f * 4096 + at[s]);
-                vb[f] = int8v{v[0], v[1], v[2], v[3], 0, 0, 0, 0};
-            }
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::FN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(va[i], vb[j], acc[i][j], 4, 4, (s & 1) * 2,
-                                                                               (int)xa[i][s >> 1], (s & 1) * 2, (int)xb[j][s >> 1]);
-        };
-        part(std::integral_constant<int, 0>{});
-        part(std::integral_constant<int, 1>{});
-        if (!half) {
-            part(std::integral_constant<int, 2>{});
-            part(std::integral_constant<int, 3>{});
-        }
-    };
-
-    fetch(0, lds0);
-    uint32_t step = 0;
-    for (;;) {
-        __syncthreads();
-        scales();
-        if (step + 1 < steps) fetch(step + 1, lds1);
-        compute(step, lds0);
-        if (++step == steps) break;
-        __syncthreads();
-        scales();
-        if (step + 1 < steps) fetch(step + 1, lds0);
-        compute(step, lds1);
-        if (++step == steps) break;
-    }
+        for (int j = 0; j < S::FN; ++j) ops.acc[i][j] = acc16{};
+    unsigned char* const buffers[2] = {lds0, lds1};
+    run_steps(ops, ops.steps, buffers);
 
     // a lane holds column lane & 31 of a fragment and rows 8 q + 4 h + r
 #pragma unroll
@@ -133,7 +157,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_product(const PParams p) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const uint32_t row = m0 + (wm * S::FM + i) * 32u + 8u * (e >> 2) + 4u * h + (e & 3);
-                if (row < p.M && col < p.N) put<DT>(p.c, (uint64_t)row * p.ldc + col, acc[i][j][e]);
+                if (row < p.M && col < p.N) put<DT>(p.c, (uint64_t)row * p.ldc + col, ops.acc[i][j][e]);
             }
         }
 }
@@ -175,7 +199,12 @@ int launch_mx4_product(const Mx4Product& a) {
     p.N = (uint32_t)a.N;
     p.row_codes = (uint32_t)A.row_codes;
     p.row_scales = (uint32_t)A.row_scales;
-    return launch_product_as<TileShape<2, 2, 2, 2>>(a, p);
+        const char* e = getenv("MXE");
+    switch (e ? atoi(e) : 128) {
+        case 256: return launch_product_as<TileShape<2, 4, 4, 2, 2>>(a, p);
+        case 64: return launch_product_as<TileShape<2, 2, 1, 1, 2>>(a, p);
+        default: return launch_product_as<TileShape<2, 2, 2, 2, 2>>(a, p);
+    }
 }
 
 }  // namespace qesgd

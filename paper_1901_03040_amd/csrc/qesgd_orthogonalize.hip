@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(256) k_orthogonal_split(const SParams p) {
     }
 }
 
-enum { kGram = 0, kPoly = 1, kApply = 2, kFinal = 3 };
+enum { kGram = 0, kPoly = 1, kApply = 2, kFinal = 3, kPartial = 4 };
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 
 struct OParams {
     const unsigned char* a;              // M rows
@@ -148,6 +149,8 @@ struct OParams {
     uint32_t d1_pitch, d2_pitch;
     float scale;                         // of the sums, into the output's scale
     float ca, cb;                        // kPoly: on the diagonal, and of G
+    float* partial;                      // kPartial: [n, splits, M, M]
+    uint32_t splits;
     // kFinal: [n, M, N] outputs
     void* out;
     float* z;
@@ -164,136 +167,574 @@ __device__ __forceinline__ void upper_tile(uint32_t t, uint32_t& i, uint32_t& j)
     i = t - j * (j + 1u) / 2u;
 }
 
+// The outputs of COUNT numbers: a lane holds column `col` and rows row + 8 q + r, r = 0..3.  Everything is read before the first store: the
+// compiler cannot know that the outputs do not overlap, and would wait for each number in turn.
+template <uint32_t DT, int COUNT, class ACC>
+__device__ __forceinline__ void finish(const OParams& p, const ACC& acc, uint32_t batch, uint32_t row, uint32_t col) {
+    if (col >= p.N) return;
+    const uint64_t base = ((uint64_t)batch * p.M + row) * p.N + col;
+    float z[COUNT], w[COUNT], s[COUNT];
+    if (p.z) {
+#pragma unroll
+        for (int e = 0; e < COUNT; ++e) {
+            const uint32_t r = 8u * (e >> 2) + (e & 3);
+            const uint64_t o = row + r < p.M ? base + (uint64_t)r * p.N : base;
+            if (row < p.M) {
+                z[e] = p.z[o];
+                if (p.u) w[e] = p.w[o];
+                if (p.zsum) s[e] = p.zsum[o];
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e) {
+        const uint32_t r = 8u * (e >> 2) + (e & 3);
+        if (row + r >= p.M) continue;
+        const uint64_t o = base + (uint64_t)r * p.N;
+        const float v = acc[e] * p.scale;
+        if (p.out) {
+            if (DT == QESGD_F32) ((float*)p.out)[o] = v;
+            else if (DT == QESGD_F16) ((_Float16*)p.out)[o] = (_Float16)v;
+            else ((__bf16*)p.out)[o] = (__bf16)v;
+        }
+        if (p.z) {
+            const float zv = z[e] + v;
+            p.z[o] = zv;
+            if (p.u) p.u[o] = w[e] + zv;
+            if (p.zsum) p.zsum[o] = s[e] + zv;
+        }
+    }
+}
+
+// A lane holds column lane & 31 of a fragment and rows 8 q + 4 h + r, r = 0..3 (h: the half of the wave).
+__device__ __forceinline__ void store_partial(const OParams& p, const float (&v)[16], uint64_t which, uint32_t row, uint32_t col, uint32_t lane) {
+    const uint32_t c = col + (lane & 31u), r0 = row + 4u * (lane >> 5);
+    float* to = p.partial + (which * p.M + r0) * p.M + c;
+    if (c < p.N)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const uint32_t r = 8u * (e >> 2) + (e & 3);
+            if (r0 + r < p.M) to[(uint64_t)r * p.M] = v[e];
+        }
+}
+
+// P = a I + b G + c G G: the sums hold c G G already.  G[row.., col] = G[col, row..] lies four in a row; its padding is zero.
+__device__ __forceinline__ void add_lower_terms(const OParams& p, float (&v)[16], uint32_t z, uint32_t row, uint32_t col, uint32_t lane) {
+    const uint32_t c = col + (lane & 31u), r0 = row + 4u * (lane >> 5);
+    if (c >= p.N) return;
+    const unsigned char* g = p.a + z * p.a_bytes + (uint64_t)c * p.pitch;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t r = r0 + 8u * q;
+        if (r >= p.M) continue;
+        const half4 hi = *(const half4*)(g + split_at(r)), lo = *(const half4*)(g + split_at(r) + 64);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * q + e] += p.cb * ((float)hi[e] + (float)lo[e]) + (r + e == c ? p.ca : 0.0f);
+    }
+}
+
+// A fragment to the split rows of the transpose, and with `both` to its own.  Numbers outside the matrix are stored as the zeros
+// that pad its rows.
+__device__ __forceinline__ void store_split(const OParams& p, const float (&v)[16], uint32_t z, uint32_t row, uint32_t col, uint32_t lane, bool both) {
+    const uint32_t c = col + (lane & 31u), h = lane >> 5;
+    uint32_t w[2][8];                    // hi and lo; word 2 q + k holds rows 8 q + 4 h + 2 k and the next
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        _Float16 hi[2], lo[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t r = row + 8u * (k >> 1) + 4u * h + 2u * (k & 1) + e;
+            split(r < p.M && c < p.N ? v[2 * k + e] : 0.0f, hi[e], lo[e]);
+        }
+        w[0][k] = (uint32_t)__builtin_bit_cast(unsigned short, hi[0]) | ((uint32_t)__builtin_bit_cast(unsigned short, hi[1]) << 16);
+        w[1][k] = (uint32_t)__builtin_bit_cast(unsigned short, lo[0]) | ((uint32_t)__builtin_bit_cast(unsigned short, lo[1]) << 16);
+    }
+    // Rows of the transpose: the halves of the wave swap words, so that a lane has 16 numbers in a row.
+    unsigned char* to = p.d2 + z * p.d2_bytes + (uint64_t)c * p.d2_pitch + split_at(row + 16u * h);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        uint32_t o[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const auto x = __builtin_amdgcn_permlane32_swap(w[half][k], w[half][4 + k], false, false);
+            o[4 * (k >> 1) + (k & 1)] = x[0];
+            o[4 * (k >> 1) + (k & 1) + 2] = x[1];
+        }
+        if (c < p.N && (row + 16u * h) * 4u < p.d2_pitch) {
+            *(uint4*)(to + half * 64) = make_uint4(o[0], o[1], o[2], o[3]);
+            *(uint4*)(to + half * 64 + 16) = make_uint4(o[4], o[5], o[6], o[7]);
+        }
+    }
+    if (!both) return;
+    // Its own rows: the four lanes of a quad turn 4 x 4 numbers around, so that lane i of the quad has row i's four columns.
+    const bool odd = (lane & 1u) != 0, low = (lane & 2u) == 0;
+    const uint32_t pick = odd ? 0x03020706u : 0x05040100u;       // bytes 0..3: own word, 4..7: the neighbour's
+    const uint32_t r0 = row + 4u * h + (lane & 3u), c4 = col + (lane & 28u);
+    unsigned char* own = p.d1 + z * p.d1_bytes + (uint64_t)r0 * p.d1_pitch + split_at(c4);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint32_t a = w[half][2 * q], b = w[half][2 * q + 1];
+            a = __builtin_amdgcn_perm((uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xB1, 0xF, 0xF, false), a, pick);
+            b = __builtin_amdgcn_perm((uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, 0xB1, 0xF, 0xF, false), b, pick);
+            const uint32_t got = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(low ? b : a), 0x4E, 0xF, 0xF, false);
+            if (r0 + 8u * q < p.M && c4 * 4u < p.d1_pitch)
+                *(uint2*)(own + (uint64_t)(8u * q) * p.d1_pitch + half * 64) = low ? make_uint2(a, got) : make_uint2(got, b);
+        }
+}
+
+template <class S>
+struct SplitOps {
+    static constexpr int PARTS = 2;                            // 16 numbers of the contraction each
+    static constexpr int LOADS = (S::BM + S::BN) * 8 / S::threads;
+    struct Frag { half8 ah[S::FM], bh[S::FN], bl[S::FN], al[S::FM]; };
+    TileLoader<S::BM, S::threads> la;
+    TileLoader<S::BN, S::threads> lb;
+    const unsigned char *a, *b;
+    uint32_t at_a, at_b;                                       // parts 2 and 3 of the row are lo of parts 0 and 1
+    acc16 acc[S::FM][S::FN];
+
+    __device__ __forceinline__ void fetch(uint32_t step, unsigned char* to) {
+        la.load(a + (uint64_t)step * kStepBytes, to, false);
+        lb.load(b + (uint64_t)step * kStepBytes, to + S::BM * kStepBytes, false);
+    }
+    __device__ __forceinline__ void fetch_pair(uint32_t) {}
+    __device__ __forceinline__ void arrive(uint32_t) {}
+    __device__ __forceinline__ void next() {}
+    __device__ __forceinline__ void read(Frag& f, const unsigned char* from, int part) {
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) f.ah[i] = *(const half8*)(from + (at_a ^ (part * 32u)) + i * 4096);
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) f.bh[j] = *(const half8*)(from + (at_b ^ (part * 32u)) + j * 4096);
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) f.bl[j] = *(const half8*)(from + (at_b ^ (part * 32u + 64u)) + j * 4096);
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) f.al[i] = *(const half8*)(from + (at_a ^ (part * 32u + 64u)) + i * 4096);
+    }
+    __device__ __forceinline__ void multiply(const Frag& f, int) {
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ah[i], f.bh[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ah[i], f.bl[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.al[i], f.bh[j], acc[i][j], 0, 0, 0);
+    }
+};
+
 template <class S, int KIND, uint32_t DT>
 __global__ void __launch_bounds__(S::threads) k_orthogonal_product(const OParams p) {
     static_assert(S::BM == S::BN, "symmetric products take square tiles");
     __shared__ __attribute__((aligned(1024))) unsigned char lds0[(S::BM + S::BN) * kStepBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char lds1[(S::BM + S::BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds2[S::BUFFERS > 2 ? (S::BM + S::BN) * kStepBytes : 16];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds3[S::BUFFERS > 2 ? (S::BM + S::BN) * kStepBytes : 16];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
     const uint32_t wm = wave / S::WN, wn = wave % S::WN;
-    const uint32_t t = tile_of_workgroup(blockIdx.x, gridDim.x), z = blockIdx.y;
+    uint32_t t = tile_of_workgroup(blockIdx.x, gridDim.x), split_k = 0, first = 0, steps = p.steps;
+    const uint32_t z = __builtin_amdgcn_readfirstlane(t / (p.tiles * p.splits));
+    t -= z * (p.tiles * p.splits);
     uint32_t tm, tn;
-    if (KIND == kGram || KIND == kPoly) {
-        upper_tile(t, tm, tn);
-    } else {
-        tm = t % p.tiles_m;
-        tn = t / p.tiles_m;
+    if (KIND == kPartial) {              // the tiles of one piece of the contraction follow one another
+        split_k = __builtin_amdgcn_readfirstlane(t / p.tiles);
+        t -= split_k * p.tiles;
+        first = __builtin_amdgcn_readfirstlane(split_k * p.steps / p.splits);
+        steps = __builtin_amdgcn_readfirstlane((split_k + 1u) * p.steps / p.splits) - first;
     }
+    if (KIND == kGram || KIND == kPoly || KIND == kPartial) upper_tile(t, tm, tn);
+    else banded_tile(t, p.tiles_m, p.tiles_n, tm, tn);
+    tm = __builtin_amdgcn_readfirstlane(tm);     // the same in every lane, which the compiler loses over divisions and roots
+    tn = __builtin_amdgcn_readfirstlane(tn);
     const uint32_t m0 = tm * S::BM, n0 = tn * S::BN;
-    const unsigned char* a = p.a + z * p.a_bytes + (uint64_t)m0 * p.pitch;
-    const unsigned char* b = p.b + z * p.b_bytes + (uint64_t)n0 * p.pitch;
-    TileLoader<S::BM, S::threads> la;
-    TileLoader<S::BN, S::threads> lb;
-    la.init(p.pitch, p.M - m0);
-    lb.init(p.pitch, p.N - n0);
-
-    acc16 acc[S::FM][S::FN] = {};
-    uint32_t at[4];                              // a lane's chunks of a row: hi of either half of the step, lo of either half
+    SplitOps<S> ops;
+    ops.a = p.a + z * p.a_bytes + (uint64_t)m0 * p.pitch + (uint64_t)first * kStepBytes;
+    ops.b = p.b + z * p.b_bytes + (uint64_t)n0 * p.pitch + (uint64_t)first * kStepBytes;
+    ops.la.init(p.pitch, p.M - m0);
+    ops.lb.init(p.pitch, p.N - n0);
+    ops.at_a = wm * S::FM * 32 * kStepBytes + lane_place(lane);
+    ops.at_b = (S::BM + wn * S::FN * 32) * kStepBytes + lane_place(lane);
 #pragma unroll
-    for (uint32_t s = 0; s < 4; ++s) at[s] = (lane & 31u) * 128u + (((2u * s + h) ^ (lane & 7u)) * 16u);
-
-    auto load = [&](uint32_t step, unsigned char* to) {
-        la.load(a + (uint64_t)step * kStepBytes, to, false);
-        lb.load(b + (uint64_t)step * kStepBytes, to + S::BM * kStepBytes, false);
-    };
-    auto compute = [&](const unsigned char* from) {
-        const unsigned char* fa = from + wm * S::FM * 32 * kStepBytes;
-        const unsigned char* fb = from + (S::BM + wn * S::FN * 32) * kStepBytes;
+    for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            half8 ah[S::FM], al[S::FM], bh[S::FN], bl[S::FN];
-#pragma unroll
-            for (int f = 0; f < S::FM; ++f) { ah[f] = *(const half8*)(fa + f * 4096 + at[s]); al[f] = *(const half8*)(fa + f * 4096 + at[s + 2]); }
-#pragma unroll
-            for (int f = 0; f < S::FN; ++f) { bh[f] = *(const half8*)(fb + f * 4096 + at[s]); bl[f] = *(const half8*)(fb + f * 4096 + at[s + 2]); }
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-                for (int j = 0; j < S::FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
-        }
-    };
-
-    load(0, lds0);
-    for (uint32_t step = 0;;) {
-        __syncthreads();
-        if (step + 1 < p.steps) load(step + 1, lds1);
-        compute(lds0);
-        if (++step == p.steps) break;
-        __syncthreads();
-        if (step + 1 < p.steps) load(step + 1, lds0);
-        compute(lds1);
-        if (++step == p.steps) break;
+        for (int j = 0; j < S::FN; ++j) ops.acc[i][j] = acc16{};
+    if constexpr (S::BUFFERS == 2) {
+        unsigned char* const buffers[2] = {lds0, lds1};
+        run_steps(ops, steps, buffers);
+    } else {
+        unsigned char* const buffers[4] = {lds0, lds1, lds2, lds3};
+        run_steps(ops, steps, buffers);
     }
+    auto& acc = ops.acc;
 
-    // A lane holds column lane & 31 of a fragment and rows 8 q + 4 h + r, r = 0..3.
+    if (KIND == kFinal) {
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j)
+                finish<DT, 16>(p, acc[i][j], z, m0 + (wm * S::FM + i) * 32u + 4u * h, n0 + (wn * S::FN + j) * 32u + (lane & 31u));
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < S::FM; ++i)
 #pragma unroll
         for (int j = 0; j < S::FN; ++j) {
-            const uint32_t col = n0 + (wn * S::FN + j) * 32u + (lane & 31u);
+            const uint32_t row = m0 + (wm * S::FM + i) * 32u, col = n0 + (wn * S::FN + j) * 32u;
+            float v[16];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t row = m0 + (wm * S::FM + i) * 32u + 8u * q + 4u * h;
-                if (KIND == kFinal) {
+            for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e] * p.scale;
+            if (KIND == kPartial) {
+                store_partial(p, v, z * p.splits + split_k, row, col, lane);
+                continue;
+            }
+            if (KIND == kPoly) add_lower_terms(p, v, z, row, col, lane);
+            store_split(p, v, z, row, col, lane, KIND == kApply || tm != tn);
+        }
+}
+
+// G from the partial sums of its contraction, added in order, 32 x 32 at a time, both halves.  A lane has one row's number of each of four
+// rows and eight pieces in flight: the sums are few and far apart.
+__global__ void __launch_bounds__(256) k_orthogonal_gram_sum(const OParams p) {
+    __shared__ float tile[32][33];
+    uint32_t ti, tj;
+    upper_tile(blockIdx.x, ti, tj);
+    const uint32_t r0 = ti * 32u, c0 = tj * 32u, z = blockIdx.y;
+    const uint32_t tx = threadIdx.x & 31u, ty = threadIdx.x >> 5;
+    const uint64_t all = (uint64_t)p.M * p.M;
+    const float* from = p.partial + (uint64_t)z * p.splits * all;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float* at[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (row + r >= p.M || col >= p.N) continue;
-                        const uint64_t o = ((uint64_t)z * p.M + row + r) * p.N + col;
-                        const float v = acc[i][j][4 * q + r] * p.scale;
-                        if (p.out) {
-                            if (DT == QESGD_F32) ((float*)p.out)[o] = v;
-                            else if (DT == QESGD_F16) ((_Float16*)p.out)[o] = (_Float16)v;
-                            else ((__bf16*)p.out)[o] = (__bf16)v;
-                        }
-                        if (p.z) {
-                            const float zv = p.z[o] + v;
-                            p.z[o] = zv;
-                            if (p.u) p.u[o] = p.w[o] + zv;
-                            if (p.zsum) p.zsum[o] += zv;
-                        }
-                    }
-                    continue;
-                }
-                float v[4];
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t r = r0 + ty + 8u * i, c = c0 + tx;
+        at[i] = from + (uint64_t)min(r, p.M - 1u) * p.M + min(c, p.M - 1u);
+    }
+    for (uint32_t k0 = 0; k0 < p.splits; k0 += 8) {
+        float x[8][4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r] * p.scale;
-                if (KIND == kPoly && col < p.N && row < p.M) {
-                    // G[row.., col] = G[col, row..]: four in a row; its padding is there and zero
-                    const unsigned char* g = p.a + z * p.a_bytes + (uint64_t)col * p.pitch + split_at(row);
+        for (uint32_t k = 0; k < 8; ++k)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float gv = (float)((const _Float16*)g)[r] + (float)((const _Float16*)(g + 64))[r];
-                        v[r] = v[r] + p.cb * gv + (row + r == col ? p.ca : 0.0f);
-                    }
-                }
-                _Float16 hi[4], lo[4];
+            for (int i = 0; i < 4; ++i) x[k][i] = at[i][(uint64_t)min(k0 + k, p.splits - 1u) * all];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) split(row + r < p.M && col < p.N ? v[r] : 0.0f, hi[r], lo[r]);
-                if (col < p.N && row * 4u < p.d2_pitch) {
-                    unsigned char* to = p.d2 + z * p.d2_bytes + (uint64_t)col * p.d2_pitch + split_at(row);
+        for (uint32_t k = 0; k < 8; ++k)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) { ((_Float16*)to)[r] = hi[r]; ((_Float16*)(to + 64))[r] = lo[r]; }
-                }
-                if (KIND == kApply || tm != tn) {
+            for (int i = 0; i < 4; ++i) v[i] += k0 + k < p.splits ? x[k][i] : 0.0f;
+    }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (row + r < p.M && col * 4u < p.d1_pitch) {
-                            unsigned char* to = p.d1 + z * p.d1_bytes + (uint64_t)(row + r) * p.d1_pitch + split_at(col);
-                            *(_Float16*)to = hi[r];
-                            *(_Float16*)(to + 64) = lo[r];
-                        }
-                    }
-                }
+    for (int i = 0; i < 4; ++i) tile[ty + 8 * i][tx] = r0 + ty + 8u * i < p.M && c0 + tx < p.M ? v[i] : 0.0f;
+    __syncthreads();
+    unsigned char* G = p.d1 + z * p.d1_bytes;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t i = ty + 8u * k;
+        _Float16 hi, lo;
+        if (r0 + i < p.M) {
+            // below the diagonal, inside its tile, the mirror's number: both halves of a product are the same bits
+            split(ti == tj && i > tx ? tile[tx][i] : tile[i][tx], hi, lo);
+            unsigned char* to = G + (uint64_t)(r0 + i) * p.d1_pitch + split_at(c0 + tx);
+            *(_Float16*)to = hi;
+            *(_Float16*)(to + 64) = lo;
+        }
+        if (ti != tj && c0 + i < p.M) {
+            split(tile[tx][i], hi, lo);
+            unsigned char* to = G + (uint64_t)(c0 + i) * p.d1_pitch + split_at(r0 + tx);
+            *(_Float16*)to = hi;
+            *(_Float16*)(to + 64) = lo;
+        }
+    }
+}
+
+// A whole matrix in one workgroup: X, its transpose and one m x m matrix (G, then P in its place) stay in LDS as split rows for all
+// steps, so a call is one launch and reads and writes its operands once.  Which shapes fit: small_layout().
+//
+// What bounds it is its chain of short phases, a barrier apart, so the work is cut into 16 x 16 tiles, whose matrix instruction takes
+// a whole group of 32 numbers at once, and dealt to 16 waves.  A step: the tiles of G's upper half, where they are few the contraction
+// in pieces to several waves whose sums one wave adds in order; P = a I + b G + c G G by the same waves; P X tile by tile, held in
+// registers until every wave has read X.  Rows are groups of 128 bytes, chunks placed as in the pipeline.  64 x 64, 16 of them: 72 us as
+// the launches of the general path, 31 us with 32 x 32 tiles on 8 waves.
+constexpr uint32_t kSmallWaves = 16, kSmallThreads = kSmallWaves * 64;
+constexpr uint32_t kSmallHeld = 4;       // tiles of P X that a wave holds
+constexpr uint32_t kSmallEach = kSmallHeld * 256 / 64;       // elements that a thread reads
+typedef float acc4 __attribute__((ext_vector_type(4)));
+
+struct SmallLayout {
+    uint32_t mt, nt;                     // tiles along the sides
+    uint32_t mg, ng;                     // groups of 32 along the sides
+    uint32_t tiles, pieces;              // of G's upper half; of the contraction
+    uint32_t Xt, G, partial, total;      // bytes: X lies at 0
+};
+
+// total = 0 where the matrix does not fit.
+inline SmallLayout small_layout(uint64_t m, uint64_t n) {
+    SmallLayout L{};
+    if (m > 96 || n > 1024) return L;
+    L.mt = (uint32_t)(m + 15) / 16;
+    L.nt = (uint32_t)(n + 15) / 16;
+    L.mg = (uint32_t)(m + 31) / 32;
+    L.ng = (uint32_t)(n + 31) / 32;
+    L.tiles = L.mt * (L.mt + 1) / 2;
+    L.pieces = L.tiles < kSmallWaves ? kSmallWaves / L.tiles : 1;
+    if (L.pieces > L.ng) L.pieces = L.ng;
+    L.Xt = L.mt * 16 * L.ng * 128;
+    L.G = L.Xt + L.nt * 16 * L.mg * 128;
+    L.partial = L.G + L.mt * 16 * L.mg * 128;
+    L.total = L.partial + (L.pieces - 1) * L.tiles * 1024;
+    if (L.total > kLdsBytes - 8 * kSmallWaves || L.mt * L.nt > kSmallHeld * kSmallWaves) L.total = 0;
+    return L;
+}
+
+struct SmallParams {
+    SParams s;
+    OParams o;                           // of the last product
+    SmallLayout L;
+    uint32_t steps;
+    float coeffs[3 * QESGD_MAX_STEPS];
+};
+
+// Byte of number k's hi in a row (its lo: the place with 64 flipped, chunk c + 4 instead of c).
+__device__ __forceinline__ uint32_t place_of(uint32_t row, uint32_t pitch, uint32_t k) {
+    return row * pitch + (k >> 5) * 128u + ((((k & 31u) >> 3) ^ ((row >> 1) & 7u)) * 16u) + (k & 7u) * 2u;
+}
+// A wave's vector instruction takes four cycles and sixteen waves share a CU, so places are put together from few: rows of a tile
+// are 16 apart from the next tile's, which leaves the swizzle (row / 2 & 7) alone.
+struct SmallPlaces {
+    uint32_t read, col, row, pitch;
+    // lane: row lane & 15, numbers 8 (lane / 16) .. + 7 of a group (read); row lane & 15, numbers 4 (lane / 16) .. + 3 (col);
+    // rows 4 (lane / 16) .. + 3, number lane & 15 (row)
+    __device__ __forceinline__ SmallPlaces(uint32_t lane, uint32_t pitch_) : pitch(pitch_) {
+        read = place_of(lane & 15u, pitch, 8u * (lane >> 4));
+        col = place_of(lane & 15u, pitch, 4u * (lane >> 4));
+        row = place_of(4u * (lane >> 4), pitch, lane & 15u);
+    }
+};
+__device__ __forceinline__ half8 read8(const unsigned char* p) { return *(const half8*)p; }
+
+// acc += A B^T over `groups` groups from g on, `by` apart; A and B: the tiles' first rows.  A lane's operand is one chunk of its row.
+__device__ __forceinline__ acc4 small_product(const unsigned char* A, uint32_t a, const unsigned char* B, uint32_t b, uint32_t g, uint32_t groups, uint32_t by) {
+    acc4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    const unsigned char *ah = A + a, *al = A + (a ^ 64u), *bh = B + b, *bl = B + (b ^ 64u);
+    for (; g < groups; g += by) {
+        const half8 vah = read8(ah + g * 128u), vbh = read8(bh + g * 128u), vbl = read8(bl + g * 128u), val = read8(al + g * 128u);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vah, vbh, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vah, vbl, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, vbh, acc, 0, 0, 0);
+    }
+    return acc;
+}
+// Tile (tr, tc): a lane holds column lane & 15 and rows 4 (lane / 16) .. + 3.  Its transpose goes to by_col, and with by_row itself there.
+__device__ __forceinline__ void put_tile(unsigned char* by_row, const SmallPlaces& pr, unsigned char* by_col, const SmallPlaces& pc, uint32_t tr,
+                                         uint32_t tc, const acc4& v) {
+    half4 hi, lo;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        _Float16 a, b;
+        split(v[r], a, b);
+        hi[r] = a;
+        lo[r] = b;
+    }
+    unsigned char* c = by_col + tc * 16u * pc.pitch + (tr >> 1) * 128u;
+    const uint32_t at = pc.col ^ ((tr & 1u) * 32u);
+    *(half4*)(c + at) = hi;
+    *(half4*)(c + (at ^ 64u)) = lo;
+    if (by_row) {
+        unsigned char* w = by_row + tr * 16u * pr.pitch + (tc >> 1) * 128u;
+        const uint32_t at0 = pr.row ^ ((tc & 1u) * 32u);
+#pragma unroll
+        for (uint32_t r = 0; r < 4; ++r) {
+            const uint32_t at1 = (at0 ^ ((r >> 1) * 16u));                  // rows 2 and 3: the next swizzle
+            *(_Float16*)(w + at1 + r * pr.pitch) = hi[r];
+            *(_Float16*)(w + (at1 ^ 64u) + r * pr.pitch) = lo[r];
+        }
+    }
+}
+
+template <uint32_t DT>
+__global__ void __launch_bounds__(kSmallThreads) k_orthogonal_small(const SmallParams p) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char X[];       // mt * 16 rows
+    __shared__ double sums[kSmallWaves];
+    const SmallLayout& L = p.L;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), z = blockIdx.x, lane = threadIdx.x & 63u;
+    SmallPlaces px(lane, L.ng * 128u), pg(lane, L.mg * 128u);
+    unsigned char* const Xt = X + L.Xt;                       // nt * 16 rows
+    unsigned char* const G = X + L.G;                         // mt * 16 rows
+    acc4* const partial = (acc4*)(X + L.partial);
+
+    // the momentum and the norm, as in k_orthogonal_momentum; what a thread has read it keeps
+    const uint64_t base = (uint64_t)z * p.s.d;
+    const uint32_t d = (uint32_t)p.s.d;
+    float x[kSmallEach];
+#pragma unroll
+    for (uint32_t k = 0; k < kSmallEach; ++k) {
+        const uint32_t i = k * kSmallThreads + threadIdx.x;
+        x[k] = i < d ? fetch<DT>(p.s.x, base + i) : 0.0f;
+    }
+    if (p.s.momentum) {
+        float m[kSmallEach];
+#pragma unroll
+        for (uint32_t k = 0; k < kSmallEach; ++k) {
+            const uint32_t i = k * kSmallThreads + threadIdx.x;
+            m[k] = i < d ? p.s.momentum[base + i] : 0.0f;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kSmallEach; ++k) {
+            const uint32_t i = k * kSmallThreads + threadIdx.x;
+            m[k] = p.s.mu * m[k] + x[k];
+            if (i < d) p.s.momentum[base + i] = m[k];
+            x[k] = p.s.nesterov ? x[k] + p.s.mu * m[k] : m[k];
+        }
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (uint32_t k = 0; k < kSmallEach; ++k) sum += (double)x[k] * (double)x[k];
+    if (((p.s.rows | p.s.cols) & 31u) != 0)                   // zeros behind the ends
+        for (uint32_t i = threadIdx.x * 16u; i < L.partial; i += kSmallThreads * 16u) *(uint4*)(X + i) = make_uint4(0, 0, 0, 0);
+    sum = wave_sum(sum);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (uint32_t i = 0; i < kSmallWaves; ++i) sum += sums[i];
+    const double norm = sqrt(sum) + (double)p.s.eps;
+    const double scale = norm > 0.0 ? (double)kScaleX / norm : 0.0;
+    const bool turned = p.s.rows > p.s.cols;
+    {
+        uint32_t r = threadIdx.x / p.s.cols, c = threadIdx.x - r * p.s.cols;
+        const uint32_t dr = kSmallThreads / p.s.cols, dc = kSmallThreads - dr * p.s.cols;
+#pragma unroll
+        for (uint32_t k = 0; k < kSmallEach; ++k) {
+            if (k * kSmallThreads + threadIdx.x < d) {
+                _Float16 hi, lo;
+                split((float)((double)x[k] * scale), hi, lo);
+                const uint32_t at = place_of(turned ? c : r, px.pitch, turned ? r : c), bt = place_of(turned ? r : c, pg.pitch, turned ? c : r);
+                *(_Float16*)(X + at) = hi;
+                *(_Float16*)(X + (at ^ 64u)) = lo;
+                *(_Float16*)(Xt + bt) = hi;
+                *(_Float16*)(Xt + (bt ^ 64u)) = lo;
+            }
+            r += dr;
+            c += dc;
+            if (c >= p.s.cols) { c -= p.s.cols; ++r; }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    __syncthreads();
+
+    // A wave has up to two tiles of G (21 at most), or a piece of one, and up to kSmallHeld of P X.
+    const bool split_up = L.pieces > 1;
+    const uint32_t piece = split_up ? __builtin_amdgcn_readfirstlane(wave / L.tiles) : 0;
+    uint32_t ti[2], tj[2], it[kSmallHeld], jt[kSmallHeld];
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k) {
+        upper_tile(min(wave + k * kSmallWaves - piece * L.tiles, L.tiles - 1), ti[k], tj[k]);
+        ti[k] = __builtin_amdgcn_readfirstlane(ti[k]);
+        tj[k] = __builtin_amdgcn_readfirstlane(tj[k]);
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < kSmallHeld; ++k) {
+        jt[k] = __builtin_amdgcn_readfirstlane((wave + k * kSmallWaves) / L.mt);
+        it[k] = wave + k * kSmallWaves - jt[k] * L.mt;
+    }
+    const uint32_t l = lane & 15u, quad = lane >> 4;
+    acc4 y[kSmallHeld] = {};
+    for (uint32_t step = 0;; ++step) {
+        // sums with these are formed where they are used: kept over the steps, they spill
+        asm volatile("" : "+v"(px.read), "+v"(px.col), "+v"(pg.read), "+v"(pg.col), "+v"(pg.row));
+        const float ca = p.coeffs[3 * step], cb = p.coeffs[3 * step + 1], cc = p.coeffs[3 * step + 2];
+        acc4 g[2] = {};
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+            if (k == 0 ? wave < L.tiles * L.pieces : wave + kSmallWaves < L.tiles) {
+                g[k] = small_product(X + ti[k] * 16u * px.pitch, px.read, X + tj[k] * 16u * px.pitch, px.read, piece, L.ng, L.pieces);
+                if (piece > 0) partial[(wave - L.tiles) * 64u + lane] = g[k];
             }
         }
+        if (split_up) __syncthreads();
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+            if (wave + k * kSmallWaves < L.tiles) {
+                for (uint32_t i = 1; i < L.pieces; ++i) g[k] += partial[((i - 1) * L.tiles + wave) * 64u + lane];
+                g[k] *= kScaleG / (kScaleX * kScaleX);
+                put_tile(ti[k] != tj[k] ? G : nullptr, pg, G, pg, ti[k], tj[k], g[k]);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k) {
+            if (wave + k * kSmallWaves < L.tiles) {
+                const acc4 gg = small_product(G + ti[k] * 16u * pg.pitch, pg.read, G + tj[k] * 16u * pg.pitch, pg.read, 0, L.mg, 1);
+                const bool diagonal = ti[k] == tj[k];
+#pragma unroll
+                for (uint32_t r = 0; r < 4; ++r)
+                    g[k][r] = gg[r] * (cc * (kScaleP / (kScaleG * kScaleG))) + (cb * (kScaleP / kScaleG)) * g[k][r] +
+                              (diagonal && quad * 4u + r == l ? ca * kScaleP : 0.0f);
+            }
+        }
+        __syncthreads();                                      // G has been read
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k)
+            if (wave + k * kSmallWaves < L.tiles) put_tile(ti[k] != tj[k] ? G : nullptr, pg, G, pg, ti[k], tj[k], g[k]);
+        __syncthreads();
+        const bool last = step + 1 == p.steps;
+#pragma unroll
+        for (uint32_t k = 0; k < kSmallHeld; ++k) {
+            const unsigned char *P = G + it[k] * 16u * pg.pitch, *T = Xt + jt[k] * 16u * pg.pitch;
+            // numbers of a row of the caller's matrix along the lanes where the result leaves: P X as it is, or its transpose
+            const bool straight = last && !turned;
+            if (jt[k] < L.nt) y[k] = small_product(straight ? P : T, pg.read, straight ? T : P, pg.read, 0, L.mg, 1);
+        }
+        if (last) break;
+        __syncthreads();                                      // the transpose has been read
+#pragma unroll
+        for (uint32_t k = 0; k < kSmallHeld; ++k) {
+            y[k] *= 1.0f / kScaleP;
+            if (jt[k] < L.nt) put_tile(Xt, pg, X, px, jt[k], it[k], y[k]);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < kSmallHeld; ++k)
+        if (jt[k] < L.nt) finish<DT, 4>(p.o, y[k], z, (turned ? jt[k] : it[k]) * 16u + quad * 4u, (turned ? it[k] : jt[k]) * 16u + l);
+}
+
+// Which tiles, and how many pieces of the contraction, from how long the workgroups take on 256 CUs.  Unit: a step of 512 workgroups
+// with 128 x 128 tiles, two a CU, 1.1 us of a full chip.  A last round of up to 256 has a CU each and takes 0.62 of that.  64 x 64: 0.40 (a
+// quarter of the work; each step reads twice as much for it).  256 x 256, one a CU: 1.86 a round (four times the work of a CU's
+// 128s, 0.93 of their time).  Measured on 20 shapes from 128 x 128 to 4096 x 25088, one product changed at a time, five steps, us:
+//   P X       512 x 4608, 2 of them 64: 349, 128: 360;  2048 x 2048 824 / 785;  1024 x 8192 699 / 640, 256: 725;  3000 x 3000 2398 / 2358 /
+//             2455;  2048 x 8192 2403 / 2153 / 2094;  4096 x 25088 28.2 / 24.3 / 24.7 ms
+//   G G       1024 x 1024, 12 of them 64: 1201, 128: 1143, 256: 1332;  4096 x 4096 5750 / 5306 / 5457
+//   X X^T     512 x 4096 64 in 1: 259, in 6: 191, 128 in 6: 233;  1024 x 8192 699 / 653 / 641;  4096 x 25088 64 in 3: 27.6, 128 in 3: 22.9, 256 in
+//             1: 24.7, in 3: 22.5 ms
+struct Cut { uint32_t edge, pieces; };
+
+double cut_cost(uint64_t groups, uint32_t edge) {
+    const uint64_t slots = edge == 256 ? 256 : 512, left = groups % slots;
+    const double rounds = (double)(groups / slots) + (left == 0 ? 0.0 : edge != 256 && left <= 256 ? 0.62 : 1.0);
+    return rounds * (edge == 256 ? 1.86 : edge == 128 ? 1.0 : 0.40);
+}
+
+// M x N (upper = M x M, the upper half) over `steps` steps, `count` of them; more than one piece only for upper.
+Cut choose_cut(uint64_t M, uint64_t N, uint64_t steps, uint64_t count, bool upper, uint32_t most_pieces) {
+    Cut best{64, 1};
+    double least = 1e300;
+    for (uint32_t edge : {64u, 128u, 256u}) {
+        const uint64_t tm = (M + edge - 1) / edge, tn = (N + edge - 1) / edge, tiles = (upper ? tm * (tm + 1) / 2 : tm * tn) * count;
+        for (uint32_t pieces = 1; pieces <= most_pieces && pieces * 4ull <= steps + 3ull; ++pieces) {
+            // a piece has at least four steps; the sums of the pieces cost a launch, and are written and read at about 4 TB/s
+            const double sums = pieces == 1 ? 0.0 : 3.0 + (double)pieces * (double)count * (double)(M * M) * 2e-6;
+            const double cost = cut_cost(tiles * pieces, edge) * (double)((steps + pieces - 1) / pieces) * 1.1 + sums;
+            if (cost < least) {
+                least = cost;
+                best = Cut{edge, pieces};
+            }
+        }
+    }
+    return best;
 }
 
 // Workspace: partial sums, X, two of its transpose, G, P.
@@ -301,7 +742,8 @@ struct Plan {
     uint64_t m, n;                       // shorter and longer side
     uint32_t parts;
     uint64_t X_pitch, Xt_pitch, G_pitch, X_bytes, Xt_bytes, G_bytes;
-    uint64_t X, Xt[2], G, P, total;
+    uint64_t X, Xt[2], G, P, partial, total;
+    Cut gram, poly, apply;
 };
 
 Plan make_plan(uint64_t rows, uint64_t cols, uint32_t count) {
@@ -322,27 +764,51 @@ Plan make_plan(uint64_t rows, uint64_t cols, uint32_t count) {
     p.Xt[1] = take(p.Xt_bytes);
     p.G = take(p.G_bytes);
     p.P = take(p.G_bytes);
+    p.gram = choose_cut(p.m, p.m, p.X_pitch / kStepBytes, count, true, 16);
+    p.poly = choose_cut(p.m, p.m, p.G_pitch / kStepBytes, count, true, 1);
+    p.apply = choose_cut(p.m, p.n, p.G_pitch / kStepBytes, count, false, 1);
+    p.partial = at;
+    if (p.gram.pieces > 1) take(p.gram.pieces * p.m * p.m * 4);
     p.total = at;
     return p;
 }
 
-template <class S, int KIND, uint32_t DT>
-int launch_product(OParams& p, uint32_t count, hipStream_t stream) {
-    p.tiles_m = (p.M + S::BM - 1) / S::BM;
-    p.tiles_n = (p.N + S::BN - 1) / S::BN;
-    p.steps = p.pitch / kStepBytes;
-    const uint64_t tiles = KIND == kGram || KIND == kPoly ? (uint64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (uint64_t)p.tiles_m * p.tiles_n;
-    if (tiles >= (1ull << 31)) return QESGD_ERR_DIM;
-    k_orthogonal_product<S, KIND, DT><<<dim3((uint32_t)tiles, count), S::threads, 0, stream>>>(p);
+int launched() {
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return QESGD_OK;
     set_last_hip_error((int)e);
     return QESGD_ERR_HIP;
 }
 
+template <class S, int KIND, uint32_t DT>
+int launch_product_as(OParams& p, uint32_t count, hipStream_t stream) {
+    constexpr bool symmetric = KIND == kGram || KIND == kPoly || KIND == kPartial;
+    p.tiles_m = (p.M + S::BM - 1) / S::BM;
+    p.tiles_n = (p.N + S::BN - 1) / S::BN;
+    const uint64_t tiles = symmetric ? (uint64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (uint64_t)p.tiles_m * p.tiles_n;
+    if (tiles * p.splits * count >= (1ull << 31)) return QESGD_ERR_DIM;
+    p.tiles = (uint32_t)tiles;
+    k_orthogonal_product<S, KIND, DT><<<p.tiles * p.splits * count, S::threads, 0, stream>>>(p);
+    return launched();
+}
+
+typedef TileShape<2, 4, 4, 2, 2> Tile256;
+typedef TileShape<2, 2, 2, 2, 2> Tile128;
+typedef TileShape<2, 2, 1, 1, 4> Tile64;
+
+template <int KIND, uint32_t DT>
+int launch_product(OParams& p, const Cut& cut, uint32_t count, hipStream_t stream) {
+    p.steps = p.pitch / kStepBytes;
+    p.splits = cut.pieces;
+    switch (cut.edge) {
+        case 256: return launch_product_as<Tile256, KIND, DT>(p, count, stream);
+        case 128: return launch_product_as<Tile128, KIND, DT>(p, count, stream);
+        default: return launch_product_as<Tile64, KIND, DT>(p, count, stream);
+    }
+}
+
 template <uint32_t DT>
 int launch_type(const Orthogonalize& a) {
-    typedef TileShape<2, 2, 2, 2> S;
     const Plan pl = make_plan(a.rows, a.cols, a.n);
     const bool turned = a.rows > a.cols;
     SParams s{};
@@ -362,8 +828,28 @@ int launch_type(const Orthogonalize& a) {
     s.Xt_bytes = pl.Xt_bytes;
     s.X_pitch = (uint32_t)pl.X_pitch;
     s.Xt_pitch = (uint32_t)pl.Xt_pitch;
+    const SmallLayout small = small_layout(pl.m, pl.n);
+    if (small.total) {
+        SmallParams p{};
+        p.s = s;
+        p.L = small;
+        p.steps = a.steps;
+        for (uint32_t i = 0; i < 3 * a.steps; ++i) p.coeffs[i] = a.coeffs[i];
+        p.o.M = (uint32_t)a.rows;
+        p.o.N = (uint32_t)a.cols;
+        p.o.scale = a.alpha / (kScaleP * kScaleX);
+        p.o.out = a.out;
+        p.o.z = a.z;
+        p.o.w = a.w;
+        p.o.u = a.u;
+        p.o.zsum = a.zsum;
+        k_orthogonal_small<DT><<<a.n, kSmallThreads, small.total, a.stream>>>(p);
+        return launched();
+    }
     k_orthogonal_momentum<DT><<<dim3(pl.parts, a.n), 256, 0, a.stream>>>(s);
+    if (const int rc = launched(); rc != QESGD_OK) return rc;
     k_orthogonal_split<DT><<<dim3((uint32_t)((a.cols + 63) / 64), (uint32_t)((a.rows + 63) / 64), a.n), 256, 0, a.stream>>>(s);
+    if (const int rc = launched(); rc != QESGD_OK) return rc;
 
     for (uint32_t i = 0; i < a.steps; ++i) {
         const float ca = a.coeffs[3 * i], cb = a.coeffs[3 * i + 1], cc = a.coeffs[3 * i + 2];
@@ -377,7 +863,17 @@ int launch_type(const Orthogonalize& a) {
         g.d1_bytes = g.d2_bytes = pl.G_bytes;
         g.d1_pitch = g.d2_pitch = (uint32_t)pl.G_pitch;
         g.scale = kScaleG / (kScaleX * kScaleX);
-        int rc = launch_product<S, kGram, 0>(g, a.n, a.stream);
+        int rc;
+        if (pl.gram.pieces > 1) {
+            g.partial = (float*)(a.workspace + pl.partial);
+            rc = launch_product<kPartial, 0>(g, pl.gram, a.n, a.stream);
+            if (rc != QESGD_OK) return rc;
+            const uint32_t t = (g.M + 31u) / 32u;
+            k_orthogonal_gram_sum<<<dim3(t * (t + 1) / 2, a.n), 256, 0, a.stream>>>(g);
+            rc = launched();
+        } else {
+            rc = launch_product<kGram, 0>(g, pl.gram, a.n, a.stream);
+        }
         if (rc != QESGD_OK) return rc;
         OParams q = g;
         q.a = q.b = a.workspace + pl.G;
@@ -387,7 +883,7 @@ int launch_type(const Orthogonalize& a) {
         q.scale = cc * (kScaleP / (kScaleG * kScaleG));
         q.ca = ca * kScaleP;
         q.cb = cb * (kScaleP / kScaleG);
-        rc = launch_product<S, kPoly, 0>(q, a.n, a.stream);
+        rc = launch_product<kPoly, 0>(q, pl.poly, a.n, a.stream);
         if (rc != QESGD_OK) return rc;
         OParams x{};
         x.a = a.workspace + pl.P;
@@ -405,7 +901,7 @@ int launch_type(const Orthogonalize& a) {
             x.d2_bytes = pl.Xt_bytes;
             x.d2_pitch = (uint32_t)pl.Xt_pitch;
             x.scale = 1.0f / kScaleP;
-            rc = launch_product<S, kApply, 0>(x, a.n, a.stream);
+            rc = launch_product<kApply, 0>(x, pl.apply, a.n, a.stream);
         } else {
             if (turned) {                // (P X)^T = Xt P, rows as the caller has them
                 OParams y = x;
@@ -419,7 +915,7 @@ int launch_type(const Orthogonalize& a) {
             x.w = a.w;
             x.u = a.u;
             x.zsum = a.zsum;
-            rc = launch_product<S, kFinal, DT>(x, a.n, a.stream);
+            rc = launch_product<kFinal, DT>(x, pl.apply, a.n, a.stream);
         }
         if (rc != QESGD_OK) return rc;
     }
@@ -428,7 +924,10 @@ int launch_type(const Orthogonalize& a) {
 
 }  // namespace
 
-size_t orthogonalize_workspace(uint64_t rows, uint64_t cols, uint32_t n) { return make_plan(rows, cols, n).total; }
+size_t orthogonalize_workspace(uint64_t rows, uint64_t cols, uint32_t n) {
+    if (small_layout(rows < cols ? rows : cols, rows < cols ? cols : rows).total) return 0;
+    return make_plan(rows, cols, n).total;
+}
 
 int launch_orthogonalize(const Orthogonalize& a) {
     switch (a.dtype) {

@@ -44,11 +44,12 @@ def allowed(x, want, coeffs, half_step, eps=EPS):
 
 def ws_for(B, rows, cols, n):
     need = B.qesgd_orthogonalize_workspace_bytes(rows, cols, n)
-    return B.alloc_workspace(need).fill_(0xFF)                 # NaN everywhere: nothing may be read before it is written
+    return B.alloc_workspace(need).fill_(0xFF) if need else None       # NaN everywhere: nothing may be read before it is written
 
 
 SHAPES = [(1, 1), (1, 7), (9, 1), (2, 2), (5, 3), (16, 16), (31, 33), (32, 32), (33, 31), (64, 64), (64, 576), (65, 130), (100, 100), (127, 129),
-          (129, 127), (128, 512), (300, 64), (500, 40), (200, 333), (257, 256), (384, 640), (1000, 520)]
+          (129, 127), (128, 512), (300, 64), (500, 40), (200, 333), (257, 256), (384, 640), (1000, 520),
+          (96, 96), (48, 341), (17, 900), (16, 1024), (64, 256), (64, 257), (96, 170), (97, 97), (1024, 90), (130, 2100), (600, 1800)]
 
 
 @pytest.mark.parametrize("kind", ["plain", "decay", "rank1"])

@@ -40,11 +40,11 @@ def coeffs(values=(3.4445, -4.7750, 2.0315)):
 def test_orthogonalize_refusals(B):
     """Addresses that are none: every call is turned down before a launch."""
     f = B.lib().qesgd_orthogonalize
-    need = B.qesgd_orthogonalize_workspace_bytes(30, 40, 2)
-    assert need > 0
+    need = B.qesgd_orthogonalize_workspace_bytes(300, 400, 2)
+    assert need > 0 and B.qesgd_orthogonalize_workspace_bytes(30, 40, 2) == 0
     x, o, ws = 0x10000, 0x20000, 0x30000
 
-    def rc(x=x, dtype=0, rows=30, cols=40, n=2, c=coeffs(), steps=1, eps=1e-7, o=o, ws=ws, size=need):
+    def rc(x=x, dtype=0, rows=300, cols=400, n=2, c=coeffs(), steps=1, eps=1e-7, o=o, ws=ws, size=need):
         return f(x, dtype, rows, cols, n, c, steps, eps, o, ws, size, None)
 
     assert rc(x=None) == B.ERR_NULL and rc(o=None) == B.ERR_NULL and rc(c=None) == B.ERR_NULL
@@ -63,11 +63,11 @@ def test_orthogonalize_refusals(B):
 
 def test_update_refusals(B):
     f = B.lib().qesgd_orthogonal_update
-    need = B.qesgd_orthogonalize_workspace_bytes(30, 40, 1)
+    need = B.qesgd_orthogonalize_workspace_bytes(300, 400, 1)
     g, m, s, z, w, u, zs, ws = (0x10000 * i for i in range(1, 9))
 
     def rc(g=g, m=m, mu=0.9, alpha=-0.1, s=s, z=z, w=w, u=u, zs=zs, size=need):
-        return f(g, 30, 40, 1, m, mu, 1, coeffs(), 1, 1e-7, alpha, s, z, w, u, zs, ws, size, None)
+        return f(g, 300, 400, 1, m, mu, 1, coeffs(), 1, 1e-7, alpha, s, z, w, u, zs, ws, size, None)
 
     assert rc(g=None) == B.ERR_NULL
     assert rc(s=None, z=None, w=None, u=None, zs=None) == B.ERR_NULL
