@@ -15,6 +15,7 @@
 // contraction, which takes X for X X^T and its transpose for P X: the last product's epilogue writes both.  G and P are symmetric:
 // only tiles on and above the diagonal are computed, and the epilogue writes them twice.
 #include <type_traits>
+#include <utility>
 
 #include "qesgd_device.h"
 #include "qesgd_matrix.h"
@@ -25,7 +26,7 @@ namespace {
 
 constexpr float kScaleX = 4096.0f;      // of X's entries (at most 1 at first; singular values near 1 keep them there): below 16
 constexpr float kScaleG = 4096.0f;      // of G's
-constexpr float kScaleP = 2048.0f;      // of P's: below 32
+constexpr float kScaleP = 256.0f;       // of P's, and of a product of two P: below 256
 
 inline uint64_t split_pitch(uint64_t k) { return round_up_to(k, 32) * 4; }
 
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(256) k_orthogonal_split(const SParams p) {
     }
 }
 
-enum { kGram = 0, kPoly = 1, kApply = 2, kFinal = 3, kPartial = 4 };
+enum { kGram = 0, kPoly = 1, kApply = 2, kFinal = 3, kPartial = 4 };   // kGram: any symmetric product
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 
 struct OParams {
@@ -520,9 +521,10 @@ __device__ __forceinline__ acc4 small_product(const unsigned char* A, uint32_t a
     const unsigned char *ah = A + a, *al = A + (a ^ 64u), *bh = B + b, *bl = B + (b ^ 64u);
     for (; g < groups; g += by) {
         const half8 vah = read8(ah + g * 128u), vbh = read8(bh + g * 128u), vbl = read8(bl + g * 128u), val = read8(al + g * 128u);
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vah, vbh, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, vbl, acc, 0, 0, 0);       // here it costs next to nothing
         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vah, vbl, acc, 0, 0, 0);
         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, vbh, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vah, vbh, acc, 0, 0, 0);
     }
     return acc;
 }
@@ -702,48 +704,48 @@ __global__ void __launch_bounds__(kSmallThreads) k_orthogonal_small(const SmallP
 }
 
 // Which tiles, and how many pieces of the contraction, from how long the workgroups take on 256 CUs.  Unit: a step of 512 workgroups
-// with 128 x 128 tiles, two a CU, 1.1 us of a full chip.  A last round of up to 256 has a CU each and takes 0.62 of that.  64 x 64: 0.40 (a
-// quarter of the work; each step reads twice as much for it).  256 x 256, one a CU: 1.86 a round (four times the work of a CU's
-// 128s, 0.93 of their time).  Measured on 20 shapes from 128 x 128 to 4096 x 25088, one product changed at a time, five steps, us:
+// with 128 x 128 tiles, two a CU, 1.1 us of a full chip, and 3 us for a launch.  A last round of up to 256 has a CU each and takes 0.70 of that.  64 x 64: 0.38 (a
+// quarter of the work; each step reads twice as much for it).  256 x 256, one a CU: 1.78 a round (twice the work of a CU's two
+// 128s, 0.89 of the time).  Measured on 20 shapes from 128 x 128 to 4096 x 25088, one product changed at a time, five steps, us:
 //   P X       512 x 4608, 2 of them 64: 349, 128: 360;  2048 x 2048 824 / 785;  1024 x 8192 699 / 640, 256: 725;  3000 x 3000 2398 / 2358 /
 //             2455;  2048 x 8192 2403 / 2153 / 2094;  4096 x 25088 28.2 / 24.3 / 24.7 ms
 //   G G       1024 x 1024, 12 of them 64: 1201, 128: 1143, 256: 1332;  4096 x 4096 5750 / 5306 / 5457
 //   X X^T     512 x 4096 64 in 1: 259, in 6: 191, 128 in 6: 233;  1024 x 8192 699 / 653 / 641;  4096 x 25088 64 in 3: 27.6, 128 in 3: 22.9, 256 in
 //             1: 24.7, in 3: 22.5 ms
-struct Cut { uint32_t edge, pieces; };
+struct Cut {
+    uint32_t edge, pieces;
+    double us;                           // by this reckoning
+};
 
 double cut_cost(uint64_t groups, uint32_t edge) {
     const uint64_t slots = edge == 256 ? 256 : 512, left = groups % slots;
-    const double rounds = (double)(groups / slots) + (left == 0 ? 0.0 : edge != 256 && left <= 256 ? 0.62 : 1.0);
-    return rounds * (edge == 256 ? 1.86 : edge == 128 ? 1.0 : 0.40);
+    const double rounds = (double)(groups / slots) + (left == 0 ? 0.0 : edge != 256 && left <= 256 ? 0.70 : 1.0);
+    return rounds * (edge == 256 ? 1.78 : edge == 128 ? 1.0 : 0.38);
 }
 
 // M x N (upper = M x M, the upper half) over `steps` steps, `count` of them; more than one piece only for upper.
 Cut choose_cut(uint64_t M, uint64_t N, uint64_t steps, uint64_t count, bool upper, uint32_t most_pieces) {
-    Cut best{64, 1};
-    double least = 1e300;
+    Cut best{64, 1, 1e300};
     for (uint32_t edge : {64u, 128u, 256u}) {
         const uint64_t tm = (M + edge - 1) / edge, tn = (N + edge - 1) / edge, tiles = (upper ? tm * (tm + 1) / 2 : tm * tn) * count;
         for (uint32_t pieces = 1; pieces <= most_pieces && pieces * 4ull <= steps + 3ull; ++pieces) {
             // a piece has at least four steps; the sums of the pieces cost a launch, and are written and read at about 4 TB/s
             const double sums = pieces == 1 ? 0.0 : 3.0 + (double)pieces * (double)count * (double)(M * M) * 2e-6;
-            const double cost = cut_cost(tiles * pieces, edge) * (double)((steps + pieces - 1) / pieces) * 1.1 + sums;
-            if (cost < least) {
-                least = cost;
-                best = Cut{edge, pieces};
-            }
+            const double cost = 3.0 + cut_cost(tiles * pieces, edge) * (double)((steps + pieces - 1) / pieces) * 1.1 + sums;
+            if (cost < best.us) best = Cut{edge, pieces, cost};
         }
     }
     return best;
 }
 
-// Workspace: partial sums, X, two of its transpose, G, P.
+// Workspace: partial sums, X, two of its transpose, G, P, for pairs of steps two more like them, and the pieces' sums.
 struct Plan {
     uint64_t m, n;                       // shorter and longer side
     uint32_t parts;
     uint64_t X_pitch, Xt_pitch, G_pitch, X_bytes, Xt_bytes, G_bytes;
-    uint64_t X, Xt[2], G, P, partial, total;
-    Cut gram, poly, apply;
+    uint64_t X, Xt[2], G, P, T, P2, partial, total;
+    Cut gram, square, apply;             // X X^T, products of m x m matrices, P X
+    bool pairs;
 };
 
 Plan make_plan(uint64_t rows, uint64_t cols, uint32_t count) {
@@ -765,8 +767,17 @@ Plan make_plan(uint64_t rows, uint64_t cols, uint32_t count) {
     p.G = take(p.G_bytes);
     p.P = take(p.G_bytes);
     p.gram = choose_cut(p.m, p.m, p.X_pitch / kStepBytes, count, true, 16);
-    p.poly = choose_cut(p.m, p.m, p.G_pitch / kStepBytes, count, true, 1);
+    p.square = choose_cut(p.m, p.m, p.G_pitch / kStepBytes, count, true, 1);
     p.apply = choose_cut(p.m, p.n, p.G_pitch / kStepBytes, count, false, 1);
+    // Two steps at once: G of the second is P G P, and one product takes X through both, P' P X: three products of m x m matrices in the
+    // place of X X^T and P X.  Singly / in pairs, us: 128 x 1024 96 / 101, 512 x 4608, 2 of them 333 / 265, 768 x 1536 216 / 212, 1000 x 2049
+    // 343 / 290, 2048 x 3000 1011 / 1015, 2048 x 8192 1887 / 1567, 4096 x 6000 5921 / 5630, 4096 x 25088 18952 / 13615.  The errors stay those of
+    // single steps where n is much larger than m and grow up to three times for square matrices, hence not below n = 2 m.
+    p.pairs = p.n >= 2 * p.m && p.gram.us + p.apply.us > 3.0 * p.square.us;
+    if (p.pairs) {
+        p.T = take(p.G_bytes);
+        p.P2 = take(p.G_bytes);
+    }
     p.partial = at;
     if (p.gram.pieces > 1) take(p.gram.pieces * p.m * p.m * 4);
     p.total = at;
@@ -851,21 +862,38 @@ int launch_type(const Orthogonalize& a) {
     k_orthogonal_split<DT><<<dim3((uint32_t)((a.cols + 63) / 64), (uint32_t)((a.rows + 63) / 64), a.n), 256, 0, a.stream>>>(s);
     if (const int rc = launched(); rc != QESGD_OK) return rc;
 
-    for (uint32_t i = 0; i < a.steps; ++i) {
-        const float ca = a.coeffs[3 * i], cb = a.coeffs[3 * i + 1], cc = a.coeffs[3 * i + 2];
-        unsigned char* const Xt = a.workspace + pl.Xt[i & 1];
-        OParams g{};
-        g.a = g.b = a.workspace + pl.X;
+    const auto at = [&](uint64_t offset) { return a.workspace + offset; };
+    // d = A B of symmetric matrices that commute, from scale sa sb to sd
+    const auto square = [&](uint64_t A, uint64_t B, uint64_t d, float scale) {
+        OParams o{};
+        o.a = at(A);
+        o.b = at(B);
+        o.a_bytes = o.b_bytes = o.d1_bytes = o.d2_bytes = pl.G_bytes;
+        o.M = o.N = (uint32_t)pl.m;
+        o.pitch = o.d1_pitch = o.d2_pitch = (uint32_t)pl.G_pitch;
+        o.d1 = o.d2 = at(d);
+        o.scale = scale;
+        return o;
+    };
+    const auto poly = [&](uint32_t step, uint64_t d) {
+        const float ca = a.coeffs[3 * step], cb = a.coeffs[3 * step + 1], cc = a.coeffs[3 * step + 2];
+        OParams o = square(pl.G, pl.G, d, cc * (kScaleP / (kScaleG * kScaleG)));
+        o.ca = ca * kScaleP;
+        o.cb = cb * (kScaleP / kScaleG);
+        return launch_product<kPoly, 0>(o, pl.square, a.n, a.stream);
+    };
+    uint32_t which = 0;                  // of the two transposes
+    // An odd step stays alone, in the middle: five steps as 2 1 2 are as exact as one by one (matrices of noise and strong directions, 128 x
+    // 1024: 1.5e-6 either way), as 2 2 1 half as exact.
+    const uint32_t alone = pl.pairs && (a.steps & 1u) ? 2u * ((a.steps / 2u + 1u) / 2u) : a.steps;
+    for (uint32_t i = 0; i < a.steps;) {
+        OParams g = square(0, 0, pl.G, kScaleG / (kScaleX * kScaleX));
+        g.a = g.b = at(pl.X);
         g.a_bytes = g.b_bytes = pl.X_bytes;
-        g.M = g.N = (uint32_t)pl.m;
         g.pitch = (uint32_t)pl.X_pitch;
-        g.d1 = g.d2 = a.workspace + pl.G;
-        g.d1_bytes = g.d2_bytes = pl.G_bytes;
-        g.d1_pitch = g.d2_pitch = (uint32_t)pl.G_pitch;
-        g.scale = kScaleG / (kScaleX * kScaleX);
         int rc;
         if (pl.gram.pieces > 1) {
-            g.partial = (float*)(a.workspace + pl.partial);
+            g.partial = (float*)at(pl.partial);
             rc = launch_product<kPartial, 0>(g, pl.gram, a.n, a.stream);
             if (rc != QESGD_OK) return rc;
             const uint32_t t = (g.M + 31u) / 32u;
@@ -874,40 +902,41 @@ int launch_type(const Orthogonalize& a) {
         } else {
             rc = launch_product<kGram, 0>(g, pl.gram, a.n, a.stream);
         }
-        if (rc != QESGD_OK) return rc;
-        OParams q = g;
-        q.a = q.b = a.workspace + pl.G;
-        q.a_bytes = q.b_bytes = pl.G_bytes;
-        q.pitch = (uint32_t)pl.G_pitch;
-        q.d1 = q.d2 = a.workspace + pl.P;
-        q.scale = cc * (kScaleP / (kScaleG * kScaleG));
-        q.ca = ca * kScaleP;
-        q.cb = cb * (kScaleP / kScaleG);
-        rc = launch_product<kPoly, 0>(q, pl.poly, a.n, a.stream);
+        const bool pair = pl.pairs && i != alone && i + 1 < a.steps;
+        if (rc == QESGD_OK) rc = poly(i++, pl.P);
+        uint64_t P = pl.P;
+        if (pair) {
+            OParams o;
+            if (rc == QESGD_OK) rc = launch_product<kGram, 0>(o = square(pl.G, pl.P, pl.T, 1.0f / kScaleP), pl.square, a.n, a.stream);
+            if (rc == QESGD_OK) rc = launch_product<kGram, 0>(o = square(pl.T, pl.P, pl.G, 1.0f / kScaleP), pl.square, a.n, a.stream);
+            if (rc == QESGD_OK) rc = poly(i++, pl.P2);
+            if (rc == QESGD_OK) rc = launch_product<kGram, 0>(o = square(pl.P2, pl.P, pl.T, 1.0f / kScaleP), pl.square, a.n, a.stream);
+            P = pl.T;
+        }
         if (rc != QESGD_OK) return rc;
         OParams x{};
-        x.a = a.workspace + pl.P;
+        x.a = at(P);
         x.a_bytes = pl.G_bytes;
         x.M = (uint32_t)pl.m;
-        x.b = Xt;
+        x.b = at(pl.Xt[which]);
         x.b_bytes = pl.Xt_bytes;
         x.N = (uint32_t)pl.n;
         x.pitch = (uint32_t)pl.G_pitch;
-        if (i + 1 < a.steps) {
-            x.d1 = a.workspace + pl.X;
+        if (i < a.steps) {
+            which ^= 1u;
+            x.d1 = at(pl.X);
             x.d1_bytes = pl.X_bytes;
             x.d1_pitch = (uint32_t)pl.X_pitch;
-            x.d2 = a.workspace + pl.Xt[(i + 1) & 1];
+            x.d2 = at(pl.Xt[which]);
             x.d2_bytes = pl.Xt_bytes;
             x.d2_pitch = (uint32_t)pl.Xt_pitch;
             x.scale = 1.0f / kScaleP;
             rc = launch_product<kApply, 0>(x, pl.apply, a.n, a.stream);
         } else {
             if (turned) {                // (P X)^T = Xt P, rows as the caller has them
-                OParams y = x;
-                y.a = x.b; y.a_bytes = x.b_bytes; y.M = x.N;
-                y.b = x.a; y.b_bytes = x.a_bytes; y.N = x.M;
-                x = y;
+                std::swap(x.a, x.b);
+                std::swap(x.a_bytes, x.b_bytes);
+                std::swap(x.M, x.N);
             }
             x.scale = a.alpha / (kScaleP * kScaleX);
             x.out = a.out;
