@@ -288,7 +288,7 @@ __device__ __forceinline__ void store_split(const OParams& p, const float (&v)[1
 template <class S>
 struct SplitOps {
     static constexpr int PARTS = 2;                            // 16 numbers of the contraction each
-    static constexpr int LOADS = (S::BM + S::BN) * 8 / S::threads;
+    static constexpr int LOADS = (S::BM + S::BN) * 8 / S::threads, PAIR_LOADS = 0;
     struct Frag { half8 ah[S::FM], bh[S::FN], bl[S::FN], al[S::FM]; };
     TileLoader<S::BM, S::threads> la;
     TileLoader<S::BN, S::threads> lb;

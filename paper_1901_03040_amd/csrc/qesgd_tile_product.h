@@ -92,11 +92,12 @@ __device__ __forceinline__ void wait_and_meet() {
 }
 
 // The contraction.  Ops: PARTS (even), LOADS (of a wave, for a step), Frag, fetch(step, buffer), read(frag, buffer, part),
-// multiply(frag, part), fetch_pair(step) (what comes for two steps at once, step even; only with two buffers), arrive(step) (its
-// data is there), next() (between two steps), at_a and at_b (places of part 0 of the lane's first fragments).  What the reads behind the last
+// multiply(frag, part), fetch_pair(step) (PAIR_LOADS loads for two steps at once, step even), arrive(step) (its data is there), next()
+// (between two steps), at_a and at_b (places of part 0 of the lane's first fragments).  What the reads behind the last
 // step find, nothing uses.
 template <int N, class Ops>
 __device__ __forceinline__ void run_steps(Ops& ops, uint32_t steps, unsigned char* const (&lds)[N]) {
+    static_assert(N == 2 || N == 4, "steps come in pairs");
     typename Ops::Frag f[2];
     auto step = [&](auto even, uint32_t t, unsigned char* here, unsigned char* there) {
         asm volatile("" : "+v"(ops.at_a), "+v"(ops.at_b));      // the parts' places are worked out where they are used, not kept in 16 registers
@@ -106,11 +107,12 @@ __device__ __forceinline__ void run_steps(Ops& ops, uint32_t steps, unsigned cha
             ops.multiply(f[p & 1], p);
             __builtin_amdgcn_sched_barrier(0);       // otherwise all reads go to the front and the instructions behind the barrier
         }
-        wait_and_meet<(N - 2) * Ops::LOADS>();
+        // of the later steps' loads as many may be left as were issued behind the next step's
+        wait_and_meet<(N - 2) * Ops::LOADS + (N > 2 ? Ops::PAIR_LOADS : 0)>();
         ops.arrive(t + 1);
         // Without a branch, which the compiler would move the matrix instructions above past: behind the end the last step comes once more.
         ops.fetch(min(t + N, steps - 1), here);
-        if (decltype(even)::value) ops.fetch_pair(t + 2);
+        if (decltype(even)::value) ops.fetch_pair(t + N);
         ops.read(f[0], there, 0);
         __builtin_amdgcn_sched_barrier(0);
         ops.multiply(f[1], Ops::PARTS - 1);
@@ -119,8 +121,11 @@ __device__ __forceinline__ void run_steps(Ops& ops, uint32_t steps, unsigned cha
     ops.fetch(0, lds[0]);
     ops.fetch_pair(0);
 #pragma unroll
-    for (int i = 1; i < N; ++i) ops.fetch(min((uint32_t)i, steps - 1), lds[i]);
-    wait_and_meet<(N - 1) * Ops::LOADS>();
+    for (int i = 1; i < N; ++i) {
+        ops.fetch(min((uint32_t)i, steps - 1), lds[i]);
+        if (i == 2) ops.fetch_pair(2);
+    }
+    wait_and_meet<(N - 1) * Ops::LOADS + (N > 2 ? Ops::PAIR_LOADS : 0)>();
     ops.arrive(0);
     ops.next();
     ops.read(f[0], lds[0], 0);
@@ -128,8 +133,8 @@ __device__ __forceinline__ void run_steps(Ops& ops, uint32_t steps, unsigned cha
         step(std::true_type{}, t, lds[0], lds[1]);
         if (t + 1 < steps) step(std::false_type{}, t + 1, lds[1], lds[2 % N]);
         if constexpr (N > 2) {
-            if (t + 2 < steps) step(std::true_type{}, t + 2, lds[2], lds[3 % N]);
-            if (t + 3 < steps) step(std::false_type{}, t + 3, lds[3 % N], lds[0]);
+            if (t + 2 < steps) step(std::true_type{}, t + 2, lds[2], lds[3]);
+            if (t + 3 < steps) step(std::false_type{}, t + 3, lds[3], lds[0]);
         }
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);             // vmcnt(0): nothing is on its way to LDS when the workgroup ends
