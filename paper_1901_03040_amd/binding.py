@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from functools import lru_cache
 from typing import Optional
 
 import torch
@@ -297,12 +298,16 @@ def qesgd_mx4_product(a_packed, b_packed, M, N, K, c, ldc, workspace=None, strea
            "qesgd_mx4_product")
 
 
-def _coeffs(coeffs):
-    """(a, b, c) of every step as a C array."""
-    flat = [float(v) for step in coeffs for v in step]
-    if len(flat) != 3 * len(coeffs):
-        raise ValueError("coeffs: three numbers for each step")
+@lru_cache(maxsize=64)
+def _coeff_array(flat):
     return (C.c_float * len(flat))(*flat)
+
+
+def _coeffs(coeffs):
+    """(a, b, c) of every step as a C array, kept by its numbers."""
+    if any(len(step) != 3 for step in coeffs):
+        raise ValueError("coeffs: three numbers for each step")
+    return _coeff_array(tuple([float(v) for step in coeffs for v in step]))
 
 
 def qesgd_orthogonalize_workspace_bytes(rows: int, cols: int, n: int) -> int:

@@ -55,12 +55,14 @@ struct Mx4Product {
     uint64_t ldc;
     float* workspace;
     hipStream_t stream;
+    uint32_t edge, pieces;          // of mx4_product_plan
 };
 
 int make_mx4_layout(uint64_t rows, uint64_t cols, qesgd_mx4_layout* out);
 int launch_mx4_quantize(const Mx4Quantize& a);
 int launch_mx4_aggregate(const Mx4Aggregate& a);
-size_t mx4_product_workspace(uint64_t M, uint64_t N, uint64_t K);
+// Chooses the kernel for (M, N, K); the bytes of workspace that it needs.
+size_t mx4_product_plan(Mx4Product& a);
 int launch_mx4_product(const Mx4Product& a);
 
 // ---- orthogonalised update ----------------------------------------------------

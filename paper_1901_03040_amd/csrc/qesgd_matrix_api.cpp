@@ -132,7 +132,12 @@ static bool product_dims_ok(uint64_t M, uint64_t N, uint64_t K) {
 }
 
 size_t qesgd_mx4_product_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
-    return product_dims_ok(M, N, K) ? mx4_product_workspace(M, N, K) : 0;
+    if (!product_dims_ok(M, N, K)) return 0;
+    Mx4Product p{};
+    p.M = M;
+    p.N = N;
+    p.K = K;
+    return mx4_product_plan(p);
 }
 
 int qesgd_mx4_product(const void* a_packed, const void* b_packed, uint64_t M, uint64_t N, uint64_t K, void* c, uint32_t dtype,
@@ -142,14 +147,14 @@ int qesgd_mx4_product(const void* a_packed, const void* b_packed, uint64_t M, ui
     if (!dtype_ok(dtype)) return QESGD_ERR_DTYPE;
     if (!aligned(a_packed, 256) || !aligned(b_packed, 256) || !aligned(c, 16) || !aligned(workspace, 16)) return QESGD_ERR_ALIGN;
     if (M > 1 && (ldc < N || ldc >= (1ull << 40) / M)) return QESGD_ERR_STRIDE;
-    const size_t need = mx4_product_workspace(M, N, K);
-    if (need > 0 && (!workspace || workspace_bytes < need)) return QESGD_ERR_WORKSPACE;
     Mx4Product p{};
-    p.a = (const unsigned char*)a_packed;
-    p.b = (const unsigned char*)b_packed;
     p.M = M;
     p.N = N;
     p.K = K;
+    const size_t need = mx4_product_plan(p);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return QESGD_ERR_WORKSPACE;
+    p.a = (const unsigned char*)a_packed;
+    p.b = (const unsigned char*)b_packed;
     p.c = c;
     p.dtype = dtype;
     p.ldc = M > 1 ? ldc : N;

@@ -17,6 +17,9 @@ namespace {
 typedef uint32_t uvec4 __attribute__((ext_vector_type(4)));
 typedef uint32_t uvec2 __attribute__((ext_vector_type(2)));
 typedef float fvec2 __attribute__((ext_vector_type(2)));
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // 128-bit accesses at any element's address: the rows of a matrix start where they start
 typedef uvec4 uvec4_any __attribute__((aligned(2)));
 typedef vec4 vec4_any __attribute__((aligned(4)));
@@ -31,18 +34,90 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
     return top >= 0x7F800000u ? 255u : b;
 }
 
+// The fp32 bits of a magnitude of 16 bits.
+template <uint32_t DT>
+__device__ __forceinline__ uint32_t half_bits(uint32_t half) {
+    if (DT == QESGD_BF16) return half << 16;
+    return __float_as_uint((float)__builtin_bit_cast(_Float16, (unsigned short)half));
+}
+
+// Eight consecutive elements of a lane as they come from memory.
+template <uint32_t DT>
+struct Eight {
+    typename std::conditional<DT == QESGD_F32, float[8], uvec4>::type v;
+
+    __device__ __forceinline__ float at(int i) const {
+        if constexpr (DT == QESGD_F32) return v[i];
+        else if (DT == QESGD_BF16) return __uint_as_float((i & 1) ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16);
+        else return (float)__builtin_bit_cast(_Float16, (unsigned short)((i & 1) ? v[i >> 1] >> 16 : v[i >> 1]));
+    }
+    // Bits of the largest magnitude, as integers: a NaN counts as the largest.
+    __device__ __forceinline__ uint32_t top() const {
+        if constexpr (DT == QESGD_F32) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+            return m;
+        } else {
+            ushort2v m = __builtin_bit_cast(ushort2v, v[0] & 0x7FFF7FFFu);
+#pragma unroll
+            for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(ushort2v, v[i] & 0x7FFF7FFFu));
+            return half_bits<DT>(max((uint32_t)m[0], (uint32_t)m[1]));
+        }
+    }
+    // From element `from` on, of which the first n (0..8) exist; the others are 0.
+    __device__ __forceinline__ void load(const void* x, uint64_t from, uint32_t n) {
+        if constexpr (DT == QESGD_F32) {
+            const float* p = (const float*)x + from;
+            if (n == 8) {
+                const vec4 a = *(const vec4_any*)p, b = *(const vec4_any*)(p + 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+            }
+        } else {
+            const unsigned short* p = (const unsigned short*)x + from;
+            if (n == 8) {
+                v = *(const uvec4_any*)p;
+            } else {
+                v = uvec4{0, 0, 0, 0};
+#pragma unroll
+                for (uint32_t i = 0; i < 7; ++i)
+                    if (i < n) v[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+            }
+        }
+    }
+};
+
+// Two 16-bit elements to byte BYTE of a word of codes.
+template <uint32_t DT, int BYTE>
+__device__ __forceinline__ uint32_t convert2(uint32_t word, uint32_t pair, float scale) {
+    if constexpr (DT == QESGD_BF16) return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(word, __builtin_bit_cast(bf16x2, pair), scale, BYTE);
+    else return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(word, __builtin_bit_cast(f16x2, pair), scale, BYTE);
+}
+
 // Codes of eight coordinates that share the scale byte sb, as one word.  `group`: number of their Philox call.
-template <bool STOCHASTIC>
-__device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t sb, uint64_t group, uint32_t worker, uint32_t round,
+template <uint32_t DT, bool STOCHASTIC>
+__device__ __forceinline__ uint32_t encode8(const Eight<DT>& x, uint32_t sb, uint64_t group, uint32_t worker, uint32_t round,
                                             uint32_t key0, uint32_t key1) {
     uint32_t word = 0;
     if (!STOCHASTIC) {
-        // the conversion divides by the power of two in its scale's exponent field, rounds to nearest even and ends at 6
+        // the conversions divide by the power of two in the scale's exponent field, round to nearest even and end at 6
         const float scale = __uint_as_float(sb << 23);
-        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[0], v[1], scale, 0);
-        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[2], v[3], scale, 1);
-        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[4], v[5], scale, 2);
-        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[6], v[7], scale, 3);
+        if constexpr (DT == QESGD_F32) {
+            word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x.v[0], x.v[1], scale, 0);
+            word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x.v[2], x.v[3], scale, 1);
+            word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x.v[4], x.v[5], scale, 2);
+            word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x.v[6], x.v[7], scale, 3);
+        } else {
+            const uint32_t w0 = x.v[0], w1 = x.v[1], w2 = x.v[2], w3 = x.v[3];
+            word = convert2<DT, 0>(word, w0, scale);
+            word = convert2<DT, 1>(word, w1, scale);
+            word = convert2<DT, 2>(word, w2, scale);
+            word = convert2<DT, 3>(word, w3, scale);
+        }
     } else {
         uint32_t rnd[4];
         philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), worker, round, key0, key1, rnd);
@@ -50,64 +125,17 @@ __device__ __forceinline__ uint32_t encode8(const float (&v)[8], uint32_t sb, ui
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t r = variate16(rnd, i);
-            const float a = __builtin_fabsf(v[i]) * inv;
-            // from 1 on the code is the exponent and the first bit of the significand, and T its next 16 bits: adding r there
-            // carries into the code iff r + T >= 2^16; below, the grid is a multiple of 1/2
-            const uint32_t high = ((__float_as_uint(a) + (r << 6)) >> 22) - 252u;
+            const float v = x.at(i), a = fminf(__builtin_fabsf(v) * inv, 6.0f);          // over 6 only at e = 125
+            // from 1 on the code is the exponent and the first bit of the significand (252 + code, and 252 is 4 modulo 8), and T its
+            // next 16 bits: adding r there carries into the code iff r + T >= 2^16; below, the grid is a multiple of 1/2
+            const uint32_t high = ((__float_as_uint(a) + (r << 6)) >> 22 & 7u) ^ 4u;
             const uint32_t low = ((uint32_t)(a * 131072.0f) + r) >> 16;
-            const uint32_t q = min(a < 1.0f ? low : high, 7u);
-            word |= (q | (__float_as_uint(v[i]) >> 31 << 3)) << (4 * i);
+            word |= ((a < 1.0f ? low : high) | (__float_as_uint(v) >> 28 & 8u)) << (4 * i);
         }
     }
     return sb == 255u ? 0u : word;
 }
 
-template <uint32_t DT>
-__device__ __forceinline__ float widen(uint32_t half) {
-    if (DT == QESGD_BF16) return __uint_as_float(half << 16);
-    return (float)__builtin_bit_cast(_Float16, (unsigned short)half);
-}
-
-template <uint32_t DT>
-__device__ __forceinline__ void widen8(uvec4 w, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = DT == QESGD_BF16 ? __uint_as_float(w[i] << 16) : widen<DT>(w[i] & 0xFFFFu);
-        v[2 * i + 1] = DT == QESGD_BF16 ? __uint_as_float(w[i] & 0xFFFF0000u) : widen<DT>(w[i] >> 16);
-    }
-}
-
-// Eight consecutive elements from element `at` on, of which the first n (0..8) exist; the others are 0.
-template <uint32_t DT>
-__device__ __forceinline__ void load8(const void* x, uint64_t at, uint32_t n, float (&v)[8]) {
-    if (DT == QESGD_F32) {
-        const float* p = (const float*)x + at;
-        if (n == 8) {
-            const vec4 a = *(const vec4_any*)p, b = *(const vec4_any*)(p + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
-        }
-    } else {
-        const unsigned short* p = (const unsigned short*)x + at;
-        if (n == 8) {
-            const uvec4 w = *(const uvec4_any*)p;
-            widen8<DT>(w, v);
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) v[i] = i < n ? widen<DT>(p[i]) : 0.0f;
-        }
-    }
-}
-
-__device__ __forceinline__ uint32_t top8(const float (&v)[8]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);    // as integers: a NaN counts as the largest
-    return m;
-}
 // Over the four lanes of a quad, which share a block.
 __device__ __forceinline__ uint32_t quad_max(uint32_t m) {
     m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, false));
@@ -136,43 +164,69 @@ struct QParams {
 };
 
 // Slots: the padded matrix, row after row.  A lane owns 8 consecutive ones (one Philox call, one word of codes), a quad a block,
-// a wave 512.  FLAT: the matrix is one row (a vector, or rows that need no padding and follow one another).
-constexpr uint32_t kQWaves = 4;
+// a wave kQChunks chunks of 512.  FLAT: the matrix is one row (a vector, or rows that need no padding and follow one another).
+constexpr uint32_t kQWaves = 4, kQChunks = 2;
 
 template <uint32_t DT, bool STOCHASTIC, bool FLAT>
 __global__ void __launch_bounds__(kQWaves * 64) k_mx4_quantize(const QParams p) {
     const uint32_t lane = threadIdx.x & 63u;
-    const uint64_t slot0 = ((uint64_t)xcd_tile(blockIdx.x, gridDim.x, p.xcd_group) * kQWaves + (threadIdx.x >> 6)) * kChunk;
-    const uint64_t slot = slot0 + lane * kLaneElems;
-    if (slot0 >= p.slots) return;
+    const uint64_t wave0 = ((uint64_t)xcd_tile(blockIdx.x, gridDim.x, p.xcd_group) * kQWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) *
+                           (kQChunks * kChunk);
+    if (wave0 >= p.slots) return;
     const uint32_t k = blockIdx.y;
     const uint64_t x0 = (uint64_t)k * p.x_stride;
-    float v[8];
-    if (FLAT && slot0 + kChunk <= p.cols) {
-        if (DT == QESGD_F32 && (((uintptr_t)p.x | (p.x_stride << 2)) & 15u) == 0) {
-            vec4 a[1], b[1];
-            load_halves_as<1, false>((const float*)p.x + x0 + slot0 + half_offset(lane), a, b);
-            halves_to_lane(a[0], b[0], v);
+    Eight<DT> v[kQChunks];
+    if (FLAT && wave0 + kQChunks * kChunk <= p.cols) {
+        if constexpr (DT == QESGD_F32) {
+            if ((((uintptr_t)p.x | (p.x_stride << 2)) & 15u) == 0) {
+                vec4 a[kQChunks], b[kQChunks];
+                load_halves_as<kQChunks, false>((const float*)p.x + x0 + wave0 + half_offset(lane), a, b);
+#pragma unroll
+                for (uint32_t c = 0; c < kQChunks; ++c) halves_to_lane(a[c], b[c], v[c].v);
+            } else {
+#pragma unroll
+                for (uint32_t c = 0; c < kQChunks; ++c) v[c].load(p.x, x0 + wave0 + c * kChunk + lane * kLaneElems, 8u);
+            }
         } else {
-            load8<DT>(p.x, x0 + slot, 8u, v);
+#pragma unroll
+            for (uint32_t c = 0; c < kQChunks; ++c) v[c].load(p.x, x0 + wave0 + c * kChunk + lane * kLaneElems, 8u);
         }
     } else {
-        uint64_t row = 0, col = slot;
-        if (!FLAT) {
-            const uint32_t g = (uint32_t)(slot >> 7);
-            row = g / p.groups;
-            col = (uint64_t)(g - (uint32_t)row * p.groups) * 128u + (slot & 127u);
+        const uint32_t group0 = (uint32_t)(wave0 >> 7), row0 = FLAT ? 0u : group0 / p.groups;       // uniform
+#pragma unroll
+        for (uint32_t c = 0; c < kQChunks; ++c) {
+            const uint64_t slot = wave0 + c * kChunk + lane * kLaneElems;
+            uint64_t row = 0, col = slot;
+            if (!FLAT) {
+                // the wave's 4 kQChunks groups of 128 end at most so many rows
+                uint32_t r = row0, g = group0 - row0 * p.groups + c * 4u + (lane >> 4);
+                if (p.groups >= 4u * kQChunks) {
+                    const uint32_t over = g >= p.groups ? 1u : 0u;
+                    r += over;
+                    g -= over ? p.groups : 0u;
+                } else {
+                    const uint32_t more = g / p.groups;
+                    r += more;
+                    g -= more * p.groups;
+                }
+                row = r;
+                col = (uint64_t)g * 128u + (lane & 15u) * 8u;
+            }
+            const uint32_t n = slot >= p.slots || col >= p.cols ? 0u : p.cols - col < 8 ? (uint32_t)(p.cols - col) : 8u;
+            v[c].load(p.x, x0 + row * p.ld + col, n);
         }
-        const uint32_t n = slot >= p.slots || col >= p.cols ? 0u : p.cols - col < 8 ? (uint32_t)(p.cols - col) : 8u;
-        load8<DT>(p.x, x0 + row * p.ld + col, n, v);
     }
-    const uint32_t sb = scale_byte<STOCHASTIC>(quad_max(top8(v)));
-    const uint32_t word = encode8<STOCHASTIC>(v, sb, slot >> 3, p.worker0 + k, p.round, p.key0, p.key1);
-    const uint32_t scales = row_bytes(sb, lane);
-    if (slot < p.slots) {                                      // slots come in 128s: a row of lanes is in or out
-        unsigned char* out = p.packed + (uint64_t)k * p.packed_stride;
-        *(uint32_t*)(out + (slot >> 1)) = word;
-        if ((lane & 15u) == 0) *(uint32_t*)(out + p.scales_off + (slot >> 5)) = scales;
+    unsigned char* out = p.packed + (uint64_t)k * p.packed_stride;
+#pragma unroll
+    for (uint32_t c = 0; c < kQChunks; ++c) {
+        const uint64_t slot = wave0 + c * kChunk + lane * kLaneElems;
+        const uint32_t sb = scale_byte<STOCHASTIC>(quad_max(v[c].top()));
+        const uint32_t word = encode8<DT, STOCHASTIC>(v[c], sb, slot >> 3, p.worker0 + k, p.round, p.key0, p.key1);
+        const uint32_t scales = row_bytes(sb, lane);
+        if (slot < p.slots) {                                  // slots come in 128s: a row of lanes is in or out
+            *(uint32_t*)(out + (slot >> 1)) = word;
+            if ((lane & 15u) == 0) *(uint32_t*)(out + p.scales_off + (slot >> 5)) = scales;
+        }
     }
 }
 
@@ -192,68 +246,78 @@ __global__ void __launch_bounds__(256) k_mx4_quantize_both(const QParams p) {
     const uint64_t x0 = (uint64_t)k * p.x_stride;
     const uint32_t col = (lane & 15u) * 8u;
     const uint32_t n = c0 + col >= p.cols ? 0u : p.cols - c0 - col < 8 ? (uint32_t)(p.cols - c0 - col) : 8u;
-#pragma unroll 4
-    for (uint32_t i = 0; i < 8; ++i) {
-        const uint32_t r = i * 16u + wave * 4u + (lane >> 4);
-        const uint64_t row = r0 + r;
-        float v[8];
-        load8<DT>(p.x, x0 + row * p.ld + c0 + col, row < p.rows ? n : 0u, v);
-        elem* to = tile + r * kTile + (r >> 5) * kRoom + col;
-        if constexpr (DT == QESGD_F32) {
-            *(vec4*)to = vec4{v[0], v[1], v[2], v[3]};
-            *(vec4*)(to + 4) = vec4{v[4], v[5], v[6], v[7]};
-        } else {
-            uvec4 w;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (DT == QESGD_BF16) w[j] = (__float_as_uint(v[2 * j]) >> 16) | (__float_as_uint(v[2 * j + 1]) & 0xFFFF0000u);
-                else w[j] = (uint32_t)__builtin_bit_cast(unsigned short, (_Float16)v[2 * j]) |
-                            ((uint32_t)__builtin_bit_cast(unsigned short, (_Float16)v[2 * j + 1]) << 16);
-            }
-            *(uvec4*)to = w;
+    for (uint32_t i0 = 0; i0 < 8; i0 += 4) {
+        Eight<DT> v[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint64_t row = r0 + (i0 + i) * 16u + wave * 4u + (lane >> 4);
+            v[i].load(p.x, x0 + row * p.ld + c0 + col, row < p.rows ? n : 0u);
         }
-        if (p.packed) {
-            const uint64_t slot = row * ((uint64_t)p.groups * 128u) + c0 + col;
-            const uint32_t sb = scale_byte<STOCHASTIC>(quad_max(top8(v)));
-            const uint32_t word = encode8<STOCHASTIC>(v, sb, slot >> 3, p.worker0 + k, p.round, p.key0, p.key1);
-            const uint32_t scales = row_bytes(sb, lane);
-            if (row < p.rows) {
-                unsigned char* out = p.packed + (uint64_t)k * p.packed_stride;
-                *(uint32_t*)(out + (slot >> 1)) = word;
-                if ((lane & 15u) == 0) *(uint32_t*)(out + p.scales_off + (slot >> 5)) = scales;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t r = (i0 + i) * 16u + wave * 4u + (lane >> 4);
+            const uint64_t row = r0 + r;
+            elem* to = tile + r * kTile + (r >> 5) * kRoom + col;
+            if constexpr (DT == QESGD_F32) {
+                *(vec4*)to = vec4{v[i].v[0], v[i].v[1], v[i].v[2], v[i].v[3]};
+                *(vec4*)(to + 4) = vec4{v[i].v[4], v[i].v[5], v[i].v[6], v[i].v[7]};
+            } else {
+                *(uvec4*)to = v[i].v;
+            }
+            if (p.packed) {
+                const uint64_t slot = row * ((uint64_t)p.groups * 128u) + c0 + col;
+                const uint32_t sb = scale_byte<STOCHASTIC>(quad_max(v[i].top()));
+                const uint32_t word = encode8<DT, STOCHASTIC>(v[i], sb, slot >> 3, p.worker0 + k, p.round, p.key0, p.key1);
+                const uint32_t scales = row_bytes(sb, lane);
+                if (row < p.rows) {
+                    unsigned char* out = p.packed + (uint64_t)k * p.packed_stride;
+                    *(uint32_t*)(out + (slot >> 1)) = word;
+                    if ((lane & 15u) == 0) *(uint32_t*)(out + p.scales_off + (slot >> 5)) = scales;
+                }
             }
         }
     }
     __syncthreads();
     const uint32_t block = lane & 3u;
+    // A lane takes one column of 32-bit elements twice, or a pair of columns of 16-bit ones once: a word of LDS either way.
 #pragma unroll 1
-    for (uint32_t i = 0; i < 2; ++i) {
-        const uint32_t c = i * 64u + wave * 16u + (lane >> 2);
-        const elem* from = tile + block * (32u * kTile + kRoom) + c;
-        float v[4][8];
-        uint32_t top = 0;
+    for (uint32_t i = 0; i < (DT == QESGD_F32 ? 2u : 1u); ++i) {
+        const uint32_t word_col = i * 64u + wave * 16u + (lane >> 2);
+        const uint32_t* from = (const uint32_t*)tile + block * (32u * kTile + kRoom) * sizeof(elem) / 4u + word_col;
+        uint32_t raw[32];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 32; ++j) raw[j] = from[j * (kTile * sizeof(elem) / 4u)];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if constexpr (DT == QESGD_F32) v[j][e] = from[(j * 8 + e) * kTile];
-                else v[j][e] = widen<DT>(from[(j * 8 + e) * kTile]);
+        for (uint32_t side = 0; side < 4u / sizeof(elem); ++side) {
+            Eight<DT> v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (DT == QESGD_F32) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[j].v[e] = __uint_as_float(raw[j * 8 + e]);
+                } else {
+                    // the lower (upper) halves of two rows' words, as a pair along the column
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[j].v[e] = __builtin_amdgcn_perm(raw[j * 8 + 2 * e + 1], raw[j * 8 + 2 * e], side ? 0x07060302u : 0x05040100u);
+                }
             }
-            top = max(top, top8(v[j]));
-        }
-        const uint32_t sb = scale_byte<STOCHASTIC>(top);
-        const uint64_t slot = (c0 + c) * ((uint64_t)p.groups_t * 128u) + r0 + block * 32u;
-        uvec4 w;
+            const uint32_t c = DT == QESGD_F32 ? word_col : word_col * 2u + side;
+            const uint32_t sb = scale_byte<STOCHASTIC>(max(max(v[0].top(), v[1].top()), max(v[2].top(), v[3].top())));
+            const uint64_t slot = (c0 + c) * ((uint64_t)p.groups_t * 128u) + r0 + block * 32u;
+            uvec4 w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            w[j] = encode8<STOCHASTIC>(v[j], sb, (slot >> 3) + j, p.worker0 + k, p.round, p.key0, p.key1);
-        uint32_t scales = sb << (8u * block);
-        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0xB1, 0xF, 0xF, false);
-        scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x4E, 0xF, 0xF, false);
-        if (c0 + c < p.cols) {
-            unsigned char* out = p.packed_t + (uint64_t)k * p.packed_t_stride;
-            *(uvec4*)(out + (slot >> 1)) = w;
-            if (block == 0) *(uint32_t*)(out + p.scales_t_off + (slot >> 5)) = scales;
+            for (int j = 0; j < 4; ++j)
+                w[j] = encode8<DT, STOCHASTIC>(v[j], sb, (slot >> 3) + j, p.worker0 + k, p.round, p.key0, p.key1);
+            uint32_t scales = sb << (8u * block);
+            scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0xB1, 0xF, 0xF, false);
+            scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x4E, 0xF, 0xF, false);
+            if (c0 + c < p.cols) {
+                unsigned char* out = p.packed_t + (uint64_t)k * p.packed_t_stride;
+                *(uvec4*)(out + (slot >> 1)) = w;
+                if (block == 0) *(uint32_t*)(out + p.scales_t_off + (slot >> 5)) = scales;
+            }
         }
     }
 }
@@ -370,9 +434,10 @@ int launch_quantize_as(const Mx4Quantize& a, QParams& p, bool flat) {
         k_mx4_quantize_both<DT, STOCHASTIC><<<dim3((uint32_t)tiles, a.K), 256, 0, a.stream>>>(p);
         return finish_launch();
     }
-    const uint64_t tiles = (p.slots + kQWaves * kChunk - 1) / (kQWaves * kChunk);
+    constexpr uint64_t tile = kQWaves * kQChunks * kChunk;
+    const uint64_t tiles = (p.slots + tile - 1) / tile;
     if (tiles >= (1ull << 31)) return QESGD_ERR_DIM;
-    p.xcd_group = xcd_group_log2(kQWaves * kChunk);
+    p.xcd_group = xcd_group_log2(tile);
     const dim3 grid((uint32_t)tiles, a.K);
     if (flat) k_mx4_quantize<DT, STOCHASTIC, true><<<grid, kQWaves * 64, 0, a.stream>>>(p);
     else k_mx4_quantize<DT, STOCHASTIC, false><<<grid, kQWaves * 64, 0, a.stream>>>(p);

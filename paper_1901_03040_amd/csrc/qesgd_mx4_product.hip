@@ -345,9 +345,11 @@ Cut choose_cut(uint64_t M, uint64_t N, uint64_t K) {
 
 }  // namespace
 
-size_t mx4_product_workspace(uint64_t M, uint64_t N, uint64_t K) {
-    const Cut cut = choose_cut(M, N, K);
-    return cut.pieces > 1 ? cut.pieces * M * N * sizeof(float) : 0;
+size_t mx4_product_plan(Mx4Product& a) {
+    const Cut cut = choose_cut(a.M, a.N, a.K);
+    a.edge = cut.edge;
+    a.pieces = cut.pieces;
+    return cut.pieces > 1 ? cut.pieces * a.M * a.N * sizeof(float) : 0;
 }
 
 int launch_mx4_product(const Mx4Product& a) {
@@ -366,7 +368,7 @@ int launch_mx4_product(const Mx4Product& a) {
     p.N = (uint32_t)a.N;
     p.row_codes = (uint32_t)A.row_codes;
     p.row_scales = (uint32_t)A.row_scales;
-    const Cut cut = choose_cut(a.M, a.N, a.K);
+    const Cut cut{a.edge, a.pieces};
     switch (cut.edge) {
         case 0:
             by_type(a.dtype, [&](auto t) { k_mx4_product_few<t.value><<<(p.N + 31) / 32, kFewWaves * 64, 0, a.stream>>>(p); });

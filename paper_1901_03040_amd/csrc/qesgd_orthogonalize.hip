@@ -14,6 +14,7 @@
 // then their lo, so a step of the pipeline is one 128-byte line of each row.  Products have both operands' rows along the
 // contraction, which takes X for X X^T and its transpose for P X: the last product's epilogue writes both.  G and P are symmetric:
 // only tiles on and above the diagonal are computed, and the epilogue writes them twice.
+#include <algorithm>
 #include <type_traits>
 #include <utility>
 
@@ -820,26 +821,16 @@ int launch_product(OParams& p, const Cut& cut, uint32_t count, hipStream_t strea
 
 template <uint32_t DT>
 int launch_type(const Orthogonalize& a) {
-    const Plan pl = make_plan(a.rows, a.cols, a.n);
-    const bool turned = a.rows > a.cols;
     SParams s{};
     s.x = a.x;
     s.momentum = a.momentum;
-    s.partial = (double*)a.workspace;
     s.d = a.rows * a.cols;
     s.rows = (uint32_t)a.rows;
     s.cols = (uint32_t)a.cols;
-    s.parts = pl.parts;
     s.mu = a.mu;
     s.eps = a.eps;
     s.nesterov = a.nesterov;
-    s.X = a.workspace + pl.X;
-    s.Xt = a.workspace + pl.Xt[0];
-    s.X_bytes = pl.X_bytes;
-    s.Xt_bytes = pl.Xt_bytes;
-    s.X_pitch = (uint32_t)pl.X_pitch;
-    s.Xt_pitch = (uint32_t)pl.Xt_pitch;
-    const SmallLayout small = small_layout(pl.m, pl.n);
+    const SmallLayout small = small_layout(std::min(a.rows, a.cols), std::max(a.rows, a.cols));
     if (small.total) {
         SmallParams p{};
         p.s = s;
@@ -857,6 +848,17 @@ int launch_type(const Orthogonalize& a) {
         k_orthogonal_small<DT><<<a.n, kSmallThreads, small.total, a.stream>>>(p);
         return launched();
     }
+
+    const Plan pl = make_plan(a.rows, a.cols, a.n);
+    const bool turned = a.rows > a.cols;
+    s.partial = (double*)a.workspace;
+    s.parts = pl.parts;
+    s.X = a.workspace + pl.X;
+    s.Xt = a.workspace + pl.Xt[0];
+    s.X_bytes = pl.X_bytes;
+    s.Xt_bytes = pl.Xt_bytes;
+    s.X_pitch = (uint32_t)pl.X_pitch;
+    s.Xt_pitch = (uint32_t)pl.Xt_pitch;
     k_orthogonal_momentum<DT><<<dim3(pl.parts, a.n), 256, 0, a.stream>>>(s);
     if (const int rc = launched(); rc != QESGD_OK) return rc;
     k_orthogonal_split<DT><<<dim3((uint32_t)((a.cols + 63) / 64), (uint32_t)((a.rows + 63) / 64), a.n), 256, 0, a.stream>>>(s);
