@@ -232,6 +232,9 @@ int qesgd_epoch_commit(float* w_inout, float* zsum_inout, uint32_t rounds, uint6
  * the orthogonalised update.  A round of a matrix parameter: the workers run their layer on packed
  * operands (qesgd_mx4_product), send packed gradients (qesgd_mx4_quantize_pack), the server takes
  * their mean (qesgd_mx4_unpack_aggregate_update) and orthogonalises it (qesgd_orthogonal_update).
+ * The conventions above hold, but: inputs of 16 bits are aligned to their elements where it says so, and
+ * NaN and infinities have the meaning given here.  `stream` belongs to the current device.  A workspace serves
+ * one call at a time: calls that may run at once (two streams, two graphs in flight) need one each.
  * ------------------------------------------------------------------------- */
 
 enum { QESGD_F32 = 0, QESGD_BF16 = 1, QESGD_F16 = 2 };              /* element types */
@@ -256,7 +259,7 @@ typedef struct qesgd_mx4_layout {
     uint64_t payload_bytes;    /* rows * (row_codes + row_scales)                       */
 } qesgd_mx4_layout;
 
-/* Host only.  QESGD_ERR_DIM: a side is 0, or rows * wide > 2^38. */
+/* Host only.  QESGD_ERR_DIM: a side is 0, or rows * wide > 2^38 (the calls below take up to 2^34). */
 int qesgd_mx4_layout_query(uint64_t rows, uint64_t cols, qesgd_mx4_layout* out);
 
 /* Quantises K workers' matrices, worker k's at x + k*x_stride, rows ld apart (both in elements; any ld >= cols,
@@ -265,7 +268,8 @@ int qesgd_mx4_layout_query(uint64_t rows, uint64_t cols, qesgd_mx4_layout* out);
  *         QESGD_MX4_STOCHASTIC: the smallest e with max|v| <= 6 * 2^e (at most 125), elements to one of
  *         the two neighbours as qesgd_quantize_pack rounds: up iff r + trunc(f * 2^16) >= 2^16, f the
  *         fraction of the way and r the variate of coordinate row*wide + column for (seed, round,
- *         worker + k); unbiased to 2^-16 of a step.
+ *         worker + k); unbiased to 2^-16 of a step.  Matrices whose roundings must not depend on one another take
+ *         different seeds, rounds or workers.
  *   packed    nullable: K blocks of qesgd_mx4_layout_query(rows, cols), packed_stride bytes apart (a multiple of 256).
  *   packed_t  nullable: the same of the transposed matrices, layout (cols, rows), blocks along the
  *         columns of x; equal to quantising a transposed copy.  Both come from one read of x: a
@@ -293,8 +297,9 @@ int qesgd_mx4_product(const void* a_packed, const void* b_packed, uint64_t M, ui
  * then X = (a I + b G + c G^2) X with G = X X^T (X^T X on the longer side), (a, b, c) = coeffs[3*i .. 3*i+2] (host
  * memory, read during the call); out = X.  Singular values s become p_steps(.. p_1(s)), p(s) = a s + b s^3 + c s^5;
  * singular vectors stay.  Norms in fp64, products of fp32 accuracy (each operand as the sum of two fp16
- * numbers, sums in fp32).  |coefficients| must keep every iterate's and polynomial's entries below 16
- * (singular values that stay near 1 do); beyond that the result is infinite or NaN.  A matrix of zeros gives zeros.
+ * numbers, sums in fp32).  The coefficients must keep the entries of every iterate X and of G
+ * below 16, the polynomials' a I + b G + c G^2 and the product of two of them below 256 (singular values that stay near 1 do);
+ * beyond that the result is infinite or NaN.  A matrix of zeros gives zeros, one with a NaN or an infinity NaN everywhere.
  *   out  same type and shape as x, may be x itself.
  *   workspace  qesgd_orthogonalize_workspace_bytes(rows, cols, n), 256-byte aligned; may be NULL when that is 0 (matrices that fit
  *        the shared memory of a CU).  rows, cols <= 2^20, n <= 65535. */

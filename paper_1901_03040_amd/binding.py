@@ -264,6 +264,17 @@ def _dtype(t: torch.Tensor, where: str) -> int:
     return code
 
 
+def _check_tensors(where: str, dtype: Optional[torch.dtype], *tensors):
+    """The kernels run on the current device, and take addresses: a tensor of the host, of another device or of another type is refused."""
+    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+    for t in tensors:
+        if t is not None:
+            if t.get_device() != device:
+                raise ValueError(f"{where}: a tensor on {t.device}, which is not the current GPU")
+            if dtype is not None and t.dtype != dtype:
+                raise QesgdError(ERR_DTYPE, where)
+
+
 def _ws(workspace):
     return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
@@ -276,13 +287,17 @@ def qesgd_mx4_layout_query(rows: int, cols: int) -> Mx4Layout:
 
 def qesgd_mx4_quantize_pack(x, ld, x_stride, rows, cols, K, mode, seed, rnd, packed, packed_stride, packed_t=None,
                             packed_t_stride=0, worker=0, stream=None):
-    _check(lib().qesgd_mx4_quantize_pack(_ptr(x), _dtype(x, "qesgd_mx4_quantize_pack"), int(ld), int(x_stride), int(rows), int(cols),
+    dtype = _dtype(x, "qesgd_mx4_quantize_pack")
+    _check_tensors("qesgd_mx4_quantize_pack", None, x, packed, packed_t)
+    _check(lib().qesgd_mx4_quantize_pack(_ptr(x), dtype, int(ld), int(x_stride), int(rows), int(cols),
                                          int(K), int(mode), int(seed), int(rnd), int(worker), _ptr(packed), int(packed_stride),
                                          _ptr(packed_t), int(packed_t_stride), _stream(stream)), "qesgd_mx4_quantize_pack")
 
 
 def qesgd_mx4_unpack_aggregate_update(packed_slab, packed_stride, K, rows, cols, w_snap, zbar_out, u_out, zsum_inout,
                                       stream=None):
+    _check_tensors("qesgd_mx4_unpack_aggregate_update", None, packed_slab)
+    _check_tensors("qesgd_mx4_unpack_aggregate_update", torch.float32, w_snap, zbar_out, u_out, zsum_inout)
     _check(lib().qesgd_mx4_unpack_aggregate_update(_ptr(packed_slab), int(packed_stride), int(K), int(rows), int(cols),
                                                    _ptr(w_snap), _ptr(zbar_out), _ptr(u_out), _ptr(zsum_inout),
                                                    _stream(stream)), "qesgd_mx4_unpack_aggregate_update")
@@ -293,8 +308,9 @@ def qesgd_mx4_product_workspace_bytes(M: int, N: int, K: int) -> int:
 
 
 def qesgd_mx4_product(a_packed, b_packed, M, N, K, c, ldc, workspace=None, stream=None):
-    _check(lib().qesgd_mx4_product(_ptr(a_packed), _ptr(b_packed), int(M), int(N), int(K), _ptr(c),
-                                   _dtype(c, "qesgd_mx4_product"), int(ldc), *_ws(workspace), _stream(stream)),
+    dtype = _dtype(c, "qesgd_mx4_product")
+    _check_tensors("qesgd_mx4_product", None, a_packed, b_packed, c, workspace)
+    _check(lib().qesgd_mx4_product(_ptr(a_packed), _ptr(b_packed), int(M), int(N), int(K), _ptr(c), dtype, int(ldc), *_ws(workspace), _stream(stream)),
            "qesgd_mx4_product")
 
 
@@ -317,8 +333,10 @@ def qesgd_orthogonalize_workspace_bytes(rows: int, cols: int, n: int) -> int:
 def qesgd_orthogonalize(x, rows, cols, n, coeffs, eps, out, workspace, stream=None):
     if out.dtype != x.dtype:
         raise QesgdError(ERR_DTYPE, "qesgd_orthogonalize")
-    _check(lib().qesgd_orthogonalize(_ptr(x), _dtype(x, "qesgd_orthogonalize"), int(rows), int(cols), int(n), _coeffs(coeffs),
-                                     len(coeffs), float(eps), _ptr(out), *_ws(workspace), _stream(stream)),
+    dtype, steps = _dtype(x, "qesgd_orthogonalize"), _coeffs(coeffs)
+    _check_tensors("qesgd_orthogonalize", None, x, out, workspace)
+    _check(lib().qesgd_orthogonalize(_ptr(x), dtype, int(rows), int(cols), int(n), steps, len(coeffs), float(eps), _ptr(out),
+                                     *_ws(workspace), _stream(stream)),
            "qesgd_orthogonalize")
 
 
@@ -326,6 +344,8 @@ def qesgd_orthogonal_update(g, rows, cols, n, momentum_inout, mu, nesterov, coef
                             u_out, zsum_inout, workspace, stream=None):
     if g.dtype != torch.float32:
         raise QesgdError(ERR_DTYPE, "qesgd_orthogonal_update")
+    _check_tensors("qesgd_orthogonal_update", None, workspace)
+    _check_tensors("qesgd_orthogonal_update", torch.float32, g, momentum_inout, step_out, z_inout, w_snap, u_out, zsum_inout)
     _check(lib().qesgd_orthogonal_update(_ptr(g), int(rows), int(cols), int(n), _ptr(momentum_inout), float(mu),
                                          int(bool(nesterov)), _coeffs(coeffs), len(coeffs), float(eps), float(alpha),
                                          _ptr(step_out), _ptr(z_inout), _ptr(w_snap), _ptr(u_out), _ptr(zsum_inout),

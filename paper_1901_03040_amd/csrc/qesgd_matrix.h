@@ -17,6 +17,10 @@ inline uint32_t dtype_bytes(uint32_t dtype) { return dtype == QESGD_F32 ? 4u : 2
 constexpr uint64_t kMx4Block = 32;                       // coordinates that share a scale
 constexpr uint64_t kMx4Pad = 128;                        // columns are padded to a multiple of this
 constexpr uint64_t kMx4MaxSlots = 1ull << 38;            // padded coordinates of one matrix: 128 of them are numbered in 32 bits
+constexpr uint64_t kMx4MaxLaunch = 1ull << 34;           // of a call that launches eight or more of them a thread: half of what follows
+
+// A launch numbers its threads in 32 bits.
+inline bool grid_ok(uint64_t groups, uint64_t threads) { return groups < (1ull << 31) && groups * threads < (1ull << 32); }
 
 struct Mx4Quantize {
     const void* x;

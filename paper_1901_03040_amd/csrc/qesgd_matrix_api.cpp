@@ -71,6 +71,7 @@ int qesgd_mx4_quantize_pack(const void* x, uint32_t dtype, uint64_t ld, uint64_t
     int rc = make_mx4_layout(rows, cols, &L);
     if (rc == QESGD_OK && packed_t) rc = make_mx4_layout(cols, rows, &T);
     if (rc != QESGD_OK) return rc;
+    if (rows * L.row_codes * 2 > kMx4MaxLaunch || (packed_t && cols * T.row_codes * 2 > kMx4MaxLaunch)) return QESGD_ERR_DIM;
     if (!dtype_ok(dtype)) return QESGD_ERR_DTYPE;
     if (K == 0 || K > QESGD_MAX_WORKERS) return QESGD_ERR_WORKERS;
     if (mode != QESGD_MX4_NEAREST && mode != QESGD_MX4_STOCHASTIC) return QESGD_ERR_MODE;
@@ -109,6 +110,7 @@ int qesgd_mx4_unpack_aggregate_update(const void* packed_slab, uint64_t packed_s
     qesgd_mx4_layout L;
     const int rc = make_mx4_layout(rows, cols, &L);
     if (rc != QESGD_OK) return rc;
+    if (rows * L.row_codes * 2 > kMx4MaxLaunch) return QESGD_ERR_DIM;
     if (K == 0 || K > QESGD_MAX_WORKERS) return QESGD_ERR_WORKERS;
     if (!aligned(packed_slab, 256) || !aligned(w_snap, 16) || !aligned(zbar_out, 16) || !aligned(u_out, 16) || !aligned(zsum_inout, 16))
         return QESGD_ERR_ALIGN;

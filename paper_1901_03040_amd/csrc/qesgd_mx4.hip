@@ -430,13 +430,13 @@ template <uint32_t DT, bool STOCHASTIC>
 int launch_quantize_as(const Mx4Quantize& a, QParams& p, bool flat) {
     if (p.packed_t) {
         const uint64_t tiles = ((a.rows + kTile - 1) / kTile) * p.groups;
-        if (tiles >= (1ull << 31)) return QESGD_ERR_DIM;
+        if (!grid_ok(tiles, 256)) return QESGD_ERR_DIM;
         k_mx4_quantize_both<DT, STOCHASTIC><<<dim3((uint32_t)tiles, a.K), 256, 0, a.stream>>>(p);
         return finish_launch();
     }
     constexpr uint64_t tile = kQWaves * kQChunks * kChunk;
     const uint64_t tiles = (p.slots + tile - 1) / tile;
-    if (tiles >= (1ull << 31)) return QESGD_ERR_DIM;
+    if (!grid_ok(tiles, kQWaves * 64)) return QESGD_ERR_DIM;
     p.xcd_group = xcd_group_log2(tile);
     const dim3 grid((uint32_t)tiles, a.K);
     if (flat) k_mx4_quantize<DT, STOCHASTIC, true><<<grid, kQWaves * 64, 0, a.stream>>>(p);
@@ -505,7 +505,7 @@ int launch_mx4_aggregate(const Mx4Aggregate& a) {
     const bool flat = a.rows == 1 || a.cols % kMx4Pad == 0;
     p.cols = flat ? a.rows * a.cols : a.cols;
     const uint64_t tiles = (p.slots + 4 * kChunk - 1) / (4 * kChunk);
-    if (tiles >= (1ull << 31)) return QESGD_ERR_DIM;
+    if (!grid_ok(tiles, 256)) return QESGD_ERR_DIM;
     p.xcd_group = xcd_group_log2(4 * kChunk);
     if (flat) k_mx4_aggregate_update<true><<<(uint32_t)tiles, 256, 0, a.stream>>>(p);
     else k_mx4_aggregate_update<false><<<(uint32_t)tiles, 256, 0, a.stream>>>(p);

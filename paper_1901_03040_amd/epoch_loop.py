@@ -131,16 +131,16 @@ class QesgdMatrixLoop:
     def _send(self):
         self._quantize(self.u, B.MX4_NEAREST, self.packed_u, self.packed_ut)
 
-    def _quantize(self, x, mode, packed, packed_t):
+    def _quantize(self, x, mode, packed, packed_t, worker=0):
         B.qesgd_mx4_quantize_pack(x, x.stride(0), 0, x.shape[0], x.shape[1], 1, mode, self.seed, self.round_id, packed, 0,
-                                  packed_t=packed_t)
+                                  packed_t=packed_t, worker=worker)
 
-    def _pack(self, x, mode):
+    def _pack(self, x, mode, worker=0):
         """Both forms of an operand [rows, cols]."""
         r, c = x.shape
-        x = x if x.stride(1) == 1 else x.contiguous()
+        x = x if x.stride(1) == 1 and x.stride(0) >= c else x.contiguous()
         forms = (B.alloc_mx4(B.qesgd_mx4_layout_query(r, c), device=self.dev), B.alloc_mx4(B.qesgd_mx4_layout_query(c, r), device=self.dev))
-        self._quantize(x, mode, *forms)
+        self._quantize(x, mode, *forms, worker)
         return forms
 
     def _product(self, a, b, M, N, K, dtype):
@@ -154,11 +154,13 @@ class QesgdMatrixLoop:
         px, pxt = self._pack(x, B.MX4_NEAREST)
         return self._product(px, self.packed_u, x.shape[0], self.out, self.inn, x.dtype), (pxt, x.shape[0])
 
-    def backward(self, dy: torch.Tensor, saved):
-        """Gradients with respect to x (dy's type) and to the parameters (fp32): dy [tokens, out] is rounded without bias."""
+    def backward(self, dy: torch.Tensor, saved, worker: int = 0):
+        """Gradients with respect to x (dy's type) and to the parameters (fp32): dy [tokens, out] is rounded without bias.  Each of a
+        round's calls takes a worker number of its own, so that their roundings do not depend on one another, nor on those of
+        the gradients (numbers 0 .. K - 1 of the quantiser; these follow)."""
         pxt, tokens = saved
         assert dy.shape == (tokens, self.out)
-        pdy, pdyt = self._pack(dy, B.MX4_STOCHASTIC)
+        pdy, pdyt = self._pack(dy, B.MX4_STOCHASTIC, self.K + worker)
         dx = self._product(pdy, self.packed_ut, tokens, self.inn, self.out, dy.dtype)
         return dx, self._product(pdyt, pxt, self.out, self.inn, tokens, torch.float32)
 

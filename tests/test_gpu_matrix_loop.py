@@ -39,14 +39,14 @@ def test_layer_and_round(loop_class, out, inn, tokens, dtype):
             for k in range(K):
                 x, dy = torch.randn(tokens, inn, generator=g).to(dtype), (torch.randn(tokens, out, generator=g) * 1e-2).to(dtype)
                 y, saved = loop.forward(x.cuda())
-                dx, dw = loop.backward(dy.cuda(), saved)
+                dx, dw = loop.backward(dy.cuda(), saved, worker=k)
                 assert y.dtype == dtype and dx.dtype == dtype and dw.dtype == torch.float32
                 x64, dy64 = x.double().numpy(), dy.double().numpy()
                 a, b = q(x64), q(u)
                 close(y, a @ b.T, inn, np.abs(a) @ np.abs(b).T, half_step)
-                a, b = q(dy64, True, seed, loop.round_id), q(u.T)
+                a, b = q(dy64, True, seed, loop.round_id, K + k), q(u.T)
                 close(dx, a @ b.T, out, np.abs(a) @ np.abs(b).T, half_step)
-                a, b = q(dy64.T, True, seed, loop.round_id), q(x64.T)
+                a, b = q(dy64.T, True, seed, loop.round_id, K + k), q(x64.T)
                 close(dw, a @ b.T, tokens, np.abs(a) @ np.abs(b).T, 2.0 ** -24)
                 grads[k] = dw
             acc = np.zeros((out, inn), np.float32)
@@ -85,3 +85,24 @@ def test_operands_that_are_not_contiguous(loop_class):
     assert torch.equal(y, loop.forward(wide[:, 7:87].contiguous())[0])
     turned = torch.randn(80, 20, generator=g).cuda().t()        # columns together
     assert torch.equal(loop.forward(turned)[0], loop.forward(turned.contiguous())[0])
+
+
+def test_gradients_that_are_broadcast(loop_class):
+    """What the backward pass of a sum hands over: one number for all, or one row for all."""
+    loop = loop_class(torch.randn(48, 80, generator=torch.Generator().manual_seed(1)).cuda(), 1, 5)
+    _, saved = loop.forward(torch.randn(20, 80, generator=torch.Generator().manual_seed(2)).cuda())
+    for dy in (torch.full((), 0.37, device="cuda").expand(20, 48), torch.randn(48, device="cuda").expand(20, 48)):
+        for got, want in zip(loop.backward(dy, saved), loop.backward(dy.contiguous(), saved)):
+            assert torch.equal(got, want)
+
+
+def test_calls_of_a_round_round_on_their_own(loop_class):
+    """Two workers with the same gradient dy, and the gradients that they send, draw different variates."""
+    loop = loop_class(torch.randn(64, 64, generator=torch.Generator().manual_seed(1)).cuda(), 2, 5)
+    _, saved = loop.forward(torch.eye(64, device="cuda"))
+    dy = torch.randn(64, 64, generator=torch.Generator().manual_seed(2)).cuda()
+    dw = [loop.backward(dy, saved, worker=k)[1] for k in range(2)]
+    assert not torch.equal(*dw)
+    loop.orthogonal_round(dy.t().expand(2, 64, 64).contiguous(), 0.0)
+    # with x = 1 the gradient is the rounded dy^T itself; the mean of the two that were sent is neither of them, nor their mean
+    assert not any(torch.equal(loop.mean, m) for m in (dw[0], dw[1], (dw[0] + dw[1]) / 2))

@@ -126,3 +126,25 @@ def test_types_that_the_binding_refuses(B):
     with pytest.raises(B.QesgdError) as e:
         B.qesgd_mx4_quantize_pack(x, 4, 0, 4, 4, 1, B.MX4_NEAREST, 0, 0, x, 0, stream=0)
     assert e.value.code == B.ERR_DTYPE
+
+
+def test_calls_that_would_number_too_many_threads(B):
+    assert quantize_rc(B, rows=(1 << 27) + 1, cols=128, ld=128) == B.ERR_DIM
+    assert quantize_rc(B, rows=1 << 21, cols=1 << 13, ld=(1 << 13) + 1, packed=None, packed_t=0x20001) == B.ERR_ALIGN     # 2^34: taken
+    assert quantize_rc(B, rows=1 << 28, cols=1, ld=1, packed=None, packed_t=0x20001) == B.ERR_DIM
+    assert quantize_rc(B, rows=1, cols=1 << 28, ld=1, packed=0x20000, packed_t=0x30000) == B.ERR_DIM          # 2^35 in the transposed form
+    f = B.lib().qesgd_mx4_unpack_aggregate_update
+    assert f(0x20000, 0, 1, (1 << 27) + 1, 128, None, 0x30000, None, None, None) == B.ERR_DIM
+    assert f(0x20000, 0, 1, 1 << 27, 128, None, 0x30004, None, None, None) == B.ERR_ALIGN
+
+
+def test_tensors_of_the_host_are_refused(B):
+    import torch
+    x, p = torch.zeros(4, 4), torch.zeros(1024, dtype=torch.uint8)
+    for call in (lambda: B.qesgd_mx4_quantize_pack(x, 4, 0, 4, 4, 1, B.MX4_NEAREST, 0, 0, p, 0, stream=0),
+                 lambda: B.qesgd_mx4_unpack_aggregate_update(p, 0, 1, 4, 4, None, x, None, None, stream=0),
+                 lambda: B.qesgd_mx4_product(p, p, 4, 4, 4, x, 4, stream=0),
+                 lambda: B.qesgd_orthogonalize(x, 4, 4, 1, R.USUAL, 1e-7, x, None, stream=0),
+                 lambda: B.qesgd_orthogonal_update(x, 4, 4, 1, None, 0.9, True, R.USUAL, 1e-7, 1.0, x, None, None, None, None, None, stream=0)):
+        with pytest.raises(ValueError, match="current GPU"):
+            call()
