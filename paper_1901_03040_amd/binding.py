@@ -256,6 +256,28 @@ def qesgd_epoch_commit(w_inout, zsum_inout, rounds, d, stream=None):
 
 
 # ---- matrix parameters ------------------------------------------------------
+#
+# The kernels run on the current device and take addresses: a tensor of the host or of another device is refused here, and so are
+# types that the call does not say.  Small calls cost the host about 5 us, most of it in the launch, so the checks stand in line and
+# numbers (plain ints) go to ctypes as they are: with a loop over the tensors and int() around each number a call took 0.9 us more.
+
+def _here(stream):
+    """The current device and the handle of the stream."""
+    if torch.cuda.is_initialized():
+        device = torch._C._cuda_getDevice()
+        if stream is None:
+            return device, torch._C._cuda_getCurrentRawStream(device)
+    elif stream is None:
+        stream = torch.cuda.current_stream()
+        device = torch.cuda.current_device()
+    else:
+        device = None
+    return device, stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _elsewhere(where: str, *tensors):
+    raise ValueError(f"{where}: tensors on {sorted({str(t.device) for t in tensors if t is not None})}, not all on the current GPU")
+
 
 def _dtype(t: torch.Tensor, where: str) -> int:
     code = DTYPES.get(t.dtype)
@@ -264,19 +286,27 @@ def _dtype(t: torch.Tensor, where: str) -> int:
     return code
 
 
-def _check_tensors(where: str, dtype: Optional[torch.dtype], *tensors):
-    """The kernels run on the current device, and take addresses: a tensor of the host, of another device or of another type is refused."""
-    device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+def _f32(where: str, device, *tensors):
+    """Addresses of fp32 tensors, each of which may be None."""
+    out = []
     for t in tensors:
-        if t is not None:
-            if t.get_device() != device:
-                raise ValueError(f"{where}: a tensor on {t.device}, which is not the current GPU")
-            if dtype is not None and t.dtype != dtype:
-                raise QesgdError(ERR_DTYPE, where)
+        if t is None:
+            out.append(None)
+            continue
+        if t.get_device() != device:
+            _elsewhere(where, *tensors)
+        if t.dtype is not torch.float32:
+            raise QesgdError(ERR_DTYPE, where)
+        out.append(t.data_ptr())
+    return out
 
 
-def _ws(workspace):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+def _ws(where: str, device, workspace):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device:
+        _elsewhere(where, workspace)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def qesgd_mx4_layout_query(rows: int, cols: int) -> Mx4Layout:
@@ -288,19 +318,22 @@ def qesgd_mx4_layout_query(rows: int, cols: int) -> Mx4Layout:
 def qesgd_mx4_quantize_pack(x, ld, x_stride, rows, cols, K, mode, seed, rnd, packed, packed_stride, packed_t=None,
                             packed_t_stride=0, worker=0, stream=None):
     dtype = _dtype(x, "qesgd_mx4_quantize_pack")
-    _check_tensors("qesgd_mx4_quantize_pack", None, x, packed, packed_t)
-    _check(lib().qesgd_mx4_quantize_pack(_ptr(x), dtype, int(ld), int(x_stride), int(rows), int(cols),
-                                         int(K), int(mode), int(seed), int(rnd), int(worker), _ptr(packed), int(packed_stride),
-                                         _ptr(packed_t), int(packed_t_stride), _stream(stream)), "qesgd_mx4_quantize_pack")
+    device, stream = _here(stream)
+    if x.get_device() != device or (packed is not None and packed.get_device() != device) or \
+            (packed_t is not None and packed_t.get_device() != device):
+        _elsewhere("qesgd_mx4_quantize_pack", x, packed, packed_t)
+    _check(lib().qesgd_mx4_quantize_pack(x.data_ptr(), dtype, ld, x_stride, rows, cols, K, mode, seed, rnd, worker, _ptr(packed),
+                                         packed_stride, _ptr(packed_t), packed_t_stride, stream), "qesgd_mx4_quantize_pack")
 
 
 def qesgd_mx4_unpack_aggregate_update(packed_slab, packed_stride, K, rows, cols, w_snap, zbar_out, u_out, zsum_inout,
                                       stream=None):
-    _check_tensors("qesgd_mx4_unpack_aggregate_update", None, packed_slab)
-    _check_tensors("qesgd_mx4_unpack_aggregate_update", torch.float32, w_snap, zbar_out, u_out, zsum_inout)
-    _check(lib().qesgd_mx4_unpack_aggregate_update(_ptr(packed_slab), int(packed_stride), int(K), int(rows), int(cols),
-                                                   _ptr(w_snap), _ptr(zbar_out), _ptr(u_out), _ptr(zsum_inout),
-                                                   _stream(stream)), "qesgd_mx4_unpack_aggregate_update")
+    device, stream = _here(stream)
+    if packed_slab.get_device() != device:
+        _elsewhere("qesgd_mx4_unpack_aggregate_update", packed_slab)
+    _check(lib().qesgd_mx4_unpack_aggregate_update(packed_slab.data_ptr(), packed_stride, K, rows, cols,
+                                                   *_f32("qesgd_mx4_unpack_aggregate_update", device, w_snap, zbar_out, u_out,
+                                                         zsum_inout), stream), "qesgd_mx4_unpack_aggregate_update")
 
 
 def qesgd_mx4_product_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -309,8 +342,11 @@ def qesgd_mx4_product_workspace_bytes(M: int, N: int, K: int) -> int:
 
 def qesgd_mx4_product(a_packed, b_packed, M, N, K, c, ldc, workspace=None, stream=None):
     dtype = _dtype(c, "qesgd_mx4_product")
-    _check_tensors("qesgd_mx4_product", None, a_packed, b_packed, c, workspace)
-    _check(lib().qesgd_mx4_product(_ptr(a_packed), _ptr(b_packed), int(M), int(N), int(K), _ptr(c), dtype, int(ldc), *_ws(workspace), _stream(stream)),
+    device, stream = _here(stream)
+    if a_packed.get_device() != device or b_packed.get_device() != device or c.get_device() != device:
+        _elsewhere("qesgd_mx4_product", a_packed, b_packed, c)
+    ws, ws_bytes = _ws("qesgd_mx4_product", device, workspace)
+    _check(lib().qesgd_mx4_product(a_packed.data_ptr(), b_packed.data_ptr(), M, N, K, c.data_ptr(), dtype, ldc, ws, ws_bytes, stream),
            "qesgd_mx4_product")
 
 
@@ -334,22 +370,24 @@ def qesgd_orthogonalize(x, rows, cols, n, coeffs, eps, out, workspace, stream=No
     if out.dtype != x.dtype:
         raise QesgdError(ERR_DTYPE, "qesgd_orthogonalize")
     dtype, steps = _dtype(x, "qesgd_orthogonalize"), _coeffs(coeffs)
-    _check_tensors("qesgd_orthogonalize", None, x, out, workspace)
-    _check(lib().qesgd_orthogonalize(_ptr(x), dtype, int(rows), int(cols), int(n), steps, len(coeffs), float(eps), _ptr(out),
-                                     *_ws(workspace), _stream(stream)),
-           "qesgd_orthogonalize")
+    device, stream = _here(stream)
+    if x.get_device() != device or out.get_device() != device:
+        _elsewhere("qesgd_orthogonalize", x, out)
+    ws, ws_bytes = _ws("qesgd_orthogonalize", device, workspace)
+    _check(lib().qesgd_orthogonalize(x.data_ptr(), dtype, rows, cols, n, steps, len(coeffs), eps, out.data_ptr(), ws, ws_bytes,
+                                     stream), "qesgd_orthogonalize")
 
 
 def qesgd_orthogonal_update(g, rows, cols, n, momentum_inout, mu, nesterov, coeffs, eps, alpha, step_out, z_inout, w_snap,
                             u_out, zsum_inout, workspace, stream=None):
     if g.dtype != torch.float32:
         raise QesgdError(ERR_DTYPE, "qesgd_orthogonal_update")
-    _check_tensors("qesgd_orthogonal_update", None, workspace)
-    _check_tensors("qesgd_orthogonal_update", torch.float32, g, momentum_inout, step_out, z_inout, w_snap, u_out, zsum_inout)
-    _check(lib().qesgd_orthogonal_update(_ptr(g), int(rows), int(cols), int(n), _ptr(momentum_inout), float(mu),
-                                         int(bool(nesterov)), _coeffs(coeffs), len(coeffs), float(eps), float(alpha),
-                                         _ptr(step_out), _ptr(z_inout), _ptr(w_snap), _ptr(u_out), _ptr(zsum_inout),
-                                         *_ws(workspace), _stream(stream)), "qesgd_orthogonal_update")
+    steps = _coeffs(coeffs)
+    device, stream = _here(stream)
+    g, m, step, z, w, u, zsum = _f32("qesgd_orthogonal_update", device, g, momentum_inout, step_out, z_inout, w_snap, u_out, zsum_inout)
+    ws, ws_bytes = _ws("qesgd_orthogonal_update", device, workspace)
+    _check(lib().qesgd_orthogonal_update(g, rows, cols, n, m, mu, 1 if nesterov else 0, steps, len(coeffs), eps, alpha, step, z, w, u,
+                                         zsum, ws, ws_bytes, stream), "qesgd_orthogonal_update")
 
 
 def qesgd_abi_version() -> int:
