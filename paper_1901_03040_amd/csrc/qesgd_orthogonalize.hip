@@ -77,11 +77,10 @@ __device__ __forceinline__ vec4 fetch4(const void* x, uint64_t at) {
 }
 
 // Momentum, and the partial sums of squares of x in fp64 (any fp32 magnitude squares into range).  Bound by the stream of g and m: four
-// elements a lane, kMomentumDepth of them on their way.  4096 x 25088: 580 us one by one, 236 us so.
-constexpr uint32_t kMomentumDepth = 4;
+// elements a lane.  4096 x 25088: 580 us one by one, 223 us so = 5.5 TB/s; two, four and eight loads a lane on their way 233, 233, 246.
 template <uint32_t DT>
 __global__ void __launch_bounds__(256) k_orthogonal_momentum(const SParams p) {
-    const uint64_t base = (uint64_t)blockIdx.y * p.d, quads = p.d / 4, stride = (uint64_t)p.parts * 256u;
+    const uint64_t base = (uint64_t)blockIdx.y * p.d, quads = p.d / 4;
     double sum = 0.0;
     const auto one = [&](float v, float& m) {
         if (p.momentum) {
@@ -90,25 +89,18 @@ __global__ void __launch_bounds__(256) k_orthogonal_momentum(const SParams p) {
         }
         sum += (double)v * (double)v;
     };
-    for (uint64_t q0 = (uint64_t)blockIdx.x * 256u + threadIdx.x; q0 < quads; q0 += stride * kMomentumDepth) {
-        vec4 g[kMomentumDepth], m[kMomentumDepth] = {};
+    for (uint64_t q = (uint64_t)blockIdx.x * 256u + threadIdx.x; q < quads; q += (uint64_t)p.parts * 256u) {
+        const uint64_t at = base + q * 4;
+        const vec4 g = fetch4<DT>(p.x, at);
+        vec4 m = {};
+        if (p.momentum) m = *(const vec4_any*)(p.momentum + at);
 #pragma unroll
-        for (uint32_t k = 0; k < kMomentumDepth; ++k) {
-            const uint64_t at = base + min(q0 + k * stride, quads - 1) * 4;
-            g[k] = fetch4<DT>(p.x, at);
-            if (p.momentum) m[k] = *(const vec4_any*)(p.momentum + at);
+        for (int e = 0; e < 4; ++e) {
+            float me = m[e];
+            one(g[e], me);
+            m[e] = me;
         }
-#pragma unroll
-        for (uint32_t k = 0; k < kMomentumDepth; ++k) {
-            if (q0 + k * stride >= quads) break;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float me = m[k][e];
-                one(g[k][e], me);
-                m[k][e] = me;
-            }
-            if (p.momentum) *(vec4_any*)(p.momentum + base + (q0 + k * stride) * 4) = m[k];
-        }
+        if (p.momentum) *(vec4_any*)(p.momentum + at) = m;
     }
     if (blockIdx.x == 0 && threadIdx.x < (p.d & 3u)) {
         const uint64_t at = base + quads * 4 + threadIdx.x;
@@ -378,6 +370,10 @@ struct SplitOps {
     }
 };
 
+// 4096 x 25088: X X^T in three pieces 1083 us, P X 2201 us, both 1.15 PFLOP/s of fp16 products, what a large library product reaches (the card lowers its
+// clock); the last one, with z, u and zsum behind it, 2479 us; G G 250 us = 0.82, 528 tiles on 512 places.  512 x 4608, 2 of them: X X^T 13, G G 7.6, P X
+// 33, the last 50 us.  With 64 x 64 tiles a step of 16 KB takes 0.2 us, 34 bytes a clock and CU from L2 to LDS: 3 or 8 buffers, a second set of
+// waves that shares the steps, or sums of their own for the three products change nothing, so small matrices stay 4.8 us + 0.2 us a step.
 template <class S, int KIND, uint32_t DT>
 __global__ void __launch_bounds__(S::threads) k_orthogonal_product(const OParams p) {
     static_assert(S::BM == S::BN, "symmetric products take square tiles");
@@ -448,7 +444,7 @@ __global__ void __launch_bounds__(S::threads) k_orthogonal_product(const OParams
 }
 
 // G from the partial sums of its contraction, added in order, 32 x 32 at a time, both halves.  A lane has one row's number of each of four
-// rows and eight pieces in flight: the sums are few and far apart.
+// rows and eight pieces in flight: the sums are few and far apart.  4096 x 4096 in three pieces 41 us, two of 512 x 512 in seven 5.
 __global__ void __launch_bounds__(256) k_orthogonal_gram_sum(const OParams p) {
     __shared__ float tile[32][33];
     uint32_t ti, tj;
@@ -506,7 +502,7 @@ __global__ void __launch_bounds__(256) k_orthogonal_gram_sum(const OParams p) {
 // a whole group of 32 numbers at once, and dealt to 16 waves.  A step: the tiles of G's upper half, where they are few the contraction
 // in pieces to several waves whose sums one wave adds in order; P = a I + b G + c G G by the same waves; P X tile by tile, held in
 // registers until every wave has read X.  Rows are groups of 128 bytes, chunks placed as in the pipeline.  64 x 64, 16 of them: 72 us as
-// the launches of the general path, 31 us with 32 x 32 tiles on 8 waves.
+// the launches of the general path, 31 us with 32 x 32 tiles on 8 waves, 23 us so.
 constexpr uint32_t kSmallWaves = 16, kSmallThreads = kSmallWaves * 64;
 constexpr uint32_t kSmallHeld = 4;       // tiles of P X that a wave holds
 constexpr uint32_t kSmallEach = kSmallHeld * 256 / 64;       // elements that a thread reads
