@@ -372,7 +372,7 @@ struct SplitOps {
 
 // 4096 x 25088: X X^T in three pieces 1083 us, P X 2201 us, both 1.15 PFLOP/s of fp16 products, what a large library product reaches (the card lowers its
 // clock); the last one, with z, u and zsum behind it, 2479 us; G G 250 us = 0.82, 528 tiles on 512 places.  512 x 4608, 2 of them: X X^T 13, G G 7.6, P X
-// 33, the last 50 us.  With 64 x 64 tiles a step of 16 KB takes 0.2 us, 34 bytes a clock and CU from L2 to LDS: 3 or 8 buffers, a second set of
+// 29, the last 46 us.  With 64 x 64 tiles a step of 16 KB takes 0.2 us, 34 bytes a clock and CU from L2 to LDS: 3 or 8 buffers, a second set of
 // waves that shares the steps, or sums of their own for the three products change nothing, so small matrices stay 4.8 us + 0.2 us a step.
 template <class S, int KIND, uint32_t DT>
 __global__ void __launch_bounds__(S::threads) k_orthogonal_product(const OParams p) {
@@ -751,7 +751,9 @@ __global__ void __launch_bounds__(kSmallThreads) k_orthogonal_small(const SmallP
 // Which tiles, and how many pieces of the contraction, from how long the workgroups take on 256 CUs.  Unit: a step of 512 workgroups
 // with 128 x 128 tiles, two a CU, 1.1 us of a full chip, and 3 us for a launch.  A last round of up to 256 has a CU each and takes 0.70 of that.  64 x 64: 0.38 (a
 // quarter of the work; each step reads twice as much for it).  256 x 256, one a CU: 1.78 a round (twice the work of a CU's two
-// 128s, 0.89 of the time).  Measured on 20 shapes from 128 x 128 to 4096 x 25088, one product changed at a time, five steps, us:
+// 128s, 0.89 of the time).  P X with 64 x 64: 0.12 for a last round of up to 256, because its stores and outputs run under other
+// workgroups' products.  Over 19 shapes and three tiles each, one step's products are 0.3% slower (P X, X X^T and G G) than with the best tile
+// of each; with 0.27 for P X too, 2.6%.  Measured on 20 shapes from 128 x 128 to 4096 x 25088, one product changed at a time, five steps, us:
 //   P X       512 x 4608, 2 of them 64: 349, 128: 360;  2048 x 2048 824 / 785;  1024 x 8192 699 / 640, 256: 725;  3000 x 3000 2398 / 2358 /
 //             2455;  2048 x 8192 2403 / 2153 / 2094;  4096 x 25088 28.2 / 24.3 / 24.7 ms
 //   G G       1024 x 1024, 12 of them 64: 1201, 128: 1143, 256: 1332;  4096 x 4096 5750 / 5306 / 5457
@@ -762,10 +764,10 @@ struct Cut {
     double us;                           // by this reckoning
 };
 
-double cut_cost(uint64_t groups, uint32_t edge) {
+double cut_cost(uint64_t groups, uint32_t edge, bool upper) {
     const uint64_t slots = edge == 256 ? 256 : 512, left = groups % slots;
-    const double rounds = (double)(groups / slots) + (left == 0 ? 0.0 : edge != 256 && left <= 256 ? 0.70 : 1.0);
-    return rounds * (edge == 256 ? 1.78 : edge == 128 ? 1.0 : 0.38);
+    const double full = edge == 256 ? 1.78 : edge == 128 ? 1.0 : 0.38, half = edge == 128 ? 0.70 : upper ? 0.27 : 0.12;
+    return (double)(groups / slots) * full + (left == 0 ? 0.0 : edge != 256 && left <= 256 ? half : full);
 }
 
 // M x N (upper = M x M, the upper half) over `steps` steps, `count` of them; more than one piece only for upper.
@@ -776,7 +778,7 @@ Cut choose_cut(uint64_t M, uint64_t N, uint64_t steps, uint64_t count, bool uppe
         for (uint32_t pieces = 1; pieces <= most_pieces && pieces * 4ull <= steps + 3ull; ++pieces) {
             // a piece has at least four steps; the sums of the pieces cost a launch, and are written and read at about 4 TB/s
             const double sums = pieces == 1 ? 0.0 : 3.0 + (double)pieces * (double)count * (double)(M * M) * 2e-6;
-            const double cost = 3.0 + cut_cost(tiles * pieces, edge) * (double)((steps + pieces - 1) / pieces) * 1.1 + sums;
+            const double cost = 3.0 + cut_cost(tiles * pieces, edge, upper) * (double)((steps + pieces - 1) / pieces) * 1.1 + sums;
             if (cost < best.us) best = Cut{edge, pieces, cost};
         }
     }
