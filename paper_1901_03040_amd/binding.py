@@ -374,7 +374,7 @@ def qesgd_orthogonalize(x, rows, cols, n, coeffs, eps, out, workspace, stream=No
     if x.get_device() != device or out.get_device() != device:
         _elsewhere("qesgd_orthogonalize", x, out)
     ws, ws_bytes = _ws("qesgd_orthogonalize", device, workspace)
-    _check(lib().qesgd_orthogonalize(x.data_ptr(), dtype, rows, cols, n, steps, len(coeffs), eps, out.data_ptr(), ws, ws_bytes,
+    _check(lib().qesgd_orthogonalize(x.data_ptr(), dtype, rows, cols, n, steps, len(coeffs), float(eps), out.data_ptr(), ws, ws_bytes,
                                      stream), "qesgd_orthogonalize")
 
 
@@ -386,8 +386,8 @@ def qesgd_orthogonal_update(g, rows, cols, n, momentum_inout, mu, nesterov, coef
     device, stream = _here(stream)
     g, m, step, z, w, u, zsum = _f32("qesgd_orthogonal_update", device, g, momentum_inout, step_out, z_inout, w_snap, u_out, zsum_inout)
     ws, ws_bytes = _ws("qesgd_orthogonal_update", device, workspace)
-    _check(lib().qesgd_orthogonal_update(g, rows, cols, n, m, mu, 1 if nesterov else 0, steps, len(coeffs), eps, alpha, step, z, w, u,
-                                         zsum, ws, ws_bytes, stream), "qesgd_orthogonal_update")
+    _check(lib().qesgd_orthogonal_update(g, rows, cols, n, m, float(mu), 1 if nesterov else 0, steps, len(coeffs), float(eps),
+                                         float(alpha), step, z, w, u, zsum, ws, ws_bytes, stream), "qesgd_orthogonal_update")
 
 
 def qesgd_abi_version() -> int:

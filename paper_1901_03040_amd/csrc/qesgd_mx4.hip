@@ -235,12 +235,13 @@ __global__ void __launch_bounds__(kQWaves * 64) k_mx4_quantize(const QParams p) 
 }
 
 // Both forms, or the transposed one alone, of a 128 x 128 tile.  The rows' form is made while the tile is read (a wave takes four
-// rows at a time, a quad a block); the raw elements go to LDS, and then a lane takes 32 rows of one column.  8192 x 4096 bf16: nearest 25 us
-// (4.1 TB/s of reads and writes), stochastic 52 us, which is its arithmetic: two Philox calls for 8 elements.
-constexpr uint32_t kTile = 128;
+// rows at a time, a quad a block); the raw elements go to LDS, and then a lane takes 32 rows of one column.  8192 x 4096 bf16: nearest 26 us
+// (4.0 TB/s of reads and writes), stochastic 52 us, which is its arithmetic: two Philox calls for 8 elements.  256 / 512 threads: 25.0 / 26.2 us
+// there, 512 x 512 f32, which waits for its loads, 5.3 / 4.6.
+constexpr uint32_t kTile = 128, kBothThreads = 512;
 
 template <uint32_t DT, bool STOCHASTIC>
-__global__ void __launch_bounds__(256) k_mx4_quantize_both(const QParams p) {
+__global__ void __launch_bounds__(kBothThreads) k_mx4_quantize_both(const QParams p) {
     typedef typename std::conditional<DT == QESGD_F32, float, unsigned short>::type elem;
     // 32 rows, then 64 bytes of room: the four blocks of a column that a quad reads at once lie in different banks
     constexpr uint32_t kRoom = 64 / sizeof(elem);
@@ -251,79 +252,69 @@ __global__ void __launch_bounds__(256) k_mx4_quantize_both(const QParams p) {
     const uint64_t x0 = (uint64_t)k * p.x_stride;
     const uint32_t col = (lane & 15u) * 8u;
     const uint32_t n = c0 + col >= p.cols ? 0u : p.cols - c0 - col < 8 ? (uint32_t)(p.cols - c0 - col) : 8u;
+    Eight<DT> v[4];
 #pragma unroll
-    for (uint32_t i0 = 0; i0 < 8; i0 += 4) {
-        Eight<DT> v[4];
+    for (uint32_t i = 0; i < 4; ++i) {
+        const uint64_t row = r0 + i * 32u + wave * 4u + (lane >> 4);
+        v[i].load(p.x, x0 + row * p.ld + c0 + col, row < p.rows ? n : 0u);
+    }
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            const uint64_t row = r0 + (i0 + i) * 16u + wave * 4u + (lane >> 4);
-            v[i].load(p.x, x0 + row * p.ld + c0 + col, row < p.rows ? n : 0u);
+    for (uint32_t i = 0; i < 4; ++i) {
+        const uint32_t r = i * 32u + wave * 4u + (lane >> 4);
+        const uint64_t row = r0 + r;
+        elem* to = tile + r * kTile + (r >> 5) * kRoom + col;
+        if constexpr (DT == QESGD_F32) {
+            *(vec4*)to = vec4{v[i].v[0], v[i].v[1], v[i].v[2], v[i].v[3]};
+            *(vec4*)(to + 4) = vec4{v[i].v[4], v[i].v[5], v[i].v[6], v[i].v[7]};
+        } else {
+            *(uvec4*)to = v[i].v;
         }
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            const uint32_t r = (i0 + i) * 16u + wave * 4u + (lane >> 4);
-            const uint64_t row = r0 + r;
-            elem* to = tile + r * kTile + (r >> 5) * kRoom + col;
-            if constexpr (DT == QESGD_F32) {
-                *(vec4*)to = vec4{v[i].v[0], v[i].v[1], v[i].v[2], v[i].v[3]};
-                *(vec4*)(to + 4) = vec4{v[i].v[4], v[i].v[5], v[i].v[6], v[i].v[7]};
-            } else {
-                *(uvec4*)to = v[i].v;
-            }
-            if (p.packed) {
-                const uint64_t slot = row * ((uint64_t)p.groups * 128u) + c0 + col;
-                const uint32_t sb = scale_byte<STOCHASTIC>(quad_max(v[i].top()));
-                const uint32_t word = encode8<DT, STOCHASTIC>(v[i], sb, slot >> 3, p.worker0 + k, p.round, p.key0, p.key1);
-                const uint32_t scales = row_bytes(sb, lane);
-                if (row < p.rows) {
-                    unsigned char* out = p.packed + (uint64_t)k * p.packed_stride;
-                    *(uint32_t*)(out + (slot >> 1)) = word;
-                    if ((lane & 15u) == 0) *(uint32_t*)(out + p.scales_off + (slot >> 5)) = scales;
-                }
+        if (p.packed) {
+            const uint64_t slot = row * ((uint64_t)p.groups * 128u) + c0 + col;
+            const uint32_t sb = scale_byte<STOCHASTIC>(quad_max(v[i].top()));
+            const uint32_t word = encode8<DT, STOCHASTIC>(v[i], sb, slot >> 3, p.worker0 + k, p.round, p.key0, p.key1);
+            const uint32_t scales = row_bytes(sb, lane);
+            if (row < p.rows) {
+                unsigned char* out = p.packed + (uint64_t)k * p.packed_stride;
+                *(uint32_t*)(out + (slot >> 1)) = word;
+                if ((lane & 15u) == 0) *(uint32_t*)(out + p.scales_off + (slot >> 5)) = scales;
             }
         }
     }
     __syncthreads();
-    const uint32_t block = lane & 3u;
-    // A lane takes one column of 32-bit elements twice, or a pair of columns of 16-bit ones once: a word of LDS either way.
-#pragma unroll 1
-    for (uint32_t i = 0; i < (DT == QESGD_F32 ? 2u : 1u); ++i) {
-        const uint32_t word_col = i * 64u + wave * 16u + (lane >> 2);
-        const uint32_t* from = (const uint32_t*)tile + block * (32u * kTile + kRoom) * sizeof(elem) / 4u + word_col;
-        uint32_t raw[32];
+    // A lane takes 32 rows of a column: one of 32-bit elements, or of 16-bit ones either of the pair that a word of LDS holds.
+    const uint32_t block = lane & 3u, word_col = DT == QESGD_F32 ? threadIdx.x >> 2 : (threadIdx.x >> 2) & 63u;
+    const uint32_t side = DT == QESGD_F32 ? 0u : threadIdx.x >> 8;
+    const uint32_t* from = (const uint32_t*)tile + block * (32u * kTile + kRoom) * sizeof(elem) / 4u + word_col;
+    uint32_t raw[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) raw[j] = from[j * (kTile * sizeof(elem) / 4u)];
+    for (int j = 0; j < 32; ++j) raw[j] = from[j * (kTile * sizeof(elem) / 4u)];
+    Eight<DT> y[4];
 #pragma unroll
-        for (uint32_t side = 0; side < 4u / sizeof(elem); ++side) {
-            Eight<DT> v[4];
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (DT == QESGD_F32) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (DT == QESGD_F32) {
+            for (int e = 0; e < 8; ++e) y[j].v[e] = __uint_as_float(raw[j * 8 + e]);
+        } else {
+            // the lower (upper) halves of two rows' words, as a pair along the column
+            const uint32_t pick = side ? 0x07060302u : 0x05040100u;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[j].v[e] = __uint_as_float(raw[j * 8 + e]);
-                } else {
-                    // the lower (upper) halves of two rows' words, as a pair along the column
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        v[j].v[e] = __builtin_amdgcn_perm(raw[j * 8 + 2 * e + 1], raw[j * 8 + 2 * e], side ? 0x07060302u : 0x05040100u);
-                }
-            }
-            const uint32_t c = DT == QESGD_F32 ? word_col : word_col * 2u + side;
-            const uint32_t sb = scale_byte<STOCHASTIC>(max(max(v[0].top(), v[1].top()), max(v[2].top(), v[3].top())));
-            const uint64_t slot = (c0 + c) * ((uint64_t)p.groups_t * 128u) + r0 + block * 32u;
-            uvec4 w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = encode8<DT, STOCHASTIC>(v[j], sb, (slot >> 3) + j, p.worker0 + k, p.round, p.key0, p.key1);
-            uint32_t scales = sb << (8u * block);
-            scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0xB1, 0xF, 0xF, false);
-            scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x4E, 0xF, 0xF, false);
-            if (c0 + c < p.cols) {
-                unsigned char* out = p.packed_t + (uint64_t)k * p.packed_t_stride;
-                *(uvec4*)(out + (slot >> 1)) = w;
-                if (block == 0) *(uint32_t*)(out + p.scales_t_off + (slot >> 5)) = scales;
-            }
+            for (int e = 0; e < 4; ++e) y[j].v[e] = __builtin_amdgcn_perm(raw[j * 8 + 2 * e + 1], raw[j * 8 + 2 * e], pick);
         }
+    }
+    const uint32_t c = DT == QESGD_F32 ? word_col : word_col * 2u + side;
+    const uint32_t sb = scale_byte<STOCHASTIC>(max(max(y[0].top(), y[1].top()), max(y[2].top(), y[3].top())));
+    const uint64_t slot = (c0 + c) * ((uint64_t)p.groups_t * 128u) + r0 + block * 32u;
+    uvec4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = encode8<DT, STOCHASTIC>(y[j], sb, (slot >> 3) + j, p.worker0 + k, p.round, p.key0, p.key1);
+    uint32_t scales = sb << (8u * block);
+    scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0xB1, 0xF, 0xF, false);
+    scales |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)scales, 0x4E, 0xF, 0xF, false);
+    if (c0 + c < p.cols) {
+        unsigned char* out = p.packed_t + (uint64_t)k * p.packed_t_stride;
+        *(uvec4*)(out + (slot >> 1)) = w;
+        if (block == 0) *(uint32_t*)(out + p.scales_t_off + (slot >> 5)) = scales;
     }
 }
 
@@ -435,8 +426,8 @@ template <uint32_t DT, bool STOCHASTIC>
 int launch_quantize_as(const Mx4Quantize& a, QParams& p, bool flat) {
     if (p.packed_t) {
         const uint64_t tiles = ((a.rows + kTile - 1) / kTile) * p.groups;
-        if (!grid_ok(tiles, 256)) return QESGD_ERR_DIM;
-        k_mx4_quantize_both<DT, STOCHASTIC><<<dim3((uint32_t)tiles, a.K), 256, 0, a.stream>>>(p);
+        if (!grid_ok(tiles, kBothThreads)) return QESGD_ERR_DIM;
+        k_mx4_quantize_both<DT, STOCHASTIC><<<dim3((uint32_t)tiles, a.K), kBothThreads, 0, a.stream>>>(p);
         return finish_launch();
     }
     constexpr uint64_t tile = kQWaves * kQChunks * kChunk;

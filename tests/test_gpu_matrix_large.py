@@ -249,3 +249,40 @@ def test_orthogonalize_beyond_32_bits(B, n, rows, cols):
         P.diagonal().add_(a)
         want = P @ (x[i, :, -2000:].double() / norm)
         assert float((out[i, :, -2000:].double() - want).norm()) <= 5 * 2.0 ** -22 * float(want.norm()) * max(1.0, a / float(torch.linalg.eigvalsh(P).abs().min()))
+
+
+def test_two_calls_at_once(B):
+    """On two streams, each with a workspace of its own: the same bits as one after the other."""
+    rows, cols = 520, 2080
+    M, N, K = 512, 1000, 25_088
+    assert B.qesgd_mx4_product_workspace_bytes(M, N, K) > 0
+    x = torch.randn(2, 1, rows, cols, generator=torch.Generator(device="cuda").manual_seed(0), device="cuda")
+    out, alone = torch.empty_like(x), torch.empty_like(x)
+    pa, pb = [packed_noise(B, M, K, i)[1] for i in range(2)], [packed_noise(B, N, K, 5 + i)[1] for i in range(2)]
+    c, c_alone = (torch.empty(2, M, N, device="cuda") for _ in range(2))
+    wx = [B.alloc_workspace(B.qesgd_orthogonalize_workspace_bytes(rows, cols, 1)) for _ in range(2)]
+    wp = [B.alloc_workspace(B.qesgd_mx4_product_workspace_bytes(M, N, K)) for _ in range(2)]
+
+    def work(i, to, product):
+        for _ in range(5):
+            B.qesgd_orthogonalize(x[i], rows, cols, 1, R.USUAL, 1e-7, to[i], wx[i])
+            B.qesgd_mx4_product(pa[i], pb[i], M, N, K, product[i], N, workspace=wp[i])
+
+    for i in range(2):
+        work(i, alone, c_alone)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i, stream in enumerate(streams):
+        with torch.cuda.stream(stream):
+            work(i, out, c)
+    torch.cuda.synchronize()
+    assert torch.equal(out, alone) and torch.equal(c, c_alone)
+
+
+def test_hyperparameters_of_other_types(B):
+    x = torch.randn(40, 60, device="cuda")
+    a, b = torch.empty_like(x), torch.empty_like(x)
+    B.qesgd_orthogonal_update(x, 40, 60, 1, None, 0.5, True, R.USUAL, 1e-7, -0.25, a, None, None, None, None, None)
+    B.qesgd_orthogonal_update(x, 40, 60, 1, None, np.float32(0.5), True, np.array(R.USUAL), np.float64(1e-7), torch.tensor(-0.25), b, None, None,
+                              None, None, None)
+    assert torch.equal(a, b)
