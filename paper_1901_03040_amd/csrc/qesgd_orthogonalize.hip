@@ -72,8 +72,17 @@ __device__ __forceinline__ double wave_sum(double v) {
 typedef vec4 vec4_any __attribute__((aligned(4)));
 template <uint32_t DT>
 __device__ __forceinline__ vec4 fetch4(const void* x, uint64_t at) {
-    if constexpr (DT == QESGD_F32) return *(const vec4_any*)((const float*)x + at);
-    else return vec4{fetch<DT>(x, at), fetch<DT>(x, at + 1), fetch<DT>(x, at + 2), fetch<DT>(x, at + 3)};
+    if constexpr (DT == QESGD_F32) {
+        return *(const vec4_any*)((const float*)x + at);
+    } else {
+        typedef uint32_t pairs __attribute__((ext_vector_type(2)));
+        typedef pairs pairs_any __attribute__((aligned(2)));
+        const pairs v = *(const pairs_any*)((const unsigned short*)x + at);
+        const uint32_t a = v[0], b = v[1];
+        if (DT == QESGD_BF16) return vec4{__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u)};
+        const auto half = [](uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (unsigned short)bits); };
+        return vec4{half(a), half(a >> 16), half(b), half(b >> 16)};
+    }
 }
 
 // Momentum, and the partial sums of squares of x in fp64 (any fp32 magnitude squares into range).  Bound by the stream of g and m: four
@@ -115,23 +124,36 @@ __global__ void __launch_bounds__(256) k_orthogonal_momentum(const SParams p) {
     if (threadIdx.x == 0) p.partial[(uint64_t)blockIdx.y * p.parts + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// X and its transpose, split, from a 64 x 64 tile of x.  A lane stores four numbers of a row.  4096 x 25088: 355 us with one, 332 us so.
+// X and its transpose, split, from a 64 x 64 tile of x.  A lane reads and stores four numbers of a row.
+// 4096 x 25088: 355 us with one, 332 with four stored at once, 271 us so; 1000 x 2049 of bf16 12.6 and 9.0.
 template <uint32_t DT>
 __global__ void __launch_bounds__(256) k_orthogonal_split(const SParams p) {
     __shared__ __attribute__((aligned(16))) float tile[64][68];
     __shared__ double part[4];
     const uint32_t r0 = blockIdx.y * 64u, c0 = blockIdx.x * 64u;
     const uint64_t base = (uint64_t)blockIdx.z * p.d;
-    const uint32_t tx = threadIdx.x & 63u, ty = threadIdx.x >> 6;
-    float v[16];
+    const uint32_t k4 = (threadIdx.x & 15u) * 4u, i16 = threadIdx.x >> 4;
+    vec4 v[4];
 #pragma unroll
-    for (uint32_t i = 0; i < 16; ++i) {
-        const uint32_t r = r0 + ty + 4u * i, c = c0 + tx;
-        const bool in = r < p.rows && c < p.cols;
-        const uint64_t at = base + (in ? (uint64_t)r * p.cols + c : 0u);
-        v[i] = p.momentum && !p.nesterov ? 0.0f : fetch<DT>(p.x, at);
-        if (p.momentum) v[i] = p.nesterov ? v[i] + p.mu * p.momentum[at] : p.momentum[at];
-        if (!in) v[i] = 0.0f;
+    for (uint32_t i = 0; i < 4; ++i) {
+        const uint32_t r = r0 + i16 + 16u * i, c = c0 + k4;
+        const uint64_t at = base + (uint64_t)r * p.cols + c;
+        v[i] = vec4{};
+        if (r < p.rows && c + 4u <= p.cols) {
+            if (!p.momentum || p.nesterov) v[i] = fetch4<DT>(p.x, at);
+            if (p.momentum) {
+                const vec4 m = *(const vec4_any*)(p.momentum + at);
+                v[i] = p.nesterov ? v[i] + p.mu * m : m;
+            }
+        } else if (r < p.rows) {
+#pragma unroll
+            for (uint32_t e = 0; e < 3; ++e) {
+                if (c + e >= p.cols) break;
+                float one = p.momentum && !p.nesterov ? 0.0f : fetch<DT>(p.x, at + e);
+                if (p.momentum) one = p.nesterov ? one + p.mu * p.momentum[at + e] : p.momentum[at + e];
+                v[i][e] = one;
+            }
+        }
     }
     double sum = 0.0;
     for (uint32_t i = threadIdx.x; i < p.parts; i += 256u) sum += p.partial[(uint64_t)blockIdx.z * p.parts + i];
@@ -142,7 +164,12 @@ __global__ void __launch_bounds__(256) k_orthogonal_split(const SParams p) {
     const double norm = sqrt(sum) + (double)p.eps;
     const double scale = norm > 0.0 ? (double)kScaleX / norm : 0.0;     // beyond fp32 where x is subnormal
 #pragma unroll
-    for (uint32_t i = 0; i < 16; ++i) tile[ty + 4u * i][tx] = (float)((double)v[i] * scale);
+    for (uint32_t i = 0; i < 4; ++i) {
+        vec4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (float)((double)v[i][e] * scale);
+        *(vec4*)&tile[i16 + 16u * i][k4] = y;
+    }
     __syncthreads();
     // rows of x: those of X where rows <= cols, of its transpose otherwise
     const bool turned = p.rows > p.cols;
@@ -161,16 +188,15 @@ __global__ void __launch_bounds__(256) k_orthogonal_split(const SParams p) {
         *(half4*)to = hi;
         *(half4*)(to + 64) = lo;
     };
-    const uint32_t k4 = (threadIdx.x & 15u) * 4u;
 #pragma unroll
     for (uint32_t i0 = 0; i0 < 64; i0 += 16) {
-        const uint32_t i = i0 + (threadIdx.x >> 4);
+        const uint32_t i = i0 + i16;
         if (r0 + i < p.rows && (c0 + k4) * 4u < pr) store4(rowwise + (uint64_t)(r0 + i) * pr + split_at(c0 + k4), *(const vec4*)&tile[i][k4]);
     }
     // a lane takes its column from four rows: neighbours are 4 rows apart, 4 * 68 words, 16 banks
 #pragma unroll
     for (uint32_t i0 = 0; i0 < 64; i0 += 16) {
-        const uint32_t i = i0 + (threadIdx.x >> 4);
+        const uint32_t i = i0 + i16;
         const vec4 x = {tile[k4][i], tile[k4 + 1][i], tile[k4 + 2][i], tile[k4 + 3][i]};
         if (c0 + i < p.cols && (r0 + k4) * 4u < pc) store4(colwise + (uint64_t)(c0 + i) * pc + split_at(r0 + k4), x);
     }
