@@ -398,7 +398,7 @@ struct SplitOps {
 
 // 4096 x 25088: X X^T in three pieces 1083 us, P X 2201 us, both 1.15 PFLOP/s of fp16 products, what a large library product reaches (the card lowers its
 // clock); the last one, with z, u and zsum behind it, 2479 us; G G 250 us = 0.82, 528 tiles on 512 places.  512 x 4608, 2 of them: X X^T 13, G G 7.6, P X
-// 29, the last 46 us.  With 64 x 64 tiles a step of 16 KB takes 0.2 us, 34 bytes a clock and CU from L2 to LDS: 3 or 8 buffers, a second set of
+// 29, the last 41 us.  With 64 x 64 tiles a step of 16 KB takes 0.2 us, 34 bytes a clock and CU from L2 to LDS: 3 or 8 buffers, a second set of
 // waves that shares the steps, or sums of their own for the three products change nothing, so small matrices stay 4.8 us + 0.2 us a step.
 template <class S, int KIND, uint32_t DT>
 __global__ void __launch_bounds__(S::threads) k_orthogonal_product(const OParams p) {
