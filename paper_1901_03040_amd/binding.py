@@ -258,7 +258,7 @@ def qesgd_epoch_commit(w_inout, zsum_inout, rounds, d, stream=None):
 # ---- matrix parameters ------------------------------------------------------
 #
 # The kernels run on the current device and take addresses: a tensor of the host or of another device is refused here, and so are
-# types that the call does not say.  Small calls cost the host about 5 us, most of it in the launch, so the checks stand in line and
+# types that the call does not say, and views with gaps or another order where the call has no stride for them.  Small calls cost the host about 5 us, most of it in the launch, so the checks stand in line and
 # numbers (plain ints) go to ctypes as they are: with a loop over the tensors and int() around each number a call took 0.9 us more.
 
 def _here(stream):
@@ -287,7 +287,7 @@ def _dtype(t: torch.Tensor, where: str) -> int:
 
 
 def _f32(where: str, device, *tensors):
-    """Addresses of fp32 tensors, each of which may be None."""
+    """Addresses of contiguous fp32 tensors, each of which may be None."""
     out = []
     for t in tensors:
         if t is None:
@@ -297,6 +297,8 @@ def _f32(where: str, device, *tensors):
             _elsewhere(where, *tensors)
         if t.dtype is not torch.float32:
             raise QesgdError(ERR_DTYPE, where)
+        if not t.is_contiguous():
+            raise QesgdError(ERR_STRIDE, where)
         out.append(t.data_ptr())
     return out
 
@@ -373,6 +375,8 @@ def qesgd_orthogonalize(x, rows, cols, n, coeffs, eps, out, workspace, stream=No
     device, stream = _here(stream)
     if x.get_device() != device or out.get_device() != device:
         _elsewhere("qesgd_orthogonalize", x, out)
+    if not (x.is_contiguous() and out.is_contiguous()):
+        raise QesgdError(ERR_STRIDE, "qesgd_orthogonalize")
     ws, ws_bytes = _ws("qesgd_orthogonalize", device, workspace)
     _check(lib().qesgd_orthogonalize(x.data_ptr(), dtype, rows, cols, n, steps, len(coeffs), float(eps), out.data_ptr(), ws, ws_bytes,
                                      stream), "qesgd_orthogonalize")

@@ -56,11 +56,8 @@ PRODUCTS = [(16, 8192, 4096), (17, 8192, 4096), (16, 8193, 4096), (16, 515, 4097
             (1, 20_000, 64), (20_000, 3, 200)]
 
 
-@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("M,N,K", PRODUCTS)
+@pytest.mark.parametrize("M,N,K,dtype", [(*c, t) for c in PRODUCTS for t in HALF_STEP if t == torch.float32 or c[2] <= 30_000])
 def test_product(B, M, N, K, dtype):
-    if dtype != torch.float32 and (M * N > 17_000_000 or K > 30_000):
-        pytest.skip("the type only changes the last store: covered by the other sizes")
     la, pa = packed_noise(B, M, K, M + K)
     lb, pb = packed_noise(B, N, K, N + 2 * K)
     if dtype == torch.float16:                                  # sums stay in range
@@ -279,6 +276,26 @@ def test_two_calls_at_once(B):
     assert torch.equal(out, alone) and torch.equal(c, c_alone)
 
 
+def test_views_are_refused(B):
+    x, out = torch.randn(64, 64, device="cuda"), torch.empty(64, 64, device="cuda")
+    row = torch.randn(64, device="cuda").expand(64, 64)
+    calls = [lambda v: B.qesgd_orthogonalize(v, 64, 64, 1, R.USUAL, 1e-7, out, None), lambda v: B.qesgd_orthogonalize(x, 64, 64, 1, R.USUAL, 1e-7, v, None)]
+    for at in range(5):
+        def update(v, at=at):
+            t = [x, None, out, None, None, None, None]
+            t[at] = v
+            if at >= 4:
+                t[3], t[4], t[5] = (torch.empty(64, 64, device="cuda") if i != at else v for i in (3, 4, 5))
+            g, m, step, z, w, u, zsum = t
+            B.qesgd_orthogonal_update(g, 64, 64, 1, m, 0.9, True, R.USUAL, 1e-7, 1.0, step, z, w, u, zsum, None)
+        calls.append(update)
+    for call in calls:
+        for v in (x.t(), row, torch.randn(64, 128, device="cuda")[:, :64]):
+            with pytest.raises(B.QesgdError) as e:
+                call(v)
+            assert e.value.code == B.ERR_STRIDE
+
+
 def test_hyperparameters_of_other_types(B):
     x = torch.randn(40, 60, device="cuda")
     a, b = torch.empty_like(x), torch.empty_like(x)
@@ -286,3 +303,16 @@ def test_hyperparameters_of_other_types(B):
     B.qesgd_orthogonal_update(x, 40, 60, 1, None, np.float32(0.5), True, np.array(R.USUAL), np.float64(1e-7), torch.tensor(-0.25), b, None, None,
                               None, None, None)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("rows,cols", [(40, 50), (1, 9), (300, 200), (200, 900), (1, 3000)])
+def test_what_is_not_finite_takes_its_whole_matrix(B, rows, cols, bad):
+    x = torch.randn(3, rows, cols, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    ws = B.alloc_workspace(B.qesgd_orthogonalize_workspace_bytes(rows, cols, 3))
+    want, out = torch.empty_like(x), torch.empty_like(x)
+    B.qesgd_orthogonalize(x, rows, cols, 3, R.USUAL, 1e-7, want, ws)
+    x[1, rows // 2, cols // 3] = bad
+    B.qesgd_orthogonalize(x, rows, cols, 3, R.USUAL, 1e-7, out, ws)
+    assert bool(torch.isnan(out[1]).all())
+    assert torch.equal(out[0], want[0]) and torch.equal(out[2], want[2])

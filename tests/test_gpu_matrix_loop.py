@@ -106,3 +106,43 @@ def test_calls_of_a_round_round_on_their_own(loop_class):
     loop.orthogonal_round(dy.t().expand(2, 64, 64).contiguous(), 0.0)
     # with x = 1 the gradient is the rounded dy^T itself; the mean of the two that were sent is neither of them, nor their mean
     assert not any(torch.equal(loop.mean, m) for m in (dw[0], dw[1], (dw[0] + dw[1]) / 2))
+
+
+def test_a_layer_and_a_round_from_a_graph(loop_class):
+    """Captured once and replayed: every replay equals the eager calls of the same round, with the program's own work between."""
+    K = 2
+
+    def start():
+        g = torch.Generator().manual_seed(3)
+        loop = loop_class(torch.randn(96, 160, generator=g).cuda(), K, 11)
+        return loop, torch.randn(50, 160, generator=g).cuda(), torch.randn(50, 96, generator=g).cuda(), torch.empty(K, 96, 160, device="cuda")
+
+    def step(loop, x, dy, grads):
+        loop.round_id = 0                                       # part of the captured calls
+        y, saved = loop.forward(x)
+        for k in range(K):
+            dx, dw = loop.backward(dy, saved, worker=k)
+            grads[k].copy_(dw)
+        loop.orthogonal_round(grads, 0.1)
+        return y, dx
+
+    eager = start()
+    want = []
+    for _ in range(4):
+        y, dx = step(*eager)
+        want.append([t.clone() for t in (y, dx, eager[0].u, eager[0].zsum, eager[0].momentum)])
+    state = start()
+    step(*state)                                                # warm, and then back to the beginning
+    fresh = start()[0]
+    for name in ("u", "z", "zsum", "momentum", "packed_u", "packed_ut"):
+        getattr(state[0], name).copy_(getattr(fresh, name))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, dx = step(*state)
+    for i in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, ref in zip((y, dx, state[0].u, state[0].zsum, state[0].momentum), want[i]):
+            assert torch.equal(got, ref), i
+        assert np.isfinite(torch.randn(1 << 16, device="cuda").sum().item())
