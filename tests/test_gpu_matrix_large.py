@@ -179,7 +179,7 @@ def newton_schulz(x, coeffs, eps=1e-7, noise=0.0):
 ORTHOGONAL = [(1, 520, 2080, 5), (1, 2080, 520, 5), (1, 520, 2080, 1), (1, 520, 2080, 2), (1, 520, 2080, 3), (1, 520, 2080, 4), (1, 520, 2080, 6),
               (1, 1030, 1999, 5), (1, 2048, 2048, 5), (1, 3001, 2011, 4), (1, 1000, 9001, 5), (1, 9001, 1000, 2), (1, 2100, 7777, 5),
               (1, 4100, 4100, 2), (1, 4096, 9000, 3), (6, 700, 900, 3), (12, 1024, 1024, 2), (40, 100, 300, 5), (3, 130, 50_001, 5),
-              (1, 2048, 8192, 3), (1, 5632, 11_264, 2), (1, 1, 100_000, 5), (1, 70_000, 2, 5), (1000, 20, 1100, 5), (300, 97, 97, 3), (70, 96, 170, 5)]
+              (1, 2048, 8192, 3), (1, 5632, 11_264, 2), (1, 1, 100_000, 5), (1, 70_000, 2, 5), (1000, 20, 1100, 5), (300, 97, 97, 3), (70, 96, 170, 5), (3, 96, 160, 5), (3, 161, 96, 5), (2, 32, 512, 5), (2, 33, 512, 5), (2, 513, 32, 5)]
 
 
 @pytest.mark.parametrize("n,rows,cols,steps", ORTHOGONAL)
