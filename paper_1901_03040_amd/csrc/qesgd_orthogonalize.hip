@@ -15,6 +15,7 @@
 // contraction, which takes X for X X^T and its transpose for P X: the last product's epilogue writes both.  G and P are symmetric:
 // only tiles on and above the diagonal are computed, and the epilogue writes them twice.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -25,9 +26,61 @@
 namespace qesgd {
 namespace {
 
-constexpr float kScaleX = 4096.0f;      // of X's entries (at most 1 at first; singular values near 1 keep them there): below 16
-constexpr float kScaleG = 4096.0f;      // of G's
-constexpr float kScaleP = 256.0f;       // of P's, and of a product of two P: below 256
+constexpr double kMost = 1099511627776.0;        // 2^40: what G, P and a product of two P may reach
+constexpr float kFirstX = 32768.0f;              // scale of the first X, whose entries are at most 1
+
+// The power of two that takes numbers up to `bound` to at most 2^15, half of fp16's range: rounding may pass the bound.
+inline double scale_for(double bound) {
+    const double b = bound < kMost ? std::max(bound, 1.0 / kMost) : kMost;        // a NaN counts as the most
+    return std::ldexp(1.0, 15 - (int)std::ceil(std::log2(b)));
+}
+
+// How large the operands of each step can be, from the coefficients alone.  The singular values of the first X are at most 1, its
+// Frobenius norm; those of the next at most the largest |a s + b s^3 + c s^5| on the way, G's are their squares, P's at most the largest
+// |a + b s^2 + c s^4|, and no entry of a matrix is larger than its largest singular value.  So the operands' scales are known before
+// the first kernel, whatever the matrix, and use fp16's range from its upper end.
+struct Scales {
+    double X[QESGD_MAX_STEPS + 1], G[QESGD_MAX_STEPS + 1], P[QESGD_MAX_STEPS];
+    double T[QESGD_MAX_STEPS], PP[QESGD_MAX_STEPS];       // G P, and the product of this step's P and the next one's
+    bool pairs;                                           // no product of two P is beyond what is taken
+};
+
+inline Scales scales_of(const float* coeffs, uint32_t steps) {
+    Scales r{};
+    r.pairs = true;
+    double S = 1.0, before = 0.0;
+    for (uint32_t i = 0; i < steps; ++i) {
+        const double a = coeffs[3 * i], b = coeffs[3 * i + 1], c = coeffs[3 * i + 2];
+        const double s = S * (1.0 + 1.0 / 65536.0), end = s * s;      // rounding moves singular values by less than that
+        double next = 0.0, most = std::abs(a);
+        const auto at = [&](double u) {
+            if (!(u > 0.0 && u <= end)) return;
+            const double v = std::abs(a + u * (b + u * c));
+            most = std::max(most, v);
+            next = std::max(next, std::sqrt(u) * v);
+        };
+        // The ends of the range, and where (a + b u + c u^2)' or (s (a + b s^2 + c s^4))' = a + 3 b u + 5 c u^2 is zero; without a b or a c, or
+        // without real roots, some of these are no numbers and no places.
+        const double q = -0.5 * (3.0 * b + std::copysign(std::sqrt(9.0 * b * b - 20.0 * a * c), b));
+        at(end);
+        at(-b / (2.0 * c));
+        at(q / (5.0 * c));
+        at(a / q);
+        r.X[i] = i == 0 ? (double)kFirstX : scale_for(S);
+        r.G[i] = scale_for(S * S);
+        r.T[i] = scale_for(S * next);
+        r.P[i] = scale_for(most);
+        if (i > 0) {
+            r.PP[i - 1] = scale_for(before * most);
+            if (!(before * most <= kMost)) r.pairs = false;
+        }
+        before = most;
+        S = std::min(next, 1.0 / 1024.0 * kMost * kMost);              // beyond what is taken, and far from the end of 64 bits
+    }
+    r.X[steps] = scale_for(S);
+    r.G[steps] = scale_for(S * S);
+    return r;
+}
 
 inline uint64_t split_pitch(uint64_t k) { return round_up_to(k, 32) * 4; }
 
@@ -162,7 +215,7 @@ __global__ void __launch_bounds__(256) k_orthogonal_split(const SParams p) {
     __syncthreads();
     sum = (part[0] + part[1]) + (part[2] + part[3]);
     const double norm = sqrt(sum) + (double)p.eps;
-    const double scale = norm > 0.0 ? (double)kScaleX / norm : 0.0;     // beyond fp32 where x is subnormal
+    const double scale = norm > 0.0 ? (double)kFirstX / norm : 0.0;     // beyond fp32 where x is subnormal
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
         vec4 y;
@@ -565,7 +618,7 @@ struct SmallParams {
     OParams o;                           // of the last product
     SmallLayout L;
     uint32_t steps;
-    float coeffs[3 * QESGD_MAX_STEPS];
+    struct Step { float g, a, b, c, y; } step[QESGD_MAX_STEPS];       // of the sums, into the scales of G, P and the next X
 };
 
 // Byte of number k's hi in a row (its lo: the place with 64 flipped, chunk c + 4 instead of c).
@@ -673,7 +726,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orthogonal_small(const SmallP
 #pragma unroll
     for (uint32_t i = 0; i < kSmallWaves; ++i) sum += sums[i];
     const double norm = sqrt(sum) + (double)p.s.eps;
-    const double scale = norm > 0.0 ? (double)kScaleX / norm : 0.0;
+    const double scale = norm > 0.0 ? (double)kFirstX / norm : 0.0;
     const bool turned = p.s.rows > p.s.cols;
     {
         uint32_t r = threadIdx.x / p.s.cols, c = threadIdx.x - r * p.s.cols;
@@ -717,7 +770,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orthogonal_small(const SmallP
     for (uint32_t step = 0;; ++step) {
         // sums with these are formed where they are used: kept over the steps, they spill
         asm volatile("" : "+v"(px.read), "+v"(px.col), "+v"(pg.read), "+v"(pg.col), "+v"(pg.row));
-        const float ca = p.coeffs[3 * step], cb = p.coeffs[3 * step + 1], cc = p.coeffs[3 * step + 2];
+        const SmallParams::Step& f = p.step[step];
         acc4 g[2] = {};
 #pragma unroll
         for (uint32_t k = 0; k < 2; ++k) {
@@ -731,7 +784,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orthogonal_small(const SmallP
         for (uint32_t k = 0; k < 2; ++k) {
             if (wave + k * kSmallWaves < L.tiles) {
                 for (uint32_t i = 1; i < L.pieces; ++i) g[k] += partial[((i - 1) * L.tiles + wave) * 64u + lane];
-                g[k] *= kScaleG / (kScaleX * kScaleX);
+                g[k] *= f.g;
                 put_tile(ti[k] != tj[k] ? G : nullptr, pg, G, pg, ti[k], tj[k], g[k]);
             }
         }
@@ -743,8 +796,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orthogonal_small(const SmallP
                 const bool diagonal = ti[k] == tj[k];
 #pragma unroll
                 for (uint32_t r = 0; r < 4; ++r)
-                    g[k][r] = gg[r] * (cc * (kScaleP / (kScaleG * kScaleG))) + (cb * (kScaleP / kScaleG)) * g[k][r] +
-                              (diagonal && quad * 4u + r == l ? ca * kScaleP : 0.0f);
+                    g[k][r] = gg[r] * f.c + f.b * g[k][r] + (diagonal && quad * 4u + r == l ? f.a : 0.0f);
             }
         }
         __syncthreads();                                      // G has been read
@@ -764,7 +816,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_orthogonal_small(const SmallP
         __syncthreads();                                      // the transpose has been read
 #pragma unroll
         for (uint32_t k = 0; k < kSmallHeld; ++k) {
-            y[k] *= 1.0f / kScaleP;
+            y[k] *= f.y;
             if (jt[k] < L.nt) put_tile(Xt, pg, X, px, jt[k], it[k], y[k]);
         }
         __syncthreads();
@@ -902,16 +954,21 @@ int launch_type(const Orthogonalize& a) {
     s.mu = a.mu;
     s.eps = a.eps;
     s.nesterov = a.nesterov;
+    const Scales sc = scales_of(a.coeffs, a.steps);
     const SmallLayout small = small_layout(std::min(a.rows, a.cols), std::max(a.rows, a.cols));
     if (small.total) {
         SmallParams p{};
         p.s = s;
         p.L = small;
         p.steps = a.steps;
-        for (uint32_t i = 0; i < 3 * a.steps; ++i) p.coeffs[i] = a.coeffs[i];
+        for (uint32_t i = 0; i < a.steps; ++i) {
+            const double X = sc.X[i], G = sc.G[i], P = sc.P[i];
+            p.step[i] = {(float)(G / (X * X)), (float)(a.coeffs[3 * i] * P), (float)(a.coeffs[3 * i + 1] * (P / G)), (float)(a.coeffs[3 * i + 2] * (P / (G * G))),
+                         (float)(sc.X[i + 1] / (P * X))};
+        }
         p.o.M = (uint32_t)a.rows;
         p.o.N = (uint32_t)a.cols;
-        p.o.scale = a.alpha / (kScaleP * kScaleX);
+        p.o.scale = (float)(a.alpha / (sc.P[a.steps - 1] * sc.X[a.steps - 1]));
         p.o.out = a.out;
         p.o.z = a.z;
         p.o.w = a.w;
@@ -937,8 +994,8 @@ int launch_type(const Orthogonalize& a) {
     if (const int rc = launched(); rc != QESGD_OK) return rc;
 
     const auto at = [&](uint64_t offset) { return a.workspace + offset; };
-    // d = A B of symmetric matrices that commute, from scale sa sb to sd
-    const auto square = [&](uint64_t A, uint64_t B, uint64_t d, float scale) {
+    // d = A B of symmetric matrices that commute; scale: d's over A's and B's
+    const auto square = [&](uint64_t A, uint64_t B, uint64_t d, double scale) {
         OParams o{};
         o.a = at(A);
         o.b = at(B);
@@ -946,22 +1003,24 @@ int launch_type(const Orthogonalize& a) {
         o.M = o.N = (uint32_t)pl.m;
         o.pitch = o.d1_pitch = o.d2_pitch = (uint32_t)pl.G_pitch;
         o.d1 = o.d2 = at(d);
-        o.scale = scale;
+        o.scale = (float)scale;
         return o;
     };
     const auto poly = [&](uint32_t step, uint64_t d) {
-        const float ca = a.coeffs[3 * step], cb = a.coeffs[3 * step + 1], cc = a.coeffs[3 * step + 2];
-        OParams o = square(pl.G, pl.G, d, cc * (kScaleP / (kScaleG * kScaleG)));
-        o.ca = ca * kScaleP;
-        o.cb = cb * (kScaleP / kScaleG);
+        const double G = sc.G[step], P = sc.P[step];
+        OParams o = square(pl.G, pl.G, d, a.coeffs[3 * step + 2] * (P / (G * G)));
+        o.ca = (float)(a.coeffs[3 * step] * P);
+        o.cb = (float)(a.coeffs[3 * step + 1] * (P / G));
         return launch_product<kPoly, 0>(o, pl.square, a.n, a.stream);
     };
     uint32_t which = 0;                  // of the two transposes
     // An odd step stays alone, in the middle: five steps as 2 1 2 are as exact as one by one (matrices of noise and strong directions, 128 x
     // 1024: 1.5e-6 either way), as 2 2 1 half as exact.
-    const uint32_t alone = pl.pairs && (a.steps & 1u) ? 2u * ((a.steps / 2u + 1u) / 2u) : a.steps;
+    const bool pairs = pl.pairs && sc.pairs;
+    const uint32_t alone = pairs && (a.steps & 1u) ? 2u * ((a.steps / 2u + 1u) / 2u) : a.steps;
     for (uint32_t i = 0; i < a.steps;) {
-        OParams g = square(0, 0, pl.G, kScaleG / (kScaleX * kScaleX));
+        const double X = sc.X[i];
+        OParams g = square(0, 0, pl.G, sc.G[i] / (X * X));
         g.a = g.b = at(pl.X);
         g.a_bytes = g.b_bytes = pl.X_bytes;
         g.pitch = (uint32_t)pl.X_pitch;
@@ -976,16 +1035,19 @@ int launch_type(const Orthogonalize& a) {
         } else {
             rc = launch_product<kGram, 0>(g, pl.gram, a.n, a.stream);
         }
-        const bool pair = pl.pairs && i != alone && i + 1 < a.steps;
+        const bool pair = pairs && i != alone && i + 1 < a.steps;
         if (rc == QESGD_OK) rc = poly(i++, pl.P);
         uint64_t P = pl.P;
+        double scale_p = sc.P[i - 1];
         if (pair) {
             OParams o;
-            if (rc == QESGD_OK) rc = launch_product<kGram, 0>(o = square(pl.G, pl.P, pl.T, 1.0f / kScaleP), pl.square, a.n, a.stream);
-            if (rc == QESGD_OK) rc = launch_product<kGram, 0>(o = square(pl.T, pl.P, pl.G, 1.0f / kScaleP), pl.square, a.n, a.stream);
+            const double G = sc.G[i - 1], T = sc.T[i - 1], G2 = sc.G[i], P2 = sc.P[i], PP = sc.PP[i - 1];
+            if (rc == QESGD_OK) rc = launch_product<kGram, 0>(o = square(pl.G, pl.P, pl.T, T / (G * scale_p)), pl.square, a.n, a.stream);
+            if (rc == QESGD_OK) rc = launch_product<kGram, 0>(o = square(pl.T, pl.P, pl.G, G2 / (T * scale_p)), pl.square, a.n, a.stream);
             if (rc == QESGD_OK) rc = poly(i++, pl.P2);
-            if (rc == QESGD_OK) rc = launch_product<kGram, 0>(o = square(pl.P2, pl.P, pl.T, 1.0f / kScaleP), pl.square, a.n, a.stream);
+            if (rc == QESGD_OK) rc = launch_product<kGram, 0>(o = square(pl.P2, pl.P, pl.T, PP / (P2 * scale_p)), pl.square, a.n, a.stream);
             P = pl.T;
+            scale_p = PP;
         }
         if (rc != QESGD_OK) return rc;
         OParams x{};
@@ -1004,7 +1066,7 @@ int launch_type(const Orthogonalize& a) {
             x.d2 = at(pl.Xt[which]);
             x.d2_bytes = pl.Xt_bytes;
             x.d2_pitch = (uint32_t)pl.Xt_pitch;
-            x.scale = 1.0f / kScaleP;
+            x.scale = (float)(sc.X[i] / (scale_p * X));
             rc = launch_product<kApply, 0>(x, pl.apply, a.n, a.stream);
         } else {
             if (turned) {                // (P X)^T = Xt P, rows as the caller has them
@@ -1012,7 +1074,7 @@ int launch_type(const Orthogonalize& a) {
                 std::swap(x.a_bytes, x.b_bytes);
                 std::swap(x.M, x.N);
             }
-            x.scale = a.alpha / (kScaleP * kScaleX);
+            x.scale = (float)(a.alpha / (scale_p * X));
             x.out = a.out;
             x.z = a.z;
             x.w = a.w;
