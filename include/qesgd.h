@@ -297,7 +297,7 @@ int qesgd_mx4_product(const void* a_packed, const void* b_packed, uint64_t M, ui
  * then X = (a I + b G + c G^2) X with G = X X^T (X^T X on the longer side), (a, b, c) = coeffs[3*i .. 3*i+2] (host
  * memory, read during the call); out = X.  Singular values s become p_steps(.. p_1(s)), p(s) = a s + b s^3 + c s^5;
  * singular vectors stay.  Norms in fp64, products of fp32 accuracy (each operand as the sum of two fp16
- * numbers, sums in fp32).  The operands' range follows from the coefficients: every singular value of an iterate X up to 2^20 and of the
+ * numbers, sums in fp32): an entry is held to 2^-22 of itself down to 2^-28 of ||x||_F, and smaller ones to 2^-50 of ||x||_F.  The operands' range follows from the coefficients: every singular value of an iterate X up to 2^20 and of the
  * polynomials a I + b G + c G^2 up to 2^40 is right, whatever the shape; beyond that the result may be infinite or NaN.  A matrix of zeros gives zeros, one with a NaN or an infinity NaN everywhere.
  *   out  same type and shape as x, may be x itself.
  *   workspace  qesgd_orthogonalize_workspace_bytes(rows, cols, n), 256-byte aligned; may be NULL when that is 0 (matrices that fit

@@ -6,9 +6,12 @@
 //
 // Arithmetic.  The iteration has to hold fp32 accuracy: small singular values grow by up to a^steps (485 for the usual
 // coefficients), and rounding errors with them.  The card's fp32 matrix rate is a sixteenth of its fp16 rate, so every operand is
-// held as hi + lo, two fp16 numbers with 22 bits between them, scaled by a power of two into fp16's range, and a product is
-// hi hi + hi lo + lo hi with fp32 sums: three fp16 products, five times the fp32 rate, and as far from 64 bits as fp32 products are
-// (2e-6 .. 3e-6 either way).  One fp16 product alone would cost three digits.
+// held as hi + lo / 2048, two fp16 numbers with 22 bits between them, scaled by a power of two into fp16's range, and a product is
+// hi hi + (hi lo + lo hi) / 2048 with fp32 sums, one for either part: three fp16 products, five times the fp32 rate.  One fp16
+// product alone would cost three digits.  What a pair of fp16 numbers cannot do is fp32's range: a number has its 22 bits down to 2^-14
+// in scaled units, 2^-28 or 2^-29 of the largest there can be, below that a bit less for every halving, and nothing is left below 2^-36.
+// Without the 2048 that began at 2^-3: a matrix with one large number, row or column lost the others' digits, 1.5e-4 of them with a
+// ratio of 1e-6, and after ten steps, which make the small ones large, of the whole result (now 2e-6 and 1e-6, test_gpu_orthogonalize_scaled.py).
 //
 // Layout of an operand ("split"): rows along the contraction, padded with zeros to a multiple of 32; 32 numbers' hi (64 bytes),
 // then their lo, so a step of the pipeline is one 128-byte line of each row.  Products have both operands' rows along the
@@ -26,7 +29,8 @@
 namespace qesgd {
 namespace {
 
-constexpr double kMost = 1099511627776.0;        // 2^40: what G, P and a product of two P may reach
+constexpr double kMost = 1099511627776.0;        // 2^40: what G and P may reach
+constexpr double kMostPair = 256.0;              // and a product of two P, whose range is that of both
 constexpr float kFirstX = 32768.0f;              // scale of the first X, whose entries are at most 1
 
 // The power of two that takes numbers up to `bound` to at most 2^15, half of fp16's range: rounding may pass the bound.
@@ -41,13 +45,11 @@ inline double scale_for(double bound) {
 // the first kernel, whatever the matrix, and use fp16's range from its upper end.
 struct Scales {
     double X[QESGD_MAX_STEPS + 1], G[QESGD_MAX_STEPS + 1], P[QESGD_MAX_STEPS];
-    double T[QESGD_MAX_STEPS], PP[QESGD_MAX_STEPS];       // G P, and the product of this step's P and the next one's
-    bool pairs;                                           // no product of two P is beyond what is taken
+    double T[QESGD_MAX_STEPS], PP[QESGD_MAX_STEPS];       // G P, and the product of this step's P and the next one's: 0 beyond kMostPair
 };
 
 inline Scales scales_of(const float* coeffs, uint32_t steps) {
     Scales r{};
-    r.pairs = true;
     double S = 1.0, before = 0.0;
     for (uint32_t i = 0; i < steps; ++i) {
         const double a = coeffs[3 * i], b = coeffs[3 * i + 1], c = coeffs[3 * i + 2];
@@ -70,10 +72,7 @@ inline Scales scales_of(const float* coeffs, uint32_t steps) {
         r.G[i] = scale_for(S * S);
         r.T[i] = scale_for(S * next);
         r.P[i] = scale_for(most);
-        if (i > 0) {
-            r.PP[i - 1] = scale_for(before * most);
-            if (!(before * most <= kMost)) r.pairs = false;
-        }
+        if (i > 0 && before * most <= kMostPair) r.PP[i - 1] = scale_for(before * most);
         before = most;
         S = std::min(next, 1.0 / 1024.0 * kMost * kMost);              // beyond what is taken, and far from the end of 64 bits
     }
@@ -84,10 +83,11 @@ inline Scales scales_of(const float* coeffs, uint32_t steps) {
 
 inline uint64_t split_pitch(uint64_t k) { return round_up_to(k, 32) * 4; }
 
-// hi and lo of a scaled number.  What is below 2^-24 in scaled units is lost: 2^-36 of the largest entries.
+// hi and lo of a scaled number.  What hi leaves is at most 2^-11 of it, so lo stays in range.
+constexpr float kLo = 2048.0f;
 __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
     hi = (_Float16)v;
-    lo = (_Float16)(v - (float)hi);
+    lo = (_Float16)((v - (float)hi) * kLo);
 }
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 
@@ -312,7 +312,7 @@ __device__ __forceinline__ void finish(const OParams& p, const ACC& acc, uint32_
         const uint32_t r = 8u * (e >> 2) + (e & 3);
         if (row + r >= p.M) continue;
         const uint64_t o = base + (uint64_t)r * p.N;
-        const float v = acc[e] * p.scale;
+        const float v = acc[e];
         if (p.out) {
             if (DT == QESGD_F32) ((float*)p.out)[o] = v;
             else if (DT == QESGD_F16) ((_Float16*)p.out)[o] = (_Float16)v;
@@ -350,7 +350,7 @@ __device__ __forceinline__ void add_lower_terms(const OParams& p, float (&v)[16]
         if (r >= p.M) continue;
         const half4 hi = *(const half4*)(g + split_at(r)), lo = *(const half4*)(g + split_at(r) + 64);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * q + e] += p.cb * ((float)hi[e] + (float)lo[e]) + (r + e == c ? p.ca : 0.0f);
+        for (int e = 0; e < 4; ++e) v[4 * q + e] += p.cb * ((float)hi[e] + (float)lo[e] * (1.0f / kLo)) + (r + e == c ? p.ca : 0.0f);
     }
 }
 
@@ -414,7 +414,7 @@ struct SplitOps {
     TileLoader<S::BN, S::threads> lb;
     const unsigned char *a, *b;
     uint32_t at_a, at_b;                                       // parts 2 and 3 of the row are lo of parts 0 and 1
-    acc16 acc[S::FM][S::FN];
+    acc16 acc[S::FM][S::FN], low[S::FM][S::FN];                // of hi hi, and of hi lo + lo hi
 
     __device__ __forceinline__ void fetch(uint32_t step, unsigned char* to) {
         la.load(a + (uint64_t)step * kStepBytes, to, false);
@@ -441,20 +441,21 @@ struct SplitOps {
 #pragma unroll
         for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-            for (int j = 0; j < S::FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ah[i], f.bl[j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < S::FN; ++j) low[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.ah[i], f.bl[j], low[i][j], 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-            for (int j = 0; j < S::FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.al[i], f.bh[j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < S::FN; ++j) low[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.al[i], f.bh[j], low[i][j], 0, 0, 0);
     }
 };
 
-// 4096 x 25088: X X^T in three pieces 1083 us, P X 2201 us, both 1.15 PFLOP/s of fp16 products, what a large library product reaches (the card lowers its
-// clock); the last one, with z, u and zsum behind it, 2479 us; G G 250 us = 0.82, 528 tiles on 512 places.  512 x 4608, 2 of them: X X^T 13, G G 7.6, P X
-// 29, the last 41 us.  With 64 x 64 tiles a step of 16 KB takes 0.2 us, 34 bytes a clock and CU from L2 to LDS: 3 or 8 buffers, a second set of
-// waves that shares the steps, or sums of their own for the three products change nothing, so small matrices stay 4.8 us + 0.2 us a step.
+// 4096 x 25088: X X^T in four pieces 1215 us, 1.04 PFLOP/s of fp16 products, P X 2212 us, 1.14, what a large library product reaches (the card lowers its
+// clock); the last one, with z, u and zsum behind it, 2526 us; G G 275 us = 0.75, 528 tiles on 512 places.  512 x 4608, 2 of them: X X^T 13.4, G G 7.5, P X
+// 30, the last 41 us.  With 64 x 64 tiles a step, 16 KB from L2 to LDS and 32 KB from there to the registers, takes 0.2 us: 3 or 8 buffers, or a second set of
+// waves that shares the steps, change nothing, so small matrices stay 4.8 us + 0.2 us a step.
+// Two waves a SIMD: two workgroups of 128 x 128 share a CU, which takes at most 256 registers a lane.
 template <class S, int KIND, uint32_t DT>
-__global__ void __launch_bounds__(S::threads) k_orthogonal_product(const OParams p) {
+__global__ void __launch_bounds__(S::threads, 2) k_orthogonal_product(const OParams p) {
     static_assert(S::BM == S::BN, "symmetric products take square tiles");
     __shared__ __attribute__((aligned(1024))) unsigned char lds0[(S::BM + S::BN) * kStepBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char lds1[(S::BM + S::BN) * kStepBytes];
@@ -487,23 +488,13 @@ __global__ void __launch_bounds__(S::threads) k_orthogonal_product(const OParams
 #pragma unroll
     for (int i = 0; i < S::FM; ++i)
 #pragma unroll
-        for (int j = 0; j < S::FN; ++j) ops.acc[i][j] = acc16{};
+        for (int j = 0; j < S::FN; ++j) ops.acc[i][j] = ops.low[i][j] = acc16{};
     if constexpr (S::BUFFERS == 2) {
         unsigned char* const buffers[2] = {lds0, lds1};
         run_steps(ops, steps, buffers);
     } else {
         unsigned char* const buffers[4] = {lds0, lds1, lds2, lds3};
         run_steps(ops, steps, buffers);
-    }
-    auto& acc = ops.acc;
-
-    if (KIND == kFinal) {
-#pragma unroll
-        for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-            for (int j = 0; j < S::FN; ++j)
-                finish<DT, 16>(p, acc[i][j], z, m0 + (wm * S::FM + i) * 32u + 4u * h, n0 + (wn * S::FN + j) * 32u + (lane & 31u));
-        return;
     }
 #pragma unroll
     for (int i = 0; i < S::FM; ++i)
@@ -512,7 +503,11 @@ __global__ void __launch_bounds__(S::threads) k_orthogonal_product(const OParams
             const uint32_t row = m0 + (wm * S::FM + i) * 32u, col = n0 + (wn * S::FN + j) * 32u;
             float v[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e] * p.scale;
+            for (int e = 0; e < 16; ++e) v[e] = __builtin_fmaf(ops.low[i][j][e], 1.0f / kLo, ops.acc[i][j][e]) * p.scale;
+            if (KIND == kFinal) {
+                finish<DT, 16>(p, v, z, row + 4u * h, col + (lane & 31u));
+                continue;
+            }
             if (KIND == kPartial) {
                 store_partial(p, v, z * p.splits + split_k, row, col, lane);
                 continue;
@@ -641,15 +636,16 @@ __device__ __forceinline__ half8 read8(const unsigned char* p) { return *(const 
 
 // acc += A B^T over `groups` groups from g on, `by` apart; A and B: the tiles' first rows.  A lane's operand is one chunk of its row.
 __device__ __forceinline__ acc4 small_product(const unsigned char* A, uint32_t a, const unsigned char* B, uint32_t b, uint32_t g, uint32_t groups, uint32_t by) {
-    acc4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    acc4 acc = {0.0f, 0.0f, 0.0f, 0.0f}, low = acc;
     const unsigned char *ah = A + a, *al = A + (a ^ 64u), *bh = B + b, *bl = B + (b ^ 64u);
     for (; g < groups; g += by) {
         const half8 vah = read8(ah + g * 128u), vbh = read8(bh + g * 128u), vbl = read8(bl + g * 128u), val = read8(al + g * 128u);
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, vbl, acc, 0, 0, 0);       // here it costs next to nothing
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vah, vbl, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, vbh, acc, 0, 0, 0);
         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vah, vbh, acc, 0, 0, 0);
+        low = __builtin_amdgcn_mfma_f32_16x16x32_f16(vah, vbl, low, 0, 0, 0);
+        low = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, vbh, low, 0, 0, 0);
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(low[r], 1.0f / kLo, acc[r]);
     return acc;
 }
 // Tile (tr, tc): a lane holds column lane & 15 and rows 4 (lane / 16) .. + 3.  Its transpose goes to by_col, and with by_row itself there.
@@ -823,35 +819,31 @@ __global__ void __launch_bounds__(kSmallThreads) k_orthogonal_small(const SmallP
     }
 #pragma unroll
     for (uint32_t k = 0; k < kSmallHeld; ++k)
-        if (jt[k] < L.nt) finish<DT, 4>(p.o, y[k], z, (turned ? jt[k] : it[k]) * 16u + quad * 4u, (turned ? it[k] : jt[k]) * 16u + l);
+        if (jt[k] < L.nt) finish<DT, 4>(p.o, y[k] * p.o.scale, z, (turned ? jt[k] : it[k]) * 16u + quad * 4u, (turned ? it[k] : jt[k]) * 16u + l);
 }
 
 // Which tiles, and how many pieces of the contraction, from how long the workgroups take on 256 CUs.  Unit: a step of 512 workgroups
 // with 128 x 128 tiles, two a CU, 1.1 us of a full chip, and 3 us for a launch.  A last round of up to 256 has a CU each and takes 0.70 of that.  64 x 64: 0.38 (a
-// quarter of the work; each step reads twice as much for it).  256 x 256, one a CU: 1.78 a round (twice the work of a CU's two
-// 128s, 0.89 of the time).  P X with 64 x 64: 0.12 for a last round of up to 256, because its stores and outputs run under other
-// workgroups' products.  Over 19 shapes and three tiles each, one step's products are 0.3% slower (P X, X X^T and G G) than with the best tile
-// of each; with 0.27 for P X too, 2.6%.  Measured on 20 shapes from 128 x 128 to 4096 x 25088, one product changed at a time, five steps, us:
-//   P X       512 x 4608, 2 of them 64: 349, 128: 360;  2048 x 2048 824 / 785;  1024 x 8192 699 / 640, 256: 725;  3000 x 3000 2398 / 2358 /
-//             2455;  2048 x 8192 2403 / 2153 / 2094;  4096 x 25088 28.2 / 24.3 / 24.7 ms
-//   G G       1024 x 1024, 12 of them 64: 1201, 128: 1143, 256: 1332;  4096 x 4096 5750 / 5306 / 5457
-//   X X^T     512 x 4096 64 in 1: 259, in 6: 191, 128 in 6: 233;  1024 x 8192 699 / 653 / 641;  4096 x 25088 64 in 3: 27.6, 128 in 3: 22.9, 256 in
-//             1: 24.7, in 3: 22.5 ms
+// quarter of the work; each step reads twice as much for it).  P X with 64 x 64: 0.12 for a last round of up to 256, because its stores and outputs
+// run under other workgroups' products.  Larger tiles have no registers for two sums of each number: 256 x 256 with one sum took 13.4 ms where these take
+// 14.1 at 4096 x 25088 and 1572 / 1607 us at 2048 x 8192, 256 x 128 tiles 14.2.  Five steps, us, by this rule / with 64 x 64 alone / with 128 x 128 alone:
+//   512 x 4608, 2 of them 267 / 267 / 426;  1024 x 8192 488 / 523 / 681;  2048 x 2048 812 / 840 / 826;  2048 x 8192 1607 / 1909 / 1626;  3000 x
+//   3000 2228 / 2445 / 2230;  1024 x 1024, 12 of them 1094 / 1254 / 1094;  4096 x 6000 5944 / 7852 / 5947;  4096 x 25088 14106 / 19925 / 14108
 struct Cut {
     uint32_t edge, pieces;
     double us;                           // by this reckoning
 };
 
 double cut_cost(uint64_t groups, uint32_t edge, bool upper) {
-    const uint64_t slots = edge == 256 ? 256 : 512, left = groups % slots;
-    const double full = edge == 256 ? 1.78 : edge == 128 ? 1.0 : 0.38, half = edge == 128 ? 0.70 : upper ? 0.27 : 0.12;
-    return (double)(groups / slots) * full + (left == 0 ? 0.0 : edge != 256 && left <= 256 ? half : full);
+    const uint64_t slots = 512, left = groups % slots;
+    const double full = edge == 128 ? 1.0 : 0.38, half = edge == 128 ? 0.70 : upper ? 0.27 : 0.12;
+    return (double)(groups / slots) * full + (left == 0 ? 0.0 : left <= 256 ? half : full);
 }
 
 // M x N (upper = M x M, the upper half) over `steps` steps, `count` of them; more than one piece only for upper.
 Cut choose_cut(uint64_t M, uint64_t N, uint64_t steps, uint64_t count, bool upper, uint32_t most_pieces) {
     Cut best{64, 1, 1e300};
-    for (uint32_t edge : {64u, 128u, 256u}) {
+    for (uint32_t edge : {64u, 128u}) {
         const uint64_t tm = (M + edge - 1) / edge, tn = (N + edge - 1) / edge, tiles = (upper ? tm * (tm + 1) / 2 : tm * tn) * count;
         for (uint32_t pieces = 1; pieces <= most_pieces && pieces * 4ull <= steps + 3ull; ++pieces) {
             // a piece has at least four steps; the sums of the pieces cost a launch, and are written and read at about 4 TB/s
@@ -928,7 +920,6 @@ int launch_product_as(OParams& p, uint32_t count, hipStream_t stream) {
     return launched();
 }
 
-typedef TileShape<2, 4, 4, 2, 2> Tile256;
 typedef TileShape<2, 2, 2, 2, 2> Tile128;
 typedef TileShape<2, 2, 1, 1, 4> Tile64;
 
@@ -937,7 +928,6 @@ int launch_product(OParams& p, const Cut& cut, uint32_t count, hipStream_t strea
     p.steps = p.pitch / kStepBytes;
     p.splits = cut.pieces;
     switch (cut.edge) {
-        case 256: return launch_product_as<Tile256, KIND, DT>(p, count, stream);
         case 128: return launch_product_as<Tile128, KIND, DT>(p, count, stream);
         default: return launch_product_as<Tile64, KIND, DT>(p, count, stream);
     }
@@ -1016,8 +1006,7 @@ int launch_type(const Orthogonalize& a) {
     uint32_t which = 0;                  // of the two transposes
     // An odd step stays alone, in the middle: five steps as 2 1 2 are as exact as one by one (matrices of noise and strong directions, 128 x
     // 1024: 1.5e-6 either way), as 2 2 1 half as exact.
-    const bool pairs = pl.pairs && sc.pairs;
-    const uint32_t alone = pairs && (a.steps & 1u) ? 2u * ((a.steps / 2u + 1u) / 2u) : a.steps;
+    const uint32_t alone = pl.pairs && (a.steps & 1u) ? 2u * ((a.steps / 2u + 1u) / 2u) : a.steps;
     for (uint32_t i = 0; i < a.steps;) {
         const double X = sc.X[i];
         OParams g = square(0, 0, pl.G, sc.G[i] / (X * X));
@@ -1035,7 +1024,7 @@ int launch_type(const Orthogonalize& a) {
         } else {
             rc = launch_product<kGram, 0>(g, pl.gram, a.n, a.stream);
         }
-        const bool pair = pairs && i != alone && i + 1 < a.steps;
+        const bool pair = pl.pairs && i != alone && i + 1 < a.steps && sc.PP[i] > 0.0;
         if (rc == QESGD_OK) rc = poly(i++, pl.P);
         uint64_t P = pl.P;
         double scale_p = sc.P[i - 1];

@@ -20,6 +20,7 @@ COEFFS = {
     "growing iterates with all terms": ((30.0, -20.0, 4.0), (3.0, 0.01, 1e-6), (2.0, -1e-4, 1e-9)),
     "large polynomials of small iterates": ((1e-4, 0.0, 0.0), (1e5, -3e12, 2e20), (1.5, -0.5, 0.0)),
     "shrinking iterates": ((1e-3, 0.0, 0.0),) * 4,
+    "only the last term": ((0.0, 0.0, 1e3), (1.5, -0.5, 0.0)),
     "zero": ((0.0, 0.0, 0.0),) * 2,
 }
 
