@@ -39,12 +39,12 @@ struct TileShape {
 
 // 16 (4) bytes a lane from base + offset to LDS, the wave's lanes one behind the other from `to` on.  In assembly, because the
 // compiler, which does not know which buffer a load goes to, waits for all loads before it reads any buffer once there are more than two.  The
-// waiting is wait_and_meet's; no register is written.  M0, which nothing else here uses, needs one wait state before the load takes it.
+// waiting is wait_and_meet's; no register is written but M0, which needs one wait state before the load takes it.
 __device__ __forceinline__ void load_to_lds_16(const unsigned char* base, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "m0", "memory");
 }
 __device__ __forceinline__ void load_to_lds_4(const unsigned char* base, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(to), "v"(offset), "s"(base) : "m0", "memory");
 }
 // Number of an LDS byte, as M0 takes it.
 __device__ __forceinline__ uint32_t lds_number(const unsigned char* p) {
