@@ -258,20 +258,23 @@ def qesgd_epoch_commit(w_inout, zsum_inout, rounds, d, stream=None):
 # ---- matrix parameters ------------------------------------------------------
 #
 # The kernels run on the current device and take addresses: a tensor of the host or of another device is refused here, and so are
-# types that the call does not say, and views with gaps or another order where the call has no stride for them.  Small calls cost the host about 5 us, most of it in the launch, so the checks stand in line and
-# numbers (plain ints) go to ctypes as they are: with a loop over the tensors and int() around each number a call took 0.9 us more.
+# types that the call does not say (packed matrices are uint8), tensors that hold less than the call reads or writes, and views whose
+# strides are not the call's: gaps, another order, a broadcast.  Small calls cost the host about 5 us, most of it in the launch, so the
+# checks (0.5 us) stand in line and numbers (plain ints) go to ctypes as they are: with a loop over the tensors and int() around each number a
+# call took 0.9 us more.
 
-def _here(stream):
-    """The current device and the handle of the stream."""
-    if torch.cuda.is_initialized():
-        device = torch._C._cuda_getDevice()
-        if stream is None:
-            return device, torch._C._cuda_getCurrentRawStream(device)
-    elif stream is None:
-        stream = torch.cuda.current_stream()
-        device = torch.cuda.current_device()
-    else:
-        device = None
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_U8 = torch.uint8
+
+
+def _here(where: str, stream, t):
+    """The current device, which t has to be on, and the handle of the stream."""
+    device = t.get_device()
+    if device < 0 or device != _current_device():
+        _elsewhere(where, t)
+    if stream is None:
+        return device, _current_stream(device)
     return device, stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -286,8 +289,38 @@ def _dtype(t: torch.Tensor, where: str) -> int:
     return code
 
 
-def _f32(where: str, device, *tensors):
-    """Addresses of contiguous fp32 tensors, each of which may be None."""
+def _view(where: str, t, *dims):
+    """For a tensor that is not contiguous, or too short if it were: refuses it unless its own last dimensions are those of the call,
+    (count, stride) from the outermost one on."""
+    if t.is_contiguous():
+        raise ValueError(f"{where}: a tensor of {t.numel()} elements, the call takes {1 + sum((n - 1) * step for n, step in dims if n > 1)}")
+    own = list(zip(t.shape, t.stride()))
+    for n, step in reversed(dims):
+        size, stride = own.pop() if own else (1, step)
+        if size < n or (n > 1 and stride != step):
+            raise QesgdError(ERR_STRIDE, where)
+
+
+@lru_cache(maxsize=256)
+def _mx4_bytes(rows, cols):
+    """Bytes of a packed matrix up to its last scale."""
+    wide = (cols + 127) // 128 * 128
+    return (rows * wide // 2 + 255) // 256 * 256 + rows * wide // 32
+
+
+def _packed(where: str, device, t, rows, cols, K=1, stride=0):
+    """Address of K packed matrices."""
+    if t.get_device() != device:
+        _elsewhere(where, t)
+    if t.dtype is not _U8:
+        raise QesgdError(ERR_DTYPE, where)
+    if not t.is_contiguous() or t.numel() < (_mx4_bytes(rows, cols) if K == 1 else (K - 1) * stride + _mx4_bytes(rows, cols)):
+        _view(where, t, (K, stride), (_mx4_bytes(rows, cols), 1))
+    return t.data_ptr()
+
+
+def _f32(where: str, device, count, *tensors):
+    """Addresses of contiguous fp32 tensors of at least `count` elements, each of which may be None."""
     out = []
     for t in tensors:
         if t is None:
@@ -299,6 +332,8 @@ def _f32(where: str, device, *tensors):
             raise QesgdError(ERR_DTYPE, where)
         if not t.is_contiguous():
             raise QesgdError(ERR_STRIDE, where)
+        if t.numel() < count:
+            _view(where, t, (count, 1))
         out.append(t.data_ptr())
     return out
 
@@ -308,6 +343,8 @@ def _ws(where: str, device, workspace):
         return None, 0
     if workspace.get_device() != device:
         _elsewhere(where, workspace)
+    if not workspace.is_contiguous():
+        raise QesgdError(ERR_STRIDE, where)
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
@@ -319,23 +356,28 @@ def qesgd_mx4_layout_query(rows: int, cols: int) -> Mx4Layout:
 
 def qesgd_mx4_quantize_pack(x, ld, x_stride, rows, cols, K, mode, seed, rnd, packed, packed_stride, packed_t=None,
                             packed_t_stride=0, worker=0, stream=None):
-    dtype = _dtype(x, "qesgd_mx4_quantize_pack")
-    device, stream = _here(stream)
-    if x.get_device() != device or (packed is not None and packed.get_device() != device) or \
-            (packed_t is not None and packed_t.get_device() != device):
-        _elsewhere("qesgd_mx4_quantize_pack", x, packed, packed_t)
-    _check(lib().qesgd_mx4_quantize_pack(x.data_ptr(), dtype, ld, x_stride, rows, cols, K, mode, seed, rnd, worker, _ptr(packed),
-                                         packed_stride, _ptr(packed_t), packed_t_stride, stream), "qesgd_mx4_quantize_pack")
+    where = "qesgd_mx4_quantize_pack"
+    dtype = _dtype(x, where)
+    device, stream = _here(where, stream, x)
+    if not x.is_contiguous() or x.numel() < (K - 1) * x_stride + (rows - 1) * ld + cols:
+        _view(where, x, (K, x_stride), (rows, ld), (cols, 1))
+    p = None if packed is None else _packed(where, device, packed, rows, cols, K, packed_stride)
+    pt = None if packed_t is None else _packed(where, device, packed_t, cols, rows, K, packed_t_stride)
+    rc = (_lib or lib()).qesgd_mx4_quantize_pack(x.data_ptr(), dtype, ld, x_stride, rows, cols, K, mode, seed, rnd, worker, p,
+                                                 packed_stride, pt, packed_t_stride, stream)
+    if rc:
+        raise QesgdError(rc, where)
 
 
 def qesgd_mx4_unpack_aggregate_update(packed_slab, packed_stride, K, rows, cols, w_snap, zbar_out, u_out, zsum_inout,
                                       stream=None):
-    device, stream = _here(stream)
-    if packed_slab.get_device() != device:
-        _elsewhere("qesgd_mx4_unpack_aggregate_update", packed_slab)
-    _check(lib().qesgd_mx4_unpack_aggregate_update(packed_slab.data_ptr(), packed_stride, K, rows, cols,
-                                                   *_f32("qesgd_mx4_unpack_aggregate_update", device, w_snap, zbar_out, u_out,
-                                                         zsum_inout), stream), "qesgd_mx4_unpack_aggregate_update")
+    where = "qesgd_mx4_unpack_aggregate_update"
+    device, stream = _here(where, stream, packed_slab)
+    slab = _packed(where, device, packed_slab, rows, cols, K, packed_stride)
+    rc = (_lib or lib()).qesgd_mx4_unpack_aggregate_update(slab, packed_stride, K, rows, cols, *_f32(where, device, rows * cols, w_snap,
+                                                                                                    zbar_out, u_out, zsum_inout), stream)
+    if rc:
+        raise QesgdError(rc, where)
 
 
 def qesgd_mx4_product_workspace_bytes(M: int, N: int, K: int) -> int:
@@ -343,13 +385,16 @@ def qesgd_mx4_product_workspace_bytes(M: int, N: int, K: int) -> int:
 
 
 def qesgd_mx4_product(a_packed, b_packed, M, N, K, c, ldc, workspace=None, stream=None):
-    dtype = _dtype(c, "qesgd_mx4_product")
-    device, stream = _here(stream)
-    if a_packed.get_device() != device or b_packed.get_device() != device or c.get_device() != device:
-        _elsewhere("qesgd_mx4_product", a_packed, b_packed, c)
-    ws, ws_bytes = _ws("qesgd_mx4_product", device, workspace)
-    _check(lib().qesgd_mx4_product(a_packed.data_ptr(), b_packed.data_ptr(), M, N, K, c.data_ptr(), dtype, ldc, ws, ws_bytes, stream),
-           "qesgd_mx4_product")
+    where = "qesgd_mx4_product"
+    dtype = _dtype(c, where)
+    device, stream = _here(where, stream, c)
+    if not c.is_contiguous() or c.numel() < (M - 1) * ldc + N:
+        _view(where, c, (M, ldc), (N, 1))
+    ws, ws_bytes = (None, 0) if workspace is None else _ws(where, device, workspace)
+    rc = (_lib or lib()).qesgd_mx4_product(_packed(where, device, a_packed, M, K), _packed(where, device, b_packed, N, K), M, N, K, c.data_ptr(),
+                                           dtype, ldc, ws, ws_bytes, stream)
+    if rc:
+        raise QesgdError(rc, where)
 
 
 @lru_cache(maxsize=64)
@@ -369,29 +414,34 @@ def qesgd_orthogonalize_workspace_bytes(rows: int, cols: int, n: int) -> int:
 
 
 def qesgd_orthogonalize(x, rows, cols, n, coeffs, eps, out, workspace, stream=None):
+    where = "qesgd_orthogonalize"
     if out.dtype != x.dtype:
-        raise QesgdError(ERR_DTYPE, "qesgd_orthogonalize")
-    dtype, steps = _dtype(x, "qesgd_orthogonalize"), _coeffs(coeffs)
-    device, stream = _here(stream)
-    if x.get_device() != device or out.get_device() != device:
-        _elsewhere("qesgd_orthogonalize", x, out)
-    if not (x.is_contiguous() and out.is_contiguous()):
-        raise QesgdError(ERR_STRIDE, "qesgd_orthogonalize")
-    ws, ws_bytes = _ws("qesgd_orthogonalize", device, workspace)
+        raise QesgdError(ERR_DTYPE, where)
+    dtype, steps = _dtype(x, where), _coeffs(coeffs)
+    device, stream = _here(where, stream, x)
+    if out.get_device() != device:
+        _elsewhere(where, x, out)
+    for t in (x, out):
+        if not t.is_contiguous():
+            raise QesgdError(ERR_STRIDE, where)
+        if t.numel() < n * rows * cols:
+            _view(where, t, (n * rows * cols, 1))
+    ws, ws_bytes = _ws(where, device, workspace)
     _check(lib().qesgd_orthogonalize(x.data_ptr(), dtype, rows, cols, n, steps, len(coeffs), float(eps), out.data_ptr(), ws, ws_bytes,
-                                     stream), "qesgd_orthogonalize")
+                                     stream), where)
 
 
 def qesgd_orthogonal_update(g, rows, cols, n, momentum_inout, mu, nesterov, coeffs, eps, alpha, step_out, z_inout, w_snap,
                             u_out, zsum_inout, workspace, stream=None):
+    where = "qesgd_orthogonal_update"
     if g.dtype != torch.float32:
-        raise QesgdError(ERR_DTYPE, "qesgd_orthogonal_update")
+        raise QesgdError(ERR_DTYPE, where)
     steps = _coeffs(coeffs)
-    device, stream = _here(stream)
-    g, m, step, z, w, u, zsum = _f32("qesgd_orthogonal_update", device, g, momentum_inout, step_out, z_inout, w_snap, u_out, zsum_inout)
-    ws, ws_bytes = _ws("qesgd_orthogonal_update", device, workspace)
+    device, stream = _here(where, stream, g)
+    g, m, step, z, w, u, zsum = _f32(where, device, n * rows * cols, g, momentum_inout, step_out, z_inout, w_snap, u_out, zsum_inout)
+    ws, ws_bytes = _ws(where, device, workspace)
     _check(lib().qesgd_orthogonal_update(g, rows, cols, n, m, float(mu), 1 if nesterov else 0, steps, len(coeffs), float(eps),
-                                         float(alpha), step, z, w, u, zsum, ws, ws_bytes, stream), "qesgd_orthogonal_update")
+                                         float(alpha), step, z, w, u, zsum, ws, ws_bytes, stream), where)
 
 
 def qesgd_abi_version() -> int:
