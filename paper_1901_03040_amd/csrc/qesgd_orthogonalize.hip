@@ -854,7 +854,8 @@ Cut choose_cut(uint64_t M, uint64_t N, uint64_t steps, uint64_t count, bool uppe
     for (uint32_t edge : {64u, 128u}) {
         const uint64_t tm = (M + edge - 1) / edge, tn = (N + edge - 1) / edge, tiles = (upper ? tm * (tm + 1) / 2 : tm * tn) * count;
         for (uint32_t pieces = 1; pieces <= most_pieces && pieces * 4ull <= steps + 3ull; ++pieces) {
-            // a piece has at least four steps; the sums of the pieces cost a launch, and are written and read at about 4 TB/s
+            // A piece has about four steps or more: ceil(steps / 4) pieces at most, the shortest of which has three (two, of five steps
+            // in two pieces); the pipeline takes any number.  The sums of the pieces cost a launch, and are written and read at about 4 TB/s.
             const double sums = pieces == 1 ? 0.0 : 3.0 + (double)pieces * (double)count * (double)(M * M) * 2e-6;
             const double cost = 3.0 + cut_cost(tiles * pieces, edge, upper) * (double)((steps + pieces - 1) / pieces) * 1.1 + sums;
             if (cost < best.us) best = Cut{edge, pieces, cost};

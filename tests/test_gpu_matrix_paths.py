@@ -122,3 +122,16 @@ def test_zeros_give_zeros_and_nan_stays_in_its_matrix(B, rows, cols, dtype):  # 
         clean = torch.empty_like(out)
         B.qesgd_orthogonalize(again.cuda(), rows, cols, 3, R.USUAL, eps, clean, ws_for(B, rows, cols, 3))
         assert torch.equal(clean[2], out[2]) and torch.equal(clean[0], out[0])
+
+
+@pytest.mark.parametrize("n,rows,cols", [(1, 33, 480), (4, 40, 450), (1, 90, 417), (2, 300, 290), (1, 257, 161)])
+def test_short_pieces_and_contractions(B, n, rows, cols):  # noqa: F811
+    """X X^T over 15, 14, 10 and 6 steps of 32, in pieces of three where it is cut up, and products of m x m matrices over 2 to 10."""
+    assert ws_for(B, rows, cols, n) is not None
+    x = matrices(n, rows, cols, "decay", rows)
+    out = torch.full((n, rows, cols), 9.0, device="cuda")
+    B.qesgd_orthogonalize(x.cuda(), rows, cols, n, R.USUAL, EPS, out, ws_for(B, rows, cols, n))
+    for i in range(n):
+        x64 = x[i].double().numpy()
+        want = R.newton_schulz(x64)
+        assert np.linalg.norm(out[i].double().cpu().numpy() - want) <= allowed(x64, want, R.USUAL, 2.0 ** -24), i
