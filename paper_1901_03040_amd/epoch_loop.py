@@ -113,6 +113,7 @@ class QesgdMatrixLoop:
         self.u = self.w.clone()
         self.round_id = 0
         self.steps_in_epoch = 0
+        self.sent = 0                                           # how often the workers have got parameters
         # the parameters as the workers hold them: blocks along the inputs for the forward pass, along the outputs for the gradient
         self.packed_u = B.alloc_mx4(B.qesgd_mx4_layout_query(self.out, self.inn), device=self.dev)
         self.packed_ut = B.alloc_mx4(B.qesgd_mx4_layout_query(self.inn, self.out), device=self.dev)
@@ -130,6 +131,7 @@ class QesgdMatrixLoop:
 
     def _send(self):
         self._quantize(self.u, B.MX4_NEAREST, self.packed_u, self.packed_ut)
+        self.sent += 1
 
     def _quantize(self, x, mode, packed, packed_t, worker=0):
         B.qesgd_mx4_quantize_pack(x, x.stride(0), 0, x.shape[0], x.shape[1], 1, mode, self.seed, self.round_id, packed, 0,
@@ -149,17 +151,19 @@ class QesgdMatrixLoop:
         return c
 
     def forward(self, x: torch.Tensor):
-        """A worker's layer: y = Q(x) Q(u)^T for x [tokens, in].  Returns y in x's type and what backward needs."""
+        """A worker's layer: y = Q(x) Q(u)^T for x [tokens, in].  Returns y in x's type and what backward needs, which holds until the
+        server sends new parameters."""
         assert x.dim() == 2 and x.shape[1] == self.inn
         px, pxt = self._pack(x, B.MX4_NEAREST)
-        return self._product(px, self.packed_u, x.shape[0], self.out, self.inn, x.dtype), (pxt, x.shape[0])
+        return self._product(px, self.packed_u, x.shape[0], self.out, self.inn, x.dtype), (pxt, x.shape[0], self.sent)
 
     def backward(self, dy: torch.Tensor, saved, worker: int = 0):
         """Gradients with respect to x (dy's type) and to the parameters (fp32): dy [tokens, out] is rounded without bias.  Each of a
         round's calls takes a worker number of its own, so that their roundings do not depend on one another, nor on those of
         the gradients (numbers 0 .. K - 1 of the quantiser; these follow)."""
-        pxt, tokens = saved
+        pxt, tokens, sent = saved
         assert dy.shape == (tokens, self.out)
+        assert sent == self.sent, "the parameters of this forward pass are gone: the server has sent others since"
         pdy, pdyt = self._pack(dy, B.MX4_STOCHASTIC, self.K + worker)
         dx = self._product(pdy, self.packed_ut, tokens, self.inn, self.out, dy.dtype)
         return dx, self._product(pdyt, pxt, self.out, self.inn, tokens, torch.float32)
