@@ -137,11 +137,12 @@ class QesgdMatrixLoop:
         B.qesgd_mx4_quantize_pack(x, x.stride(0), 0, x.shape[0], x.shape[1], 1, mode, self.seed, self.round_id, packed, 0,
                                   packed_t=packed_t, worker=worker)
 
-    def _pack(self, x, mode, worker=0):
-        """Both forms of an operand [rows, cols]."""
+    def _pack(self, x, mode, worker=0, columns=True):
+        """Both forms of an operand [rows, cols], or that along its rows alone."""
         r, c = x.shape
         x = x if x.stride(1) == 1 and x.stride(0) >= c else x.contiguous()
-        forms = (B.alloc_mx4(B.qesgd_mx4_layout_query(r, c), device=self.dev), B.alloc_mx4(B.qesgd_mx4_layout_query(c, r), device=self.dev))
+        forms = (B.alloc_mx4(B.qesgd_mx4_layout_query(r, c), device=self.dev),
+                 B.alloc_mx4(B.qesgd_mx4_layout_query(c, r), device=self.dev) if columns else None)
         self._quantize(x, mode, *forms, worker)
         return forms
 
@@ -150,12 +151,14 @@ class QesgdMatrixLoop:
         B.qesgd_mx4_product(a, b, M, N, K, c, N, workspace=B.alloc_workspace(B.qesgd_mx4_product_workspace_bytes(M, N, K), self.dev))
         return c
 
-    def forward(self, x: torch.Tensor):
+    def forward(self, x: torch.Tensor, gradients: bool = True):
         """A worker's layer: y = Q(x) Q(u)^T for x [tokens, in].  Returns y in x's type and what backward needs, which holds until the
-        server sends new parameters."""
+        server sends new parameters.  gradients: False where no backward pass follows; x is then packed along its rows alone (the form
+        along the columns is for dw, and for a token or two it is the larger part of the work: 128 rows of padding for each)."""
         assert x.dim() == 2 and x.shape[1] == self.inn
-        px, pxt = self._pack(x, B.MX4_NEAREST)
-        return self._product(px, self.packed_u, x.shape[0], self.out, self.inn, x.dtype), (pxt, x.shape[0], self.sent)
+        px, pxt = self._pack(x, B.MX4_NEAREST, columns=gradients)
+        y = self._product(px, self.packed_u, x.shape[0], self.out, self.inn, x.dtype)
+        return y, (pxt, x.shape[0], self.sent) if gradients else None
 
     def backward(self, dy: torch.Tensor, saved, worker: int = 0):
         """Gradients with respect to x (dy's type) and to the parameters (fp32): dy [tokens, out] is rounded without bias.  Each of a

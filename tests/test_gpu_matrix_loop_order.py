@@ -29,3 +29,16 @@ def test_backward_belongs_to_the_parameters_of_its_forward(loop_class):
     loop.begin_epoch()
     with pytest.raises(AssertionError, match="parameters"):
         loop.backward(dy, saved)
+
+
+@pytest.mark.parametrize("tokens,dtype", [(1, torch.bfloat16), (1, torch.float32), (17, torch.float16), (130, torch.bfloat16)])
+def test_a_forward_pass_alone(loop_class, tokens, dtype):
+    """Without gradients the same y, bit for bit, and nothing to go back with."""
+    g = torch.Generator().manual_seed(tokens)
+    loop = loop_class(torch.randn(200, 384, generator=g).cuda(), 1, 5)
+    x = torch.randn(tokens, 384, generator=g).to(dtype).cuda()
+    y, saved = loop.forward(x, gradients=False)
+    assert saved is None and y.dtype == dtype
+    assert torch.equal(y, loop.forward(x)[0])
+    with pytest.raises(TypeError):
+        loop.backward(torch.zeros_like(y), saved)
