@@ -40,12 +40,16 @@ struct TileShape {
 // 16 (4) bytes a lane from base + offset to LDS, the wave's lanes one behind the other from `to` on.  In assembly, because the
 // compiler, which does not know which buffer a load goes to, waits for all loads before it reads any buffer once there are more than two.  The
 // waiting is wait_and_meet's; no register is written but M0, which needs one wait state before the load takes it.
+// The compiler warns that M0 is a register it gives no value to keep; it is named all the same, for the instructions before which the compiler sets M0 itself.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds_16(const unsigned char* base, uint32_t offset, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "m0", "memory");
 }
 __device__ __forceinline__ void load_to_lds_4(const unsigned char* base, uint32_t offset, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(to), "v"(offset), "s"(base) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 // Number of an LDS byte, as M0 takes it.
 __device__ __forceinline__ uint32_t lds_number(const unsigned char* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)p;
