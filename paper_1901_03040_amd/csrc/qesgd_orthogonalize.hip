@@ -572,11 +572,12 @@ __global__ void __launch_bounds__(256) k_orthogonal_gram_sum(const OParams p) {
 // A whole matrix in one workgroup: X, its transpose and one m x m matrix (G, then P in its place) stay in LDS as split rows for all
 // steps, so a call is one launch and reads and writes its operands once.  Which shapes fit: small_layout().
 //
-// What bounds it is its chain of short phases, a barrier apart, so the work is cut into 16 x 16 tiles, whose matrix instruction takes
+// What bounds it is its chain of short phases, five barriers a step (six where the contraction is in pieces), so the work is cut into 16 x 16 tiles, whose matrix instruction takes
 // a whole group of 32 numbers at once, and dealt to 16 waves.  A step: the tiles of G's upper half, where they are few the contraction
 // in pieces to several waves whose sums one wave adds in order; P = a I + b G + c G G by the same waves; P X tile by tile, held in
 // registers until every wave has read X.  Rows are groups of 128 bytes, chunks placed as in the pipeline.  64 x 64, 16 of them: 72 us as
-// the launches of the general path, 31 us with 32 x 32 tiles on 8 waves, 23 us so.
+// the launches of the general path, 31 us with 32 x 32 tiles on 8 waves, 23 us so: 7 us and 2.9 us a step, whether 16 matrices or one.  Vector
+// instructions take 57% of a SIMD's cycles, LDS 35% of a CU's (two fifths of that bank conflicts), the matrix units 8%.
 constexpr uint32_t kSmallWaves = 16, kSmallThreads = kSmallWaves * 64;
 constexpr uint32_t kSmallHeld = 4;       // tiles of P X that a wave holds
 constexpr uint32_t kSmallEach = kSmallHeld * 256 / 64;       // elements that a thread reads
@@ -896,9 +897,10 @@ Plan make_plan(uint64_t rows, uint64_t cols, uint32_t count) {
     p.square = choose_cut(p.m, p.m, p.G_pitch / kStepBytes, count, true, 1);
     p.apply = choose_cut(p.m, p.n, p.G_pitch / kStepBytes, count, false, 1);
     // Two steps at once: G of the second is P G P, and one product takes X through both, P' P X: three products of m x m matrices in the
-    // place of X X^T and P X.  Singly / in pairs, us: 128 x 1024 96 / 101, 512 x 4608, 2 of them 333 / 265, 768 x 1536 216 / 212, 1000 x 2049
-    // 343 / 290, 2048 x 3000 1011 / 1015, 2048 x 8192 1887 / 1567, 4096 x 6000 5921 / 5630, 4096 x 25088 18952 / 13615.  The errors stay those of
-    // single steps where n is much larger than m and grow up to three times for square matrices, hence not below n = 2 m.
+    // place of X X^T and P X.  Singly / in pairs, us: 128 x 1024 97 / 101, 512 x 4608, 2 of them 327 / 284, 768 x 1536 197 / 198, 1000 x 2049
+    // 304 / 284, 2048 x 3000 1014 / 1027, 2048 x 8192 1965 / 1643, 4096 x 6000 5820 / 5566, 4096 x 25088 19874 / 14143.  For matrices of noise and
+    // strong directions the errors are those of single steps where n is much larger than m, and grow up to three times for square matrices, hence not below n = 2 m; where one
+    // direction holds nearly all of the norm, five times at 520 x 4160 (5e-6, and 2.4e-6 with fp32 products).
     p.pairs = p.n >= 2 * p.m && p.gram.us + p.apply.us > 3.0 * p.square.us;
     if (p.pairs) {
         p.T = take(p.G_bytes);
