@@ -290,15 +290,26 @@ def _dtype(t: torch.Tensor, where: str) -> int:
 
 
 def _view(where: str, t, *dims):
-    """For a tensor that is not contiguous, or too short if it were: refuses it unless its own last dimensions are those of the call,
-    (count, stride) from the outermost one on."""
+    """For a tensor that is not contiguous, or too short if it were: refuses it unless all that the call reads or writes, (count, stride) from
+    the outermost dimension on, are elements of the view, in its order.  The call's dimensions are laid into the view's from the
+    innermost on, as many into one as it has room for (a convolution's weights are a matrix whose columns are three of four dimensions)."""
     if t.is_contiguous():
         raise ValueError(f"{where}: a tensor of {t.numel()} elements, the call takes {1 + sum((n - 1) * step for n, step in dims if n > 1)}")
-    own = list(zip(t.shape, t.stride()))
-    for n, step in reversed(dims):
-        size, stride = own.pop() if own else (1, step)
-        if size < n or (n > 1 and stride != step):
-            raise QesgdError(ERR_STRIDE, where)
+    own = []
+    for size, stride in zip(t.shape, t.stride()):
+        if own and own[-1][1] == size * stride:
+            own[-1] = (own[-1][0] * size, stride)
+        elif size != 1:
+            own.append((size, stride))
+    left = [d for d in dims if d[0] > 1]
+    while left and own and 0 < own[-1][1] <= left[-1][1] and t.numel():
+        size, stride = own.pop()
+        at = 0
+        while left and left[-1][1] % stride == 0 and at + (left[-1][0] - 1) * (left[-1][1] // stride) < size:
+            n, step = left.pop()
+            at += (n - 1) * (step // stride)
+    if left or not t.numel():
+        raise QesgdError(ERR_STRIDE, where)
 
 
 @lru_cache(maxsize=256)

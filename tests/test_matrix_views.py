@@ -61,6 +61,64 @@ def test_views(B):
         refused(B, B.ERR_STRIDE, lambda: B._view("a", t, *dims))
 
 
+def test_dimensions_that_the_call_does_not_have(B):
+    """Any number of the tensor's dimensions may make up one of the call's."""
+    conv = torch.zeros(9, 8, 3, 3)
+    for t, dims in ((conv[::2], ((1, 0), (5, 144), (72, 1))), (conv[:, ::2], ((9, 72), (4, 18), (9, 1))), (conv[::2, 1:5], ((1, 0), (5, 144), (36, 1))),
+                    (conv[::2], ((5, 144), (8, 9), (9, 1))), (conv[::2], ((5, 144), (7, 9), (5, 1))), (conv[:, :, 1:], ((1, 0), (72, 9), (6, 1))),
+                    (conv[:, :, 1:], ((9, 72), (8, 9), (6, 1))), (conv[::2][None, :, None], ((1, 0), (5, 144), (72, 1)))):
+        assert not t.is_contiguous()
+        B._view("a", t, *dims)
+    for t, dims in ((conv.to(memory_format=torch.channels_last), ((1, 0), (9, 72), (72, 1))), (conv.permute(0, 2, 3, 1), ((1, 0), (9, 72), (72, 1))),
+                    (conv[:, ::2], ((1, 0), (9, 36), (36, 1))), (conv[:, ::2], ((1, 0), (9, 72), (36, 1))), (conv[::2], ((1, 0), (9, 72), (72, 1))),
+                    (conv[::2], ((1, 0), (6, 144), (72, 1))), (conv[::2], ((1, 0), (5, 144), (73, 1))), (conv[:, :, :, 1], ((1, 0), (9, 72), (24, 1))),
+                    (torch.zeros(4, 0, 3)[:, :, ::2], ((1, 0), (2, 3), (2, 1)))):
+        if t.is_contiguous():
+            with pytest.raises(ValueError):
+                B._view("a", t, *dims)
+        else:
+            refused(B, B.ERR_STRIDE, lambda: B._view("a", t, *dims))
+
+
+def reached(dims):
+    """Offsets that the call takes, relative to the first, in its order."""
+    at = [0]
+    for n, step in dims:
+        at = [a + i * step for a in at for i in range(n)]
+    return at
+
+
+def test_what_is_taken_lies_in_the_view(B):
+    """Random views and calls: one is taken only if every element that it reaches is one of the view's, and always if it goes through the
+    view's own dimensions or through a part of them."""
+    import random
+    rng = random.Random(0)
+    taken, base = 0, torch.arange(2 ** 20)
+    for _ in range(20_000):
+        shape = [rng.randint(1, 5) for _ in range(rng.randint(1, 4))]
+        strides, step = [], 1
+        for size in reversed(shape):
+            step *= rng.choice([1, 1, 1, 2, 3])
+            strides.insert(0, 0 if rng.random() < 0.05 else step)
+            step *= size
+        if rng.random() < 0.2:
+            rng.shuffle(strides)
+        t = base.as_strided(shape, strides)
+        if t.is_contiguous():
+            continue
+        mine = set(t.reshape(-1).tolist())
+        own = rng.random() < 0.5
+        dims = [(rng.randint(1, size), stride) for size, stride in zip(shape, strides)] if own else [(rng.randint(1, 6), rng.randint(1, 40)) for _ in range(rng.randint(1, 3))]
+        try:
+            B._view("a", t, *dims)
+            taken += 1
+            assert set(reached(dims)) <= mine, (shape, strides, dims)
+        except B.QesgdError:
+            ordered = all(0 < b <= a for a, b in zip(strides, strides[1:])) and all(s > 0 for s in strides)
+            assert not (own and ordered and all(a >= n * b for (a, b, n) in zip(strides, strides[1:], shape[1:]))), (shape, strides, dims)
+    assert taken > 1000
+
+
 def test_vectors_and_workspaces(B):
     v = torch.zeros(100)
     assert B._f32("a", -1, 100, v, None) == [v.data_ptr(), None]
