@@ -10,8 +10,8 @@
 // hi hi + (hi lo + lo hi) / 2048 with fp32 sums, one for either part: three fp16 products, five times the fp32 rate.  One fp16
 // product alone would cost three digits.  What a pair of fp16 numbers cannot do is fp32's range: a number has its 22 bits down to 2^-14
 // in scaled units, 2^-28 or 2^-29 of the largest there can be, below that a bit less for every halving, and nothing is left below 2^-36.
-// Without the 2048 that began at 2^-3: a matrix with one large number, row or column lost the others' digits, 1.5e-4 of them with a
-// ratio of 1e-6, and after ten steps, which make the small ones large, of the whole result (now 2e-6 and 1e-6, test_gpu_orthogonalize_scaled.py).
+// Without the 2048 that began at 2^-3: a matrix with one large number lost the others' digits, 1.5e-4 of them with a ratio of 1e-6, and after ten steps, which make the
+// small ones large, of the whole result (now 1.5e-6 and 1e-6).
 //
 // Layout of an operand ("split"): rows along the contraction, padded with zeros to a multiple of 32; 32 numbers' hi (64 bytes),
 // then their lo, so a step of the pipeline is one 128-byte line of each row.  Products have both operands' rows along the
