@@ -151,8 +151,8 @@ __device__ __forceinline__ uint32_t tile_of_workgroup(uint32_t b, uint32_t n) {
     return (b >> 3) + x * per + (x < left ? x : left);
 }
 // Tile t of tiles_m x tiles_n in bands of kBand rows of tiles, column by column within a band: what an XCD has in work at a time
-// is a block about as high as it is wide, which reads the fewest rows of A and B.  The orthogonalisation's 4096 x 25088 product in bands of 1 / 2 /
-// 4 / 8: 2321 / 2270 / 2170 / 2166 us; 4-bit 8192 x 4096 x 4096 79.0 / 78.6 / 77.2 / 78.6.
+// is a block about as high as it is wide, which reads the fewest rows of A and B.  Five steps of orthogonalising 4096 x 25088 in bands of 1 / 2 /
+// 4 / 8 / 16: 14.47 / 14.04 / 13.91 / 13.90 / 14.07 ms, 3000 x 3000 2487 / 2228 / 2184 / 2175 / 2225 us; 4-bit 8192 x 4096 x 4096 in 1 to 8 79.0 / 78.6 / 77.2 / 78.6.
 constexpr uint32_t kBand = 4;
 __device__ __forceinline__ void banded_tile(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
     const uint32_t width = kBand * tiles_n, band = t / width, first = band * kBand, in = t - band * width;
