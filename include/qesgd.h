@@ -297,9 +297,10 @@ int qesgd_mx4_product(const void* a_packed, const void* b_packed, uint64_t M, ui
  * then X = (a I + b G + c G^2) X with G = X X^T (X^T X on the longer side), (a, b, c) = coeffs[3*i .. 3*i+2] (host
  * memory, read during the call); out = X.  Singular values s become p_steps(.. p_1(s)), p(s) = a s + b s^3 + c s^5;
  * singular vectors stay.  Norms in fp64, products of fp32 accuracy (each operand as the sum of two fp16 numbers, sums in fp32).
- * Operands: numbers are held to 2^-22 of themselves down to 2^-28 of the largest that the coefficients allow in that operand, smaller ones to 2^-50 of
- * it; the first X is at most 1, so an entry of x keeps its digits down to 2^-28 of ||x||_F.  Their range follows from the coefficients: singular
- * values of an iterate X up to 2^20 and values of a + b s^2 + c s^4 up to 2^40 are right, whatever the shape; beyond that the result may be infinite or NaN.
+ * Operands: their range follows from the coefficients and a largest singular value of 1; numbers are held to 2^-22 of themselves down to 2^-28 of the
+ * largest that these allow in that operand, smaller ones to 2^-50 of it (so an entry of x keeps its digits down to 2^-28 of ||x||_F).  Singular values of an
+ * iterate X up to 2^7 and values of a + b s^2 + c s^4 up to 2^18 are right, whatever the shape; beyond that the result may be infinite or NaN.  Where
+ * coefficients would take 1 beyond that, and the matrix stays within it, numbers are held to 2^-37, the polynomials' to 2^-33.
  * A matrix of zeros gives zeros, one with a NaN or an infinity NaN everywhere.
  *   out  same type and shape as x, may be x itself.
  *   workspace  qesgd_orthogonalize_workspace_bytes(rows, cols, n), 256-byte aligned; may be NULL when that is 0 (matrices that fit

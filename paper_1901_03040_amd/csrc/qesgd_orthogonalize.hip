@@ -29,13 +29,14 @@
 namespace qesgd {
 namespace {
 
-constexpr double kMost = 1099511627776.0;        // 2^40: what G and P may reach
+constexpr double kMostX = 16384.0, kMostP = 262144.0;       // 2^14: what X, G and G P may reach, 2^18: P
 constexpr double kMostPair = 256.0;              // and a product of two P, whose range is that of both
 constexpr float kFirstX = 32768.0f;              // scale of the first X, whose entries are at most 1
 
-// The power of two that takes numbers up to `bound` to at most 2^15, half of fp16's range: rounding may pass the bound.
-inline double scale_for(double bound) {
-    const double b = bound < kMost ? std::max(bound, 1.0 / kMost) : kMost;        // a NaN counts as the most
+// The power of two that takes numbers up to `bound`, or up to `most` where that is less, to at most 2^15, half of fp16's range: rounding
+// may pass the bound.
+inline double scale_for(double bound, double most) {
+    const double b = bound < most ? std::max(bound, std::ldexp(1.0, -40)) : most;
     return std::ldexp(1.0, 15 - (int)std::ceil(std::log2(b)));
 }
 
@@ -43,6 +44,10 @@ inline double scale_for(double bound) {
 // Frobenius norm; those of the next at most the largest |a s + b s^3 + c s^5| on the way, G's are their squares, P's at most the largest
 // |a + b s^2 + c s^4|, and no entry of a matrix is larger than its largest singular value.  So the operands' scales are known before
 // the first kernel, whatever the matrix, and use fp16's range from its upper end.
+//
+// A matrix can be far from these bounds: of m equal singular values each is m^(-1/2), and polynomials that do not bring them together take 1 and that
+// to numbers many digits apart.  The scales therefore end at 2^14 and 2^18, where numbers are still held to 2^-37 (P to 2^-33): with bounds of 2^40
+// there a 200 x 333 matrix and three such polynomials had no digit left.
 struct Scales {
     double X[QESGD_MAX_STEPS + 1], G[QESGD_MAX_STEPS + 1], P[QESGD_MAX_STEPS];
     double T[QESGD_MAX_STEPS], PP[QESGD_MAX_STEPS];       // G P, and the product of this step's P and the next one's: 0 beyond kMostPair
@@ -68,16 +73,16 @@ inline Scales scales_of(const float* coeffs, uint32_t steps) {
         at(-b / (2.0 * c));
         at(q / (5.0 * c));
         at(a / q);
-        r.X[i] = i == 0 ? (double)kFirstX : scale_for(S);
-        r.G[i] = scale_for(S * S);
-        r.T[i] = scale_for(S * next);
-        r.P[i] = scale_for(most);
-        if (i > 0 && before * most <= kMostPair) r.PP[i - 1] = scale_for(before * most);
+        r.X[i] = i == 0 ? (double)kFirstX : scale_for(S, kMostX);
+        r.G[i] = scale_for(S * S, kMostX);
+        r.T[i] = scale_for(S * next, kMostX);
+        r.P[i] = scale_for(most, kMostP);
+        if (i > 0 && before * most <= kMostPair) r.PP[i - 1] = scale_for(before * most, kMostPair);
         before = most;
-        S = std::min(next, 1.0 / 1024.0 * kMost * kMost);              // beyond what is taken, and far from the end of 64 bits
+        S = std::min(next, std::ldexp(1.0, 70));                       // beyond what is taken, and far from the end of 64 bits
     }
-    r.X[steps] = scale_for(S);
-    r.G[steps] = scale_for(S * S);
+    r.X[steps] = scale_for(S, kMostX);
+    r.G[steps] = scale_for(S * S, kMostX);
     return r;
 }
 
