@@ -1,0 +1,602 @@
+"""What is measured of the operators for layers of experts: E matrices [N, K] of 4-bit microscaled codes, each token multiplied with k of them.
+
+A case is a dict of plain values.  Its "kind" says which calls make up one pass:
+
+  route    logits -> each token's experts, their gates, and the tokens' rows sorted by expert (qesgd_route); with "backward" also
+           the gradient of the logits (qesgd_route_backward)
+  layer    the forward pass of a layer on packed parameters: the tokens' rows quantised in the experts' order
+           (qesgd_mx4_quantize_groups), their products (qesgd_mx4_grouped_product), their weighted sum (qesgd_combine)
+  train    a layer's products in training: rows and their gradients quantised along both sides, the forward product, the gradient
+           of the tokens and that of the experts' matrices (qesgd_mx4_grouped_gradient)
+  combine  the weighted sum of the experts' rows and its gradients (qesgd_combine, qesgd_combine_backward)
+  vector   rows of a few tokens as they are, not quantised, times packed matrices (qesgd_mx4_vector_product): one matrix (E = 1)
+           or each row's expert's
+
+Rows sorted by expert: pair t * k + j (token t, choice j) of expert e lies among the rows offsets[e] .. offsets[e + 1]; order[row] is the
+pair, slots[pair] the row, -1 where there is none (a token whose logits are all -inf has no experts).
+
+The packed form: a matrix [rows, cols] is padded with zeros to a multiple of 128 columns; two 4-bit elements (E2M1: sign,
+0 .5 1 1.5 2 3 4 6) per byte, the even column in the low half; behind the codes, at the next multiple of 256 bytes, one byte
+e + 127 for each 32 columns, 255 where one of the 32 is not finite.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def listed():
+    return [
+        # the least: the choice of experts for one token; all latency
+        dict(name="route-1", kind="route", T=1, E=64, k=2, gate="all", dtype="f32", masked=0.0, backward=False),
+        # a training step's batch
+        dict(name="route-8192", kind="route", T=8192, E=64, k=2, gate="chosen", dtype="bf16", masked=0.0, backward=True),
+        # a very large batch over many experts, odd in everything, with padded tokens and experts that some tokens may not take
+        dict(name="route-160001-odd", kind="route", T=160_001, E=257, k=6, gate="all", dtype="f32", masked=0.02, backward=True),
+        # a few sequences' next tokens through small experts: four rows each
+        dict(name="layer-64", kind="layer", T=64, E=32, k=2, N=512, K=512, dtype="f32", masked=0.0),
+        # a large batch through large experts
+        dict(name="layer-16384", kind="layer", T=16_384, E=16, k=2, N=4096, K=4096, dtype="bf16", masked=0.0),
+        # a training step of a small layer
+        dict(name="train-96", kind="train", T=96, E=4, k=2, N=256, K=512, dtype="f32", mode="nearest", masked=0.0),
+        # odd in everything: rows that start nowhere aligned, padded tokens
+        dict(name="train-3001-odd", kind="train", T=3001, E=13, k=3, N=1000, K=2049, dtype="f16", mode="stochastic", masked=0.05),
+        # the largest: a training step of large experts; gradients rounded without bias
+        dict(name="train-8192", kind="train", T=8192, E=8, k=2, N=4096, K=4096, dtype="bf16", mode="stochastic", masked=0.0),
+        # three experts a token, odd rows, padded tokens
+        dict(name="combine-517-odd", kind="combine", T=517, E=13, k=3, N=1001, dtype="f32", masked=0.05),
+        # a large batch
+        dict(name="combine-16384", kind="combine", T=16_384, E=16, k=2, N=4096, dtype="bf16", masked=0.0),
+        # one token through a square layer
+        dict(name="vector-1x4096", kind="vector", T=1, E=1, k=1, N=4096, K=4096, dtype="bf16", masked=0.0),
+        # a dozen sequences' next tokens through four of 64 experts each, odd widths
+        dict(name="vector-12-of-64", kind="vector", T=12, E=64, k=4, N=1411, K=2049, dtype="f32", masked=0.0),
+    ]
+
+
+def log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["route", "layer", "layer", "train", "train", "combine", "vector", "vector"])
+    dtype = rng.choice(["f32", "bf16", "bf16", "f16"])
+    masked = rng.choice([0.0, 0.0, 0.02, 0.2])
+    if kind == "route":
+        E = log_int(rng, 2, 512)
+        T = log_int(rng, 1, min(200_000, 41_000_000 // E))
+        return dict(kind=kind, T=T, E=E, k=min(E, rng.randint(1, 8)), gate=rng.choice(["all", "chosen"]), dtype=dtype, masked=masked,
+                    backward=rng.random() < 0.7)
+    if kind == "combine":
+        k, N = rng.randint(1, 8), log_int(rng, 32, 8192)
+        return dict(kind=kind, T=log_int(rng, 1, 130_000_000 // (N * k)), E=max(k, log_int(rng, 1, 64)), k=k, N=N, dtype=dtype, masked=masked)
+    if kind == "vector":
+        N, K = log_int(rng, 64, 8192), log_int(rng, 32, 8192)
+        if rng.random() < 0.5:
+            N, K = max(64, N // 64 * 64), max(64, K // 64 * 64)
+        if rng.random() < 0.4:
+            return dict(kind=kind, T=rng.choice([1, 1, 1, 2, 3, 4, 7, 16]), E=1, k=1, N=N, K=K, dtype=dtype, masked=0.0)
+        E = max(2, min(128, log_int(rng, 2, 64), 400_000_000 // (N * K)))
+        return dict(kind=kind, T=rng.choice([1, 1, 2, 4, 8, 13, 16]), E=E, k=min(E, rng.randint(1, 8)), N=N, K=K, dtype=dtype, masked=0.0)
+    N, K = log_int(rng, 64, 4096), log_int(rng, 64, 4096)
+    if rng.random() < 0.5:
+        N, K = max(64, N // 64 * 64), max(64, K // 64 * 64)
+    E = max(1, min(log_int(rng, 1, 64), 134_000_000 // (N * K)))
+    k = min(E, rng.randint(1, 4))
+    T = max(1, min(log_int(rng, 16, 16_384), 16_384 * 4096 * 4096 // (N * K * k)))
+    if kind == "layer":
+        return dict(kind=kind, T=T, E=E, k=k, N=N, K=K, dtype=dtype, masked=masked)
+    return dict(kind=kind, T=T, E=E, k=k, N=N, K=K, dtype=dtype, mode=rng.choice(["stochastic", "nearest"]), masked=masked)
+
+
+# ---- inputs ---------------------------------------------------------------
+
+def generator(seed, stream):
+    return torch.Generator(device=DEV).manual_seed(((int(seed) + 1) << 8) + stream)
+
+
+def router_logits(T, E, masked, seed, dtype):
+    """Some experts are wanted more than others.  masked: that share of the tokens is padding, and has no expert at all; of another such
+    share each expert is closed with probability one half."""
+    g = generator(seed, 40)
+    x = torch.randn((T, E), generator=g, device=DEV) + 0.5 * torch.randn((E,), generator=g, device=DEV)
+    if masked:
+        u = torch.rand((T, 1), generator=g, device=DEV)
+        closed = (u < masked) | ((u < 2 * masked) & (torch.rand((T, E), generator=g, device=DEV) < 0.5))
+        x = torch.where(closed, -math.inf, x)
+    return x.to(dtype)
+
+
+def gradients(shape, seed, stream, dtype):
+    """Heavy tails and rows of different size, as gradients have them, and some exact zeros."""
+    g = generator(seed, stream)
+    x = torch.randn(shape, generator=g, device=DEV)
+    x *= torch.exp(torch.randn(shape[:-1] + (1,), generator=g, device=DEV)) * 1e-3
+    x *= 1.0 + 4.0 * (torch.rand(shape, generator=g, device=DEV) < 0.02)
+    x *= torch.rand(shape, generator=g, device=DEV) > 0.01
+    return x.to(dtype)
+
+
+def activations(shape, seed, stream, dtype):
+    """What comes out of a norm: a few channels are much larger."""
+    g = generator(seed, stream)
+    x = torch.randn(shape, generator=g, device=DEV)
+    x *= 1.0 + 7.0 * (torch.rand(shape[-1:], generator=g, device=DEV) < 0.01)
+    return x.to(dtype)
+
+
+def up(v, a):
+    return (v + a - 1) // a * a
+
+
+def packed_sizes(rows, cols):
+    """(bytes of a row of codes, where the scales begin, bytes of a row of scales, bytes in all)"""
+    wide = up(cols, 128)
+    at = up(rows * wide // 2, 256)
+    return wide // 2, at, wide // 32, at + up(rows * wide // 32, 256)
+
+
+def packed_buffer(rows, cols, n=None):
+    size = packed_sizes(rows, cols)[3]
+    return torch.zeros((size,) if n is None else (n, size), dtype=torch.uint8, device=DEV)
+
+
+def group_columns(R, E):
+    """Columns of the form along the groups' rows: each group is padded to a multiple of 128."""
+    return (R + 127 * min(E, R)) // 128 * 128
+
+
+def packed_weights(w):
+    """w [E, rows, cols] in 32 bits -> its 4-bit forms, as the server sends them."""
+    E, rows, cols = w.shape
+    half, at, per, _ = packed_sizes(rows, cols)
+    v = torch.nn.functional.pad(w, (0, half * 2 - cols))
+    q, e = nearest_parts(v)
+    code = (torch.bucketize(q.abs(), torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], device=DEV)) + 8 * (q < 0)).to(torch.uint8)
+    b = packed_buffer(rows, cols, E)
+    b[:, :rows * half] = (code[:, :, 0::2] | (code[:, :, 1::2] << 4)).reshape(E, -1)
+    b[:, at:at + rows * per] = (e + 127).to(torch.uint8).reshape(E, -1)
+    return b
+
+
+def prepare(case, seed):
+    kind, T, E, k, t = case["kind"], case["T"], case["E"], case["k"], DTYPES[case["dtype"]]
+    R = T * k
+    state = dict(case=case, seed=int(seed), kept={})
+    logits = router_logits(T, E, case["masked"], seed, t)
+    routed = dict(experts=torch.full((T, k), -1, dtype=torch.int32, device=DEV), gates=torch.zeros((T, k), device=DEV),
+                  offsets=torch.zeros(E + 1, dtype=torch.int32, device=DEV), order=torch.full((R,), -1, dtype=torch.int32, device=DEV),
+                  slots=torch.full((T, k), -1, dtype=torch.int32, device=DEV))
+    if kind == "route":
+        state.update(routed, logits=logits, dgates=torch.randn((T, k), generator=generator(seed, 1), device=DEV),
+                     dlogits=torch.zeros((T, E), dtype=t, device=DEV))
+        return state
+    # the other passes begin behind the router
+    experts, gates, offsets, order, slots = route_plain(logits, k, "chosen", routed["order"])
+    state.update(experts=experts, gates=gates, offsets=offsets, order=order, slots=slots,
+                 cap=max(1, int((offsets[1:] - offsets[:-1]).max())))          # rows of the largest group, for the plain form
+    if kind == "combine":
+        N = case["N"]
+        state.update(rows=activations((R, N), seed, 0, t), dy=gradients((T, N), seed, 1, t), y=torch.empty((T, N), dtype=t, device=DEV),
+                     drows=torch.zeros((R, N), dtype=t, device=DEV), dgates=torch.empty((T, k), device=DEV))
+        return state
+    N, K = case["N"], case["K"]
+    w = torch.randn((E, N, K), generator=generator(seed, 2), device=DEV) / math.sqrt(K)
+    state.update(x=activations((T, K), seed, 0, t), w=packed_weights(w), rows=torch.zeros((R, N), dtype=t, device=DEV))
+    if kind == "layer":
+        state.update(px=packed_buffer(R, K), y=torch.empty((T, N), dtype=t, device=DEV))
+    elif kind == "train":
+        Rp = group_columns(R, E)
+        state.update(wt=packed_weights(w.transpose(1, 2).contiguous()), drows=gradients((R, N), seed, 1, t),
+                     px=packed_buffer(R, K), pxt=packed_buffer(K, Rp), pd=packed_buffer(R, N), pdt=packed_buffer(N, Rp),
+                     dxrows=torch.zeros((R, K), dtype=t, device=DEV), dx=torch.empty((T, K), dtype=t, device=DEV),
+                     dw=torch.empty((E, N, K), device=DEV))
+    return state
+
+
+# ---- plain form -----------------------------------------------------------
+
+def philox(c, key):
+    """Philox4x32-10 of counters c (four int64 tensors of 32-bit values); the four output words."""
+    low = 0xFFFFFFFF
+    k0, k1 = key & low, key >> 32
+    c0, c1, c2, c3 = c
+    for _ in range(10):
+        a, b = c0 * 0xD2511F53, c2 * 0xCD9E8D57
+        c0, c1, c2, c3 = ((b >> 32) & low) ^ c1 ^ k0, b & low, ((a >> 32) & low) ^ c3 ^ k1, a & low
+        k0, k1 = (k0 + 0x9E3779B9) & low, (k1 + 0xBB67AE85) & low
+    return c0, c1, c2, c3
+
+
+def variates(rows, wide, seed, rnd):
+    """The 16-bit variates of a padded matrix: coordinate i = row * wide + column takes half i & 1 of word (i & 7) >> 1 of the call for i >> 3."""
+    g = torch.arange(rows * wide // 8, dtype=torch.int64, device=DEV)
+    words = torch.stack(philox((g & 0xFFFFFFFF, g >> 32, torch.zeros_like(g), torch.full_like(g, rnd)), seed), 1)
+    return torch.stack((words & 0xFFFF, words >> 16), 2).reshape(rows, wide)
+
+
+def power_of_two(e):
+    """2^e in 32 bits for e of -127 .. 126, from its bits."""
+    return ((e.int() + 128) << 23).view(torch.float32) * 0.5
+
+
+def scaled(x, stochastic):
+    """Magnitudes over their block's scale, and the exponent of each block: x [..., padded columns] in 32 bits."""
+    blocks = x.reshape(x.shape[:-1] + (-1, 32))
+    amax = blocks.abs().amax(-1)
+    frac, e = torch.frexp(amax)                              # amax = frac * 2^e, frac in [1/2, 1)
+    e = e - 3                                                # amax / 2^e in [4, 8)
+    if stochastic:
+        e = e + (frac > 0.75).to(e.dtype)                    # ... in (3, 6]: nothing is cut off
+    e = torch.where(amax == 0, -127, e).clamp(-127, 125)
+    return blocks.abs() * power_of_two(-e - 1)[..., None] * 2.0, e
+
+
+def nearest_parts(x):
+    a, e = scaled(x, False)
+    step = torch.where(a < 2, 0.5, torch.where(a < 4, 1.0, 2.0))
+    q = (torch.round(a / step) * step).clamp(max=6.0)        # ties to the even code
+    return torch.where(x < 0, -q.reshape(x.shape), q.reshape(x.shape)), e
+
+
+def mx4_values(x, mode, seed=0, rnd=0):
+    """The values that the 4-bit form of x [rows, cols] stands for, blocks along the rows."""
+    rows, cols = x.shape
+    wide = up(cols, 128)
+    v = torch.nn.functional.pad(x.float(), (0, wide - cols))
+    if mode == "nearest":
+        q, e = nearest_parts(v)
+    else:
+        a, e = scaled(v, True)
+        step = torch.where(a < 2, 0.5, torch.where(a < 4, 1.0, 2.0))
+        low = torch.floor(a / step)
+        part = torch.floor((a / step - low) * 65536.0)
+        r = variates(rows, wide, seed, rnd).reshape(a.shape)
+        q = ((low + (r + part >= 65536).float()) * step).clamp(max=6.0).reshape(v.shape)
+        q = torch.where(v < 0, -q, q)
+    return (q.reshape(e.shape + (32,)) * power_of_two(e)[..., None]).reshape(rows, wide)[:, :cols]
+
+
+def mx4_decode(packed, rows, cols):
+    """[E, bytes] -> [E, rows, cols] in 32 bits."""
+    half, at, per, _ = packed_sizes(rows, cols)
+    E = packed.shape[0]
+    codes = packed[:, :rows * half].reshape(E, rows, half)
+    code = torch.stack((codes & 15, codes >> 4), 3).reshape(E, rows, half * 2)
+    grid = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], device=DEV)
+    e = packed[:, at:at + rows * per].reshape(E, rows, per).int() - 127
+    return (grid[code.int()].reshape(E, rows, per, 32) * power_of_two(e)[..., None]).reshape(E, rows, half * 2)[:, :, :cols]
+
+
+def route_plain(logits, k, gate, order):
+    """experts, gates, offsets, order and slots; behind the last row of an expert, order keeps what it has."""
+    x = logits.float()
+    T, E = x.shape
+    top, experts = torch.sort(x, dim=1, descending=True, stable=True)           # ties: the lower index comes first
+    top, experts = top[:, :k], experts[:, :k]
+    none = top == -math.inf
+    highest = top[:, :1]
+    base = torch.where(highest == -math.inf, 0.0, highest)                      # a token without experts
+    parts = torch.exp(top - base)
+    total = (torch.exp(x - base) if gate == "all" else parts).sum(1, keepdim=True)
+    gates = torch.where(none, 0.0, parts / torch.where(total == 0, 1.0, total))
+    experts = torch.where(none, -1, experts)
+    pair_of = torch.where(experts < 0, E, experts).reshape(-1)
+    pairs = torch.sort(pair_of, stable=True)[1]
+    counts = torch.zeros(E + 1, dtype=torch.int64, device=x.device).scatter_add_(0, pair_of, torch.ones_like(pair_of))[:E]
+    offsets = torch.cat((torch.zeros(1, dtype=torch.int64, device=x.device), counts.cumsum(0)))
+    place = torch.arange(T * k, device=x.device)
+    taken = place < offsets[-1]
+    slots = torch.empty_like(place).scatter_(0, pairs, torch.where(taken, place, -1))
+    order = torch.where(taken, pairs, order.long())
+    return (experts.int(), gates, offsets.int(), order.int(), slots.reshape(T, k).int())
+
+
+def groups_of(offsets, R):
+    """The expert of each row; E for rows behind the last."""
+    row = torch.arange(R, device=offsets.device)
+    return torch.searchsorted(offsets[1:].long().contiguous(), row, right=True)
+
+
+def grouped(a, offsets, cap, E):
+    """Rows a [R, n] -> [E, cap, n], groups padded with zeros; and where each row went (rows without a group to a place of their own)."""
+    R = a.shape[0]
+    e = groups_of(offsets, R)
+    at = torch.where(e < E, e * cap + torch.arange(R, device=a.device) - offsets.long()[e.clamp(max=E - 1)], E * cap)
+    out = torch.zeros((E * cap + 1, a.shape[1]), device=a.device)
+    out[at] = a
+    return out[:E * cap].reshape(E, cap, -1), at
+
+
+def grouped_rows(y, at, before):
+    """[E, cap, n] -> rows [R, n] in the type of `before`, which rows without a group keep."""
+    flat = torch.cat((y.reshape(-1, y.shape[2]), y.new_zeros(1, y.shape[2])))
+    there = (at < flat.shape[0] - 1)[:, None]
+    return torch.where(there, flat[at].to(before.dtype), before)
+
+
+def along_groups(a, offsets, E, mode, seed=0, rnd=0):
+    """The values of the 4-bit form of a's rows along each group (blocks of 32 rows, groups padded to 128): [E * cap128, n] as [E, c, n]."""
+    R = a.shape[0]
+    Rp = group_columns(R, E)
+    counts = (offsets[1:] - offsets[:-1]).long()
+    padded = (counts + 127) // 128 * 128
+    begin = padded.cumsum(0) - padded
+    e = groups_of(offsets, R)
+    inside = e.clamp(max=E - 1)
+    at = torch.where(e < E, begin[inside] + torch.arange(R, device=a.device) - offsets.long()[inside], Rp)
+    wide = torch.zeros((Rp + 1, a.shape[1]), device=a.device)
+    wide[at] = a.float()
+    wide[Rp] = 0
+    v = mx4_values(wide[:Rp].t().contiguous(), mode, seed, rnd).t()
+    return v[at.clamp(max=Rp - 1)] * (e < E)[:, None]
+
+
+def combine_plain(rows, slots, gates):
+    picked = rows[slots.long().clamp(min=0)].float()
+    weight = torch.where(slots < 0, 0.0, 1.0 if gates is None else gates)
+    return (picked * weight[:, :, None]).sum(1)
+
+
+def plain(state):
+    case, seed = state["case"], state["seed"]
+    kind, E, k = case["kind"], case["E"], case["k"]
+    if kind == "route":
+        x, dgates = state["logits"].float(), state["dgates"]
+        experts, gates, offsets, order, slots = route_plain(state["logits"], k, case["gate"], state["order"])
+        if not case["backward"]:
+            return [experts, gates, offsets, order, slots]
+        s = (gates * dgates).sum(1, keepdim=True)
+        at = experts.long().clamp(min=0)
+        if case["gate"] == "all":
+            top = x.amax(1, keepdim=True)
+            p = torch.exp(x - torch.where(top == -math.inf, 0.0, top))
+            total = p.sum(1, keepdim=True)
+            p = p / torch.where(total == 0, 1.0, total)
+            dl = -p * s
+            dl = dl.scatter_add(1, at, gates * dgates)
+        else:
+            dl = torch.zeros_like(x).scatter_add(1, at, gates * (dgates - s))
+        return [experts, gates, offsets, order, slots, dl.to(state["logits"].dtype)]
+    if kind == "combine":
+        rows, dy, slots, gates, t = state["rows"], state["dy"], state["slots"], state["gates"], state["rows"].dtype
+        y = combine_plain(rows, slots, gates).to(t)
+        token = torch.div(state["order"].long().clamp(min=0), k, rounding_mode="floor")
+        there = state["order"] >= 0
+        gate = torch.where(there, gates.reshape(-1)[state["order"].long().clamp(min=0)], 0.0)
+        drows = torch.where(there[:, None], (gate[:, None] * dy.float()[token]).to(t), state["drows"])
+        dgates = (rows[slots.long().clamp(min=0)].float() * dy.float()[:, None, :]).sum(2)
+        return [y, drows, torch.where(slots < 0, 0.0, dgates)]
+    offsets, cap, t, N, K = state["offsets"], state["cap"], state["x"].dtype, case["N"], case["K"]
+    token = torch.div(state["order"].long().clamp(min=0), k, rounding_mode="floor")
+    x = state["x"][token]
+    w = mx4_decode(state["w"], N, K)
+    if kind == "vector":
+        a, at = grouped(x.float(), offsets, cap, E)
+        return grouped_rows(torch.matmul(a, w.transpose(1, 2).contiguous()), at, state["rows"])
+    a, at = grouped(mx4_values(x, "nearest"), offsets, cap, E)
+    if kind == "layer":
+        y = torch.matmul(a, w.transpose(1, 2).contiguous())
+        return combine_plain(grouped_rows(y, at, state["rows"].float()), state["slots"], state["gates"]).to(t)
+    mode, d = case["mode"], state["drows"]
+    y = grouped_rows(torch.matmul(a, w.transpose(1, 2).contiguous()), at, state["rows"])
+    dd, at = grouped(mx4_values(d, mode, seed, 5), offsets, cap, E)
+    dx = grouped_rows(torch.matmul(dd, mx4_decode(state["wt"], K, N).transpose(1, 2).contiguous()), at, state["dxrows"].float())
+    dx = combine_plain(dx, state["slots"], None).to(t)
+    dt, _ = grouped(along_groups(d, offsets, E, mode, seed, 5), offsets, cap, E)
+    xt, _ = grouped(along_groups(x, offsets, E, "nearest"), offsets, cap, E)
+    return [y, dx, torch.matmul(dt.transpose(1, 2).contiguous(), xt)]
+
+
+# ---- the library's calls --------------------------------------------------
+
+def run(state):
+    if not own:
+        return plain(state)
+    from paper_1901_03040_amd import binding as B
+    case, seed, kept = state["case"], state["seed"], state["kept"]
+    kind, T, E, k = case["kind"], case["T"], case["E"], case["k"]
+    R = T * k
+    if kind == "route":
+        gate = B.GATE_ALL if case["gate"] == "all" else B.GATE_CHOSEN
+        if not kept:                                         # a worker keeps its scratch from step to step
+            kept["ws"] = B.alloc_workspace(B.qesgd_route_workspace_bytes(T, E, k), DEV)
+        B.qesgd_route(state["logits"], E, T, E, k, gate, state["experts"], state["gates"], state["offsets"], state["order"], state["slots"],
+                      workspace=kept["ws"])
+        out = [state[n] for n in ("experts", "gates", "offsets", "order", "slots")]
+        if not case["backward"]:
+            return out
+        B.qesgd_route_backward(state["logits"], E, T, E, k, gate, state["experts"], state["gates"], state["dgates"], state["dlogits"], E)
+        return out + [state["dlogits"]]
+    slots, gates, offsets, order = (state[n] for n in ("slots", "gates", "offsets", "order"))
+    N = case["N"]
+    if kind == "combine":
+        B.qesgd_combine(state["rows"], N, R, slots, gates, T, k, N, state["y"], N)
+        B.qesgd_combine_backward(state["dy"], N, state["rows"], N, R, slots, gates, T, k, N, state["drows"], N, state["dgates"])
+        return [state["y"], state["drows"], state["dgates"]]
+    K, x, w = case["K"], state["x"], state["w"]
+    if kind == "vector":
+        if not kept:
+            kept["ws"] = B.alloc_workspace(B.qesgd_mx4_vector_product_workspace_bytes(R, N, K, E), DEV)
+        if E == 1:
+            B.qesgd_mx4_vector_product(x, K, T, None, 1, w, w.stride(0), None, 1, R, N, K, state["rows"], N, workspace=kept["ws"])
+        else:
+            B.qesgd_mx4_vector_product(x, K, T, order, k, w, w.stride(0), offsets, E, R, N, K, state["rows"], N, workspace=kept["ws"])
+        return state["rows"]
+    if kind == "layer":
+        if not kept:
+            kept["ws"] = B.alloc_workspace(B.qesgd_mx4_grouped_product_workspace_bytes(R, N, K, E), DEV)
+        B.qesgd_mx4_quantize_groups(x, K, T, order, k, offsets, E, R, K, B.MX4_NEAREST, 0, 0, state["px"])
+        B.qesgd_mx4_grouped_product(state["px"], w, w.stride(0), offsets, E, R, N, K, state["rows"], N, workspace=kept["ws"])
+        B.qesgd_combine(state["rows"], N, R, slots, gates, T, k, N, state["y"], N)
+        return state["y"]
+    mode, wt = B.MX4_STOCHASTIC if case["mode"] == "stochastic" else B.MX4_NEAREST, state["wt"]
+    if not kept:
+        need = max(B.qesgd_mx4_grouped_product_workspace_bytes(R, N, K, E), B.qesgd_mx4_grouped_product_workspace_bytes(R, K, N, E),
+                   B.qesgd_mx4_grouped_gradient_workspace_bytes(R, N, K, E))
+        kept["ws"] = B.alloc_workspace(need, DEV)
+    B.qesgd_mx4_quantize_groups(x, K, T, order, k, offsets, E, R, K, B.MX4_NEAREST, 0, 0, state["px"], packed_t=state["pxt"])
+    B.qesgd_mx4_grouped_product(state["px"], w, w.stride(0), offsets, E, R, N, K, state["rows"], N, workspace=kept["ws"])
+    B.qesgd_mx4_quantize_groups(state["drows"], N, R, None, 1, offsets, E, R, N, mode, seed, 5, state["pd"], packed_t=state["pdt"])
+    B.qesgd_mx4_grouped_product(state["pd"], wt, wt.stride(0), offsets, E, R, K, N, state["dxrows"], K, workspace=kept["ws"])
+    B.qesgd_mx4_grouped_gradient(state["pdt"], state["pxt"], offsets, E, R, N, K, state["dw"], workspace=kept["ws"])
+    B.qesgd_combine(state["dxrows"], K, R, slots, None, T, k, K, state["dx"], K)
+    return [state["rows"], state["dx"], state["dw"]]
+
+
+# ---- what it has to do ----------------------------------------------------
+
+def work(case):
+    kind, T, E, k = case["kind"], case["T"], case["E"], case["k"]
+    R, size = T * k, 4 if case["dtype"] == "f32" else 2
+    routing = 4 * (R + E + 1)                                # order and offsets
+    if kind == "route":
+        back = 2 * size * T * E + 12 * R if case["backward"] else 0
+        return {"bytes": size * T * E + 16 * R + 4 * (E + 1) + back, "flops": 0}
+    N = case["N"]
+    if kind == "combine":
+        return {"bytes": size * N * (R + T) + 8 * R + size * N * (T + 2 * R) + 12 * R, "flops": 0}
+    K = case["K"]
+    code = lambda r, c: r * (-(-c // 2) + -(-c // 32))  # noqa: E731
+    if kind == "vector":
+        hit = min(E, R)                                      # matrices that are read, at most; hardly more where there are many experts
+        hit = 1 if E == 1 else max(1, round(E * (1 - (1 - 1 / E) ** R))) if R < 4 * E else hit
+        return {"bytes": size * (T * K + R * N) + hit * code(N, K) + (routing if E > 1 else 0), "flops": 2 * R * N * K}
+    if kind == "layer":
+        return {"bytes": size * (T * K + T * N) + 2 * code(R, K) + E * code(N, K) + 2 * size * R * N + routing + 8 * R, "flops": 2 * R * N * K}
+    packed = 2 * (2 * code(R, K) + 2 * code(R, N)) + E * (code(N, K) + code(K, N))
+    return {"bytes": size * (T * K + 2 * R * N + 2 * R * K + T * K) + packed + 4 * E * N * K + routing + 4 * R, "flops": 6 * R * N * K}
+
+
+# ---- in 64 bits -----------------------------------------------------------
+
+def exact_mx4(x, mode, seed=0, rnd=0):
+    """From the definition: the scale from the largest magnitude's binary exponent, the element from the list of values."""
+    rows, cols = x.shape
+    wide = -(-cols // 128) * 128
+    v = torch.zeros((rows, wide), dtype=torch.float64, device=x.device)
+    v[:, :cols] = x.double()
+    out = torch.empty_like(v)
+    values = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, 8.0], dtype=torch.float64, device=x.device)
+    top = v.view(rows, -1, 32).abs().amax(2)
+    e = (top.view(torch.int64) >> 52) - 1023 - 2                 # floor(log2(top)) - 2; 0 has the lowest exponent
+    power = lambda e: ((e + 1023) << 52).view(torch.float64)  # noqa: E731
+    if mode == "stochastic":
+        e = torch.where((top > 0) & (top > 6 * power(e.clamp(min=-1000))), e + 1, e)
+    s = power(e.clamp(-127, 125)).repeat_interleave(32, 1)
+    part = max(1, (1 << 24) // wide)
+    for r in range(0, rows, part):
+        a = v[r:r + part].abs() / s[r:r + part]
+        at = (torch.searchsorted(values, a, right=True) - 1).clamp(0, 7)
+        low, high = values[at], values[at + 1]
+        f = (a - low) / (high - low)
+        if mode == "nearest":
+            more = (f > 0.5) | ((f == 0.5) & (at % 2 == 1))
+        else:
+            n = a.shape[0]
+            i = torch.arange(r * wide, (r + n) * wide, device=x.device).view(n, wide)
+            g = i[:, ::8].reshape(-1) // 8
+            words = philox((g % (1 << 32), g // (1 << 32), torch.zeros_like(g), torch.full_like(g, rnd)), seed)
+            word = torch.stack(words, -1)[:, [0, 0, 1, 1, 2, 2, 3, 3]].view(n, wide)
+            u = torch.where(i % 2 == 0, word % 65536, word // 65536)
+            more = u.double() + torch.floor(f * 65536) >= 65536
+        q = torch.minimum(torch.where(more, high, low), values[7])
+        out[r:r + part] = torch.sign(v[r:r + part]) * q * s[r:r + part]
+    return out[:, :cols]
+
+
+def exact_decode(packed, rows, cols):
+    half, at, per, _ = packed_sizes(rows, cols)
+    byte = packed[:rows * half].view(rows, half, 1).int()
+    four = torch.cat((byte % 16, byte // 16), 2).view(rows, -1)
+    size = torch.where(four % 8 < 2, (four % 8) / 2, (2 + four % 2) * (1 << (four % 8) // 2) / 4.0).double()
+    scale = (packed[at:at + rows * per].view(rows, per).long() + 1023 - 127 << 52).view(torch.float64).repeat_interleave(32, 1)
+    return (torch.where(four >= 8, -size, size) * scale)[:, :cols]
+
+
+def exact_route(case, s):
+    """By ranks: an expert is chosen when fewer than k others come before it."""
+    T, E, k = case["T"], case["E"], case["k"]
+    l = s["logits"].double()
+    p = torch.softmax(torch.where((l == -math.inf).all(1, keepdim=True), 0.0, l), 1) * (l > -math.inf)
+    experts, gates = [], []
+    left = l.clone()
+    for j in range(k):
+        best = left.amax(1)
+        at = torch.where(left == best[:, None], torch.arange(E, device=l.device), E).amin(1)
+        experts.append(torch.where(best > -math.inf, at, -1))
+        gates.append(p.gather(1, at[:, None])[:, 0])
+        left.scatter_(1, at[:, None], -math.inf)
+    experts, gates = torch.stack(experts, 1), torch.stack(gates, 1)
+    gates = torch.where(experts < 0, 0.0, gates)
+    if case["gate"] == "chosen":
+        gates = gates / gates.sum(1, keepdim=True).clamp(min=1e-300)
+    if not case["backward"]:
+        return [None, gates, None, None, None]
+    dg = s["dgates"].double()
+    s1 = (gates * dg).sum(1, keepdim=True)
+    dl = -p * s1 if case["gate"] == "all" else torch.zeros_like(l)
+    for j in range(k):
+        add = gates[:, j] * (dg[:, j] if case["gate"] == "all" else dg[:, j] - s1[:, 0])
+        dl.scatter_add_(1, experts[:, j:j + 1].clamp(min=0), torch.where(experts[:, j] < 0, 0.0, add)[:, None])
+    return [None, gates, None, None, None, dl]
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    kind, T, E, k = case["kind"], case["T"], case["E"], case["k"]
+    if kind == "route":
+        return exact_route(case, s)
+    slots, gates = s["slots"].long(), s["gates"].double()
+    N = case["N"]
+
+    def total(rows, weights):
+        out = torch.zeros((T, rows.shape[1]), dtype=torch.float64, device=rows.device)
+        for j in range(k):
+            there = slots[:, j] >= 0
+            out[there] += weights[there, j:j + 1] * rows[slots[there, j]].double()
+        return out
+
+    if kind == "combine":
+        dy, drows, dg = s["dy"].double(), s["drows"].double(), torch.zeros_like(gates)
+        for j in range(k):
+            there = slots[:, j] >= 0
+            drows[slots[there, j]] = gates[there, j:j + 1] * dy[there]
+            dg[there, j] = (s["rows"][slots[there, j]].double() * dy[there]).sum(1)
+        return [total(s["rows"], gates), drows, dg]
+    K, ends = case["K"], s["offsets"].tolist()
+    token = s["order"].long().clamp(min=0) // k
+    rows = torch.zeros((T * k, N), dtype=torch.float64, device=DEV)
+    x = s["x"][token]
+    a = x.double() if kind == "vector" else exact_mx4(x, "nearest")
+    for e in range(E):
+        lo, hi = ends[e], ends[e + 1]
+        if lo < hi:
+            rows[lo:hi] = a[lo:hi] @ exact_decode(s["w"][e], N, K).mT
+    if kind == "vector":
+        return rows
+    if kind == "layer":
+        return total(rows, gates)
+    d = exact_mx4(s["drows"], case["mode"], s["seed"], 5)
+    dxrows, dw = torch.zeros((T * k, K), dtype=torch.float64, device=DEV), torch.zeros((E, N, K), dtype=torch.float64, device=DEV)
+    # along the rows of a group: the groups one behind the other, each from a multiple of 128 on
+    Rp, at = group_columns(T * k, E), 0
+    begin = []
+    dt, xt = (torch.zeros((n, Rp), dtype=torch.float64, device=DEV) for n in (N, K))
+    for e in range(E):
+        lo, hi = ends[e], ends[e + 1]
+        begin.append(at)
+        dt[:, at:at + hi - lo] = s["drows"][lo:hi].double().mT
+        xt[:, at:at + hi - lo] = x[lo:hi].double().mT
+        at += -(-(hi - lo) // 128) * 128
+    dt, xt = exact_mx4(dt, case["mode"], s["seed"], 5), exact_mx4(xt, "nearest")
+    for e in range(E):
+        lo, hi = ends[e], ends[e + 1]
+        if lo < hi:
+            dxrows[lo:hi] = d[lo:hi] @ exact_decode(s["wt"][e], K, N).mT
+            dw[e] = dt[:, begin[e]:begin[e] + hi - lo] @ xt[:, begin[e]:begin[e] + hi - lo].mT
+    return [rows, total(dxrows, torch.ones_like(gates)), dw]
