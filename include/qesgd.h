@@ -85,7 +85,8 @@ enum {
     QESGD_ERR_DTYPE = -15,     /* dtype not QESGD_F32, QESGD_BF16 or QESGD_F16         */
     QESGD_ERR_MODE = -16,      /* mode not QESGD_MX4_NEAREST or QESGD_MX4_STOCHASTIC   */
     QESGD_ERR_STEPS = -17,     /* steps == 0 or steps > QESGD_MAX_STEPS                */
-    QESGD_ERR_COEFF = -18      /* a coefficient, eps, alpha or mu not finite, eps < 0  */
+    QESGD_ERR_COEFF = -18,     /* a coefficient, eps, alpha or mu not finite, eps < 0  */
+    QESGD_ERR_EXPERTS = -19    /* E not in [1, QESGD_MAX_EXPERTS], or k not in [1, min(E, QESGD_MAX_CHOICES)] */
 };
 
 enum { QESGD_NORM_L2 = 0, QESGD_NORM_MAX = 1 };
@@ -318,6 +319,94 @@ int qesgd_orthogonal_update(const float* g, uint64_t rows, uint64_t cols, uint32
                             const float* coeffs, uint32_t steps, float eps, float alpha, float* step_out, float* z_inout,
                             const float* w_snap, float* u_out, float* zsum_inout, void* workspace, size_t workspace_bytes,
                             void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Layers of experts: E matrix parameters of one shape [N, K] (a batch of qesgd_orthogonal_update), each token multiplied with k of
+ * them.  A worker's forward pass: qesgd_route chooses each token's experts and sorts the (token, choice) pairs by expert,
+ * qesgd_mx4_quantize_groups packs the tokens' rows in that order, qesgd_mx4_grouped_product multiplies each group of rows with its
+ * expert's packed matrix, qesgd_combine adds the rows up.  Backward: qesgd_combine_backward, the same two calls with the
+ * matrices' transposed forms, qesgd_mx4_grouped_gradient, qesgd_combine (gates NULL) and qesgd_route_backward.  For the next tokens of a few
+ * sequences qesgd_mx4_vector_product takes the rows as they are.  Nothing here waits for the host: the groups' sizes stay on the device.
+ *
+ * Groups: offsets [E + 1] int32 on the device, not falling; group e is rows offsets[e] .. offsets[e+1] - 1, any of them may be empty.
+ * R is the number of rows that the buffers have room for, offsets[E] <= R; rows outside of every group are neither read nor
+ * written.  Offsets beyond 0 .. R are taken as the nearest of the two, whatever they hold no call reads or writes outside its buffers.
+ * R, N, K and T in [1, 2^20] unless said otherwise, E in [1, QESGD_MAX_EXPERTS], k in [1, min(E, QESGD_MAX_CHOICES)].  Inputs and
+ * outputs of 16 and 32 bits are aligned to their elements, their rows ld >= row elements apart.
+ * ------------------------------------------------------------------------- */
+
+#define QESGD_MAX_EXPERTS 1024u
+#define QESGD_MAX_CHOICES 16u
+enum { QESGD_GATE_ALL = 0, QESGD_GATE_CHOSEN = 1 };
+
+/* Each token's k largest logits, ties to the lower expert, in falling order; logits [T, E] in dtype, T * k <= 2^28, T * E <= 2^36.
+ *   A logit of -infinity closes that expert to that token: it is never chosen, and where fewer than k are open the choices
+ *   behind them are -1, with gate 0 (a padded token has none at all).  A NaN counts as the largest; with a NaN or +infinity among a token's logits its gates are NaN.
+ *   gate_kind  QESGD_GATE_ALL: the chosen ones' shares of the softmax over all E logits; QESGD_GATE_CHOSEN: softmax over the chosen.
+ *   experts [T, k] int32, gates [T, k] fp32
+ *   offsets [E + 1]; order [T*k]: the pairs t*k + j sorted by expert, those of one expert in rising order; slots [T*k]: the place of each
+ *   pair in order, -1 for a choice of -1.  order is written up to offsets[E].
+ *   workspace  qesgd_route_workspace_bytes(T, E, k), 16-byte aligned; may be NULL when that is 0. */
+size_t qesgd_route_workspace_bytes(uint64_t T, uint32_t E, uint32_t k);
+int qesgd_route(const void* logits, uint32_t dtype, uint64_t ld, uint64_t T, uint32_t E, uint32_t k, uint32_t gate_kind,
+                int32_t* experts, float* gates, int32_t* offsets, int32_t* order, int32_t* slots,
+                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradient of the gates with respect to the logits: s = sum_j gates_j dgates_j;
+ *   QESGD_GATE_ALL: dlogits_e = sum_{j: experts_j = e} gates_j dgates_j - p_e s, p the softmax over all;
+ *   QESGD_GATE_CHOSEN: dlogits_e = sum_{j: experts_j = e} gates_j (dgates_j - s), 0 elsewhere.
+ * 0 for closed experts.  logits, experts and gates as in (and from) qesgd_route; logits may be NULL for QESGD_GATE_CHOSEN.  dlogits [T, E] in
+ * dtype, rows ld_d apart; choices outside 0 .. E-1 are left out. */
+int qesgd_route_backward(const void* logits, uint32_t dtype, uint64_t ld, uint64_t T, uint32_t E, uint32_t k, uint32_t gate_kind,
+                         const int32_t* experts, const float* gates, const float* dgates, void* dlogits, uint64_t ld_d, void* stream);
+
+/* out[t] = sum_j gates[t*k+j] * rows[slots[t*k+j]], added in order of j in fp32, rounded once; slots outside 0 .. R-1 are left out.
+ * rows [R, N] and out [T, N] in dtype.  gates NULL: 1 each (the gradient of tokens that went to k experts).  slots NULL: row t*k+j (then T*k <= R).
+ * T, R and N up to 2^28, T * k < 2^31. */
+int qesgd_combine(const void* rows, uint32_t dtype, uint64_t ld, uint64_t R, const int32_t* slots, const float* gates, uint64_t T, uint32_t k,
+                  uint64_t N, void* out, uint64_t ld_out, void* stream);
+
+/* drows[slots[t*k+j]] = gates[t*k+j] * dy[t] in dtype; dgates[t*k+j] = <dy[t], rows[slots[t*k+j]]> in fp32, 0 for a slot outside 0 .. R-1.
+ * drows and dgates may each be NULL, but not both; rows that no slot names are left as they are.  drows may be rows itself. */
+int qesgd_combine_backward(const void* dy, uint32_t dtype, uint64_t ld_dy, const void* rows, uint64_t ld, uint64_t R, const int32_t* slots,
+                           const float* gates, uint64_t T, uint32_t k, uint64_t N, void* drows, uint64_t ld_d, float* dgates, void* stream);
+
+/* Columns of the form along the groups' rows: every group begins at a multiple of 128, at most R rows in at most E groups.  0 for sizes out of range. */
+uint64_t qesgd_mx4_grouped_columns(uint64_t R, uint32_t E);
+
+/* Packs rows in the groups' order: row r of a group is row order[r] / per of x [T, cols] (order NULL: row r; rows outside x are zeros).
+ *   packed    nullable: layout (R, cols), as qesgd_mx4_quantize_pack of the gathered rows; rows outside of every group are left as they are
+ *   packed_t  nullable: layout (cols, qesgd_mx4_grouped_columns(R, E)): each column of x cut into blocks of 32 rows of one group; group e's
+ *         rows begin at column sum_{i<e} up(size_i, 128), and zeros follow them to the next multiple of 128.  Equal to quantising that
+ *         padded, transposed matrix; what follows the last group is left as it is.
+ * One of the two must be given.  mode, seed, round and worker as in qesgd_mx4_quantize_pack.  per in [1, 2^20]. */
+int qesgd_mx4_quantize_groups(const void* x, uint32_t dtype, uint64_t ld, uint64_t T, const int32_t* order, uint32_t per, const int32_t* offsets,
+                              uint32_t E, uint64_t R, uint64_t cols, uint32_t mode, uint64_t seed, uint32_t round, uint32_t worker,
+                              void* packed, void* packed_t, void* stream);
+
+/* C[r, n] = sum_k A[r, k] B_e[n, k] for the rows r of every group e: A packed, layout (R, K); B_e packed, layout (N, K), b_stride bytes
+ * apart (a multiple of 256).  Products exact, sums in fp32, C [R, N] in dtype, rounded once.
+ * workspace: qesgd_mx4_grouped_product_workspace_bytes(R, N, K, E), 16-byte aligned; may be NULL when that is 0. */
+size_t qesgd_mx4_grouped_product_workspace_bytes(uint64_t R, uint64_t N, uint64_t K, uint32_t E);
+int qesgd_mx4_grouped_product(const void* a_packed, const void* b_slab, uint64_t b_stride, const int32_t* offsets, uint32_t E, uint64_t R,
+                              uint64_t N, uint64_t K, void* c, uint32_t dtype, uint64_t ldc, void* workspace, size_t workspace_bytes, void* stream);
+
+/* D_e[n, k] = sum over the rows r of group e of A[r, n] B[r, k], from the forms along the groups' rows: A layout (N, columns), B layout
+ * (K, columns), columns = qesgd_mx4_grouped_columns(R, E).  D [E, N, K] in dtype without padding; zeros for an empty group.
+ * A layer's weight gradients: A = the gradients' form, B = the activations'. */
+size_t qesgd_mx4_grouped_gradient_workspace_bytes(uint64_t R, uint64_t N, uint64_t K, uint32_t E);
+int qesgd_mx4_grouped_gradient(const void* a_packed_t, const void* b_packed_t, const int32_t* offsets, uint32_t E, uint64_t R, uint64_t N,
+                               uint64_t K, void* d, uint32_t dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* y[r, n] = sum_k x[row, k] W_e[n, k] for the rows of every group, x not quantised: row = order[r] / per, or r where order is NULL, of x
+ * [T, K] in dtype; rows outside x count as zeros.  W_e packed, layout (N, K), w_stride bytes apart.  offsets NULL: one group of all R rows (E = 1).
+ * Products are exact (x as a sum of one, two or three bf16 numbers for bf16, f16 and f32), sums in fp32, y [R, N] in dtype.  Right for any
+ * R, made for the next tokens of a few sequences: what it takes is the reading of the matrices that have rows.
+ * Scale bytes of the format (up to 252, and 255); elements of W below 2^-126 may count as 0; an element of x in f32 keeps 2^-24 of itself down to 2^-102, smaller ones may lose digits. */
+size_t qesgd_mx4_vector_product_workspace_bytes(uint64_t R, uint64_t N, uint64_t K, uint32_t E);
+int qesgd_mx4_vector_product(const void* x, uint32_t dtype, uint64_t ld, uint64_t T, const int32_t* order, uint32_t per, const void* w_slab,
+                             uint64_t w_stride, const int32_t* offsets, uint32_t E, uint64_t R, uint64_t N, uint64_t K, void* y, uint64_t ldy,
+                             void* workspace, size_t workspace_bytes, void* stream);
 
 const char* qesgd_strerror(int code);
 /* hipError_t (as int) of the last failed launch on the calling thread, 0 if none. */

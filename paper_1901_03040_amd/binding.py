@@ -25,10 +25,12 @@ OK = 0
 ERR_NULL, ERR_DIM, ERR_LEVELS, ERR_BUCKET, ERR_WORKERS = -1, -2, -3, -4, -5
 ERR_NORM_KIND, ERR_ALIGN, ERR_STRIDE, ERR_WORKSPACE, ERR_HIP = -6, -7, -8, -9, -10
 ERR_BITS, ERR_DELTA, ERR_ROUNDS, ERR_SCRATCH = -11, -12, -13, -14
-ERR_DTYPE, ERR_MODE, ERR_STEPS, ERR_COEFF = -15, -16, -17, -18
+ERR_DTYPE, ERR_MODE, ERR_STEPS, ERR_COEFF, ERR_EXPERTS = -15, -16, -17, -18, -19
 NOALLOC_SCRATCH_BYTES = 4 << 20
 MX4_NEAREST, MX4_STOCHASTIC = 0, 1
 MAX_STEPS = 32
+MAX_EXPERTS, MAX_CHOICES = 1024, 16
+GATE_ALL, GATE_CHOSEN = 0, 1
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -132,6 +134,29 @@ def lib():
         L.qesgd_orthogonalize.restype = C.c_int
         L.qesgd_orthogonal_update.argtypes = [vp, u64, u64, u32, vp, f32, u32, vp, u32, f32, f32, vp, vp, vp, vp, vp, vp, sz, vp]
         L.qesgd_orthogonal_update.restype = C.c_int
+        L.qesgd_route_workspace_bytes.argtypes = [u64, u32, u32]
+        L.qesgd_route_workspace_bytes.restype = sz
+        L.qesgd_route.argtypes = [vp, u32, u64, u64, u32, u32, u32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.qesgd_route.restype = C.c_int
+        L.qesgd_route_backward.argtypes = [vp, u32, u64, u64, u32, u32, u32, vp, vp, vp, vp, u64, vp]
+        L.qesgd_route_backward.restype = C.c_int
+        L.qesgd_combine.argtypes = [vp, u32, u64, u64, vp, vp, u64, u32, u64, vp, u64, vp]
+        L.qesgd_combine.restype = C.c_int
+        L.qesgd_combine_backward.argtypes = [vp, u32, u64, vp, u64, u64, vp, vp, u64, u32, u64, vp, u64, vp, vp]
+        L.qesgd_combine_backward.restype = C.c_int
+        L.qesgd_mx4_grouped_columns.argtypes = [u64, u32]
+        L.qesgd_mx4_grouped_columns.restype = u64
+        L.qesgd_mx4_quantize_groups.argtypes = [vp, u32, u64, u64, vp, u32, vp, u32, u64, u64, u32, u64, u32, u32, vp, vp, vp]
+        L.qesgd_mx4_quantize_groups.restype = C.c_int
+        L.qesgd_mx4_grouped_product.argtypes = [vp, vp, u64, vp, u32, u64, u64, u64, vp, u32, u64, vp, sz, vp]
+        L.qesgd_mx4_grouped_product.restype = C.c_int
+        L.qesgd_mx4_grouped_gradient.argtypes = [vp, vp, vp, u32, u64, u64, u64, vp, u32, vp, sz, vp]
+        L.qesgd_mx4_grouped_gradient.restype = C.c_int
+        L.qesgd_mx4_vector_product.argtypes = [vp, u32, u64, u64, vp, u32, vp, u64, vp, u32, u64, u64, u64, vp, u64, vp, sz, vp]
+        L.qesgd_mx4_vector_product.restype = C.c_int
+        for name in ("grouped_product", "grouped_gradient", "vector_product"):
+            f = getattr(L, f"qesgd_mx4_{name}_workspace_bytes")
+            f.argtypes, f.restype = [u64, u64, u64, u32], sz
         L.qesgd_strerror.argtypes = [C.c_int]
         L.qesgd_strerror.restype = C.c_char_p
         L.qesgd_last_hip_error.argtypes = []
@@ -453,6 +478,160 @@ def qesgd_orthogonal_update(g, rows, cols, n, momentum_inout, mu, nesterov, coef
     ws, ws_bytes = _ws(where, device, workspace)
     _check(lib().qesgd_orthogonal_update(g, rows, cols, n, m, float(mu), 1 if nesterov else 0, steps, len(coeffs), float(eps),
                                          float(alpha), step, z, w, u, zsum, ws, ws_bytes, stream), where)
+
+
+# ---- layers of experts ------------------------------------------------------
+#
+# The same checks as above.  experts, offsets, order and slots are int32, gates and their gradients fp32, all contiguous.
+
+_I32 = torch.int32
+
+
+def _i32(where: str, device, t, count):
+    """Address of a contiguous int32 tensor of at least `count` elements."""
+    if t.get_device() != device:
+        _elsewhere(where, t)
+    if t.dtype is not _I32:
+        raise QesgdError(ERR_DTYPE, where)
+    if not t.is_contiguous():
+        raise QesgdError(ERR_STRIDE, where)
+    if t.numel() < count:
+        _view(where, t, (count, 1))
+    return t.data_ptr()
+
+
+def _rows(where: str, device, t, dtype, rows, ld, cols):
+    """Address of `rows` rows of `cols` elements, ld apart, in the type of that code."""
+    if t.get_device() != device:
+        _elsewhere(where, t)
+    if DTYPES.get(t.dtype) != dtype:
+        raise QesgdError(ERR_DTYPE, where)
+    if not t.is_contiguous() or t.numel() < (rows - 1) * ld + cols:
+        _view(where, t, (rows, ld), (cols, 1))
+    return t.data_ptr()
+
+
+def qesgd_route_workspace_bytes(T: int, E: int, k: int) -> int:
+    return int(lib().qesgd_route_workspace_bytes(int(T), int(E), int(k)))
+
+
+def qesgd_route(logits, ld, T, E, k, gate_kind, experts, gates, offsets, order, slots, workspace=None, stream=None):
+    where = "qesgd_route"
+    dtype = _dtype(logits, where)
+    device, stream = _here(where, stream, logits)
+    x = _rows(where, device, logits, dtype, T, ld, E)
+    pairs = T * k
+    g, = _f32(where, device, pairs, gates)
+    ws, ws_bytes = _ws(where, device, workspace)
+    rc = (_lib or lib()).qesgd_route(x, dtype, ld, T, E, k, gate_kind, _i32(where, device, experts, pairs), g, _i32(where, device, offsets, E + 1),
+                                     _i32(where, device, order, pairs), _i32(where, device, slots, pairs), ws, ws_bytes, stream)
+    if rc:
+        raise QesgdError(rc, where)
+
+
+def qesgd_route_backward(logits, ld, T, E, k, gate_kind, experts, gates, dgates, dlogits, ld_d, stream=None):
+    where = "qesgd_route_backward"
+    dtype = _dtype(dlogits, where)
+    device, stream = _here(where, stream, dlogits)
+    x = None if logits is None else _rows(where, device, logits, dtype, T, ld, E)
+    g, dg = _f32(where, device, T * k, gates, dgates)
+    rc = (_lib or lib()).qesgd_route_backward(x, dtype, ld, T, E, k, gate_kind, _i32(where, device, experts, T * k), g, dg,
+                                              _rows(where, device, dlogits, dtype, T, ld_d, E), ld_d, stream)
+    if rc:
+        raise QesgdError(rc, where)
+
+
+def qesgd_combine(rows, ld, R, slots, gates, T, k, N, out, ld_out, stream=None):
+    where = "qesgd_combine"
+    dtype = _dtype(out, where)
+    device, stream = _here(where, stream, out)
+    s = None if slots is None else _i32(where, device, slots, T * k)
+    g, = _f32(where, device, T * k, gates)
+    rc = (_lib or lib()).qesgd_combine(_rows(where, device, rows, dtype, R, ld, N), dtype, ld, R, s, g, T, k, N,
+                                       _rows(where, device, out, dtype, T, ld_out, N), ld_out, stream)
+    if rc:
+        raise QesgdError(rc, where)
+
+
+def qesgd_combine_backward(dy, ld_dy, rows, ld, R, slots, gates, T, k, N, drows, ld_d, dgates, stream=None):
+    where = "qesgd_combine_backward"
+    dtype = _dtype(dy, where)
+    device, stream = _here(where, stream, dy)
+    s = None if slots is None else _i32(where, device, slots, T * k)
+    g, dg = _f32(where, device, T * k, gates, dgates)
+    x = None if rows is None else _rows(where, device, rows, dtype, R, ld, N)
+    d = None if drows is None else _rows(where, device, drows, dtype, R, ld_d, N)
+    rc = (_lib or lib()).qesgd_combine_backward(_rows(where, device, dy, dtype, T, ld_dy, N), dtype, ld_dy, x, ld, R, s, g, T, k, N, d, ld_d, dg, stream)
+    if rc:
+        raise QesgdError(rc, where)
+
+
+def qesgd_mx4_grouped_columns(R: int, E: int) -> int:
+    return int(lib().qesgd_mx4_grouped_columns(int(R), int(E)))
+
+
+def qesgd_mx4_quantize_groups(x, ld, T, order, per, offsets, E, R, cols, mode, seed, rnd, packed, packed_t=None, worker=0, stream=None):
+    where = "qesgd_mx4_quantize_groups"
+    dtype = _dtype(x, where)
+    device, stream = _here(where, stream, x)
+    p = None if packed is None else _packed(where, device, packed, R, cols)
+    pt = None if packed_t is None else _packed(where, device, packed_t, cols, (R + 127 * min(E, R)) // 128 * 128)
+    rc = (_lib or lib()).qesgd_mx4_quantize_groups(_rows(where, device, x, dtype, T, ld, cols), dtype, ld, T,
+                                                   None if order is None else _i32(where, device, order, R), per,
+                                                   _i32(where, device, offsets, E + 1), E, R, cols, mode, seed, rnd, worker, p, pt, stream)
+    if rc:
+        raise QesgdError(rc, where)
+
+
+def qesgd_mx4_grouped_product_workspace_bytes(R: int, N: int, K: int, E: int) -> int:
+    return int(lib().qesgd_mx4_grouped_product_workspace_bytes(int(R), int(N), int(K), int(E)))
+
+
+def qesgd_mx4_grouped_product(a_packed, b_slab, b_stride, offsets, E, R, N, K, c, ldc, workspace=None, stream=None):
+    where = "qesgd_mx4_grouped_product"
+    dtype = _dtype(c, where)
+    device, stream = _here(where, stream, c)
+    ws, ws_bytes = _ws(where, device, workspace)
+    rc = (_lib or lib()).qesgd_mx4_grouped_product(_packed(where, device, a_packed, R, K), _packed(where, device, b_slab, N, K, E, b_stride), b_stride,
+                                                   _i32(where, device, offsets, E + 1), E, R, N, K, _rows(where, device, c, dtype, R, ldc, N), dtype,
+                                                   ldc, ws, ws_bytes, stream)
+    if rc:
+        raise QesgdError(rc, where)
+
+
+def qesgd_mx4_grouped_gradient_workspace_bytes(R: int, N: int, K: int, E: int) -> int:
+    return int(lib().qesgd_mx4_grouped_gradient_workspace_bytes(int(R), int(N), int(K), int(E)))
+
+
+def qesgd_mx4_grouped_gradient(a_packed_t, b_packed_t, offsets, E, R, N, K, d, workspace=None, stream=None):
+    where = "qesgd_mx4_grouped_gradient"
+    dtype = _dtype(d, where)
+    device, stream = _here(where, stream, d)
+    columns = (R + 127 * min(E, R)) // 128 * 128
+    ws, ws_bytes = _ws(where, device, workspace)
+    rc = (_lib or lib()).qesgd_mx4_grouped_gradient(_packed(where, device, a_packed_t, N, columns), _packed(where, device, b_packed_t, K, columns),
+                                                    _i32(where, device, offsets, E + 1), E, R, N, K, _rows(where, device, d, dtype, E, N * K, N * K),
+                                                    dtype, ws, ws_bytes, stream)
+    if rc:
+        raise QesgdError(rc, where)
+
+
+def qesgd_mx4_vector_product_workspace_bytes(R: int, N: int, K: int, E: int) -> int:
+    return int(lib().qesgd_mx4_vector_product_workspace_bytes(int(R), int(N), int(K), int(E)))
+
+
+def qesgd_mx4_vector_product(x, ld, T, order, per, w_slab, w_stride, offsets, E, R, N, K, y, ldy, workspace=None, stream=None):
+    where = "qesgd_mx4_vector_product"
+    dtype = _dtype(y, where)
+    device, stream = _here(where, stream, y)
+    ws, ws_bytes = _ws(where, device, workspace)
+    rc = (_lib or lib()).qesgd_mx4_vector_product(_rows(where, device, x, dtype, T, ld, K), dtype, ld, T,
+                                                  None if order is None else _i32(where, device, order, R), per,
+                                                  _packed(where, device, w_slab, N, K, E, w_stride), w_stride,
+                                                  None if offsets is None else _i32(where, device, offsets, E + 1), E, R, N, K,
+                                                  _rows(where, device, y, dtype, R, ldy, N), ldy, ws, ws_bytes, stream)
+    if rc:
+        raise QesgdError(rc, where)
 
 
 def qesgd_abi_version() -> int:

@@ -318,6 +318,7 @@ const char* qesgd_strerror(int code) {
         case QESGD_ERR_MODE: return "mode must be 0 (nearest) or 1 (stochastic)";
         case QESGD_ERR_STEPS: return "steps must be in [1, 32]";
         case QESGD_ERR_COEFF: return "coefficients, eps, alpha and mu must be finite, eps not negative";
+        case QESGD_ERR_EXPERTS: return "E must be in [1, 1024], k in [1, min(E, 16)]";
         default: return "unknown error code";
     }
 }

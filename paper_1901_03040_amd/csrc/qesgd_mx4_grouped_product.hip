@@ -1,0 +1,210 @@
+// Products of packed 4-bit rows grouped by expert, on the tiles of the product of two matrices.
+//
+//   C[r, n] = sum_k A[r, k] B_e[n, k] for the rows r of group e        a tile's rows end with its group
+//   D_e[n, k] = sum over the rows r of group e of A[r, n] B[r, k]      a tile's contraction is its group's rows
+//
+// Element products are exact, sums are fp32.
+#include "qesgd_experts.h"
+#include "qesgd_groups.h"
+#include "qesgd_mx4_tiles.h"
+
+namespace qesgd {
+namespace {
+
+struct PParams {
+    const unsigned char* a;
+    const unsigned char* b;
+    uint64_t a_scales, b_scales, b_stride;
+    const int32_t* offsets;
+    uint32_t E, R;
+    void* c;
+    uint64_t ldc;
+    uint32_t N, K;                        // rows of B_e; columns of D_e
+    uint32_t row_codes, row_scales;       // of either operand
+    uint32_t tiles_m, tiles_n;            // of one expert's D; tiles_n of C
+};
+
+template <class S>
+__device__ __forceinline__ void multiply_tile(Mx4Ops<S>& ops, uint32_t steps, unsigned char* lds0, unsigned char* lds1, unsigned char* lds2, unsigned char* lds3) {
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) ops.acc[i][j] = acc16{};
+    if constexpr (S::BUFFERS == 2) {
+        unsigned char* const buffers[2] = {lds0, lds1};
+        run_steps(ops, steps, buffers);
+    } else {
+        unsigned char* const buffers[4] = {lds0, lds1, lds2, lds3};
+        run_steps(ops, steps, buffers);
+    }
+}
+
+template <class S, uint32_t DT>
+__global__ void __launch_bounds__(S::threads) k_mx4_grouped_product(const PParams p) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds0[(S::BM + S::BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds1[(S::BM + S::BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds2[S::BUFFERS > 2 ? (S::BM + S::BN) * kStepBytes : 16];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds3[S::BUFFERS > 2 ? (S::BM + S::BN) * kStepBytes : 16];
+    __shared__ __attribute__((aligned(1024))) unsigned char scales[Mx4Ops<S>::scale_buffers * Mx4Ops<S>::scale_bytes];
+    constexpr uint32_t lg = S::BM == 64 ? 6 : S::BM == 128 ? 7 : 8;
+    static_assert((1 << lg) == S::BM, "tiles of a power of two");
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
+    const uint32_t wm = wave / S::WN, wn = wave % S::WN;
+    // the workgroups that have a tile are dealt to the XCDs among themselves: those behind the last tile come last of all
+    const uint32_t all = all_tiles(p.offsets, p.E, p.R, lg) * p.tiles_n;
+    if (blockIdx.x >= all) return;
+    const uint32_t t = tile_of_workgroup(blockIdx.x, all);
+    Group g;
+    if (!group_of_tile(p.offsets, p.E, p.R, lg, p.tiles_n, t, g)) return;
+    uint32_t tm, tn;
+    banded_tile(t - g.first, (g.hi - g.lo + S::BM - 1u) >> lg, p.tiles_n, tm, tn);
+    tm = __builtin_amdgcn_readfirstlane(tm);
+    tn = __builtin_amdgcn_readfirstlane(tn);
+    const uint32_t m0 = g.lo + tm * S::BM, n0 = tn * S::BN;
+    const unsigned char* b = p.b + g.e * p.b_stride;
+    Mx4Ops<S> ops;
+    ops.a = p.a + (uint64_t)m0 * p.row_codes;
+    ops.b = b + (uint64_t)n0 * p.row_codes;
+    ops.la.init(p.row_codes, g.hi - m0);
+    ops.lb.init(p.row_codes, p.N - n0);
+    ops.scales = scales;
+    ops.init_scales(p.a + p.a_scales + (uint64_t)m0 * p.row_scales, b + p.b_scales + (uint64_t)n0 * p.row_scales, g.hi - m0, p.N - n0,
+                    p.row_scales, p.row_scales, wm, wn);
+    ops.at_a = wm * S::FM * 32 * kStepBytes + lane_place(lane);
+    ops.at_b = (S::BM + wn * S::FN * 32) * kStepBytes + lane_place(lane);
+    ops.steps = (p.row_codes + kStepBytes - 1u) / kStepBytes;
+    ops.half = p.row_codes % kStepBytes != 0;
+    ops.h = h;
+    multiply_tile(ops, ops.steps, lds0, lds1, lds2, lds3);
+
+    const bool whole = m0 + S::BM <= g.hi && n0 + S::BN <= p.N;
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j)
+            store_fragment<DT>(p.c, p.ldc, g.hi, p.N, m0 + (wm * S::FM + i) * 32u + 4u * h, n0 + (wn * S::FN + j) * 32u + (lane & 31u), whole, ops.acc[i][j]);
+}
+
+template <class S, uint32_t DT>
+__global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PParams p) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds0[(S::BM + S::BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds1[(S::BM + S::BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds2[S::BUFFERS > 2 ? (S::BM + S::BN) * kStepBytes : 16];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds3[S::BUFFERS > 2 ? (S::BM + S::BN) * kStepBytes : 16];
+    __shared__ __attribute__((aligned(1024))) unsigned char scales[Mx4Ops<S>::scale_buffers * Mx4Ops<S>::scale_bytes];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
+    const uint32_t wm = wave / S::WN, wn = wave % S::WN;
+    const uint32_t tiles = p.tiles_m * p.tiles_n;
+    const uint32_t t = tile_of_workgroup(blockIdx.x, gridDim.x), e = __builtin_amdgcn_readfirstlane(t / tiles);
+    uint32_t tm, tn;
+    banded_tile(t - e * tiles, p.tiles_m, p.tiles_n, tm, tn);
+    tm = __builtin_amdgcn_readfirstlane(tm);
+    tn = __builtin_amdgcn_readfirstlane(tn);
+    const Group g = group_number(p.offsets, p.E, p.R, 7, e);
+    // bytes of a row's codes before the group and of the group, as far as the rows go
+    const uint32_t begin = __builtin_amdgcn_readfirstlane(min(g.first * 64u, p.row_codes));
+    const uint32_t bytes = __builtin_amdgcn_readfirstlane(min(((g.hi - g.lo + 127u) >> 7) * 64u, p.row_codes - begin));
+    const uint32_t m0 = tm * S::BM, n0 = tn * S::BN;
+    Mx4Ops<S> ops;
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) ops.acc[i][j] = acc16{};
+    if (bytes) {
+        ops.a = p.a + (uint64_t)m0 * p.row_codes + begin;
+        ops.b = p.b + (uint64_t)n0 * p.row_codes + begin;
+        ops.la.init(p.row_codes, p.N - m0);
+        ops.lb.init(p.row_codes, p.K - n0);
+        ops.scales = scales;
+        ops.init_scales(p.a + p.a_scales + (uint64_t)m0 * p.row_scales + begin / 16u, p.b + p.b_scales + (uint64_t)n0 * p.row_scales + begin / 16u,
+                        p.N - m0, p.K - n0, p.row_scales, bytes / 16u, wm, wn);
+        ops.at_a = wm * S::FM * 32 * kStepBytes + lane_place(lane);
+        ops.at_b = (S::BM + wn * S::FN * 32) * kStepBytes + lane_place(lane);
+        ops.steps = (bytes + kStepBytes - 1u) / kStepBytes;
+        ops.half = bytes % kStepBytes != 0;
+        ops.h = h;
+        multiply_tile(ops, ops.steps, lds0, lds1, lds2, lds3);
+    }
+    void* d = (unsigned char*)p.c + (uint64_t)e * p.N * p.K * (DT == QESGD_F32 ? 4u : 2u);
+    const bool whole = m0 + S::BM <= p.N && n0 + S::BN <= p.K;
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j)
+            store_fragment<DT>(d, p.K, p.N, p.K, m0 + (wm * S::FM + i) * 32u + 4u * h, n0 + (wn * S::FN + j) * 32u + (lane & 31u), whole, ops.acc[i][j]);
+}
+
+template <class S>
+int launch_product_tiles(const GroupProduct& a, PParams& p) {
+    p.tiles_n = (p.N + S::BN - 1) / S::BN;
+    // the most tiles that R rows in E groups make
+    const uint64_t groups = a.E < a.R ? a.E : a.R, tiles_m = (a.R + (S::BM - 1) * groups) / S::BM;
+    if (!grid_ok(tiles_m * p.tiles_n, S::threads)) return QESGD_ERR_DIM;
+    by_type(a.dtype, [&](auto t) { k_mx4_grouped_product<S, t.value><<<(uint32_t)(tiles_m * p.tiles_n), S::threads, 0, a.stream>>>(p); });
+    return launched();
+}
+
+template <class S>
+int launch_gradient_tiles(const GroupProduct& a, PParams& p) {
+    p.tiles_m = (p.N + S::BM - 1) / S::BM;
+    p.tiles_n = (p.K + S::BN - 1) / S::BN;
+    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n * a.E;
+    if (!grid_ok(tiles, S::threads)) return QESGD_ERR_DIM;
+    by_type(a.dtype, [&](auto t) { k_mx4_grouped_gradient<S, t.value><<<(uint32_t)tiles, S::threads, 0, a.stream>>>(p); });
+    return launched();
+}
+
+}  // namespace
+
+size_t grouped_product_workspace(const GroupProduct&) { return 0; }
+size_t grouped_gradient_workspace(const GroupProduct&) { return 0; }
+
+int launch_grouped_product(const GroupProduct& a) {
+    qesgd_mx4_layout A, B;
+    int rc = make_mx4_layout(a.R, a.K, &A);
+    if (rc == QESGD_OK) rc = make_mx4_layout(a.N, a.K, &B);
+    if (rc != QESGD_OK) return rc;
+    PParams p{};
+    p.a = a.a;
+    p.b = a.b;
+    p.a_scales = A.scales_off;
+    p.b_scales = B.scales_off;
+    p.b_stride = a.b_stride;
+    p.offsets = a.offsets;
+    p.E = a.E;
+    p.R = (uint32_t)a.R;
+    p.c = a.c;
+    p.ldc = a.ldc;
+    p.N = (uint32_t)a.N;
+    p.row_codes = (uint32_t)A.row_codes;
+    p.row_scales = (uint32_t)A.row_scales;
+    const uint64_t rows = (a.R + a.E - 1) / a.E;
+    if (rows <= 64) return launch_product_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
+    if (rows <= 512) return launch_product_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
+    return launch_product_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
+}
+
+int launch_grouped_gradient(const GroupProduct& a) {
+    qesgd_mx4_layout A, B;
+    const uint64_t columns = grouped_columns(a.R, a.E);
+    int rc = columns ? make_mx4_layout(a.N, columns, &A) : QESGD_ERR_DIM;
+    if (rc == QESGD_OK) rc = make_mx4_layout(a.K, columns, &B);
+    if (rc != QESGD_OK) return rc;
+    PParams p{};
+    p.a = a.a;
+    p.b = a.b;
+    p.a_scales = A.scales_off;
+    p.b_scales = B.scales_off;
+    p.offsets = a.offsets;
+    p.E = a.E;
+    p.R = (uint32_t)a.R;
+    p.c = a.c;
+    p.N = (uint32_t)a.N;
+    p.K = (uint32_t)a.K;
+    p.row_codes = (uint32_t)A.row_codes;
+    p.row_scales = (uint32_t)A.row_scales;
+    if (a.N * a.K <= 512 * 512) return launch_gradient_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
+    return launch_gradient_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
+}
+
+}  // namespace qesgd

@@ -1,0 +1,349 @@
+"""Rows grouped by expert on the GPU against the 64-bit reference: every byte of both packed forms, products and their gradients within
+their rounding, and what lies outside of the groups untouched."""
+import numpy as np
+import pytest
+import torch
+
+import expert_reference as X
+import matrix_reference as R
+from expert_reference import ONE, TYPES, host
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1901_03040_amd import binding
+    assert torch.cuda.is_available()
+    binding.lib()
+    return binding
+
+
+def ints(v):
+    return torch.from_numpy(np.asarray(v, np.int32)).cuda()
+
+
+def tokens(T, cols, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(T, cols, generator=g) * torch.exp2(torch.randint(-6, 3, (T, 1), generator=g).float())
+    return x.to(dtype)
+
+
+def planes(B, packed, rows, cols):
+    lay = B.qesgd_mx4_layout_query(rows, cols)
+    b = packed.cpu().numpy()
+    return b[:rows * lay.row_codes].reshape(rows, -1), b[lay.scales_off:lay.scales_off + rows * lay.row_scales].reshape(rows, -1), lay
+
+
+QUANTIZE = [(1, 1, 1, 1, 1), (1, 5, 2, 3, 2), (40, 33, 3, 5, 1), (37, 300, 2, 4, 2), (150, 129, 4, 3, 3), (64, 128, 1, 64, 1), (300, 130, 2, 1, 1),
+            (90, 257, 3, 70, 3), (20, 2050, 2, 200, 2)]
+
+
+@pytest.mark.parametrize("kind", ["ragged", "even", "one", "none"])
+@pytest.mark.parametrize("mode", ["nearest", "stochastic"])
+@pytest.mark.parametrize("T,cols,k,E,per", QUANTIZE)
+def test_quantize_every_byte(B, T, cols, k, E, per, mode, kind):
+    dtype = list(TYPES.values())[(T + cols) % 3]
+    rng = np.random.default_rng(T * cols)
+    n = T * k
+    ld = cols + 3
+    base = torch.zeros(T * ld + 9, dtype=dtype, device="cuda")
+    x = tokens(T, cols, dtype, cols)
+    torch.as_strided(base, (T, cols), (ld, 1), 1).copy_(x)
+    order = rng.permutation(n)
+    if n > 20:
+        order[::11] = -1                                        # a row without a token
+        order[7] = T * per + 5                                  # ... and one beyond them
+    offsets = X.group_sizes(rng, E, n, kind)
+    source = np.where(order < 0, T, order // per)
+    rows = np.concatenate((host(x), np.zeros((1, cols))))[np.minimum(source, T)]
+    seed, rnd, worker = 0x123456789ABCDEF, 9, 5
+    columns = B.qesgd_mx4_grouped_columns(n, E)
+    assert columns == X.group_columns(n, E)
+    m = B.MX4_STOCHASTIC if mode == "stochastic" else B.MX4_NEAREST
+    code, scale = R.quantize(rows, mode == "stochastic", seed, rnd, worker)
+    turned, begin, end = X.padded(rows, offsets, columns)
+    code_t, scale_t = R.quantize(turned, mode == "stochastic", seed, rnd, worker) if columns else (None, None)
+    for which in ("rows", "groups", "both"):
+        p = B.alloc_mx4(B.qesgd_mx4_layout_query(n, cols)).fill_(0xA5)
+        pt = B.alloc_mx4(B.qesgd_mx4_layout_query(cols, columns)).fill_(0xA5)
+        B.qesgd_mx4_quantize_groups(base[1:], ld, T, ints(order), per, ints(offsets), E, n, cols, m, seed, rnd, None if which == "groups" else p,
+                                    packed_t=None if which == "rows" else pt, worker=worker)
+        if which != "groups":
+            got, sc, lay = planes(B, p, n, cols)
+            lo, hi = offsets[0], offsets[-1]
+            assert np.array_equal(got[lo:hi], R.pack(code)[lo:hi]) and np.array_equal(sc[lo:hi], scale[lo:hi]), which
+            assert (got[hi:] == 0xA5).all() and (sc[hi:] == 0xA5).all() and (got[:lo] == 0xA5).all()
+            b = p.cpu().numpy()
+            assert (b[n * lay.row_codes:lay.scales_off] == 0xA5).all() and (b[lay.scales_off + n * lay.row_scales:] == 0xA5).all()
+        if which != "rows":
+            got, sc, lay = planes(B, pt, cols, columns)
+            assert np.array_equal(got[:, :end // 2], R.pack(code_t)[:, :end // 2]) and np.array_equal(sc[:, :end // 32], scale_t[:, :end // 32]), which
+            assert (got[:, end // 2:] == 0xA5).all() and (sc[:, end // 32:] == 0xA5).all()
+            b = pt.cpu().numpy()
+            assert (b[cols * lay.row_codes:lay.scales_off] == 0xA5).all() and (b[lay.scales_off + cols * lay.row_scales:] == 0xA5).all()
+
+
+def test_quantize_without_an_order_equals_the_matrix_call(B):
+    """One group of all rows, in their own order: the packed form of the matrix, bit for bit."""
+    n, cols = 70, 200
+    x = tokens(n, cols, torch.bfloat16, 1).cuda()
+    a, b = (B.alloc_mx4(B.qesgd_mx4_layout_query(n, cols)).fill_(0) for _ in range(2))
+    B.qesgd_mx4_quantize_groups(x, cols, n, None, 1, ints([0, n]), 1, n, cols, B.MX4_STOCHASTIC, 7, 1, a, worker=2)
+    B.qesgd_mx4_quantize_pack(x, cols, 0, n, cols, 1, B.MX4_STOCHASTIC, 7, 1, b, 0, worker=2)
+    assert torch.equal(a, b)
+
+
+def test_offsets_that_hold_anything_stay_inside_the_buffers(B):
+    """Falling, negative and far too large offsets: rows come and go, but nothing outside of the buffers is written, and no call waits for ever."""
+    n, N, K, E, T = 100, 70, 140, 5, 60
+    x = tokens(T, K, torch.float32, 1).cuda()
+    w, _ = X.packed_weights(np.random.default_rng(0).standard_normal((E, N, K)))
+    w = w.cuda()
+    order = ints(np.random.default_rng(1).integers(-3, 400, n))
+    columns = B.qesgd_mx4_grouped_columns(n, E)
+    for offsets in ([0, 100, 0, 100, 0, 100], [-5, 10, 1 << 30, 20, 400, -1], [100, 80, 60, 40, 20, 0], [2147483647] * 6, [-2147483648] * 6,
+                    [0, 2147483647, -1, 2147483647, -1, 2147483647]):
+        o = ints(offsets)
+        lay, lay_t = B.qesgd_mx4_layout_query(n, K), B.qesgd_mx4_layout_query(K, columns)
+        guarded = {"p": torch.full((lay.bytes + 512,), 0xA5, dtype=torch.uint8, device="cuda"),
+                   "t": torch.full((lay_t.bytes + 512,), 0xA5, dtype=torch.uint8, device="cuda"),
+                   "c": torch.full((n * N + 512,), 7.0, device="cuda"), "d": torch.full((E * N * K + 512,), 7.0, device="cuda"),
+                   "y": torch.full((n * N + 512,), 7.0, device="cuda")}
+        p, t, c, d, y = (guarded[i][256:-256] for i in "ptcdy")
+        B.qesgd_mx4_quantize_groups(x, K, T, order, 3, o, E, n, K, B.MX4_STOCHASTIC, 1, 1, p, packed_t=t)
+        B.qesgd_mx4_quantize_groups(x, K, T, order, 3, o, E, n, K, B.MX4_NEAREST, 1, 1, p)
+        B.qesgd_mx4_grouped_product(p, w, w.stride(0), o, E, n, N, K, c, N, workspace=B.alloc_workspace(B.qesgd_mx4_grouped_product_workspace_bytes(n, N, K, E)))
+        g = B.alloc_mx4(B.qesgd_mx4_layout_query(N, columns)).fill_(0)
+        B.qesgd_mx4_grouped_gradient(g, t, o, E, n, N, K, d, workspace=B.alloc_workspace(B.qesgd_mx4_grouped_gradient_workspace_bytes(n, N, K, E)))
+        B.qesgd_mx4_vector_product(x, K, T, order, 3, w, w.stride(0), o, E, n, N, K, y, N,
+                                   workspace=B.alloc_workspace(B.qesgd_mx4_vector_product_workspace_bytes(n, N, K, E)))
+        torch.cuda.synchronize()
+        for name, v in guarded.items():
+            assert (v[:256] == v[0]).all() and (v[-256:] == v[0]).all() and float(v[0]) in (7.0, 165.0), (offsets, name)
+
+
+def packed_noise(B, rows, cols, n, seed, spread=3):
+    """Any bytes with zeros behind the last column are packed matrices: [n, bytes] and their values [n, rows, cols]."""
+    lay = B.qesgd_mx4_layout_query(rows, cols)
+    g = torch.Generator().manual_seed(seed)
+    p = torch.randint(0, 256, (n, lay.bytes), generator=g, dtype=torch.uint8)
+    p[:, lay.scales_off:] = torch.randint(127 - spread, 127 + spread, (n, lay.bytes - lay.scales_off), generator=g, dtype=torch.uint8)
+    b = p.numpy()
+    codes = b[:, :rows * lay.row_codes].reshape(n, rows, -1)
+    codes[:, :, (cols + 1) // 2:] = 0
+    if cols % 2:
+        codes[:, :, cols // 2] &= 15
+    scales = b[:, lay.scales_off:lay.scales_off + rows * lay.row_scales].reshape(n, rows, -1)
+    code = np.stack((codes & 15, codes >> 4), 4 - 1).reshape(n, rows, -1)
+    return p, np.stack([R.values(code[i], scales[i], cols) for i in range(n)])
+
+
+PRODUCTS = [(1, 1, 1, 1), (1, 16, 32, 3), (2, 33, 129, 2), (20, 130, 384, 4), (37, 1000, 300, 5), (64, 64, 2049, 8), (100, 65, 640, 1), (130, 40, 1000, 40),
+            (300, 257, 511, 3), (700, 140, 200, 2), (1300, 300, 256, 1), (1400, 70, 4100, 2), (96, 48, 128, 100), (2100, 520, 130, 3)]
+
+
+def product_limit(a, b, want, dtype):
+    """A sum of n exact products in fp32 in any order is off by at most n 2^-24 of the sum of magnitudes; then one rounding."""
+    return a.shape[1] * ONE * (np.abs(a) @ np.abs(b).T) + X.rounded(want, dtype)
+
+
+@pytest.mark.parametrize("kind", ["ragged", "even", "one", "none"])
+@pytest.mark.parametrize("n,N,K,E", PRODUCTS)
+def test_product(B, n, N, K, E, kind):
+    dtype = list(TYPES.values())[(n + N + K) % 3]
+    offsets = X.group_sizes(np.random.default_rng(n + K), E, n, kind)
+    pa, a = packed_noise(B, n, K, 1, n + K)
+    pb, b = packed_noise(B, N, K, E, N + 2 * K)
+    slab = torch.zeros(E, pb.shape[1] + 512, dtype=torch.uint8)
+    slab[:, :pb.shape[1]] = pb
+    slab = slab.cuda()
+    ldc = N + 5
+    ws = B.alloc_workspace(B.qesgd_mx4_grouped_product_workspace_bytes(n, N, K, E))
+    out = []
+    for _ in range(2):
+        c = torch.full((n, ldc), 3.0, dtype=dtype, device="cuda")
+        B.qesgd_mx4_grouped_product(pa[0].cuda(), slab, slab.stride(0), ints(offsets), E, n, N, K, c, ldc, workspace=ws)
+        out.append(c)
+    assert torch.equal(*out)                                    # no order of additions that comes and goes
+    got = host(out[0])
+    assert (got[:, N:] == 3.0).all() and (got[offsets[-1]:] == 3.0).all() and (got[:offsets[0]] == 3.0).all()
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        want = a[0][lo:hi] @ b[e].T
+        off = np.abs(got[lo:hi, :N] - want) - product_limit(a[0][lo:hi], b[e], want, dtype)
+        assert (off <= 0).all(), (e, np.argwhere(off > 0)[:4])
+
+
+GRADIENTS = [(1, 1, 1, 1), (2, 33, 129, 2), (40, 130, 384, 4), (128, 64, 64, 1), (129, 100, 65, 2), (500, 65, 40, 3), (700, 300, 257, 5), (1500, 64, 520, 3),
+             (300, 48, 96, 64), (90, 600, 700, 2)]
+
+
+@pytest.mark.parametrize("kind", ["ragged", "even", "one", "none"])
+@pytest.mark.parametrize("n,N,K,E", GRADIENTS)
+def test_gradient(B, n, N, K, E, kind):
+    dtype = list(TYPES.values())[(n + N + K) % 3]
+    offsets = X.group_sizes(np.random.default_rng(n + K), E, n, kind)
+    columns = X.group_columns(n, E)
+    pa, a = packed_noise(B, N, columns, 1, n + K)
+    pb, b = packed_noise(B, K, columns, 1, N + 2 * K)
+    a, b = a[0], b[0]
+    ws = B.alloc_workspace(B.qesgd_mx4_grouped_gradient_workspace_bytes(n, N, K, E))
+    out = []
+    for _ in range(2):
+        d = torch.full((E * N * K + 64,), 3.0, dtype=dtype, device="cuda")
+        B.qesgd_mx4_grouped_gradient(pa[0].cuda(), pb[0].cuda(), ints(offsets), E, n, N, K, d, workspace=ws)
+        out.append(d)
+    assert torch.equal(*out) and (out[0][E * N * K:] == 3.0).all()
+    got, at = host(out[0])[:E * N * K].reshape(E, N, K), 0
+    for e in range(E):
+        wide = R.up(offsets[e + 1] - offsets[e], 128)           # whatever the group's padding holds counts: the quantiser leaves zeros
+        x, y = a[:, at:at + wide], b[:, at:at + wide]
+        want = x @ y.T
+        off = np.abs(got[e] - want) - product_limit(x, y, want, dtype)
+        assert (off <= 0).all(), (e, np.argwhere(off > 0)[:4])
+        at += wide
+
+
+def test_nan_stays_in_its_row_and_group(B):
+    n, N, K, E = 40, 50, 300, 3
+    offsets = [0, 13, 13, 40]
+    x = tokens(n, K, torch.float32, 1)
+    x[5, 250] = float("nan")
+    w = torch.randn(E, N, K, generator=torch.Generator().manual_seed(2)).double().numpy()
+    w[2, 7, 17] = np.inf
+    wp, _ = X.packed_weights(w)
+    p = B.alloc_mx4(B.qesgd_mx4_layout_query(n, K))
+    B.qesgd_mx4_quantize_groups(x.cuda(), K, n, None, 1, ints(offsets), E, n, K, B.MX4_NEAREST, 0, 0, p)
+    c = torch.empty(n, N, device="cuda")
+    B.qesgd_mx4_grouped_product(p, wp.cuda(), wp.stride(0), ints(offsets), E, n, N, K, c, N,
+                                workspace=B.alloc_workspace(B.qesgd_mx4_grouped_product_workspace_bytes(n, N, K, E)))
+    want = torch.zeros(n, N, dtype=torch.bool)
+    want[5] = True
+    want[13:, 7] = True
+    assert torch.equal(torch.isnan(c).cpu(), want)
+
+
+@pytest.mark.parametrize("mode", ["nearest", "stochastic"])
+def test_a_layers_gradients(B, mode):
+    """y, dx and dw from the tokens and the rows' gradients, each against 64 bits with the codes that the formats say."""
+    T, k, E, N, K, seed = 90, 2, 4, 70, 200, 77
+    n = T * k
+    rng = np.random.default_rng(4)
+    offsets = X.group_sizes(rng, E, n, "ragged")
+    order = rng.permutation(n)
+    x, dr = tokens(T, K, torch.float32, 1), tokens(n, N, torch.float32, 2)
+    w = rng.standard_normal((E, N, K))
+    (wp, wv), (wtp, wtv) = X.packed_weights(w), X.packed_weights(w.transpose(0, 2, 1).copy())
+    o, st = ints(offsets), mode == "stochastic"
+    columns = X.group_columns(n, E)
+    px, pd = B.alloc_mx4(B.qesgd_mx4_layout_query(n, K)), B.alloc_mx4(B.qesgd_mx4_layout_query(n, N))
+    pxt, pdt = B.alloc_mx4(B.qesgd_mx4_layout_query(K, columns)), B.alloc_mx4(B.qesgd_mx4_layout_query(N, columns))
+    B.qesgd_mx4_quantize_groups(x.cuda(), K, T, ints(order), k, o, E, n, K, B.MX4_NEAREST, 0, 0, px, packed_t=pxt)
+    B.qesgd_mx4_quantize_groups(dr.cuda(), N, n, None, 1, o, E, n, N, B.MX4_STOCHASTIC if st else B.MX4_NEAREST, seed, 3, pd, packed_t=pdt)
+    y, dx, dw = torch.zeros(n, N, device="cuda"), torch.zeros(n, K, device="cuda"), torch.empty(E, N, K, device="cuda")
+    B.qesgd_mx4_grouped_product(px, wp.cuda(), wp.stride(0), o, E, n, N, K, y, N)
+    B.qesgd_mx4_grouped_product(pd, wtp.cuda(), wtp.stride(0), o, E, n, K, N, dx, K)
+    B.qesgd_mx4_grouped_gradient(pdt, pxt, o, E, n, N, K, dw)
+    rows, d = host(x)[order // k], host(dr)
+    a, b = X.q(rows), X.q(d, st, seed, 3)
+    turned, begin, _ = X.padded(rows, offsets, columns)
+    turned_d, _, _ = X.padded(d, offsets, columns)
+    at, bt = X.q(turned), X.q(turned_d, st, seed, 3)
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        for got, u, v in ((host(y)[lo:hi], a[lo:hi], wv[e]), (host(dx)[lo:hi], b[lo:hi], wtv[e]),
+                          (host(dw)[e], bt[:, begin[e]:begin[e] + hi - lo], at[:, begin[e]:begin[e] + hi - lo])):
+            want = u @ v.T
+            assert (np.abs(got - want) <= (u.shape[1] + 1) * ONE * (np.abs(u) @ np.abs(v).T) + ONE * np.abs(want)).all()
+
+
+def test_gradients_are_those_of_the_product(B):
+    """Operands that 4 bits hold exactly along either side: the gradients are the product's, checked against differences, which are exact
+    for a function that is linear in either operand."""
+    E, n, N, K = 3, 160, 64, 96
+    g = torch.Generator().manual_seed(6)
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+    def exact(r, c):
+        x = grid[torch.randint(0, 8, (r, c), generator=g)] * (torch.randint(0, 2, (r, c), generator=g) * 2.0 - 1)
+        x[:, ::16] = 6.0
+        x[::8, :] = 4.0
+        return x
+
+    offsets = [0, 64, 96, 160]
+    x, dy, w = exact(n, K), exact(n, N), torch.stack([exact(N, K) for _ in range(E)])
+    o, columns = ints(offsets), X.group_columns(n, E)
+    px, pd = B.alloc_mx4(B.qesgd_mx4_layout_query(n, K)), B.alloc_mx4(B.qesgd_mx4_layout_query(n, N))
+    pxt, pdt = B.alloc_mx4(B.qesgd_mx4_layout_query(K, columns)), B.alloc_mx4(B.qesgd_mx4_layout_query(N, columns))
+    wt, _ = X.packed_weights(w.transpose(1, 2).double().numpy())
+    B.qesgd_mx4_quantize_groups(x.cuda(), K, n, None, 1, o, E, n, K, B.MX4_NEAREST, 0, 0, px, packed_t=pxt)
+    B.qesgd_mx4_quantize_groups(dy.cuda(), N, n, None, 1, o, E, n, N, B.MX4_NEAREST, 0, 0, pd, packed_t=pdt)
+    dx, dw = torch.empty(n, K, device="cuda"), torch.empty(E, N, K, device="cuda")
+    B.qesgd_mx4_grouped_product(pd, wt.cuda(), wt.stride(0), o, E, n, K, N, dx, K)
+    B.qesgd_mx4_grouped_gradient(pdt, pxt, o, E, n, N, K, dw)
+
+    def loss(a, b):
+        return sum(float(((a[lo:hi].double() @ b[e].double().T) * dy[lo:hi].double()).sum()) for e, (lo, hi) in enumerate(zip(offsets[:-1], offsets[1:])))
+
+    base = loss(x, w)
+    for r, c in ((0, 0), (63, 5), (64, 95), (95, 1), (159, 40)):
+        step = x.clone()
+        step[r, c] += 1.0
+        assert abs(loss(step, w) - base - float(dx[r, c])) <= 1e-9
+    for e, r, c in ((0, 0, 0), (1, 63, 95), (2, 30, 17)):
+        step = w.clone()
+        step[e, r, c] += 1.0
+        assert abs(loss(x, step) - base - float(dw[e, r, c])) <= 1e-9
+
+
+def test_side_stream_and_graphs(B):
+    T, k, E, N, K = 100, 2, 6, 200, 500
+    n = T * k
+    rng = np.random.default_rng(3)
+    offsets, order = ints(X.group_sizes(rng, E, n, "ragged")), ints(rng.permutation(n))
+    x, d = tokens(T, K, torch.bfloat16, 1).cuda(), tokens(n, N, torch.bfloat16, 2).cuda()
+    w = X.packed_weights(rng.standard_normal((E, N, K)))[0].cuda()
+    columns = X.group_columns(n, E)
+    px, pd = B.alloc_mx4(B.qesgd_mx4_layout_query(n, K)), B.alloc_mx4(B.qesgd_mx4_layout_query(n, N))
+    pxt, pdt = B.alloc_mx4(B.qesgd_mx4_layout_query(K, columns)), B.alloc_mx4(B.qesgd_mx4_layout_query(N, columns))
+    y, dw = torch.zeros(n, N, dtype=torch.bfloat16, device="cuda"), torch.zeros(E, N, K, device="cuda")
+    ws = B.alloc_workspace(max(256, B.qesgd_mx4_grouped_product_workspace_bytes(n, N, K, E), B.qesgd_mx4_grouped_gradient_workspace_bytes(n, N, K, E)))
+
+    def work():
+        B.qesgd_mx4_quantize_groups(x, K, T, order, k, offsets, E, n, K, B.MX4_NEAREST, 0, 0, px, packed_t=pxt)
+        B.qesgd_mx4_quantize_groups(d, N, n, None, 1, offsets, E, n, N, B.MX4_STOCHASTIC, 5, 6, pd, packed_t=pdt)
+        B.qesgd_mx4_grouped_product(px, w, w.stride(0), offsets, E, n, N, K, y, N, workspace=ws)
+        B.qesgd_mx4_grouped_gradient(pdt, pxt, offsets, E, n, N, K, dw, workspace=ws)
+
+    work()
+    torch.cuda.synchronize()
+    want = y.clone(), dw.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y.zero_(), dw.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        work()
+    side.synchronize()
+    assert torch.equal(y, want[0]) and torch.equal(dw, want[1])
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for graph in graphs:
+        with torch.cuda.graph(graph):
+            work()
+    for i in range(4):
+        for t in (y, dw, px, pxt, pd, pdt):
+            t.zero_()
+        graphs[i & 1].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(dw, want[1]), i
+        assert np.isfinite(torch.randn(1 << 16, device="cuda").sum().item())
+    # the sizes are the device's: the same graph with other groups
+    offsets.copy_(ints(X.group_sizes(rng, E, n, "even")))
+    work()
+    torch.cuda.synchronize()
+    want = y.clone(), dw.clone()
+    y.zero_(), dw.zero_()
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want[0]) and torch.equal(dw, want[1])
