@@ -160,6 +160,16 @@ class QesgdMatrixLoop:
         y = self._product(px, self.packed_u, x.shape[0], self.out, self.inn, x.dtype)
         return y, (pxt, x.shape[0], self.sent) if gradients else None
 
+    def next_tokens(self, x: torch.Tensor) -> torch.Tensor:
+        """The layer on a few rows x [tokens, in] as they are, not quantised: y = x Q(u)^T in x's type."""
+        assert x.dim() == 2 and x.shape[1] == self.inn
+        x = _rows(x)
+        T = x.shape[0]
+        y = torch.empty((T, self.out), dtype=x.dtype, device=self.dev)
+        ws = B.alloc_workspace(B.qesgd_mx4_vector_product_workspace_bytes(T, self.out, self.inn, 1), self.dev)
+        B.qesgd_mx4_vector_product(x, x.stride(0), T, None, 1, self.packed_u, 0, None, 1, T, self.out, self.inn, y, self.out, workspace=ws)
+        return y
+
     def backward(self, dy: torch.Tensor, saved, worker: int = 0):
         """Gradients with respect to x (dy's type) and to the parameters (fp32): dy [tokens, out] is rounded without bias.  Each of a
         round's calls takes a worker number of its own, so that their roundings do not depend on one another, nor on those of
@@ -190,3 +200,135 @@ class QesgdMatrixLoop:
         assert self.steps_in_epoch > 0
         B.qesgd_epoch_commit(self.w, self.zsum, self.steps_in_epoch, self.w.numel())
         return self.w
+
+
+def _rows(x: torch.Tensor) -> torch.Tensor:
+    """x [rows, cols] with its columns one after the other, copied only where they are not."""
+    return x if x.stride(1) == 1 and x.stride(0) >= x.shape[1] else x.contiguous()
+
+
+class QesgdExpertLoop(QesgdMatrixLoop):
+    """The epoch loop of a layer of experts: E matrix parameters [out, in], each token multiplied with the k that its logits choose.  The
+    workers run it on the 4-bit form of the parameters, the router and the rows' way to their experts and back included; the rounds are
+    those of a matrix parameter for all experts at once, each orthogonalised by itself."""
+
+    def __init__(self, w0: torch.Tensor, K: int, seed: int, *, choices: int = 2, gate_kind: int = B.GATE_CHOSEN, mu: float = 0.95,
+                 nesterov: bool = True, coeffs=QUINTIC, eps: float = 1e-7):
+        """w0: fp32 CUDA tensor [E, out, in] (copied).  K workers.  choices: experts of a token.  gate_kind: softmax over the chosen
+        experts' logits or over all of them."""
+        assert w0.is_cuda and w0.dtype == torch.float32 and w0.dim() == 3
+        self.E, self.out, self.inn = w0.shape
+        self.K, self.seed, self.mu, self.nesterov, self.coeffs, self.eps = K, seed, mu, nesterov, coeffs, eps
+        self.choices, self.gate_kind = choices, gate_kind
+        self.dev = w0.device
+        self.w = w0.contiguous().clone()
+        self.z, self.zsum, self.mean, self.momentum = (torch.zeros_like(self.w) for _ in range(4))
+        self.u = self.w.clone()
+        self.round_id = 0
+        self.steps_in_epoch = 0
+        self.sent = 0
+        self.packed_u = B.alloc_mx4(B.qesgd_mx4_layout_query(self.out, self.inn), self.E, device=self.dev)
+        self.packed_ut = B.alloc_mx4(B.qesgd_mx4_layout_query(self.inn, self.out), self.E, device=self.dev)
+        # a worker's gradients of all experts go out as one matrix [E * out, in]
+        self.packed = B.alloc_mx4(B.qesgd_mx4_layout_query(self.E * self.out, self.inn), K, device=self.dev)
+        self.ws = B.alloc_workspace(B.qesgd_orthogonalize_workspace_bytes(self.out, self.inn, self.E), self.dev)
+        self.begin_epoch()
+
+    def _send(self):
+        for e in range(0, self.E, 64):                          # a call takes 64 matrices
+            n = min(64, self.E - e)
+            p, pt = self.packed_u[e:], self.packed_ut[e:]
+            B.qesgd_mx4_quantize_pack(self.u[e:], self.inn, self.out * self.inn, self.out, self.inn, n, B.MX4_NEAREST, self.seed, self.round_id,
+                                      p, p.stride(0), packed_t=pt, packed_t_stride=pt.stride(0))
+        self.sent += 1
+
+    def route(self, logits: torch.Tensor):
+        """experts [T, k], gates [T, k], offsets [E + 1], order [T k] and slots [T k] for logits [T, E]; a logit of -inf closes an expert to a token."""
+        assert logits.dim() == 2 and logits.shape[1] == self.E
+        logits, k = _rows(logits), self.choices
+        T = logits.shape[0]
+        experts, order, slots = (torch.empty(n, dtype=torch.int32, device=self.dev) for n in ((T, k), T * k, T * k))
+        gates, offsets = torch.empty((T, k), device=self.dev), torch.empty(self.E + 1, dtype=torch.int32, device=self.dev)
+        B.qesgd_route(logits, logits.stride(0), T, self.E, k, self.gate_kind, experts, gates, offsets, order, slots,
+                      workspace=B.alloc_workspace(B.qesgd_route_workspace_bytes(T, self.E, k), self.dev))
+        return experts, gates, offsets, order, slots
+
+    def _pack_groups(self, x, T, order, per, offsets, R, mode, worker=0, columns=True):
+        cols = x.shape[1]
+        forms = (B.alloc_mx4(B.qesgd_mx4_layout_query(R, cols), device=self.dev),
+                 B.alloc_mx4(B.qesgd_mx4_layout_query(cols, B.qesgd_mx4_grouped_columns(R, self.E)), device=self.dev) if columns else None)
+        B.qesgd_mx4_quantize_groups(x, x.stride(0), T, order, per, offsets, self.E, R, cols, mode, self.seed, self.round_id, forms[0],
+                                    packed_t=forms[1], worker=worker)
+        return forms
+
+    def _grouped(self, a, slab, offsets, R, N, K, dtype):
+        c = torch.empty((R, N), dtype=dtype, device=self.dev)
+        B.qesgd_mx4_grouped_product(a, slab, slab.stride(0), offsets, self.E, R, N, K, c, N,
+                                    workspace=B.alloc_workspace(B.qesgd_mx4_grouped_product_workspace_bytes(R, N, K, self.E), self.dev))
+        return c
+
+    def _combine(self, rows, slots, gates, T, R):
+        N = rows.shape[1]
+        out = torch.empty((T, N), dtype=rows.dtype, device=self.dev)
+        B.qesgd_combine(rows, N, R, slots, gates, T, self.choices, N, out, N)
+        return out
+
+    def forward(self, x: torch.Tensor, logits: torch.Tensor, gradients: bool = True):
+        """A worker's layer: y[t] = sum_j gates[t, j] Q(x[t]) Q(u[experts[t, j]])^T for x [tokens, in] and the router's logits [tokens, E].
+        Returns y in x's type and what backward needs."""
+        assert x.dim() == 2 and x.shape[1] == self.inn and x.shape[0] == logits.shape[0]
+        x, logits = _rows(x), _rows(logits)
+        T, k = x.shape[0], self.choices
+        R = T * k
+        experts, gates, offsets, order, slots = self.route(logits)
+        px, pxt = self._pack_groups(x, T, order, k, offsets, R, B.MX4_NEAREST, columns=gradients)
+        rows = self._grouped(px, self.packed_u, offsets, R, self.out, self.inn, x.dtype)
+        y = self._combine(rows, slots, gates, T, R)
+        return y, (pxt, rows, logits, experts, gates, offsets, slots, T, self.sent) if gradients else None
+
+    def next_tokens(self, x: torch.Tensor, logits: torch.Tensor) -> torch.Tensor:
+        """The layer on a few tokens' rows as they are, not quantised."""
+        assert x.dim() == 2 and x.shape[1] == self.inn and x.shape[0] == logits.shape[0]
+        x = _rows(x)
+        T, k = x.shape[0], self.choices
+        R = T * k
+        _, gates, offsets, order, slots = self.route(logits)
+        rows = torch.empty((R, self.out), dtype=x.dtype, device=self.dev)
+        ws = B.alloc_workspace(B.qesgd_mx4_vector_product_workspace_bytes(R, self.out, self.inn, self.E), self.dev)
+        B.qesgd_mx4_vector_product(x, x.stride(0), T, order, k, self.packed_u, self.packed_u.stride(0), offsets, self.E, R, self.out, self.inn,
+                                   rows, self.out, workspace=ws)
+        return self._combine(rows, slots, gates, T, R)
+
+    def backward(self, dy: torch.Tensor, saved, worker: int = 0):
+        """Gradients with respect to x (dy's type), to the logits (their type) and to the parameters (fp32 [E, out, in]): the rows' gradients are
+        rounded without bias, with the worker numbers of QesgdMatrixLoop."""
+        pxt, rows, logits, experts, gates, offsets, slots, T, sent = saved
+        assert dy.shape == (T, self.out) and dy.dtype == rows.dtype
+        assert sent == self.sent, "the parameters of this forward pass are gone: the server has sent others since"
+        dy, k = _rows(dy), self.choices
+        R = T * k
+        drows, dgates = torch.empty_like(rows), torch.empty_like(gates)
+        B.qesgd_combine_backward(dy, dy.stride(0), rows, self.out, R, slots, gates, T, k, self.out, drows, self.out, dgates)
+        pd, pdt = self._pack_groups(drows, R, None, 1, offsets, R, B.MX4_STOCHASTIC, self.K + worker)
+        dx = self._combine(self._grouped(pd, self.packed_ut, offsets, R, self.inn, self.out, dy.dtype), slots, None, T, R)
+        dw = torch.empty((self.E, self.out, self.inn), device=self.dev)
+        B.qesgd_mx4_grouped_gradient(pdt, pxt, offsets, self.E, R, self.out, self.inn, dw,
+                                     workspace=B.alloc_workspace(B.qesgd_mx4_grouped_gradient_workspace_bytes(R, self.out, self.inn, self.E), self.dev))
+        dlogits = torch.empty((T, self.E), dtype=logits.dtype, device=self.dev)
+        B.qesgd_route_backward(logits, logits.stride(0), T, self.E, k, self.gate_kind, experts, gates, dgates, dlogits, self.E)
+        return dx, dlogits, dw
+
+    def orthogonal_round(self, grad_slab: torch.Tensor, step_size: float, last: bool = False) -> torch.Tensor:
+        """Row k of grad_slab [K, E, out, in] is worker k's gradient.  Each expert's step is orthogonalised by itself; one of which no token
+        came has a step only from its momentum.  Returns u."""
+        assert grad_slab.shape == (self.K, self.E, self.out, self.inn) and grad_slab[0].is_contiguous()
+        rows = self.E * self.out
+        B.qesgd_mx4_quantize_pack(grad_slab, self.inn, grad_slab.stride(0), rows, self.inn, self.K, B.MX4_STOCHASTIC, self.seed, self.round_id,
+                                  self.packed, self.packed.stride(0))
+        B.qesgd_mx4_unpack_aggregate_update(self.packed, self.packed.stride(0), self.K, rows, self.inn, None, self.mean, None, None)
+        B.qesgd_orthogonal_update(self.mean, self.out, self.inn, self.E, self.momentum, self.mu, self.nesterov, self.coeffs, self.eps,
+                                  -step_size, None, self.z, self.w, self.u, None if last else self.zsum, self.ws)
+        self.round_id += 1
+        self.steps_in_epoch += 1
+        self._send()
+        return self.u
