@@ -341,7 +341,7 @@ enum { QESGD_GATE_ALL = 0, QESGD_GATE_CHOSEN = 1 };
 
 /* Each token's k largest logits, ties to the lower expert, in falling order; logits [T, E] in dtype, T * k <= 2^28, T * E <= 2^36.
  *   A logit of -infinity closes that expert to that token: it is never chosen, and where fewer than k are open the choices
- *   behind them are -1, with gate 0 (a padded token has none at all).  A NaN counts as the largest; with a NaN or +infinity among a token's logits its gates are NaN.
+ *   behind them are -1, with gate 0 (a padded token has none at all).  A NaN counts as +infinity; with either of them among a token's logits its gates are NaN.
  *   gate_kind  QESGD_GATE_ALL: the chosen ones' shares of the softmax over all E logits; QESGD_GATE_CHOSEN: softmax over the chosen.
  *   experts [T, k] int32, gates [T, k] fp32
  *   offsets [E + 1]; order [T*k]: the pairs t*k + j sorted by expert, those of one expert in rising order; slots [T*k]: the place of each

@@ -24,7 +24,8 @@ struct RParams {
     int32_t* order;
     int32_t* slots;
     uint32_t* counts;                 // [blocks, E]
-    uint32_t block_tokens, blocks;
+    uint32_t* totals;                 // [E], behind them
+    uint32_t blocks;
     uint32_t bits;                    // of E: those that an expert's number can have, and of -1 as E
 };
 
@@ -41,14 +42,8 @@ __device__ __forceinline__ void put_element(void* x, uint64_t at, float v) {
     else ((__bf16*)x)[at] = (__bf16)v;
 }
 
-// Order of logits as integers: 0 for a closed expert, a NaN above all, the two zeros alike.
-__device__ __forceinline__ uint32_t rank_of(float v) {
-    const uint32_t b = __float_as_uint(v + 0.0f);
-    if (v != v) return 0xFFFFFFFFu;
-    if (b == 0xFF800000u) return 0u;
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float logit_of(uint32_t rank) { return __uint_as_float(rank & 0x80000000u ? rank ^ 0x80000000u : ~rank); }
+// A logit as the choice compares it: a NaN as infinity.
+__device__ __forceinline__ float compared(float v) { return v != v ? INFINITY : v; }
 
 // Over L lanes (8 .. 64): each step combines halves that hold the same number, so mirrors do for the middle ones.
 template <int L, class F>
@@ -61,8 +56,11 @@ __device__ __forceinline__ uint32_t over_lanes(uint32_t v, F f) {
     if (L >= 64) { const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false); v = f(r[0], r[1]); }
     return v;
 }
+__device__ __forceinline__ float larger(float a, float b) { return a > b ? a : b; }            // of numbers that are none of them NaN
 template <int L>
-__device__ __forceinline__ uint32_t most(uint32_t v) { return over_lanes<L>(v, [](uint32_t a, uint32_t b) { return max(a, b); }); }
+__device__ __forceinline__ float most(float v) {
+    return __uint_as_float(over_lanes<L>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(larger(__uint_as_float(a), __uint_as_float(b))); }));
+}
 template <int L>
 __device__ __forceinline__ uint32_t least(uint32_t v) { return over_lanes<L>(v, [](uint32_t a, uint32_t b) { return min(a, b); }); }
 template <int L>
@@ -70,46 +68,65 @@ __device__ __forceinline__ float total(float v) {
     return __uint_as_float(over_lanes<L>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 
+// exp(x) for x <= 0 (a NaN: NaN), 0 below 2^-126.  By x log2(e), whose rounding moves the result by |x| 2^-24 of itself: for the terms of a sum, where
+// those that count have a small |x|.
+__device__ __forceinline__ float exp_of_sum(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+// The same with the product's rest: right to two steps whatever x.
+__device__ __forceinline__ float exp_below(float x) {
+    const float high = x * 1.44269504f;
+    const float rest = __builtin_fmaf(x, 1.925963033e-8f, __builtin_fmaf(x, 1.44269504f, -high));
+    const float r = __builtin_amdgcn_exp2f(high);
+    return x < -104.0f ? 0.0f : __builtin_fmaf(r, rest * 0.693147181f, r);       // also -infinity, which has no rest
+}
+
 // One token in L lanes, C logits each: expert c * L + l.  Lane j of them (j < k) ends with choice j in `expert` (-1: none) and `gate`.
 template <uint32_t DT, int L, int C>
 __device__ __forceinline__ void choose(const RParams& p, uint64_t t, uint32_t l, int32_t& expert, float& gate) {
-    uint32_t rank[C];
+    float v[C];
+    float best = -INFINITY;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const uint32_t e = (uint32_t)c * L + l;
-        rank[c] = e < p.E ? rank_of(element<DT>(p.logits, t * p.ld + e)) : 0u;
+        v[c] = e < p.E ? element<DT>(p.logits, t * p.ld + e) : -INFINITY;
     }
-    uint32_t all_rank[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) all_rank[c] = rank[c];
-    uint32_t top = 0, mine = 0, mine_e = 0xFFFFFFFFu;
-    for (uint32_t j = 0; j < p.k; ++j) {
-        uint32_t best = rank[0], at = l;
-#pragma unroll
-        for (int c = 1; c < C; ++c)
-            if (rank[c] > best) { best = rank[c]; at = (uint32_t)c * L + l; }
-        const uint32_t high = most<L>(best);
-        const uint32_t e = least<L>(best == high ? at : 0xFFFFFFFFu);
-        if (j == 0) top = high;
-        if (l == j) { mine = high; mine_e = high ? e : 0xFFFFFFFFu; }
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-            if ((uint32_t)c * L + l == e) rank[c] = 0u;
+    for (int c = 0; c < C; ++c) {
+        v[c] = compared(v[c]);
+        best = larger(v[c], best);
     }
-    const float base = logit_of(top);
-    const float part = mine ? expf(logit_of(mine) - base) : 0.0f;
-    float sum = part;
+    float high = most<L>(best);
+    const float base = high;                                   // of infinity: every gate is NaN, as infinity - infinity is
+    float sum = 0.0f;
     if (p.all) {
-        sum = 0.0f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) sum += all_rank[c] ? expf(logit_of(all_rank[c]) - base) : 0.0f;
+        for (int c = 0; c < C; ++c) sum += exp_of_sum(v[c] - base);
     }
-    sum = total<L>(sum);
+    float mine = -INFINITY;
+    uint32_t mine_e = 0xFFFFFFFFu;
+    for (uint32_t j = 0;;) {
+        // the lowest expert among the largest
+        uint32_t at = 0xFFFFFFFFu;
+#pragma unroll
+        for (int c = C - 1; c >= 0; --c) at = v[c] == high ? (uint32_t)c * L + l : at;
+        const uint32_t e = least<L>(at);
+        if (l == j && high > -INFINITY) { mine = high; mine_e = e; }
+        if (++j >= p.k) break;
+        best = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            v[c] = (uint32_t)c * L + l == e ? -INFINITY : v[c];
+            best = larger(v[c], best);
+        }
+        high = most<L>(best);
+    }
+    const bool open = mine > -INFINITY;
+    const float part = open ? exp_below(mine - base) : 0.0f;
+    sum = total<L>(p.all ? sum : part);
     expert = (int32_t)mine_e;
-    gate = mine ? part / sum : 0.0f;
+    gate = open ? part / sum : 0.0f;
 }
 
-constexpr uint32_t kChooseWaves = 4;
+constexpr uint32_t kChooseWaves = 4, kBlockTokens = 64;
 
 // The choices of a block of tokens and how many pairs each expert has there.
 template <uint32_t DT, int L, int C>
@@ -118,7 +135,7 @@ __global__ void __launch_bounds__(kChooseWaves * 64) k_route_choose(const RParam
     for (uint32_t e = threadIdx.x; e < p.E; e += kChooseWaves * 64u) count[e] = 0u;
     __syncthreads();
     const uint32_t l = threadIdx.x & (L - 1u), part = threadIdx.x / L;
-    const uint32_t first = blockIdx.x * p.block_tokens, n = min(p.block_tokens, p.T - first);
+    const uint32_t first = blockIdx.x * kBlockTokens, n = min(kBlockTokens, p.T - first);
     // every part of a wave makes as many turns: the exchanges between lanes are the whole wave's
     for (uint32_t i = part; i < ((n + 64u / L - 1u) & ~(64u / L - 1u)); i += kChooseWaves * 64u / L) {
         const uint64_t t = first + min(i, n - 1u);
@@ -135,7 +152,43 @@ __global__ void __launch_bounds__(kChooseWaves * 64) k_route_choose(const RParam
     for (uint32_t e = threadIdx.x; e < p.E; e += kChooseWaves * 64u) p.counts[(uint64_t)blockIdx.x * p.E + e] = count[e];
 }
 
-constexpr uint32_t kPlaceWaves = 4;
+// Many blocks: counts[block, e] becomes the pairs of e in the blocks before, totals[e] those of all.  A workgroup has four experts, a thread a stretch
+// of blocks of one of them.
+constexpr uint32_t kScanExperts = 4, kScanParts = 256;
+__global__ void __launch_bounds__(kScanExperts * kScanParts) k_route_scan(const RParams p) {
+    __shared__ uint32_t sums[kScanExperts * kScanParts / 64][kScanExperts];
+    const uint32_t col = threadIdx.x % kScanExperts, part = threadIdx.x / kScanExperts;
+    const uint32_t e = blockIdx.x * kScanExperts + col;
+    const uint32_t length = (p.blocks + kScanParts - 1u) / kScanParts, from = part * length, to = min(from + length, p.blocks);
+    uint32_t sum = 0;
+    if (e < p.E)
+#pragma unroll 8
+        for (uint32_t b = from; b < to; ++b) sum += p.counts[(uint64_t)b * p.E + e];
+    // over the parts: a wave has 16 of each expert, 4 lanes apart
+    uint32_t behind = sum;
+#pragma unroll
+    for (uint32_t d = kScanExperts; d < 64u; d *= 2) {
+        const uint32_t v = __shfl_up(behind, d);
+        if ((threadIdx.x & 63u) >= d) behind += v;
+    }
+    const uint32_t wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63u) >= 64u - kScanExperts) sums[wave][col] = behind;
+    __syncthreads();
+    uint32_t before = behind - sum;
+    for (uint32_t w = 0; w < wave; ++w) before += sums[w][col];
+    if (e >= p.E) return;
+    if (part == kScanParts - 1u) p.totals[e] = before + sum;
+    for (uint32_t b0 = from; b0 < to; b0 += 8u) {
+        uint32_t c[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) c[i] = b0 + i < to ? p.counts[(uint64_t)(b0 + i) * p.E + e] : 0u;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            if (b0 + i < to) p.counts[(uint64_t)(b0 + i) * p.E + e] = before;
+            before += c[i];
+        }
+    }
+}
 
 // The lanes whose expert is this lane's.
 __device__ __forceinline__ uint64_t alike(uint32_t e, uint32_t bits) {
@@ -148,86 +201,151 @@ __device__ __forceinline__ uint64_t alike(uint32_t e, uint32_t bits) {
     return same;
 }
 
-// Pairs first .. first + n of the block, wave w's share of them in order: order and slots.  at [waves, E]: the first places of each wave's.
-__device__ __forceinline__ void place(const RParams& p, uint64_t first, uint32_t n, uint32_t share, uint32_t* at) {
+// The n pairs of a block, from `first` on, in WAVES waves' shares of up to TURNS * 64: order and slots.  expert[i]: that of pair share * wave + i * 64 + lane, -1 for
+// none.  whole [E]: each expert's pairs in all blocks; at [WAVES, E]: at[0] those in the blocks before this one, the rest 0.  Only the
+// first block writes the offsets.
+template <uint32_t WAVES, uint32_t TURNS>
+__device__ __forceinline__ void place(const RParams& p, uint64_t first, uint32_t n, uint32_t share, const int32_t (&expert)[TURNS], const uint32_t* whole, uint32_t* at,
+                                      uint32_t* waves) {
+    constexpr uint32_t threads = WAVES * 64u;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    // pairs of every wave but the last, counted one wave further on, where their number is wanted
+    if (wave + 1u < WAVES) {
+#pragma unroll
+        for (uint32_t i = 0; i < TURNS; ++i)
+            if (expert[i] >= 0) atomicAdd(&at[(wave + 1u) * p.E + expert[i]], 1u);
+    }
+    __syncthreads();
+    uint32_t before = 0;
+    for (uint32_t base = 0; base < p.E; base += threads) {
+        const uint32_t e = base + threadIdx.x, own = e < p.E ? whole[e] : 0u;
+        const uint32_t behind = wave_prefix(own);
+        if (lane == 63u) waves[wave] = behind;
+        __syncthreads();
+        uint32_t add = before;
+#pragma unroll
+        for (uint32_t w = 0; w < WAVES; ++w) add += w < wave ? waves[w] : 0u;
+        if (e < p.E) {
+            uint32_t to = add + behind - own;
+            if (blockIdx.x == 0) p.offsets[e] = (int32_t)to;
+            uint32_t mine[WAVES];
+#pragma unroll
+            for (uint32_t w = 0; w < WAVES; ++w) mine[w] = at[w * p.E + e];
+#pragma unroll
+            for (uint32_t w = 0; w < WAVES; ++w) {
+                to += mine[w];
+                at[w * p.E + e] = to;
+            }
+        }
+#pragma unroll
+        for (uint32_t w = 0; w < WAVES; ++w) before += waves[w];
+        __syncthreads();
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[p.E] = (int32_t)before;
     volatile uint32_t* own = at + wave * p.E;
-    const uint32_t from = wave * share, to = min(from + share, n);
-    for (uint32_t i0 = from; i0 < to; i0 += 64u) {
-        const uint32_t i = i0 + lane;
-        const int32_t expert = i < to ? p.experts[first + i] : -1;
-        const uint32_t e = expert < 0 ? p.E : (uint32_t)expert;
+#pragma unroll
+    for (uint32_t t = 0; t < TURNS; ++t) {
+        const uint32_t i = wave * share + t * 64u + lane, e = expert[t] < 0 ? p.E : (uint32_t)expert[t];
+        if (wave * share + t * 64u >= n || t * 64u >= share) break;      // uniform
         const uint64_t same = alike(e, p.bits);
         const uint32_t earlier = (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
-        uint32_t to_place = 0;
-        if (expert >= 0) to_place = own[e] + earlier;
+        uint32_t slot = 0;
+        if (expert[t] >= 0) slot = own[e] + earlier;
         // the wave's reads are done before its first lane of each expert moves the place on: one wave's LDS operations stay in order
         __builtin_amdgcn_wave_barrier();
-        if (expert >= 0 && earlier == 0) own[e] = to_place + (uint32_t)__popcll(same);
+        if (expert[t] >= 0 && earlier == 0) own[e] = slot + (uint32_t)__popcll(same);
         __builtin_amdgcn_wave_barrier();
-        if (i < to) {
-            p.slots[first + i] = expert < 0 ? -1 : (int32_t)to_place;
-            if (expert >= 0) p.order[to_place] = (int32_t)(first + i);
+        if (i < n && t * 64u + lane < share) {
+            p.slots[first + i] = expert[t] < 0 ? -1 : (int32_t)slot;
+            if (expert[t] >= 0) p.order[slot] = (int32_t)(first + i);
         }
     }
 }
+// A wave's share of n pairs, in whole turns.
+template <uint32_t WAVES>
+__device__ __forceinline__ uint32_t share_of(uint32_t n) { return (((n + WAVES - 1u) / WAVES) + 63u) & ~63u; }
 
-// counts [blocks, E] holds each block's pairs; every workgroup adds up the blocks before it, and all of them for the experts' first places.
+constexpr uint32_t kPlaceWaves = 4, kPlaceTurns = kBlockTokens * QESGD_MAX_CHOICES / (kPlaceWaves * 64);
+
+// A block's pairs to their places.  SCANNED: counts holds what k_route_scan makes of it; otherwise every workgroup adds up the blocks for itself, its
+// threads dealt to experts and blocks.
+template <bool SCANNED>
 __global__ void __launch_bounds__(kPlaceWaves * 64) k_route_place(const RParams p) {
     extern __shared__ uint32_t shared[];
     constexpr uint32_t threads = kPlaceWaves * 64u;
     uint32_t* at = shared;                                   // [waves, E]
-    uint32_t* whole = shared + kPlaceWaves * p.E;            // [E]: of all blocks
+    uint32_t* whole = shared + kPlaceWaves * p.E;            // [E]
     uint32_t* waves = whole + p.E;
-    for (uint32_t e = threadIdx.x; e < p.E; e += threads) {
-        uint32_t sum = 0, before = 0;
-#pragma unroll 8
-        for (uint32_t b = 0; b < p.blocks; ++b) {
-            const uint32_t c = p.counts[(uint64_t)b * p.E + e];
-            before += b < blockIdx.x ? c : 0u;
-            sum += c;
-        }
-        whole[e] = sum;
-        at[e] = before;
-        for (uint32_t w = 1; w < kPlaceWaves; ++w) at[w * p.E + e] = 0u;
-    }
-    __syncthreads();
-    const uint32_t first_token = blockIdx.x * p.block_tokens, n = min(p.block_tokens, p.T - first_token) * p.k;
+    const uint32_t first_token = blockIdx.x * kBlockTokens, n = min(kBlockTokens, p.T - first_token) * p.k, share = share_of<kPlaceWaves>(n);
     const uint64_t first = (uint64_t)first_token * p.k;
-    const uint32_t share = (((n + kPlaceWaves - 1u) / kPlaceWaves) + 63u) & ~63u;
-    // pairs of every wave but the last, counted one wave further on, where their number is wanted
-    for (uint32_t i = threadIdx.x; i < n; i += threads) {
-        const uint32_t w = i / share + 1u;
-        const int32_t expert = p.experts[first + i];
-        if (w < kPlaceWaves && expert >= 0) atomicAdd(&at[w * p.E + expert], 1u);
+    int32_t expert[kPlaceTurns];
+#pragma unroll
+    for (uint32_t t = 0; t < kPlaceTurns; ++t) {
+        const uint32_t i = (threadIdx.x >> 6) * share + t * 64u + (threadIdx.x & 63u);
+        expert[t] = t * 64u < share && i < n ? p.experts[first + i] : -1;
     }
+    for (uint32_t i = threadIdx.x; i < kPlaceWaves * p.E; i += threads)
+        at[i] = SCANNED && i < p.E ? p.counts[(uint64_t)blockIdx.x * p.E + i] : 0u;
+    for (uint32_t e = threadIdx.x; e < p.E; e += threads) whole[e] = SCANNED ? p.totals[e] : 0u;
     __syncthreads();
-    // experts' first places; only the first workgroup writes them out
-    uint32_t pairs = 0;
-    {
-        uint32_t before = 0;
-        for (uint32_t base = 0; base < p.E; base += threads) {
-            const uint32_t e = base + threadIdx.x, own = e < p.E ? whole[e] : 0u;
-            const uint32_t behind = wave_prefix(own);
-            if ((threadIdx.x & 63u) == 63u) waves[threadIdx.x >> 6] = behind;
-            __syncthreads();
-            uint32_t add = before;
-            for (uint32_t w = 0; w < threadIdx.x >> 6; ++w) add += waves[w];
-            if (e < p.E) {
-                uint32_t place = add + behind - own;
-                if (blockIdx.x == 0) p.offsets[e] = (int32_t)place;
-                for (uint32_t w = 0; w < kPlaceWaves; ++w) {
-                    place += at[w * p.E + e];
-                    at[w * p.E + e] = place;
+    if (!SCANNED) {
+        uint32_t across = 64;
+        while (across < p.E && across < threads) across *= 2;
+        const uint32_t part = threadIdx.x / across, parts = threads / across;
+        for (uint32_t e = threadIdx.x % across; e < p.E; e += across) {
+            uint32_t sum = 0, before = 0;
+            for (uint32_t b0 = part; b0 < p.blocks; b0 += 32u * parts) {
+                uint32_t c[32];
+#pragma unroll
+                for (uint32_t i = 0; i < 32; ++i) c[i] = b0 + i * parts < p.blocks ? p.counts[(uint64_t)(b0 + i * parts) * p.E + e] : 0u;
+#pragma unroll
+                for (uint32_t i = 0; i < 32; ++i) {
+                    before += b0 + i * parts < blockIdx.x ? c[i] : 0u;
+                    sum += c[i];
                 }
             }
-            for (uint32_t w = 0; w < kPlaceWaves; ++w) before += waves[w];
-            __syncthreads();
+            if (sum) atomicAdd(&whole[e], sum);
+            if (before) atomicAdd(&at[e], before);
         }
-        pairs = before;
+        __syncthreads();
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[p.E] = (int32_t)pairs;
-    place(p, first, n, share, at);
+    place<kPlaceWaves, kPlaceTurns>(p, first, n, share, expert, whole, at, waves);
+}
+
+// All of it in one workgroup, for the next tokens of some sequences.
+constexpr uint32_t kSmallWaves = 16, kSmallPairs = 2048;
+template <uint32_t DT, int L, int C>
+__global__ void __launch_bounds__(kSmallWaves * 64) k_route_small(const RParams p) {
+    extern __shared__ uint32_t shared[];
+    constexpr uint32_t threads = kSmallWaves * 64u;
+    __shared__ int32_t experts[kSmallPairs];
+    uint32_t* at = shared;                                   // [waves, E]
+    uint32_t* whole = shared + kSmallWaves * p.E;            // [E]
+    uint32_t* waves = whole + p.E;
+    for (uint32_t i = threadIdx.x; i < (kSmallWaves + 1u) * p.E; i += threads) shared[i] = 0u;
+    __syncthreads();
+    const uint32_t l = threadIdx.x & (L - 1u), part = threadIdx.x / L;
+    for (uint32_t i = part; i < ((p.T + 64u / L - 1u) & ~(64u / L - 1u)); i += threads / L) {
+        const uint64_t t = min(i, p.T - 1u);
+        int32_t expert;
+        float gate;
+        choose<DT, L, C>(p, t, l, expert, gate);
+        if (i < p.T && l < p.k) {
+            p.experts[t * p.k + l] = expert;
+            p.gates[t * p.k + l] = gate;
+            experts[t * p.k + l] = expert;
+            if (expert >= 0) atomicAdd(&whole[expert], 1u);
+        }
+    }
+    __syncthreads();
+    const uint32_t n = p.T * p.k, share = share_of<kSmallWaves>(n);
+    int32_t expert[kSmallPairs / threads];
+#pragma unroll
+    for (uint32_t t = 0; t < kSmallPairs / threads; ++t) {
+        const uint32_t i = (threadIdx.x >> 6) * share + t * 64u + (threadIdx.x & 63u);
+        expert[t] = t * 64u < share && i < n ? experts[i] : -1;
+    }
+    place<kSmallWaves, kSmallPairs / threads>(p, 0, n, share, expert, whole, at, waves);
 }
 
 // Gradient of the gates.
@@ -268,25 +386,29 @@ __global__ void __launch_bounds__(256) k_route_backward(const BParams p) {
             if (e == c * L + (int32_t)l) add[c] += v;
     }
     if (p.all) {
-        float top = -INFINITY;
-        uint32_t high = 0;
+        float high = -INFINITY;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const uint32_t e = (uint32_t)c * L + l;
             x[c] = e < p.E ? element<DT>(p.logits, t * p.ld + e) : -INFINITY;
-            high = max(high, rank_of(x[c]));
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            x[c] = compared(x[c]);
+            high = larger(x[c], high);
         }
         high = most<L>(high);
-        top = logit_of(high);
         float sum = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            x[c] = x[c] == -INFINITY ? 0.0f : expf(x[c] - top);
+            // closed is 0, also where all are
+            x[c] = x[c] == -INFINITY ? 0.0f : exp_below(x[c] - high);
             sum += x[c];
         }
         sum = total<L>(sum);
+        const float part = s / sum;
 #pragma unroll
-        for (int c = 0; c < C; ++c) add[c] -= x[c] == 0.0f ? 0.0f : x[c] / sum * s;
+        for (int c = 0; c < C; ++c) add[c] -= x[c] == 0.0f ? 0.0f : x[c] * part;
     }
     if (i >= p.T) return;
 #pragma unroll
@@ -296,31 +418,43 @@ __global__ void __launch_bounds__(256) k_route_backward(const BParams p) {
     }
 }
 
-// f(lanes of a token, logits of a lane): the least room for E logits.
+// f(lanes of a token, logits of a lane): few lanes, because the exchanges between them cost the same for one token or four, and hardly more logits than
+// there are.
 template <class F>
 void by_experts(uint32_t E, F&& f) {
     using std::integral_constant;
-    if (E <= 8) f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    else if (E <= 16) f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    else if (E <= 32) f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-    else if (E <= 64) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    else if (E <= 128) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-    else if (E <= 256) f(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    else if (E <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
-    else f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+#define QESGD_LANES(lanes, each) if (E <= lanes * each) return f(integral_constant<int, lanes>{}, integral_constant<int, each>{})
+    QESGD_LANES(8, 1);
+    QESGD_LANES(16, 1);
+    QESGD_LANES(16, 2);
+    QESGD_LANES(16, 3);
+    QESGD_LANES(16, 4);
+    QESGD_LANES(16, 5);
+    QESGD_LANES(16, 6);
+    QESGD_LANES(16, 8);
+    QESGD_LANES(16, 10);
+    QESGD_LANES(16, 12);
+    QESGD_LANES(16, 14);
+    QESGD_LANES(16, 17);
+    QESGD_LANES(16, 20);
+    QESGD_LANES(32, 12);
+    QESGD_LANES(32, 16);
+    QESGD_LANES(64, 10);
+    QESGD_LANES(64, 12);
+    QESGD_LANES(64, 16);
+#undef QESGD_LANES
 }
 
-uint32_t route_block_tokens(uint64_t T, uint32_t E) {
-    uint64_t blocks = (T + 63) / 64;
-    if (blocks > 256) blocks = 256;
-    return (uint32_t)((T + blocks - 1) / blocks);
-}
+// Where one workgroup does all of it.
+bool route_small(uint64_t T, uint32_t E, uint32_t k) { return T * k <= kSmallPairs && T <= 128; }
+uint64_t route_blocks(uint64_t T) { return (T + kBlockTokens - 1) / kBlockTokens; }
+bool route_scanned(uint64_t blocks, uint32_t E) { return blocks * E > 16384; }
 
 }  // namespace
 
 size_t route_workspace(uint64_t T, uint32_t E, uint32_t k) {
-    const uint64_t tokens = route_block_tokens(T, E);
-    return ((T + tokens - 1) / tokens) * E * sizeof(uint32_t);
+    if (route_small(T, E, k)) return 0;
+    return (route_blocks(T) + 1) * E * sizeof(uint32_t);
 }
 
 int launch_route(const Route& a) {
@@ -336,15 +470,30 @@ int launch_route(const Route& a) {
     p.offsets = a.offsets;
     p.order = a.order;
     p.slots = a.slots;
-    p.counts = a.workspace;
-    p.block_tokens = route_block_tokens(a.T, a.E);
-    p.blocks = (p.T + p.block_tokens - 1) / p.block_tokens;
     while ((1u << p.bits) <= a.E) ++p.bits;
+    if (route_small(a.T, a.E, a.k)) {
+        by_type(a.dtype, [&](auto t) {
+            by_experts(a.E, [&](auto l, auto c) {
+                k_route_small<t.value, l.value, c.value><<<1, kSmallWaves * 64, ((kSmallWaves + 1) * a.E + kSmallWaves) * sizeof(uint32_t), a.stream>>>(p);
+            });
+        });
+        return launched();
+    }
+    p.counts = a.workspace;
+    p.blocks = (uint32_t)route_blocks(a.T);
+    p.totals = p.counts + (uint64_t)p.blocks * a.E;
     by_type(a.dtype, [&](auto t) {
         by_experts(a.E, [&](auto l, auto c) { k_route_choose<t.value, l.value, c.value><<<p.blocks, kChooseWaves * 64, 0, a.stream>>>(p); });
     });
     if (const int rc = launched(); rc != QESGD_OK) return rc;
-    k_route_place<<<p.blocks, kPlaceWaves * 64, ((kPlaceWaves + 1) * a.E + kPlaceWaves) * sizeof(uint32_t), a.stream>>>(p);
+    const uint32_t lds = ((kPlaceWaves + 1) * a.E + kPlaceWaves) * sizeof(uint32_t);
+    if (route_scanned(p.blocks, a.E)) {
+        k_route_scan<<<(a.E + kScanExperts - 1) / kScanExperts, kScanExperts * kScanParts, 0, a.stream>>>(p);
+        if (const int rc = launched(); rc != QESGD_OK) return rc;
+        k_route_place<true><<<p.blocks, kPlaceWaves * 64, lds, a.stream>>>(p);
+    } else {
+        k_route_place<false><<<p.blocks, kPlaceWaves * 64, lds, a.stream>>>(p);
+    }
     return launched();
 }
 
