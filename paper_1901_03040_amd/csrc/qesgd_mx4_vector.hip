@@ -34,11 +34,13 @@ struct VParams {
     void* y;
     uint64_t ldy;
     uint32_t splits;                  // waves that share a row's columns: 1 .. kVWaves
-    uint32_t part_columns;            // columns of x that lie in LDS at a time, a multiple of 128 * splits
-    uint32_t lds_rows;
+    uint32_t part_columns;            // columns of x that lie in LDS at a time, a multiple of 128
 };
 
-constexpr uint32_t kVWaves = 16;
+constexpr uint32_t kVBatch = 2;           // pairs of steps whose blocks a wave has on their way at a time, twice
+
+// bf16 numbers that hold an element.
+constexpr uint32_t parts_of(uint32_t dtype) { return dtype == QESGD_F32 ? 3 : dtype == QESGD_F16 ? 2 : 1; }
 
 template <uint32_t DT>
 __device__ __forceinline__ void put_row(void* y, uint64_t at, float v) {
@@ -92,11 +94,12 @@ __device__ __forceinline__ void block_values(const uvec4& codes, uint32_t byte, 
     }
 }
 
-template <uint32_t DT>
+// TILES of 16 rows at a time.
+template <uint32_t DT, uint32_t TILES, uint32_t kVWaves>
 __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VParams p) {
-    constexpr uint32_t PARTS = DT == QESGD_F32 ? 3 : DT == QESGD_F16 ? 2 : 1, ROWS = 16 / PARTS;
-    extern __shared__ __attribute__((aligned(16))) unsigned char rows_lds[];            // [lds_rows][part_columns bf16 and 16 bytes]
-    __shared__ __attribute__((aligned(16))) float sums[kVWaves][4][64];
+    constexpr uint32_t PARTS = parts_of(DT), ROWS = TILES * 16 / PARTS;
+    extern __shared__ __attribute__((aligned(16))) unsigned char rows_lds[];            // rows of part_columns bf16 and 16 bytes
+    __shared__ __attribute__((aligned(16))) float sums[kVWaves][TILES][4][64];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t l = lane & 15u, block = lane >> 4;
     const uint32_t e = blockIdx.y;
@@ -112,50 +115,102 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
     const unsigned char* codes = w + (uint64_t)row * p.row_codes + block * 16u;
     const unsigned char* scales = w + p.scales_off + (uint64_t)row * p.row_scales + block;
     const uint32_t steps = p.row_codes / 64u, pitch = p.part_columns * 2u + 16u;
+    // blocks of the pairs of steps from + s, + 2 splits .. before step `last` of a part: a pair's are a line of memory
+    const auto fetch = [&](uvec4 (&c)[2 * kVBatch], uint32_t (&byte)[2 * kVBatch], uint32_t from, uint32_t s, uint32_t last) {
+#pragma unroll
+        for (uint32_t q = 0; q < kVBatch; ++q) {
+            if (s + q * 2u * p.splits >= last) break;                  // uniform
+#pragma unroll
+            for (uint32_t h = 0; h < 2; ++h) {
+                const uint32_t step = from + min(s + q * 2u * p.splits + h, last - 1u);
+                c[2 * q + h] = *(const uvec4*)(codes + step * 64u);
+                byte[2 * q + h] = scales[step * 4u];
+            }
+        }
+    };
     for (uint32_t r0 = lo; r0 < hi; r0 += ROWS) {
         const uint32_t rows = min(ROWS, hi - r0);
-        acc4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (uint32_t c0 = 0; c0 < steps * 128u; c0 += p.part_columns) {
-            const uint32_t here = min(p.part_columns, steps * 128u - c0), eights = here / 8u;
-            __syncthreads();
-            for (uint32_t i = threadIdx.x; i < rows * eights; i += kVWaves * 64u) {
-                const uint32_t r = i / eights, col = (i - r * eights) * 8u;
-                const int32_t pair = p.order ? p.order[r0 + r] : (int32_t)(r0 + r);
-                const uint32_t s = pair < 0 ? p.T : p.per == 1 ? (uint32_t)pair : (uint32_t)pair / p.per;
-                const uint32_t n = s >= p.T || c0 + col >= p.K ? 0u : min(p.K - c0 - col, 8u);
-                Eight<DT> v;
-                v.load(p.x, n ? s * p.ld + c0 + col : 0u, n);
-                uvec4 parts[PARTS];
-                split<DT, PARTS>(v, parts);
+        acc4 acc[TILES];
 #pragma unroll
-                for (uint32_t q = 0; q < PARTS; ++q) *(uvec4*)(rows_lds + (r * PARTS + q) * pitch + col * 2u) = parts[q];
+        for (uint32_t m = 0; m < TILES; ++m) acc[m] = acc4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (uint32_t c0 = 0; c0 < steps * 128u; c0 += p.part_columns) {
+            const uint32_t here = min(p.part_columns, steps * 128u - c0), eights = here / 8u, last = here / 128u;
+            // the wave's first blocks are on their way while the rows are brought in
+            uvec4 c[2 * kVBatch], next_c[2 * kVBatch];
+            uint32_t byte[2 * kVBatch], next_byte[2 * kVBatch];
+            fetch(c, byte, c0 / 128u, 2u * share, last);
+            __syncthreads();
+            // some pieces a thread on their way at a time, as the registers allow
+            constexpr uint32_t kPieces = DT == QESGD_F32 && kVWaves == 16 ? 2 : 4;
+            for (uint32_t i0 = threadIdx.x; i0 < rows * eights; i0 += kPieces * kVWaves * 64u) {
+                Eight<DT> v[kPieces];
+                uint32_t to[kPieces];
+#pragma unroll
+                for (uint32_t q = 0; q < kPieces; ++q) {
+                    const uint32_t i = i0 + q * (kVWaves * 64u);
+                    if (i >= rows * eights) break;
+                    const uint32_t r = i / eights, col = (i - r * eights) * 8u;
+                    const int32_t pair = p.order ? p.order[r0 + r] : (int32_t)(r0 + r);
+                    const uint32_t s = pair < 0 ? p.T : p.per == 1 ? (uint32_t)pair : (uint32_t)pair / p.per;
+                    const uint32_t n = s >= p.T || c0 + col >= p.K ? 0u : min(p.K - c0 - col, 8u);
+                    v[q].load(p.x, n ? s * p.ld + c0 + col : 0u, n);
+                    to[q] = r * PARTS * pitch + col * 2u;
+                }
+#pragma unroll
+                for (uint32_t q = 0; q < kPieces; ++q) {
+                    if (i0 + q * (kVWaves * 64u) >= rows * eights) break;
+                    uvec4 parts[PARTS];
+                    split<DT, PARTS>(v[q], parts);
+#pragma unroll
+                    for (uint32_t h = 0; h < PARTS; ++h) *(uvec4*)(rows_lds + to[q] + h * pitch) = parts[h];
+                }
             }
             __syncthreads();
             // rows of the instruction beyond those there are read the last one: what comes of them is not stored
-            const unsigned char* x = rows_lds + min(l, rows * PARTS - 1u) * pitch + block * 64u;
-            for (uint32_t s = share; s < here / 128u; s += p.splits) {
-                const uint32_t step = c0 / 128u + s;
-                const uvec4 c = *(const uvec4*)(codes + step * 64u);
-                const uint32_t byte = scales[step * 4u];
-                bf16x8 b[4];
-                block_values(c, byte, b);
+            const unsigned char* x[TILES];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(x + s * 256u + i * 16u), b[i], acc, 0, 0, 0);
+            for (uint32_t m = 0; m < TILES; ++m) x[m] = rows_lds + min(m * 16u + l, rows * PARTS - 1u) * pitch + block * 64u;
+            for (uint32_t s = 2u * share; s < last; s += 2u * kVBatch * p.splits) {
+                fetch(next_c, next_byte, c0 / 128u, s + 2u * kVBatch * p.splits, last);
+#pragma unroll
+                for (uint32_t q = 0; q < 2 * kVBatch; ++q) {
+                    const uint32_t step = s + (q >> 1) * 2u * p.splits + (q & 1u);
+                    if (step >= last) break;                           // uniform
+                    bf16x8 b[4];
+                    block_values(c[q], byte[q], b);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (uint32_t m = 0; m < TILES; ++m)
+                            acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(x[m] + step * 256u + i * 16u), b[i], acc[m], 0, 0, 0);
+                }
+#pragma unroll
+                for (uint32_t q = 0; q < 2 * kVBatch; ++q) {
+                    c[q] = next_c[q];
+                    byte[q] = next_byte[q];
+                }
             }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sums[wave][i][lane] = acc[i];
+        for (uint32_t m = 0; m < TILES; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums[wave][m][i][lane] = acc[m][i];
         __syncthreads();
-        // sums[wave][i][lane]: row 4 * (lane / 16) + i of the instruction, column lane % 16
+        // sums[wave][m][i][lane]: row 16 m + 4 (lane / 16) + i of the instructions, column lane % 16
         for (uint32_t i = threadIdx.x; i < (kVWaves / p.splits) * 16u * rows; i += kVWaves * 64u) {
             const uint32_t col = i & 15u, r = (i >> 4) % rows, set = (i >> 4) / rows;
             const uint32_t n = (blockIdx.x * (kVWaves / p.splits) + set) * 16u + col;
             if (n >= p.N) continue;
             float v = 0.0f;
+#pragma unroll
             for (int q = PARTS - 1; q >= 0; --q) {
                 const uint32_t m = r * PARTS + q;
-                for (uint32_t s = 0; s < p.splits; ++s) v += sums[set * p.splits + s][m & 3u][(m >> 2) * 16u + col];
+                const float* from = &sums[set * p.splits][m >> 4][m & 3u][(m >> 2 & 3u) * 16u + col];
+                float part[kVWaves];
+#pragma unroll
+                for (uint32_t s = 0; s < kVWaves; ++s) part[s] = s < p.splits ? from[s * (TILES * 256u)] : 0.0f;
+#pragma unroll
+                for (uint32_t s = 0; s < kVWaves; ++s) v += part[s];
             }
             put_row<DT>(p.y, (uint64_t)(r0 + r) * p.ldy + n, v);
         }
@@ -187,18 +242,42 @@ int launch_vector_product(const VectorProduct& a) {
     p.row_scales = (uint32_t)W.row_scales;
     p.y = a.y;
     p.ldy = a.ldy;
-    const uint32_t steps = p.row_codes / 64u, parts = a.dtype == QESGD_F32 ? 3 : a.dtype == QESGD_F16 ? 2 : 1, rows = 16 / parts;
+    const uint32_t steps = p.row_codes / 64u, parts = parts_of(a.dtype), across_rows = (p.N + 15) / 16;
+    const uint32_t hit = a.E < a.R ? a.E : (uint32_t)a.R;
+    // rows that an expert has at a time, of which two in three are in its share twice over
+    const uint32_t rows = (uint32_t)(a.E == 1 ? a.R : (2 * a.R + a.E - 1) / a.E);
+    uint32_t tiles = 1;
+    while (tiles < parts && tiles * 16 / parts < rows) ++tiles;
+    const uint32_t at_a_time = tiles * 16 / parts;
+    const uint32_t lds_rows = parts * (a.R < at_a_time ? (uint32_t)a.R : at_a_time);
+    // Workgroups of 8 waves, two on a CU, where there is little to bring into LDS, else of 16, which bring it in faster.  8 / 16 waves, us, graph of 32 calls: one row
+    // x 4096 x 4096 bf16 5.5 / 5.8, f32 6.2 / 8.7, x 512 x 512 f32 3.9 / 6.3; 8 rows bf16 8.7 / 7.2, 16 rows f32 26.6 / 21.8, 4 rows x 4096 x 25088
+    // bf16 28.9 / 21.5.  And as many waves to a row of W as make kVWavesFew or kVWavesMany of them, beyond which each has more steps instead: 12 tokens x 4 of 64
+    // experts 1411 x 2049 with two waves a row 21.3, with one 18.4; one row x 8192 x 8192 bf16 13.1 with 8, 15.9 with 16.
+    constexpr uint32_t kVWavesFew = 2048, kVWavesMany = 4096;
+    const uint32_t waves = (uint64_t)(rows < at_a_time ? rows : at_a_time) * parts * steps * 256u < 32768u ? 8 : 16;
     p.splits = 1;
-    while (p.splits < kVWaves && p.splits * 2 <= steps) p.splits *= 2;
-    p.lds_rows = parts * (a.R < rows ? (uint32_t)a.R : rows);
-    // 60 KB for the rows, so that two workgroups with their sums fit a CU
-    const uint32_t unit = 128u * p.splits, most = (60u * 1024u / p.lds_rows - 16u) / 2u / unit * unit, all = (steps * 128u + unit - 1) / unit * unit;
-    p.part_columns = most < unit ? unit : most < all ? most : all;
-    const uint32_t bytes = p.lds_rows * (p.part_columns * 2u + 16u);
-    const uint32_t across = 16u * (kVWaves / p.splits), blocks = (p.N + across - 1) / across;
+    while (p.splits < waves && p.splits * 4 <= steps + 1 && (uint64_t)across_rows * hit * p.splits < (waves == 8 ? kVWavesFew : kVWavesMany)) p.splits *= 2;
+    const uint32_t across = 16u * (waves / p.splits), blocks = (p.N + across - 1) / across;
+    // the rows whole, where a CU has one workgroup anyway, or else as much of them as leaves room for two
+    const bool alone = (uint64_t)blocks * hit <= 256;
+    const uint32_t room = (alone ? 140u : 60u) * 1024u * waves / 16u - tiles * 1024u * waves * (alone ? 1u : 0u);
+    const uint32_t most = (room / lds_rows - 16u) / 2u / 128u * 128u;
+    p.part_columns = most < steps * 128u ? most : steps * 128u;
+    const uint32_t bytes = lds_rows * (p.part_columns * 2u + 16u);
     const dim3 grid(blocks, a.E);
-    if (!grid_ok((uint64_t)blocks * a.E, kVWaves * 64)) return QESGD_ERR_DIM;
-    by_type(a.dtype, [&](auto t) { k_mx4_vector_product<t.value><<<grid, kVWaves * 64, bytes, a.stream>>>(p); });
+    if (!grid_ok((uint64_t)blocks * a.E, waves * 64)) return QESGD_ERR_DIM;
+    by_type(a.dtype, [&](auto t) {
+        constexpr uint32_t DT = t.value, PARTS = parts_of(DT);
+        const auto go = [&](auto w) {
+            constexpr uint32_t W = w.value;
+            if (tiles == 1) k_mx4_vector_product<DT, 1, W><<<grid, W * 64, bytes, a.stream>>>(p);
+            else if (tiles == 2) k_mx4_vector_product<DT, PARTS >= 2 ? 2 : 1, W><<<grid, W * 64, bytes, a.stream>>>(p);
+            else k_mx4_vector_product<DT, PARTS >= 3 ? 3 : 1, W><<<grid, W * 64, bytes, a.stream>>>(p);
+        };
+        if (waves == 16) go(std::integral_constant<uint32_t, 16>{});
+        else go(std::integral_constant<uint32_t, 8>{});
+    });
     return launched();
 }
 
