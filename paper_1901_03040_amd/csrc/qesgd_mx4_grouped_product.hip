@@ -22,7 +22,42 @@ struct PParams {
     uint32_t N, K;                        // rows of B_e; columns of D_e
     uint32_t row_codes, row_scales;       // of either operand
     uint32_t tiles_m, tiles_n;            // of one expert's D; tiles_n of C
+    bool stream;                          // C or D in whole lines that nothing finds in a cache again
 };
+
+// Non-temporal stores where the result is larger than what the memory-side cache keeps for its reader, and made of whole lines (parts of
+// lines cost such a store a read): D 537 MB 266 -> 222 us, 64 experts of 2048 x 1024 142 -> 107; C 268 MB in bf16 340 -> 317; 134 MB and less
+// the same; rows of 2049 numbers 38 -> 50.
+constexpr uint64_t kStreamBytes = 192ull << 20;
+inline bool streamed(const void* c, uint64_t row_bytes, uint64_t rows) { return row_bytes * rows >= kStreamBytes && ((uintptr_t)c | row_bytes) % 128 == 0; }
+
+template <uint32_t DT>
+__device__ __forceinline__ void put_stream(void* c, uint64_t at, float v) {
+    if (DT == QESGD_F32) __builtin_nontemporal_store(v, (float*)c + at);
+    else if (DT == QESGD_F16) __builtin_nontemporal_store((_Float16)v, (_Float16*)c + at);
+    else __builtin_nontemporal_store((__bf16)v, (__bf16*)c + at);
+}
+
+// The wave's fragments to rows and columns from row0 and col0 on, of rows up to M and columns up to N.
+template <class S, uint32_t DT>
+__device__ __forceinline__ void store_tile(const Mx4Ops<S>& ops, void* c, uint64_t ldc, uint32_t M, uint32_t N, uint32_t row0, uint32_t col0, bool whole, bool stream) {
+    const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+            // a lane holds column lane & 31 of a fragment and rows 8 q + 4 h + r
+            const uint32_t row = row0 + i * 32u + 4u * (lane >> 5), col = col0 + j * 32u + (lane & 31u);
+            if (whole && stream) {
+                asm volatile("; streamed");              // keeps the two arms apart, which the compiler would merge into ordinary stores
+                const uint64_t base = (uint64_t)row * ldc + col;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) put_stream<DT>(c, base + (8u * (e >> 2) + (e & 3)) * ldc, ops.acc[i][j][e]);
+            } else {
+                store_fragment<DT>(c, ldc, M, N, row, col, whole, ops.acc[i][j]);
+            }
+        }
+}
 
 template <class S>
 __device__ __forceinline__ void multiply_tile(Mx4Ops<S>& ops, uint32_t steps, unsigned char* lds0, unsigned char* lds1, unsigned char* lds2, unsigned char* lds3) {
@@ -77,12 +112,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_product(const PParam
     ops.h = h;
     multiply_tile(ops, ops.steps, lds0, lds1, lds2, lds3);
 
-    const bool whole = m0 + S::BM <= g.hi && n0 + S::BN <= p.N;
-#pragma unroll
-    for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-        for (int j = 0; j < S::FN; ++j)
-            store_fragment<DT>(p.c, p.ldc, g.hi, p.N, m0 + (wm * S::FM + i) * 32u + 4u * h, n0 + (wn * S::FN + j) * 32u + (lane & 31u), whole, ops.acc[i][j]);
+    store_tile<S, DT>(ops, p.c, p.ldc, g.hi, p.N, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= g.hi && n0 + S::BN <= p.N, p.stream);
 }
 
 template <class S, uint32_t DT>
@@ -94,10 +124,10 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
     __shared__ __attribute__((aligned(1024))) unsigned char scales[Mx4Ops<S>::scale_buffers * Mx4Ops<S>::scale_bytes];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
     const uint32_t wm = wave / S::WN, wn = wave % S::WN;
-    const uint32_t tiles = p.tiles_m * p.tiles_n;
-    const uint32_t t = tile_of_workgroup(blockIdx.x, gridDim.x), e = __builtin_amdgcn_readfirstlane(t / tiles);
+    // experts differ in rows, so every XCD gets its share of each one's tiles, a run of them: 8 experts of 4096 x 4096, 16384 rows 357 -> 266 us
+    const uint32_t tiles = p.tiles_m * p.tiles_n, e = __builtin_amdgcn_readfirstlane(blockIdx.x / tiles);
     uint32_t tm, tn;
-    banded_tile(t - e * tiles, p.tiles_m, p.tiles_n, tm, tn);
+    banded_tile(tile_of_workgroup(blockIdx.x - e * tiles, tiles), p.tiles_m, p.tiles_n, tm, tn);
     tm = __builtin_amdgcn_readfirstlane(tm);
     tn = __builtin_amdgcn_readfirstlane(tn);
     const Group g = group_number(p.offsets, p.E, p.R, 7, e);
@@ -126,12 +156,31 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
         multiply_tile(ops, ops.steps, lds0, lds1, lds2, lds3);
     }
     void* d = (unsigned char*)p.c + (uint64_t)e * p.N * p.K * (DT == QESGD_F32 ? 4u : 2u);
-    const bool whole = m0 + S::BM <= p.N && n0 + S::BN <= p.K;
-#pragma unroll
-    for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-        for (int j = 0; j < S::FN; ++j)
-            store_fragment<DT>(d, p.K, p.N, p.K, m0 + (wm * S::FM + i) * 32u + 4u * h, n0 + (wn * S::FN + j) * 32u + (lane & 31u), whole, ops.acc[i][j]);
+    store_tile<S, DT>(ops, d, p.K, p.N, p.K, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= p.N && n0 + S::BN <= p.K, p.stream);
+}
+
+// Tiles of `edge` rows that the groups make, from their mean size: half a tile more than their rows, and one at least.
+uint64_t group_tiles(const GroupProduct& a, uint64_t edge) {
+    const uint64_t groups = a.E < a.R ? a.E : a.R, tiles = a.R / edge + groups / 2;
+    return tiles > groups ? tiles : groups;
+}
+
+// The edge of the tiles from how long they take on 256 CUs (tile_us), the larger one where it hardly matters.  Measured, us, with 64 / 128 / 256:
+//   products   16 experts, 32768 rows, N = K = 4096 655 / 402 / 339;  13, 9003, 1000, 2049 33 / 25.9 / 22.7;  8, 2048, 2048, 2048 15.5 / 13.7 / 18.1;
+//              64, 1024, 1024, 1024 11.5 / 9.2 / 12.5;  8, 256, 4096, 4096 17.8 / 16.3 / 27.2;  64, 16384, 2048, 1024 70 / 46 / 46
+//   gradients  8, 16384, 4096, 4096 759 / 344 / 266;  64, 4096, 1024, 1024 109 / 65 / 59;  16, 1024, 512, 512 8.9 / 8.3 / 9.7
+template <class F>
+uint32_t choose_edge(F&& tiles, double steps) {
+    uint32_t best = 64;
+    double least = 1e300;
+    for (uint32_t edge : {64u, 128u, 256u}) {
+        const double us = tile_us(tiles(edge), edge, steps);
+        if (us <= least * 1.02) {
+            least = us;
+            best = edge;
+        }
+    }
+    return best;
 }
 
 template <class S>
@@ -178,10 +227,13 @@ int launch_grouped_product(const GroupProduct& a) {
     p.N = (uint32_t)a.N;
     p.row_codes = (uint32_t)A.row_codes;
     p.row_scales = (uint32_t)A.row_scales;
-    const uint64_t rows = (a.R + a.E - 1) / a.E;
-    if (rows <= 64) return launch_product_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
-    if (rows <= 512) return launch_product_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
-    return launch_product_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
+    p.stream = streamed(a.c, a.ldc * dtype_bytes(a.dtype), a.R);
+    const uint64_t steps = (a.K + 255) / 256;
+    switch (choose_edge([&](uint64_t edge) { return group_tiles(a, edge) * ((a.N + edge - 1) / edge); }, (double)steps)) {
+        case 64: return launch_product_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
+        case 128: return launch_product_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
+        default: return launch_product_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
+    }
 }
 
 int launch_grouped_gradient(const GroupProduct& a) {
@@ -203,8 +255,14 @@ int launch_grouped_gradient(const GroupProduct& a) {
     p.K = (uint32_t)a.K;
     p.row_codes = (uint32_t)A.row_codes;
     p.row_scales = (uint32_t)A.row_scales;
-    if (a.N * a.K <= 512 * 512) return launch_gradient_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
-    return launch_gradient_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
+    p.stream = streamed(a.c, a.K * dtype_bytes(a.dtype), a.E * a.N);
+    // the contraction of a group of the mean size, and as much as two steps for the beginning and the end of a tile
+    const double steps = 2.5 + (double)a.R / (double)a.E / 256.0;
+    switch (choose_edge([&](uint64_t edge) { return a.E * ((a.N + edge - 1) / edge) * ((a.K + edge - 1) / edge); }, steps)) {
+        case 64: return launch_gradient_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
+        case 128: return launch_gradient_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
+        default: return launch_gradient_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
+    }
 }
 
 }  // namespace qesgd

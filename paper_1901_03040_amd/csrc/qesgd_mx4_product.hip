@@ -176,8 +176,7 @@ int launch_tiles(const Mx4Product& a, PParams& p, uint32_t pieces) {
     return launched();
 }
 
-// Which kernel, and how many pieces of the contraction, from how long the workgroups take on 256 CUs.  A step of 256 columns takes, us:
-// 64 x 64 tiles 0.30 while a CU has one, 0.62 with two; 128 x 128 0.85 and 1.5; 256 x 256 1.2 on an empty chip, 2.3 on a full one.
+// Which kernel, and how many pieces of the contraction, from how long the workgroups take (tile_us).
 // Measured over 26 shapes, us with 64 / 128 / 256:
 //   64 x 4096 x 4096 6.9 / 13.4 / 26.2;  512 x 4096 x 4096 12.5 / 14.9 / 27.7;  1024 x 4096 x 4096 22.6 / 17.6 / 28.3;  4096 x 4096 x 4096
 //   82.7 / 50.2 / 40.8;  3000 x 5000 x 700 26.8 / 19.9 / 16.0
@@ -186,13 +185,6 @@ int launch_tiles(const Mx4Product& a, PParams& p, uint32_t pieces) {
 // edge 0: k_mx4_product_few, up to 16 rows where every wave has one step at most.  Few / 64 x 64: 1 x 4096 x 4096 5.5 / 6.8, 16 x 4096 x 4096 6.5 / 6.8,
 // 32 x 4096 x 4096 8.1 / 7.0, 1 x 16384 x 4096 10.6 / 7.5 (calls from Python: 4.9 is what the call itself takes).
 struct Cut { uint32_t edge, pieces; };
-
-double cut_us(uint64_t groups, uint32_t edge, uint64_t steps) {
-    const uint64_t slots = edge == 256 ? 256 : 512, left = groups % slots;
-    const double full = edge == 256 ? 2.3 : edge == 128 ? 1.5 : 0.62;
-    const double last = left == 0 ? 0.0 : edge == 256 ? 1.2 + 1.1 * (double)left / 256.0 : left <= 256 ? (edge == 128 ? 0.85 : 0.30) : full;
-    return ((double)(groups / slots) * full + last) * (double)steps + (double)((groups + slots - 1) / slots);
-}
 
 Cut choose_cut(uint64_t M, uint64_t N, uint64_t K) {
     const uint64_t steps = (K + 255) / 256;
@@ -203,7 +195,7 @@ Cut choose_cut(uint64_t M, uint64_t N, uint64_t K) {
         const uint64_t tiles = ((M + edge - 1) / edge) * ((N + edge - 1) / edge);
         // a piece has at least four steps; the sums of the pieces cost a launch, and are written and read at about 4 TB/s
         for (uint32_t pieces = 1; pieces <= 16 && (pieces == 1 || (pieces * 4 <= steps && tiles * pieces <= 1024)); ++pieces) {
-            const double us = cut_us(tiles * pieces, edge, (steps + pieces - 1) / pieces) + (pieces == 1 ? 0.0 : 2.0 + (double)pieces * (double)(M * N) * 2e-6);
+            const double us = tile_us(tiles * pieces, edge, (double)((steps + pieces - 1) / pieces)) + (pieces == 1 ? 0.0 : 2.0 + (double)pieces * (double)(M * N) * 2e-6);
             if (us < least) {
                 least = us;
                 best = Cut{edge, pieces};
