@@ -33,11 +33,14 @@ struct Piece {
     static constexpr uint32_t V = DT == QESGD_F32 ? 4 : 8;
     uvec4 v;
 
+    // STREAM: non-temporal
+    template <bool STREAM>
     __device__ __forceinline__ void load(const void* x, uint64_t at, uint32_t n) {
         if constexpr (DT == QESGD_F32) {
             const float* p = (const float*)x + at;
             if (n >= V) {
-                v = __builtin_bit_cast(uvec4, *(const vec4_any*)p);
+                if (STREAM) v = __builtin_bit_cast(uvec4, __builtin_nontemporal_load((const vec4_any*)p));
+                else v = __builtin_bit_cast(uvec4, *(const vec4_any*)p);
             } else {
                 v = uvec4{0, 0, 0, 0};
 #pragma unroll
@@ -47,7 +50,8 @@ struct Piece {
         } else {
             const unsigned short* p = (const unsigned short*)x + at;
             if (n >= V) {
-                v = *(const uvec4_any*)p;
+                if (STREAM) v = __builtin_nontemporal_load((const uvec4_any*)p);
+                else v = *(const uvec4_any*)p;
             } else {
                 v = uvec4{0, 0, 0, 0};
 #pragma unroll
@@ -69,11 +73,13 @@ struct Piece {
             else v[i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)x[2 * i], (_Float16)x[2 * i + 1]});
         }
     }
+    template <bool STREAM>
     __device__ __forceinline__ void store(void* x, uint64_t at, uint32_t n) const {
         if constexpr (DT == QESGD_F32) {
             float* p = (float*)x + at;
             if (n >= V) {
-                *(vec4_any*)p = __builtin_bit_cast(vec4, v);
+                if (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(vec4, v), (vec4_any*)p);
+                else *(vec4_any*)p = __builtin_bit_cast(vec4, v);
             } else {
 #pragma unroll
                 for (uint32_t i = 0; i < V - 1; ++i)
@@ -82,7 +88,8 @@ struct Piece {
         } else {
             unsigned short* p = (unsigned short*)x + at;
             if (n >= V) {
-                *(uvec4_any*)p = v;
+                if (STREAM) __builtin_nontemporal_store(v, (uvec4_any*)p);
+                else *(uvec4_any*)p = v;
             } else {
 #pragma unroll
                 for (uint32_t i = 0; i < V - 1; ++i)
@@ -92,8 +99,8 @@ struct Piece {
     }
 };
 
-// A thread a piece of a token's row.
-template <uint32_t DT>
+// A thread a piece of a token's row.  STREAM: out is written non-temporally.
+template <uint32_t DT, bool STREAM>
 __global__ void __launch_bounds__(256) k_combine(const CParams p) {
     constexpr uint32_t V = Piece<DT>::V;
     const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x;
@@ -109,22 +116,26 @@ __global__ void __launch_bounds__(256) k_combine(const CParams p) {
         if (slot >= p.R) continue;
         const float g = p.gates ? p.gates[pair] : 1.0f;
         Piece<DT> x;
-        x.load(p.rows, slot * p.ld + col, n);
+        x.template load<false>(p.rows, slot * p.ld + col, n);
 #pragma unroll
         for (uint32_t e = 0; e < V; ++e) sum[e] += g * x.at(e);
     }
     Piece<DT> y;
     y.set(sum);
-    y.store(p.out, t * p.ld_out + col, n);
+    y.template store<STREAM>(p.out, t * p.ld_out + col, n);
 }
 
-// W waves a token; KM: at least k.
-template <uint32_t DT, int W, int KM>
+// Policies of the backward pass: rows' gradients written non-temporally, and rows read so too.
+enum { kKept = 0, kStreamOut = 1, kStreamBoth = 2 };
+
+// L lanes a token (256: a workgroup); KM: at least k.
+template <uint32_t DT, uint32_t L, int KM, int POLICY>
 __global__ void __launch_bounds__(256) k_combine_backward(const CParams p) {
-    constexpr uint32_t V = Piece<DT>::V, tokens = 4 / W;
+    constexpr uint32_t V = Piece<DT>::V, tokens = 256 / L;
+    constexpr bool OUT = POLICY != kKept, IN = POLICY == kStreamBoth;
     __shared__ float sums[4][KM];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint64_t t = (uint64_t)blockIdx.x * tokens + wave / W;
+    const uint32_t lane = threadIdx.x % L;
+    const uint64_t t = (uint64_t)blockIdx.x * tokens + threadIdx.x / L;
     const bool there = t < p.T;
     float dot[KM], gate[KM];
     uint32_t slot[KM];
@@ -140,14 +151,14 @@ __global__ void __launch_bounds__(256) k_combine_backward(const CParams p) {
         }
     }
     if (there) {
-        for (uint32_t c = (wave % W) * 64u + lane; c < p.vectors; c += W * 64u) {
+        for (uint32_t c = lane; c < p.vectors; c += L) {
             const uint32_t col = c * V, n = p.N - col;
             Piece<DT> d, x[KM];
-            d.load(p.dy, t * p.ld_dy + col, n);
+            d.template load<false>(p.dy, t * p.ld_dy + col, n);
             if (p.dgates) {
 #pragma unroll
                 for (int j = 0; j < KM; ++j)
-                    if (slot[j] < p.R) x[j].load(p.rows, slot[j] * p.ld + col, n);
+                    if (slot[j] < p.R) x[j].template load<IN>(p.rows, slot[j] * p.ld + col, n);
 #pragma unroll
                 for (int j = 0; j < KM; ++j)
                     if (slot[j] < p.R) {
@@ -164,28 +175,28 @@ __global__ void __launch_bounds__(256) k_combine_backward(const CParams p) {
                         for (uint32_t e = 0; e < V; ++e) v[e] = gate[j] * d.at(e);
                         Piece<DT> y;
                         y.set(v);
-                        y.store(p.drows, slot[j] * p.ld_d + col, n);
+                        y.template store<OUT>(p.drows, slot[j] * p.ld_d + col, n);
                     }
             }
         }
     }
     if (!p.dgates) return;
+    constexpr uint32_t W = L < 64 ? L : 64;
 #pragma unroll
-    for (int j = 0; j < KM; ++j) {
-        for (int m = 1; m < 64; m <<= 1) dot[j] += __shfl_xor(dot[j], m);
-        if (lane == 0) sums[wave][j] = dot[j];
+    for (int j = 0; j < KM; ++j)
+#pragma unroll
+        for (uint32_t m = 1; m < W; m <<= 1) dot[j] += __shfl_xor(dot[j], (int)m);
+    if (L <= 64) {
+#pragma unroll
+        for (int j = 0; j < KM; ++j)
+            if (there && lane == (uint32_t)j % W && (uint32_t)j < p.k) p.dgates[t * p.k + j] = dot[j];
+        return;
     }
+#pragma unroll
+    for (int j = 0; j < KM; ++j)
+        if ((threadIdx.x & 63u) == 0) sums[threadIdx.x >> 6][j] = dot[j];
     __syncthreads();
-    if (threadIdx.x < tokens * KM) {
-        const uint32_t of = threadIdx.x / KM, j = threadIdx.x % KM;
-        const uint64_t token = (uint64_t)blockIdx.x * tokens + of;
-        if (token < p.T && j < p.k) {
-            float v = 0.0f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) v += sums[of * W + w][j];
-            p.dgates[token * p.k + j] = v;
-        }
-    }
+    if (threadIdx.x < p.k) p.dgates[t * p.k + threadIdx.x] = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
 }
 
 CParams params(const Combine& a) {
@@ -212,31 +223,54 @@ CParams params(const Combine& a) {
 
 }  // namespace
 
+// A result of whole lines, of a call that moves more than the memory-side cache keeps for the next one, is written non-temporally, us without / with:
+// 16384 tokens x 2 rows x 4096 bf16 78 / 58, gradients 134 / 131, and 112 with the rows read so too, where they alone are more than that cache; 8192 tokens 30 / 30, 68 / 51 and
+// 58; 65536 x 1 x 1024 40 / 40, 77 / 59 and 63; small calls the same.
+constexpr uint64_t kStreamMoved = 128ull << 20, kStreamRows = 256ull << 20;
+static bool whole_lines(const void* p, uint64_t ld, uint32_t dtype) { return ((uintptr_t)p | ld * dtype_bytes(dtype)) % 128 == 0; }
+
 int launch_combine(const Combine& a) {
     const CParams p = params(a);
-    const uint64_t groups = ((uint64_t)p.T * p.vectors + 255) / 256;
+    const uint64_t groups = ((uint64_t)p.T * p.vectors + 255) / 256, moved = a.N * (a.T * a.k + a.T) * dtype_bytes(a.dtype);
     if (!grid_ok(groups, 256)) return QESGD_ERR_DIM;
-    by_type(a.dtype, [&](auto t) { k_combine<t.value><<<(uint32_t)groups, 256, 0, a.stream>>>(p); });
+    const bool stream = moved >= kStreamMoved && whole_lines(a.out, a.ld_out, a.dtype);
+    by_type(a.dtype, [&](auto t) {
+        if (stream) k_combine<t.value, true><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+        else k_combine<t.value, false><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+    });
     return launched();
 }
 
 int launch_combine_backward(const Combine& a) {
     const CParams p = params(a);
-    const bool wide = p.vectors > 128;
-    const uint64_t groups = wide ? p.T : (p.T + 3) / 4;
+    // lanes of a token: a workgroup for long rows, for short ones no more than have work
+    const uint32_t lanes = p.vectors > 128 ? 256 : p.vectors > 16 ? 64 : p.vectors > 8 ? 16 : 8;
+    const uint64_t tokens = 256 / lanes, groups = (p.T + tokens - 1) / tokens, rows = a.N * a.T * a.k * dtype_bytes(a.dtype);
     if (!grid_ok(groups, 256)) return QESGD_ERR_DIM;
-    const auto by_choices = [&](auto f) {
+    const bool stream = a.drows && 2 * rows >= kStreamMoved && whole_lines(a.drows, a.ld_d, a.dtype);
+    const auto go = [&](auto t, auto l, auto km) {
+        constexpr uint32_t DT = t.value, L = l.value;
+        constexpr int KM = km.value;
+        // rows of up to 256 bytes are not streamed: a call of them has to have a million
+        if (L == 256 && stream && rows >= kStreamRows) k_combine_backward<DT, L, KM, L == 256 ? kStreamBoth : kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+        else if (L >= 64 && stream) k_combine_backward<DT, L, KM, L >= 64 ? kStreamOut : kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+        else k_combine_backward<DT, L, KM, kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+    };
+    const auto by_choices = [&](auto t, auto l) {
         using std::integral_constant;
-        if (p.k <= 2) f(integral_constant<int, 2>{});
-        else if (p.k <= 4) f(integral_constant<int, 4>{});
-        else if (p.k <= 8) f(integral_constant<int, 8>{});
-        else f(integral_constant<int, 16>{});
+        if (p.k <= 2) go(t, l, integral_constant<int, 2>{});
+        else if (p.k <= 4) go(t, l, integral_constant<int, 4>{});
+        else if (p.k <= 8) go(t, l, integral_constant<int, 8>{});
+        else go(t, l, integral_constant<int, 16>{});
     };
     by_type(a.dtype, [&](auto t) {
-        by_choices([&](auto km) {
-            if (wide) k_combine_backward<t.value, 4, km.value><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
-            else k_combine_backward<t.value, 1, km.value><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
-        });
+        using std::integral_constant;
+        switch (lanes) {
+            case 8: by_choices(t, integral_constant<uint32_t, 8>{}); break;
+            case 16: by_choices(t, integral_constant<uint32_t, 16>{}); break;
+            case 64: by_choices(t, integral_constant<uint32_t, 64>{}); break;
+            default: by_choices(t, integral_constant<uint32_t, 256>{}); break;
+        }
     });
     return launched();
 }
