@@ -159,6 +159,244 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
     store_tile<S, DT>(ops, d, p.K, p.N, p.K, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= p.N && n0 + S::BN <= p.K, p.stream);
 }
 
+// ---- large tiles, one after the other ------------------------------------------
+//
+// A workgroup takes every gridDim-th tile.  The loads of a tile's first two steps are on their way while the last two of the tile before are multiplied,
+// and while that one is stored: a tile of its own workgroup begins with a launch, a search and a trip to memory, 6 us where 16 steps take 33.
+// Steps come in pairs, because buffers and scales do: where a tile has an odd number, its last one comes once more with scales of zero.
+
+// Tiles before each group and offsets, in LDS.
+struct GroupTable {
+    uint32_t first[QESGD_MAX_EXPERTS + 1];
+    uint32_t row[QESGD_MAX_EXPERTS + 1];
+};
+// By the first wave.
+__device__ __forceinline__ void fill_table(GroupTable& table, const int32_t* offsets, uint32_t E, uint32_t R, uint32_t lg) {
+    const uint32_t lane = threadIdx.x & 63u;
+    uint32_t before = 0;
+    for (uint32_t base = 0; base < E; base += 64u) {
+        uint32_t lo, hi;
+        const uint32_t behind = before + wave_prefix(group_tiles(offsets, E, R, lg, base + lane, lo, hi));
+        if (base + lane < E) {
+            table.first[base + lane + 1u] = behind;
+            table.row[base + lane] = lo;
+            if (base + lane + 1u == E) table.row[E] = hi;
+        }
+        before = lane_value(behind, 63u);
+    }
+    if (lane == 0) table.first[0] = 0;
+}
+// The group with tile number `tile` of the groups' tiles.  Uniform.
+__device__ __forceinline__ uint32_t table_group(const GroupTable& table, uint32_t E, uint32_t tile) {
+    const uint32_t lane = threadIdx.x & 63u;
+    uint32_t base = 0;
+    for (; base + 64u < E; base += 64u)
+        if (tile < (uint32_t)__builtin_amdgcn_readfirstlane((int)table.first[base + 64u])) break;
+    const uint64_t found = __ballot(tile < table.first[min(base + lane + 1u, E)]);
+    return base + (found ? (uint32_t)__builtin_ctzll(found) : 0u);
+}
+
+// What the loads of a tile need beside the operands, and where its result goes.
+struct ChainTile {
+    uint32_t steps;                       // of 256 columns, the last one maybe half
+    bool half;
+    uint32_t m0, n0, rows_a, rows_b;
+    uint32_t e;
+};
+
+template <class S>
+struct Mx4Chain : Mx4Ops<S> {
+    using B = Mx4Ops<S>;
+    uint32_t first;                       // mask of the scales of a step's first half
+
+    __device__ __forceinline__ void aim(const unsigned char* a, const unsigned char* b, const unsigned char* sa, const unsigned char* sb, uint32_t pitch,
+                                        uint32_t row_scales, uint32_t bytes, const ChainTile& t, uint32_t wm, uint32_t wn) {
+        B::a = a;
+        B::b = b;
+        B::la.init(pitch, t.rows_a);
+        B::lb.init(pitch, t.rows_b);
+        B::init_scales(sa, sb, t.rows_a, t.rows_b, row_scales, bytes / 16u, wm, wn);
+        B::steps = t.steps;
+        B::half = t.half;
+    }
+    __device__ __forceinline__ void fetch(uint32_t step, unsigned char* to) { B::fetch(min(step, B::steps - 1u), to); }
+    __device__ __forceinline__ void fetch_pair(uint32_t step, uint32_t buffer) {
+        const uint32_t word = min(step * 8u + (threadIdx.x & 3u) * 4u, B::last_word);
+        const uint32_t to = lds_number(B::scales) + buffer * B::scale_bytes + B::scale_at;
+#pragma unroll
+        for (int i = 0; i < B::NA; ++i) load_to_lds_4(B::sa, B::off_a[i] + word, to + i * S::threads * 4);
+#pragma unroll
+        for (int i = 0; i < B::NB; ++i) load_to_lds_4(B::sb, B::off_b[i] + word, to + S::BM * 16 + i * S::threads * 4);
+    }
+    // Step `step` of a tile of `steps`.
+    __device__ __forceinline__ void arrive(uint32_t step, uint32_t steps, bool half, uint32_t buffer) {
+        const unsigned char* from = B::scales + buffer * B::scale_bytes + (step & 1u) * 8u;
+#pragma unroll
+        for (int f = 0; f < S::FM; ++f) { const uint2 v = *(const uint2*)(from + B::scale_at_a + f * 512); B::ya[f][0] = v.x; B::ya[f][1] = v.y; }
+#pragma unroll
+        for (int f = 0; f < S::FN; ++f) { const uint2 v = *(const uint2*)(from + B::scale_at_b + f * 512); B::yb[f][0] = v.x; B::yb[f][1] = v.y; }
+        first = step < steps ? 0xFFFFFFFFu : 0u;
+        B::second = step < steps && !(half && step + 1u == steps) ? 0xFFFFFFFFu : 0u;
+    }
+    __device__ __forceinline__ void next() {
+#pragma unroll
+        for (int f = 0; f < S::FM; ++f) { B::xa[f][0] = (B::ya[f][0] & first) >> (8u * B::h); B::xa[f][1] = (B::ya[f][1] & B::second) >> (8u * B::h); }
+#pragma unroll
+        for (int f = 0; f < S::FN; ++f) { B::xb[f][0] = (B::yb[f][0] & first) >> (8u * B::h); B::xb[f][1] = (B::yb[f][1] & B::second) >> (8u * B::h); }
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j) B::acc[i][j] = acc16{};
+    }
+};
+
+// advance(tile): aims ops at the workgroup's next tile, false where there is none; finish(tile): stores the sums.
+template <class S, class Advance, class Finish>
+__device__ __forceinline__ void run_chain(Mx4Chain<S>& ops, unsigned char* const (&lds)[2], Advance&& advance, Finish&& finish) {
+    static_assert(S::BUFFERS == 2 && Mx4Chain<S>::scale_buffers == 2, "a tile's buffers take turns");
+    constexpr int PARTS = Mx4Ops<S>::PARTS;
+    typename Mx4Ops<S>::Frag f[2];
+    ChainTile here, there;
+    if (!advance(here)) return;
+    uint32_t pair = 0;
+    ops.fetch(0, lds[0]);
+    ops.fetch_pair(0, 0);
+    ops.fetch(1, lds[1]);
+    ops.clear();
+    wait_and_meet<Mx4Ops<S>::LOADS>();
+    ops.arrive(0, here.steps, here.half, 0);
+    ops.next();
+    ops.read(f[0], lds[0], 0);
+    // one step of `here`: the step behind it is number `then` of a tile of `steps`, and the loads are those of step `load` of the tile that ops aims at
+    const auto step = [&](auto even, uint32_t then, uint32_t steps, bool half, uint32_t load) {
+        constexpr bool EVEN = decltype(even)::value;
+        asm volatile("" : "+v"(ops.at_a), "+v"(ops.at_b));
+#pragma unroll
+        for (int p = 0; p + 1 < PARTS; ++p) {
+            ops.read(f[(p + 1) & 1], lds[EVEN ? 0 : 1], p + 1);
+            ops.multiply(f[p & 1], p);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        wait_and_meet<0>();
+        ops.arrive(then, steps, half, EVEN ? pair : pair ^ 1u);
+        ops.fetch(load, lds[EVEN ? 0 : 1]);
+        if (EVEN) ops.fetch_pair(load, pair ^ 1u);
+        ops.read(f[0], lds[EVEN ? 1 : 0], 0);
+        __builtin_amdgcn_sched_barrier(0);
+        ops.multiply(f[1], PARTS - 1);
+        ops.next();
+    };
+    for (;;) {
+        bool more = false;
+        for (uint32_t t = 0; t < here.steps; t += 2) {
+            const bool last = t + 2u >= here.steps;
+            if (last) more = advance(there);
+            const bool on = last && more;              // otherwise the loads behind the end are of this tile's last step again, and nothing uses them
+            step(std::true_type{}, t + 1u, here.steps, here.half, on ? 0u : t + 2u);
+            step(std::false_type{}, on ? 0u : t + 2u, on ? there.steps : here.steps, on ? there.half : here.half, on ? 1u : t + 3u);
+            pair ^= 1u;
+        }
+        finish(here);
+        if (!more) break;
+        ops.clear();
+        here = there;
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);             // vmcnt(0): nothing is on its way to LDS when the workgroup ends
+}
+
+// GRADIENT: D_e = A_e B_e^T over the columns of group e, tiles of each expert dealt to the XCDs; else C, tiles of the groups' rows.
+template <class S, uint32_t DT, bool GRADIENT>
+__global__ void __launch_bounds__(S::threads) k_mx4_grouped_chain(const PParams p) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds0[(S::BM + S::BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds1[(S::BM + S::BN) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char scales[Mx4Ops<S>::scale_buffers * Mx4Ops<S>::scale_bytes];
+    __shared__ GroupTable table;
+    constexpr uint32_t lg = GRADIENT ? 7 : S::BM == 64 ? 6 : S::BM == 128 ? 7 : 8;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t wm = wave / S::WN, wn = wave % S::WN;
+    if (wave == 0) fill_table(table, p.offsets, p.E, p.R, lg);
+    __syncthreads();
+    const uint32_t tiles = p.tiles_m * p.tiles_n;
+    const uint32_t all = GRADIENT ? tiles * p.E : (uint32_t)__builtin_amdgcn_readfirstlane((int)table.first[p.E]) * p.tiles_n;
+    Mx4Chain<S> ops;
+    ops.scales = scales;
+    ops.h = lane >> 5;
+    ops.at_a = wm * S::FM * 32 * kStepBytes + lane_place(lane);
+    ops.at_b = (S::BM + wn * S::FN * 32) * kStepBytes + lane_place(lane);
+    uint32_t v = blockIdx.x;
+    const auto place = [&](ChainTile& t, uint32_t& begin, uint32_t& bytes) {
+        uint32_t tm, tn;
+        if constexpr (GRADIENT) {
+            t.e = v / tiles;
+            banded_tile(tile_of_workgroup(v - t.e * tiles, tiles), p.tiles_m, p.tiles_n, tm, tn);
+            const uint32_t from = (uint32_t)__builtin_amdgcn_readfirstlane((int)table.first[t.e]);
+            const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)table.first[t.e + 1u]);
+            begin = min(from * 64u, p.row_codes);
+            bytes = min((to - from) * 64u, p.row_codes - begin);
+            t.m0 = tm * S::BM;
+            t.n0 = tn * S::BN;
+            t.rows_a = p.N - t.m0;
+            t.rows_b = p.K - t.n0;
+        } else {
+            const uint32_t tile = tile_of_workgroup(v, all);
+            t.e = table_group(table, p.E, tile / p.tiles_n);
+            const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)table.row[t.e]), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)table.row[t.e + 1u]);
+            const uint32_t from = (uint32_t)__builtin_amdgcn_readfirstlane((int)table.first[t.e]);
+            banded_tile(tile - from * p.tiles_n, (hi - lo + S::BM - 1u) >> lg, p.tiles_n, tm, tn);
+            begin = 0;
+            bytes = p.row_codes;
+            t.m0 = lo + tm * S::BM;
+            t.n0 = tn * S::BN;
+            t.rows_a = hi - t.m0;
+            t.rows_b = p.N - t.n0;
+        }
+        t.m0 = __builtin_amdgcn_readfirstlane(t.m0);
+        t.n0 = __builtin_amdgcn_readfirstlane(t.n0);
+        t.rows_a = __builtin_amdgcn_readfirstlane(t.rows_a);
+        t.rows_b = __builtin_amdgcn_readfirstlane(t.rows_b);
+        t.steps = (bytes + kStepBytes - 1u) / kStepBytes;
+        t.half = bytes % kStepBytes != 0;
+    };
+    const auto finish = [&](const ChainTile& t) {
+        if constexpr (GRADIENT) {
+            void* d = (unsigned char*)p.c + (uint64_t)t.e * p.N * p.K * (DT == QESGD_F32 ? 4u : 2u);
+            store_tile<S, DT>(ops, d, p.K, p.N, p.K, t.m0 + wm * S::FM * 32u, t.n0 + wn * S::FN * 32u, t.rows_a >= S::BM && t.rows_b >= S::BN, p.stream);
+        } else {
+            store_tile<S, DT>(ops, p.c, p.ldc, t.m0 + t.rows_a, p.N, t.m0 + wm * S::FM * 32u, t.n0 + wn * S::FN * 32u, t.rows_a >= S::BM && t.rows_b >= S::BN, p.stream);
+        }
+    };
+    if constexpr (GRADIENT) {
+        // experts without rows have no steps: their zeros come first
+        ops.clear();
+        for (; v < all; v += gridDim.x) {
+            ChainTile t;
+            uint32_t begin, bytes;
+            place(t, begin, bytes);
+            if (!bytes) finish(t);
+        }
+        v = blockIdx.x;
+    }
+    const auto advance = [&](ChainTile& t) {
+        for (; v < all; v += gridDim.x) {
+            uint32_t begin, bytes;
+            place(t, begin, bytes);
+            if (!bytes) continue;
+            const uint32_t b_row = GRADIENT ? 0u : t.e;
+            const unsigned char* b = p.b + b_row * p.b_stride;
+            ops.aim(p.a + (uint64_t)t.m0 * p.row_codes + begin, b + (uint64_t)t.n0 * p.row_codes + begin,
+                    p.a + p.a_scales + (uint64_t)t.m0 * p.row_scales + begin / 16u, b + p.b_scales + (uint64_t)t.n0 * p.row_scales + begin / 16u,
+                    p.row_codes, p.row_scales, bytes, t, wm, wn);
+            v += gridDim.x;
+            return true;
+        }
+        return false;
+    };
+    unsigned char* const buffers[2] = {lds0, lds1};
+    run_chain(ops, buffers, advance, finish);
+}
+
 // Tiles of `edge` rows that the groups make, from their mean size: half a tile more than their rows, and one at least.
 uint64_t group_tiles(const GroupProduct& a, uint64_t edge) {
     const uint64_t groups = a.E < a.R ? a.E : a.R, tiles = a.R / edge + groups / 2;
@@ -190,6 +428,22 @@ int launch_product_tiles(const GroupProduct& a, PParams& p) {
     const uint64_t groups = a.E < a.R ? a.E : a.R, tiles_m = (a.R + (S::BM - 1) * groups) / S::BM;
     if (!grid_ok(tiles_m * p.tiles_n, S::threads)) return QESGD_ERR_DIM;
     by_type(a.dtype, [&](auto t) { k_mx4_grouped_product<S, t.value><<<(uint32_t)(tiles_m * p.tiles_n), S::threads, 0, a.stream>>>(p); });
+    return launched();
+}
+
+// One workgroup a CU, as its LDS has room for.  Where it gets three tiles or more; with fewer their search costs more than it saves.  A workgroup a tile / the chain,
+// us: products of 16 experts, 32768 rows, N = K = 4096 317 / 302 (3.7 PFLOP/s), 8, 16384 169 / 163, 64, 16384, 2048, 1024 43.8 / 39.0, but 13, 9003, 1000,
+// 2049 (164 tiles) 22.9 / 25.2; gradients 8, 16384, 4096, 4096 225 / 210, but 13, 9003, 1000, 2049 (468 tiles) 37 / 42.
+constexpr uint64_t kChainTiles = 512;
+template <class S, bool GRADIENT>
+int launch_chain(const GroupProduct& a, PParams& p) {
+    const uint64_t groups = a.E < a.R ? a.E : a.R;
+    p.tiles_m = (p.N + S::BM - 1) / S::BM;
+    p.tiles_n = ((GRADIENT ? p.K : p.N) + S::BN - 1) / S::BN;
+    const uint64_t tiles = GRADIENT ? (uint64_t)p.tiles_m * p.tiles_n * a.E : (a.R + (S::BM - 1) * groups) / S::BM * p.tiles_n;
+    if (!grid_ok(tiles, S::threads)) return QESGD_ERR_DIM;
+    const uint32_t places = tiles < 256 ? (uint32_t)tiles : 256u;
+    by_type(a.dtype, [&](auto t) { k_mx4_grouped_chain<S, t.value, GRADIENT><<<places, S::threads, 0, a.stream>>>(p); });
     return launched();
 }
 
@@ -232,8 +486,10 @@ int launch_grouped_product(const GroupProduct& a) {
     switch (choose_edge([&](uint64_t edge) { return group_tiles(a, edge) * ((a.N + edge - 1) / edge); }, (double)steps)) {
         case 64: return launch_product_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
         case 128: return launch_product_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
-        default: return launch_product_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
+        default: break;
     }
+    return group_tiles(a, 256) * ((a.N + 255) / 256) > kChainTiles ? launch_chain<TileShape<2, 4, 4, 2, 2>, false>(a, p)
+                                                                  : launch_product_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
 }
 
 int launch_grouped_gradient(const GroupProduct& a) {
@@ -261,8 +517,10 @@ int launch_grouped_gradient(const GroupProduct& a) {
     switch (choose_edge([&](uint64_t edge) { return a.E * ((a.N + edge - 1) / edge) * ((a.K + edge - 1) / edge); }, steps)) {
         case 64: return launch_gradient_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
         case 128: return launch_gradient_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
-        default: return launch_gradient_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
+        default: break;
     }
+    return a.E * ((a.N + 255) / 256) * ((a.K + 255) / 256) > kChainTiles ? launch_chain<TileShape<2, 4, 4, 2, 2>, true>(a, p)
+                                                                        : launch_gradient_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
 }
 
 }  // namespace qesgd

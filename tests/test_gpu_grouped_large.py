@@ -1,0 +1,147 @@
+"""Grouped products that are large enough for workgroups with several tiles one after the other, and for streaming stores, against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import expert_reference as X
+from expert_reference import ONE, TYPES
+from test_gpu_grouped import ints, packed_noise
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1901_03040_amd import binding
+    assert torch.cuda.is_available()
+    binding.lib()
+    return binding
+
+
+def within(got, a, b, dtype):
+    """got = a b^T: n exact products added in fp32 in any order, one rounding.  a [M, n] and b [N, n] in 64 bits on the GPU."""
+    want, size = a @ b.T, a.abs() @ b.abs().T
+    limit = a.shape[1] * ONE * size + X.HALF_STEP[dtype] * want.abs() * (1 + 2.0 ** -10) + X.LEAST[dtype]
+    off = (got.double() - want).abs() - limit
+    return bool((off <= 0).all())
+
+
+def on_gpu(v):
+    return torch.from_numpy(v).cuda()
+
+
+# steps of the contraction: one half, one, two with a half, an odd number, many
+@pytest.mark.parametrize("kind", ["ragged", "even", "one", "none"])
+@pytest.mark.parametrize("n,N,K,E", [(10_000, 4100, 100, 5), (9000, 4100, 250, 3), (10_000, 4096, 300, 70), (12_000, 3900, 700, 2), (17_000, 2060, 1100, 4)])
+def test_product(B, n, N, K, E, kind):
+    dtype = list(TYPES.values())[(n + K) % 3]
+    offsets = X.group_sizes(np.random.default_rng(K), E, n, kind)
+    pa, a = packed_noise(B, n, K, 1, n + K)
+    pb, b = packed_noise(B, N, K, E, N + 2 * K)
+    pa, pb, a = pa[0].cuda(), pb.cuda(), on_gpu(a[0])
+    ws = B.alloc_workspace(B.qesgd_mx4_grouped_product_workspace_bytes(n, N, K, E))
+    out = []
+    for _ in range(2):
+        c = torch.full((n, N), 3.0, dtype=dtype, device="cuda")
+        B.qesgd_mx4_grouped_product(pa, pb, pb.stride(0), ints(offsets), E, n, N, K, c, N, workspace=ws)
+        out.append(c)
+    assert torch.equal(*out)
+    assert (c[offsets[-1]:] == 3.0).all() and (c[:offsets[0]] == 3.0).all()
+    for e in range(E):
+        lo, hi = int(offsets[e]), int(offsets[e + 1])
+        assert within(c[lo:hi], a[lo:hi], on_gpu(b[e]), dtype), e
+
+
+@pytest.mark.parametrize("kind", ["ragged", "even", "one", "none"])
+@pytest.mark.parametrize("n,N,K,E", [(1500, 3000, 2000, 7), (700, 2500, 2310, 9), (300, 1030, 1000, 40), (9000, 4096, 2300, 4)])
+def test_gradient(B, n, N, K, E, kind):
+    dtype = list(TYPES.values())[(n + N) % 3]
+    offsets = X.group_sizes(np.random.default_rng(K), E, n, kind)
+    columns = X.group_columns(n, E)
+    pa, a = packed_noise(B, N, columns, 1, n + K)
+    pb, b = packed_noise(B, K, columns, 1, N + 2 * K)
+    pa, pb, a, b = pa[0].cuda(), pb[0].cuda(), on_gpu(a[0]), on_gpu(b[0])
+    ws = B.alloc_workspace(B.qesgd_mx4_grouped_gradient_workspace_bytes(n, N, K, E))
+    out = []
+    for _ in range(2):
+        d = torch.full((E, N, K), 3.0, dtype=dtype, device="cuda")
+        B.qesgd_mx4_grouped_gradient(pa, pb, ints(offsets), E, n, N, K, d, workspace=ws)
+        out.append(d)
+    assert torch.equal(*out)
+    at = 0
+    for e in range(E):
+        wide = int(offsets[e + 1] - offsets[e] + 127) // 128 * 128
+        assert within(d[e], a[:, at:at + wide], b[:, at:at + wide], dtype), e
+        at += wide
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_streamed_results(B, dtype):
+    """Results of 192 MiB and more, in whole lines and with rows that are none."""
+    t = TYPES[dtype]
+    size = torch.empty((), dtype=t).element_size()
+    E, K = 3, 128
+    for N in (8192, 8200):
+        n = (200 << 20) // (N * size) + 77
+        offsets = X.group_sizes(np.random.default_rng(N), E, n, "ragged")
+        pa, a = packed_noise(B, n, K, 1, n)
+        pb, b = packed_noise(B, N, K, E, N)
+        c = torch.full((n, N), 3.0, dtype=t, device="cuda")
+        B.qesgd_mx4_grouped_product(pa[0].cuda(), pb.cuda(), pb.shape[1], ints(offsets), E, n, N, K, c, N)
+        a = on_gpu(a[0])
+        assert (c[offsets[-1]:] == 3.0).all()
+        for e in range(E):
+            lo, hi = int(offsets[e]), int(offsets[e + 1])
+            assert within(c[lo:hi], a[lo:hi], on_gpu(b[e]), t), (N, e)
+        del c
+    # gradients: enough experts for as much
+    N, K, n = 1024, 1024, 500
+    E = (200 << 20) // (N * K * size) + 1
+    offsets, columns = X.group_sizes(np.random.default_rng(1), E, n, "ragged"), X.group_columns(n, E)
+    pa, a = packed_noise(B, N, columns, 1, 5)
+    pb, b = packed_noise(B, K, columns, 1, 6)
+    d = torch.full((E, N, K), 3.0, dtype=t, device="cuda")
+    B.qesgd_mx4_grouped_gradient(pa[0].cuda(), pb[0].cuda(), ints(offsets), E, n, N, K, d)
+    a, b, at = on_gpu(a[0]), on_gpu(b[0]), 0
+    for e in range(E):
+        wide = int(offsets[e + 1] - offsets[e] + 127) // 128 * 128
+        assert within(d[e], a[:, at:at + wide], b[:, at:at + wide], t), e
+        at += wide
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_weighted_sum_of_many_rows(B, dtype):
+    """Calls that stream: rows of more than the memory-side cache, tokens of 128 MiB and more; and rows that are no whole lines."""
+    t = TYPES[dtype]
+    size = torch.empty((), dtype=t).element_size()
+    for N, k in ((4096, 2), (4100, 2), (512, 1)):
+        T = (300 << 20) // (N * size * k) + 5
+        n = T * k
+        g = torch.Generator(device="cuda").manual_seed(N)
+        rows, dy = torch.randn(n, N, generator=g, device="cuda").to(t), torch.randn(T, N, generator=g, device="cuda").to(t)
+        gates = torch.rand(T, k, generator=g, device="cuda")
+        slots = torch.randperm(n, generator=g, device="cuda").int()
+        slots[::13] = -1
+        out, drows, dgates = torch.empty_like(dy), torch.full_like(rows, 9.0), torch.empty_like(gates)
+        B.qesgd_combine(rows, N, n, slots, gates, T, k, N, out, N)
+        B.qesgd_combine_backward(dy, N, rows, N, n, slots, gates, T, k, N, drows, N, dgates)
+        s, half, least = slots.reshape(T, k).long(), X.HALF_STEP[t], X.LEAST[t]
+        touched = torch.zeros(n, dtype=torch.bool, device="cuda")
+        for t0 in range(0, T, 8192):
+            p = slice(t0, min(T, t0 + 8192))
+            want = torch.zeros(s[p].shape[0], N, dtype=torch.float64, device="cuda")
+            mag = torch.zeros_like(want)
+            for j in range(k):
+                there = s[p, j] >= 0
+                r = rows[s[p, j].clamp(min=0)].double() * there[:, None]
+                w, d = gates[p, j:j + 1].double(), dy[p].double()
+                want += w * r
+                mag += (w * r).abs()
+                dot, dmag = (r * d).sum(1), (r * d).abs().sum(1)
+                assert ((dgates[p, j].double() - dot).abs() <= (N + 1) * ONE * dmag).all()
+                at = s[p, j][there]
+                v = (w * d)[there]
+                assert ((drows[at].double() - v).abs() <= (half + ONE) * v.abs() * (1 + 2.0 ** -10) + least).all()
+                touched[at] = True
+            assert ((out[p].double() - want).abs() <= (k + 1) * ONE * mag + half * want.abs() * (1 + 2.0 ** -10) + least).all()
+        assert (drows[~touched] == 9.0).all()
