@@ -31,6 +31,7 @@ constexpr uint32_t kQWaves = 4, kQChunks = 2;
 
 template <uint32_t DT, bool STOCHASTIC, bool FLAT>
 __global__ void __launch_bounds__(kQWaves * 64) k_mx4_quantize(const QParams p) {
+    if (STOCHASTIC) round_down();
     const uint32_t lane = threadIdx.x & 63u;
     const uint64_t wave0 = ((uint64_t)xcd_tile(blockIdx.x, gridDim.x, p.xcd_group) * kQWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) *
                            (kQChunks * kChunk);
@@ -100,6 +101,7 @@ constexpr uint32_t kTile = 128, kBothThreads = 512;
 
 template <uint32_t DT, bool STOCHASTIC>
 __global__ void __launch_bounds__(kBothThreads) k_mx4_quantize_both(const QParams p) {
+    if (STOCHASTIC) round_down();
     typedef typename std::conditional<DT == QESGD_F32, float, unsigned short>::type elem;
     // 32 rows, then 64 bytes of room: the four blocks of a column that a quad reads at once lie in different banks
     constexpr uint32_t kRoom = 64 / sizeof(elem);

@@ -97,7 +97,10 @@ __device__ __forceinline__ uint32_t convert2(uint32_t word, uint32_t pair, float
     else return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(word, __builtin_bit_cast(f16x2, pair), scale, BYTE);
 }
 
-// Codes of eight coordinates that share the scale byte sb, as one word.  `group`: number of their Philox call.
+// From here on fp32 results that do not fit are cut off: what encode8 wants of subnormal numbers.  All else that the quantising kernels compute in fp32 is exact.
+__device__ __forceinline__ void round_down() { __builtin_amdgcn_s_setreg(1 | (2 - 1) << 11, 3); }     // the two bits of the mode register for fp32
+
+// Codes of eight coordinates that share the scale byte sb, as one word.  `group`: number of their Philox call.  STOCHASTIC: after round_down.
 template <uint32_t DT, bool STOCHASTIC>
 __device__ __forceinline__ uint32_t encode8(const Eight<DT>& x, uint32_t sb, uint64_t group, uint32_t worker, uint32_t round,
                                             uint32_t key0, uint32_t key1) {
@@ -125,11 +128,12 @@ __device__ __forceinline__ uint32_t encode8(const Eight<DT>& x, uint32_t sb, uin
         for (int i = 0; i < 8; ++i) {
             const uint32_t r = variate16(rnd, i);
             const float v = x.at(i), a = fminf(__builtin_fabsf(v) * inv, 6.0f);          // over 6 only at e = 125
-            // from 1 on the code is the exponent and the first bit of the significand (252 + code, and 252 is 4 modulo 8), and T its
-            // next 16 bits: adding r there carries into the code iff r + T >= 2^16; below, the grid is a multiple of 1/2
-            const uint32_t high = ((__float_as_uint(a) + (r << 6)) >> 22 & 7u) ^ 4u;
-            const uint32_t low = ((uint32_t)(a * 131072.0f) + r) >> 16;
-            word |= ((a < 1.0f ? low : high) | (__float_as_uint(v) >> 28 & 8u)) << (4 * i);
+            // Times the least normal number an element's code is bits 22 to 24, which above 1 are the exponent and the first bit of the significand and below,
+            // as the number is subnormal, a multiple of 1/2; T is the 16 bits under them, cut off and not rounded (see round_down), and
+            // adding r there carries into the code iff r + T >= 2^16.
+            const uint32_t code = __float_as_uint(a * 0x1p-126f) + (r << 6);
+            const uint32_t with_sign = (code & 0x01C00000u) | (__float_as_uint(v) >> 6 & ~0x01C00000u);
+            word = __builtin_amdgcn_alignbit(with_sign >> 22, word, 4);
         }
     }
     return sb == 255u ? 0u : word;

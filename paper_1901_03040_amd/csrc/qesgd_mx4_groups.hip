@@ -15,7 +15,7 @@ struct GParams {
     uint64_t ld;
     uint32_t T;
     const int32_t* order;
-    uint32_t per;
+    uint32_t per, per_factor, per_shift;          // n / per = the upper half of n * per_factor, shifted
     const int32_t* offsets;
     uint32_t E, R, cols;
     uint32_t groups;                  // of 128 columns in a row
@@ -28,10 +28,18 @@ struct GParams {
     uint32_t key0, key1, round, worker;
 };
 
-// The row of x that row r takes; T or more where there is none.
-__device__ __forceinline__ uint32_t source(const GParams& p, uint32_t r) {
-    const int32_t pair = p.order ? p.order[r] : (int32_t)r;
-    return pair < 0 ? p.T : p.per == 1 ? (uint32_t)pair : (uint32_t)pair / p.per;
+// The rows of x that rows row[i] take, p.T for a row that is none of them (in[i] false) or has none.  All of order's numbers are on their way before the first is
+// used: the loads of x wait for them once.
+template <int N>
+__device__ __forceinline__ void sources(const GParams& p, const uint32_t (&row)[N], const bool (&in)[N], uint32_t (&out)[N]) {
+    int32_t pair[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) pair[i] = p.order ? p.order[min(row[i], p.R - 1u)] : (int32_t)row[i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t n = (uint32_t)pair[i], q = p.per == 1u ? n : __umulhi(n, p.per_factor) >> p.per_shift;
+        out[i] = in[i] && pair[i] >= 0 ? min(q, p.T) : p.T;
+    }
 }
 
 // Along the rows: a lane owns 8 consecutive slots of the padded matrix, a quad a block, a wave kGChunks chunks of 512.
@@ -39,25 +47,37 @@ constexpr uint32_t kGWaves = 4, kGChunks = 2;
 
 template <uint32_t DT, bool STOCHASTIC>
 __global__ void __launch_bounds__(kGWaves * 64) k_mx4_group_rows(const GParams p) {
+    if (STOCHASTIC) round_down();
     const uint32_t lane = threadIdx.x & 63u;
     const uint32_t begin = held(p.offsets[0], p.R), end = held(p.offsets[p.E], p.R);
     const uint64_t wave0 = ((uint64_t)blockIdx.x * kGWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * (kGChunks * kChunk);
-    const uint32_t group0 = (uint32_t)(wave0 >> 7);
-    Eight<DT> v[kGChunks];
+    const uint32_t group0 = (uint32_t)(wave0 >> 7), row0 = group0 / p.groups;                // uniform
+    if (row0 >= end) return;
+    uint32_t row[kGChunks], col[kGChunks], from[kGChunks];
     bool in[kGChunks];
 #pragma unroll
     for (uint32_t c = 0; c < kGChunks; ++c) {
-        const uint32_t group = group0 + c * 4u + (lane >> 4), row = group / p.groups;
-        const uint32_t col = (group - row * p.groups) * 128u + (lane & 15u) * 8u;
-        in[c] = row >= begin && row < end;
-        uint32_t n = 0;
-        uint64_t from = 0;
-        if (in[c]) {
-            const uint32_t s = source(p, row);
-            n = s >= p.T || col >= p.cols ? 0u : min(p.cols - col, 8u);
-            from = s * p.ld + col;
+        // the wave's 4 kGChunks groups of 128 end at most so many rows
+        uint32_t r = row0, g = group0 - row0 * p.groups + c * 4u + (lane >> 4);
+        if (p.groups >= 4u * kGChunks) {
+            const uint32_t over = g >= p.groups ? 1u : 0u;
+            r += over;
+            g -= over ? p.groups : 0u;
+        } else {
+            const uint32_t more = g / p.groups;
+            r += more;
+            g -= more * p.groups;
         }
-        v[c].load(p.x, from, n);
+        row[c] = r;
+        col[c] = g * 128u + (lane & 15u) * 8u;
+        in[c] = r >= begin && r < end;
+    }
+    sources(p, row, in, from);
+    Eight<DT> v[kGChunks];
+#pragma unroll
+    for (uint32_t c = 0; c < kGChunks; ++c) {
+        const uint32_t n = from[c] >= p.T || col[c] >= p.cols ? 0u : min(p.cols - col[c], 8u);
+        v[c].load(p.x, n ? from[c] * p.ld + col[c] : 0u, n);
     }
 #pragma unroll
     for (uint32_t c = 0; c < kGChunks; ++c) {
@@ -78,6 +98,7 @@ constexpr uint32_t kTile = 128, kBothThreads = 512;
 
 template <uint32_t DT, bool STOCHASTIC>
 __global__ void __launch_bounds__(kBothThreads) k_mx4_group_both(const GParams p) {
+    if (STOCHASTIC) round_down();
     typedef typename std::conditional<DT == QESGD_F32, float, unsigned short>::type elem;
     // 32 rows, then 64 bytes of room: the four blocks of a column that a quad reads at once lie in different banks
     constexpr uint32_t kRoom = 64 / sizeof(elem);
@@ -89,12 +110,19 @@ __global__ void __launch_bounds__(kBothThreads) k_mx4_group_both(const GParams p
     const uint32_t r0 = g.lo + (tr - g.first) * kTile, c0 = tc * kTile;
     const uint32_t col = (lane & 15u) * 8u;
     const uint32_t n = c0 + col >= p.cols ? 0u : min(p.cols - c0 - col, 8u);
+    uint32_t rows[4], from_row[4];
+    bool in[4];
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+        rows[i] = r0 + i * 32u + wave * 4u + (lane >> 4);
+        in[i] = rows[i] < g.hi;
+    }
+    sources(p, rows, in, from_row);
     Eight<DT> v[4];
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
-        const uint32_t row = r0 + i * 32u + wave * 4u + (lane >> 4);
-        const uint32_t s = row < g.hi ? source(p, row) : p.T;
-        v[i].load(p.x, s < p.T ? s * p.ld + c0 + col : 0u, s < p.T ? n : 0u);
+        const bool there = from_row[i] < p.T && n;
+        v[i].load(p.x, there ? from_row[i] * p.ld + c0 + col : 0u, there ? n : 0u);
     }
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
@@ -166,6 +194,11 @@ int launch_quantize_groups(const GroupQuantize& a) {
     p.T = (uint32_t)a.T;
     p.order = a.order;
     p.per = a.per;
+    // for numbers up to 2^31 (Granlund and Montgomery's division by a constant)
+    uint32_t log = 0;
+    while ((1u << log) < a.per) ++log;
+    p.per_factor = (uint32_t)((1ull << (31u + log)) / a.per + 1u);
+    p.per_shift = log ? log - 1u : 0u;
     p.offsets = a.offsets;
     p.E = a.E;
     p.R = (uint32_t)a.R;
