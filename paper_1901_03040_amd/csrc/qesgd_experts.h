@@ -117,6 +117,14 @@ struct VectorProduct {
 size_t vector_product_workspace(const VectorProduct& a);
 int launch_vector_product(const VectorProduct& a);
 
+// n / d for n < 2^31 as the upper half of n * factor, shifted, d >= 2 (Granlund and Montgomery's division by a constant).
+inline void divide_by(uint32_t d, uint32_t& factor, uint32_t& shift) {
+    uint32_t log = 0;
+    while ((1u << log) < d) ++log;
+    factor = (uint32_t)((1ull << (31u + log)) / d + 1u);
+    shift = log ? log - 1u : 0u;
+}
+
 inline uint64_t grouped_columns(uint64_t R, uint64_t E) { return (R + (kMx4Pad - 1) * (E < R ? E : R)) / kMx4Pad * kMx4Pad; }
 
 }  // namespace qesgd

@@ -64,6 +64,22 @@ struct Eight {
             return half_bits<DT>(max((uint32_t)m[0], (uint32_t)m[1]));
         }
     }
+    // From element `from` on; zeros where there is none.
+    __device__ __forceinline__ void load_whole(const void* x, uint64_t from, bool there) {
+        if constexpr (DT == QESGD_F32) {
+            vec4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
+            if (there) {
+                const float* p = (const float*)x + from;
+                a = *(const vec4_any*)p;
+                b = *(const vec4_any*)(p + 4);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+        } else {
+            v = uvec4{0, 0, 0, 0};
+            if (there) v = *(const uvec4_any*)((const unsigned short*)x + from);
+        }
+    }
     // From element `from` on, of which the first n (0..8) exist; the others are 0.
     __device__ __forceinline__ void load(const void* x, uint64_t from, uint32_t n) {
         if constexpr (DT == QESGD_F32) {

@@ -194,11 +194,7 @@ int launch_quantize_groups(const GroupQuantize& a) {
     p.T = (uint32_t)a.T;
     p.order = a.order;
     p.per = a.per;
-    // for numbers up to 2^31 (Granlund and Montgomery's division by a constant)
-    uint32_t log = 0;
-    while ((1u << log) < a.per) ++log;
-    p.per_factor = (uint32_t)((1ull << (31u + log)) / a.per + 1u);
-    p.per_shift = log ? log - 1u : 0u;
+    divide_by(a.per, p.per_factor, p.per_shift);
     p.offsets = a.offsets;
     p.E = a.E;
     p.R = (uint32_t)a.R;

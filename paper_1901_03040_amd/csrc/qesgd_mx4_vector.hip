@@ -25,7 +25,7 @@ struct VParams {
     uint64_t ld;
     uint32_t T;
     const int32_t* order;
-    uint32_t per;
+    uint32_t per, per_factor, per_shift;
     const unsigned char* w;
     uint64_t w_stride, scales_off;
     const int32_t* offsets;
@@ -52,7 +52,30 @@ __device__ __forceinline__ void put_row(void* y, uint64_t at, float v) {
 // The upper 16 bits of v: a bf16 number no larger than v, so that nothing overflows.
 __device__ __forceinline__ uint32_t upper(float v) { return __float_as_uint(v) & 0xFFFF0000u; }
 
-// Eight elements as PARTS times eight bf16 numbers, the largest parts first.  Infinities and NaN are whole in the first one.
+// An element as PARTS bf16 numbers, each in the upper half of a word, the largest part first.  Infinities and NaN are whole in the first one.
+template <uint32_t DT, uint32_t PARTS>
+__device__ __forceinline__ void split_one(float x, uint32_t (&part)[PARTS]) {
+    if constexpr (PARTS == 1) {
+        part[0] = __float_as_uint(x);                          // is one already
+    } else {
+        const bool fine = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+        float v = x;
+#pragma unroll
+        for (uint32_t q = 0; q < PARTS; ++q) {
+            part[q] = upper(v);
+            v = fine ? v - __uint_as_float(part[q]) : 0.0f;
+        }
+        part[0] = x != x ? 0x7FC00000u : part[0];
+    }
+}
+template <uint32_t DT>
+__device__ __forceinline__ float element_at(const void* x, uint64_t at) {
+    if (DT == QESGD_F32) return ((const float*)x)[at];
+    if (DT == QESGD_BF16) return __uint_as_float((uint32_t)((const unsigned short*)x)[at] << 16);
+    return (float)((const _Float16*)x)[at];
+}
+
+// Eight elements as PARTS times eight bf16 numbers.
 template <uint32_t DT, uint32_t PARTS>
 __device__ __forceinline__ void split(const Eight<DT>& x, uvec4 (&out)[PARTS]) {
     if constexpr (DT == QESGD_BF16) {
@@ -60,24 +83,11 @@ __device__ __forceinline__ void split(const Eight<DT>& x, uvec4 (&out)[PARTS]) {
     } else {
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
-            uint32_t part[2][PARTS];
+            uint32_t low[PARTS], high[PARTS];
+            split_one<DT, PARTS>(x.at(2 * i), low);
+            split_one<DT, PARTS>(x.at(2 * i + 1), high);
 #pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) {
-                float v = x.at(2 * i + h);
-                const bool fine = (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u;
-#pragma unroll
-                for (uint32_t q = 0; q < PARTS; ++q) {
-                    part[h][q] = upper(v);
-                    v = v - __uint_as_float(part[h][q]);
-                }
-                if (!fine) {
-                    part[h][0] = x.at(2 * i + h) != x.at(2 * i + h) ? 0x7FC00000u : part[h][0];
-#pragma unroll
-                    for (uint32_t q = 1; q < PARTS; ++q) part[h][q] = 0u;
-                }
-            }
-#pragma unroll
-            for (uint32_t q = 0; q < PARTS; ++q) out[q][i] = part[0][q] >> 16 | part[1][q];
+            for (uint32_t q = 0; q < PARTS; ++q) out[q][i] = low[q] >> 16 | high[q];
         }
     }
 }
@@ -134,36 +144,46 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
 #pragma unroll
         for (uint32_t m = 0; m < TILES; ++m) acc[m] = acc4{0.0f, 0.0f, 0.0f, 0.0f};
         for (uint32_t c0 = 0; c0 < steps * 128u; c0 += p.part_columns) {
-            const uint32_t here = min(p.part_columns, steps * 128u - c0), eights = here / 8u, last = here / 128u;
+            const uint32_t here = min(p.part_columns, steps * 128u - c0), last = here / 128u;
             // the wave's first blocks are on their way while the rows are brought in
             uvec4 c[2 * kVBatch], next_c[2 * kVBatch];
             uint32_t byte[2 * kVBatch], next_byte[2 * kVBatch];
             fetch(c, byte, c0 / 128u, 2u * share, last);
             __syncthreads();
-            // some pieces a thread on their way at a time, as the registers allow
-            constexpr uint32_t kPieces = DT == QESGD_F32 && kVWaves == 16 ? 2 : 4;
-            for (uint32_t i0 = threadIdx.x; i0 < rows * eights; i0 += kPieces * kVWaves * 64u) {
+            // whole pieces of eight, some of a thread's on their way at a time, and then the elements that are left and zeros behind them
+            const uint32_t filled = p.K > c0 ? min(here, p.K - c0) : 0u, whole = filled / 8u;
+            const auto source = [&](uint32_t r) {
+                const int32_t pair = p.order ? p.order[r0 + r] : (int32_t)(r0 + r);
+                return pair < 0 ? p.T : p.per == 1u ? (uint32_t)pair : __umulhi((uint32_t)pair, p.per_factor) >> p.per_shift;
+            };
+            constexpr uint32_t kPieces = kVWaves == 8 ? 1 : DT == QESGD_BF16 ? 4 : 2;
+            for (uint32_t i0 = threadIdx.x; i0 < rows * whole; i0 += kPieces * kVWaves * 64u) {
                 Eight<DT> v[kPieces];
                 uint32_t to[kPieces];
 #pragma unroll
                 for (uint32_t q = 0; q < kPieces; ++q) {
                     const uint32_t i = i0 + q * (kVWaves * 64u);
-                    if (i >= rows * eights) break;
-                    const uint32_t r = i / eights, col = (i - r * eights) * 8u;
-                    const int32_t pair = p.order ? p.order[r0 + r] : (int32_t)(r0 + r);
-                    const uint32_t s = pair < 0 ? p.T : p.per == 1 ? (uint32_t)pair : (uint32_t)pair / p.per;
-                    const uint32_t n = s >= p.T || c0 + col >= p.K ? 0u : min(p.K - c0 - col, 8u);
-                    v[q].load(p.x, n ? s * p.ld + c0 + col : 0u, n);
+                    if (i >= rows * whole) break;
+                    const uint32_t r = i / whole, col = (i - r * whole) * 8u, s = source(r);
+                    v[q].load_whole(p.x, s < p.T ? s * p.ld + c0 + col : 0u, s < p.T);
                     to[q] = r * PARTS * pitch + col * 2u;
                 }
 #pragma unroll
                 for (uint32_t q = 0; q < kPieces; ++q) {
-                    if (i0 + q * (kVWaves * 64u) >= rows * eights) break;
+                    if (i0 + q * (kVWaves * 64u) >= rows * whole) break;
                     uvec4 parts[PARTS];
                     split<DT, PARTS>(v[q], parts);
 #pragma unroll
                     for (uint32_t h = 0; h < PARTS; ++h) *(uvec4*)(rows_lds + to[q] + h * pitch) = parts[h];
                 }
+            }
+            const uint32_t rest = here - whole * 8u;
+            for (uint32_t i = threadIdx.x; i < rows * rest; i += kVWaves * 64u) {
+                const uint32_t r = i / rest, col = whole * 8u + i - r * rest, s = source(r);
+                uint32_t part[PARTS];
+                split_one<DT, PARTS>(col < filled && s < p.T ? element_at<DT>(p.x, s * p.ld + c0 + col) : 0.0f, part);
+#pragma unroll
+                for (uint32_t h = 0; h < PARTS; ++h) *(unsigned short*)(rows_lds + (r * PARTS + h) * pitch + col * 2u) = (unsigned short)(part[h] >> 16);
             }
             __syncthreads();
             // rows of the instruction beyond those there are read the last one: what comes of them is not stored
@@ -230,6 +250,7 @@ int launch_vector_product(const VectorProduct& a) {
     p.T = (uint32_t)a.T;
     p.order = a.order;
     p.per = a.per;
+    divide_by(a.per, p.per_factor, p.per_shift);
     p.w = a.w;
     p.w_stride = a.w_stride;
     p.scales_off = W.scales_off;
@@ -250,8 +271,8 @@ int launch_vector_product(const VectorProduct& a) {
     while (tiles < parts && tiles * 16 / parts < rows) ++tiles;
     const uint32_t at_a_time = tiles * 16 / parts;
     const uint32_t lds_rows = parts * (a.R < at_a_time ? (uint32_t)a.R : at_a_time);
-    // Workgroups of 8 waves, two on a CU, where there is little to bring into LDS, else of 16, which bring it in faster.  8 / 16 waves, us, graph of 32 calls: one row
-    // x 4096 x 4096 bf16 5.5 / 5.8, f32 6.2 / 8.7, x 512 x 512 f32 3.9 / 6.3; 8 rows bf16 8.7 / 7.2, 16 rows f32 26.6 / 21.8, 4 rows x 4096 x 25088
+    // Workgroups of 8 waves, two or three on a CU, where there is little to bring into LDS, else of 16, which bring it in faster.  8 / 16 waves, us, graph of 32 calls: one row
+    // x 4096 x 4096 bf16 5.5 / 5.8, f32 6.2 / 8.7, x 512 x 512 f32 3.9 / 6.3; 8 rows bf16 8.7 / 7.1, 16 rows f32 26.6 / 17.4, 4 rows x 4096 x 25088
     // bf16 28.9 / 21.5.  And as many waves to a row of W as make kVWavesFew or kVWavesMany of them, beyond which each has more steps instead: 12 tokens x 4 of 64
     // experts 1411 x 2049 with two waves a row 21.3, with one 18.4; one row x 8192 x 8192 bf16 13.1 with 8, 15.9 with 16.
     constexpr uint32_t kVWavesFew = 2048, kVWavesMany = 4096;
