@@ -43,7 +43,7 @@ __device__ __forceinline__ void put_element(void* x, uint64_t at, float v) {
 }
 
 // A logit as the choice compares it: a NaN as infinity.
-__device__ __forceinline__ float compared(float v) { return v != v ? INFINITY : v; }
+__device__ __forceinline__ float compared(float v) { return __builtin_fminf(v, INFINITY); }
 
 // Over L lanes (8 .. 64): each step combines halves that hold the same number, so mirrors do for the middle ones.
 template <int L, class F>
@@ -56,7 +56,7 @@ __device__ __forceinline__ uint32_t over_lanes(uint32_t v, F f) {
     if (L >= 64) { const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false); v = f(r[0], r[1]); }
     return v;
 }
-__device__ __forceinline__ float larger(float a, float b) { return a > b ? a : b; }            // of numbers that are none of them NaN
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }            // of numbers that are none of them NaN
 template <int L>
 __device__ __forceinline__ float most(float v) {
     return __uint_as_float(over_lanes<L>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(larger(__uint_as_float(a), __uint_as_float(b))); }));
@@ -79,19 +79,23 @@ __device__ __forceinline__ float exp_below(float x) {
     return x < -104.0f ? 0.0f : __builtin_fmaf(r, rest * 0.693147181f, r);       // also -infinity, which has no rest
 }
 
+// A token's logits, expert c * L + l, from element `from` on; behind the last one as closed ones.  All are loaded without asking, the last one more than once.
+template <uint32_t DT, int L, int C>
+__device__ __forceinline__ void load_logits(const void* x, uint64_t from, uint32_t E, uint32_t l, float (&v)[C]) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) v[c] = element<DT>(x, from + min((uint32_t)c * L + l, E - 1u));
+#pragma unroll
+    for (int c = 0; c < C; ++c) v[c] = (uint32_t)c * L + l < E ? compared(v[c]) : -INFINITY;
+}
+
 // One token in L lanes, C logits each: expert c * L + l.  Lane j of them (j < k) ends with choice j in `expert` (-1: none) and `gate`.
 template <uint32_t DT, int L, int C>
 __device__ __forceinline__ void choose(const RParams& p, uint64_t t, uint32_t l, int32_t& expert, float& gate) {
     float v[C];
     float best = -INFINITY;
+    load_logits<DT, L, C>(p.logits, t * p.ld, p.E, l, v);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const uint32_t e = (uint32_t)c * L + l;
-        v[c] = e < p.E ? element<DT>(p.logits, t * p.ld + e) : -INFINITY;
-    }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        v[c] = compared(v[c]);
         best = larger(v[c], best);
     }
     float high = most<L>(best);
@@ -387,14 +391,9 @@ __global__ void __launch_bounds__(256) k_route_backward(const BParams p) {
     }
     if (p.all) {
         float high = -INFINITY;
+        load_logits<DT, L, C>(p.logits, t * p.ld, p.E, l, x);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const uint32_t e = (uint32_t)c * L + l;
-            x[c] = e < p.E ? element<DT>(p.logits, t * p.ld + e) : -INFINITY;
-        }
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            x[c] = compared(x[c]);
             high = larger(x[c], high);
         }
         high = most<L>(high);
