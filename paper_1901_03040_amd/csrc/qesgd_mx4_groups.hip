@@ -2,6 +2,9 @@
 //
 // The form along a group's rows is what a contraction over the group needs: group e's columns begin at a multiple of 128 (of 64 bytes of
 // codes, of four scales), so the product walks whole blocks and no block holds rows of two experts.
+//
+// A row goes to k experts and is read k times, from the memory-side cache where x fits it.  16384 tokens x 2 x 4096 bf16 along the rows 47 us (54 beside other work)
+// = 340 MB at 7.2 TB/s; 8192 x 2, both forms, 36 us nearest and 73 stochastic, which is its arithmetic (two Philox calls for 8 elements).
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_launch.h"
@@ -43,6 +46,7 @@ __device__ __forceinline__ void sources(const GParams& p, const uint32_t (&row)[
 }
 
 // Along the rows: a lane owns 8 consecutive slots of the padded matrix, a quad a block, a wave kGChunks chunks of 512.
+// One, two and four chunks a wave: 52 / 47 / 49 us there, stochastic 90 / 80 / 77.
 constexpr uint32_t kGWaves = 4, kGChunks = 2;
 
 template <uint32_t DT, bool STOCHASTIC>

