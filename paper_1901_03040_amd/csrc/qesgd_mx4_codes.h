@@ -139,17 +139,25 @@ __device__ __forceinline__ uint32_t encode8(const Eight<DT>& x, uint32_t sb, uin
     } else {
         uint32_t rnd[4];
         philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), worker, round, key0, key1, rnd);
-        const float inv = __uint_as_float((254u - sb) << 23);              // 2^-e
+        // Times 2^-126, the least normal number, an element's code is bits 22 to 24, which above 1 are the exponent and the first bit of the significand and
+        // below, as the number is subnormal, a multiple of 1/2; T is the 16 bits under them, cut off and not rounded (see round_down),
+        // and adding r there carries into the code iff r + T >= 2^16.
+        const auto append = [&](float v, uint32_t r) {
+            const uint32_t code = __float_as_uint(v) + (r << 6);
+            word = __builtin_amdgcn_alignbit(word, (code & 0x80000000u) | (code << 6 & ~0x80000000u), 28);         // the sign and those bits behind the word
+        };
+        const float inv = __builtin_ldexpf(1.0f, 1 - (int)sb);             // 2^-e 2^-126, a subnormal number from e = 1 on
+        if (__builtin_expect(__ballot(sb > 150u) == 0, 1)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t r = variate16(rnd, i);
-            const float v = x.at(i), a = fminf(__builtin_fabsf(v) * inv, 6.0f);          // over 6 only at e = 125
-            // Times the least normal number an element's code is bits 22 to 24, which above 1 are the exponent and the first bit of the significand and below,
-            // as the number is subnormal, a multiple of 1/2; T is the 16 bits under them, cut off and not rounded (see round_down), and
-            // adding r there carries into the code iff r + T >= 2^16.
-            const uint32_t code = __float_as_uint(a * 0x1p-126f) + (r << 6);
-            const uint32_t with_sign = (code & 0x01C00000u) | (__float_as_uint(v) >> 6 & ~0x01C00000u);
-            word = __builtin_amdgcn_alignbit(with_sign >> 22, word, 4);
+            for (int i = 7; i >= 0; --i) append(x.at(i) * inv, variate16(rnd, i));
+        } else {
+            // beyond e = 23 that is too small for a number; and where e stays at 125, what lies over 6 ends there
+            const float by = __uint_as_float((254u - sb) << 23);
+#pragma unroll
+            for (int i = 7; i >= 0; --i) {
+                const float v = x.at(i);
+                append(__builtin_copysignf(fminf(__builtin_fabsf(v) * by, 6.0f) * 0x1p-126f, v), variate16(rnd, i));
+            }
         }
     }
     return sb == 255u ? 0u : word;

@@ -8,7 +8,7 @@
 // first places, and inside a block a pair finds the earlier ones of its expert by comparing the bits of the experts' numbers across the wave.  Only
 // integers are counted, so the result is the same however the work falls.
 //
-// Measured: one token of 64 experts 3.7 us, 8192 tokens of 64 bf16 4.9 + 4.9 us (choice, places), which is launches and chains of trips to memory; 160001 of 257 f32, six each,
+// Measured: one token of 64 experts 3.7 us, 8192 tokens of 64 bf16 7.7 us (choice and places), which is launches and chains of trips to memory; 160001 of 257 f32, six each,
 // 60 (choice: 165 MB, vector instructions, a third of them to find the largest six times) + 12.5 + 14 us, gradient 68 us = 4.8 TB/s.
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
@@ -133,8 +133,9 @@ __device__ __forceinline__ void choose(const RParams& p, uint64_t t, uint32_t l,
     gate = open ? part / sum : 0.0f;
 }
 
-// Blocks of 64 tokens: with 626 tokens of a wave each in turn 160001 tokens took 576 us to choose.
-constexpr uint32_t kChooseWaves = 4, kBlockTokens = 64;
+// Blocks of 64 tokens, all at once where 16 lanes take one; a wave that takes many in turn waits for each one's logits.  With 4 / 8 / 16 waves a block, both launches: 8192
+// tokens of 64 experts 9.0 / 8.0 / 7.7 us, 2048 of 512 29.5 / 20.5 / 17.5, 160001 of 257 76 / 79 / 77.
+constexpr uint32_t kChooseWaves = 16, kBlockTokens = 64;
 
 // The choices of a block of tokens and how many pairs each expert has there.
 template <uint32_t DT, int L, int C>
@@ -273,6 +274,7 @@ __device__ __forceinline__ void place(const RParams& p, uint64_t first, uint32_t
 template <uint32_t WAVES>
 __device__ __forceinline__ uint32_t share_of(uint32_t n) { return (((n + WAVES - 1u) / WAVES) + 63u) & ~63u; }
 
+constexpr uint64_t kRouteScan = 64;
 constexpr uint32_t kPlaceWaves = 4, kPlaceTurns = kBlockTokens * QESGD_MAX_CHOICES / (kPlaceWaves * 64);
 
 // A block's pairs to their places.  SCANNED: counts holds what k_route_scan makes of it; otherwise every workgroup adds up the blocks for itself, its
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(kPlaceWaves * 64) k_route_place(const RParams 
     for (uint32_t e = threadIdx.x; e < p.E; e += threads) whole[e] = SCANNED ? p.totals[e] : 0u;
     __syncthreads();
     if (!SCANNED) {
-        uint32_t across = 64;
+        uint32_t across = 4;
         while (across < p.E && across < threads) across *= 2;
         const uint32_t part = threadIdx.x / across, parts = threads / across;
         for (uint32_t e = threadIdx.x % across; e < p.E; e += across) {
@@ -448,11 +450,15 @@ void by_experts(uint32_t E, F&& f) {
 #undef QESGD_LANES
 }
 
-// Where one workgroup does all of it: up to two tokens for every 16 lanes.  256 tokens of 64 experts, 8 each, took 14.3 us so and 12.4 us in two launches.
+// Where one workgroup does all of it: up to two tokens for every 16 lanes.  256 tokens of 64 experts, 8 each, took 14.3 us so and 9.0 us in two launches.
 bool route_small(uint64_t T, uint32_t E, uint32_t k) { return T * k <= kSmallPairs && T <= 128; }
 uint64_t route_blocks(uint64_t T) { return (T + kBlockTokens - 1) / kBlockTokens; }
-// Where every block adding up the counts of all would read more than a launch costs.
-bool route_scanned(uint64_t blocks, uint32_t E) { return blocks * E > 16384; }
+// Where every block would have to add up the counts of so many that its threads make more than two turns of 32.
+bool route_scanned(uint64_t blocks, uint32_t E) {
+    uint64_t across = 4;
+    while (across < E && across < kPlaceWaves * 64) across *= 2;
+    return blocks * across * ((E + across - 1) / across) > kRouteScan * kPlaceWaves * 64;
+}
 
 }  // namespace
 
