@@ -482,12 +482,13 @@ def qesgd_orthogonal_update(g, rows, cols, n, momentum_inout, mu, nesterov, coef
 
 # ---- layers of experts ------------------------------------------------------
 #
-# The same checks as above.  experts, offsets, order and slots are int32, gates and their gradients fp32, all contiguous.
+# The same checks as above.  experts, offsets, order and slots are int32, gates and their gradients fp32, all contiguous.  These calls have five to eight tensors each: what is
+# contiguous, of the right type and long enough, as nearly all are, is seen in line, and the functions below look at the rest (a function for each tensor: 0.1 us more for each).
 
-_I32 = torch.int32
+_I32, _F32 = torch.int32, torch.float32
 
 
-def _i32(where: str, device, t, count):
+def _ints(where: str, device, t, count):
     """Address of a contiguous int32 tensor of at least `count` elements."""
     if t.get_device() != device:
         _elsewhere(where, t)
@@ -500,11 +501,11 @@ def _i32(where: str, device, t, count):
     return t.data_ptr()
 
 
-def _rows(where: str, device, t, dtype, rows, ld, cols):
-    """Address of `rows` rows of `cols` elements, ld apart, in the type of that code."""
+def _rows(where: str, device, t, kind, rows, ld, cols):
+    """Address of `rows` rows of `cols` elements of that type, ld apart."""
     if t.get_device() != device:
         _elsewhere(where, t)
-    if DTYPES.get(t.dtype) != dtype:
+    if t.dtype is not kind:
         raise QesgdError(ERR_DTYPE, where)
     if not t.is_contiguous() or t.numel() < (rows - 1) * ld + cols:
         _view(where, t, (rows, ld), (cols, 1))
@@ -516,52 +517,65 @@ def qesgd_route_workspace_bytes(T: int, E: int, k: int) -> int:
 
 
 def qesgd_route(logits, ld, T, E, k, gate_kind, experts, gates, offsets, order, slots, workspace=None, stream=None):
-    where = "qesgd_route"
+    where, kind, pairs = "qesgd_route", logits.dtype, T * k
     dtype = _dtype(logits, where)
     device, stream = _here(where, stream, logits)
-    x = _rows(where, device, logits, dtype, T, ld, E)
-    pairs = T * k
-    g, = _f32(where, device, pairs, gates)
-    ws, ws_bytes = _ws(where, device, workspace)
-    rc = (_lib or lib()).qesgd_route(x, dtype, ld, T, E, k, gate_kind, _i32(where, device, experts, pairs), g, _i32(where, device, offsets, E + 1),
-                                     _i32(where, device, order, pairs), _i32(where, device, slots, pairs), ws, ws_bytes, stream)
+    x = logits.data_ptr() if logits.is_contiguous() and logits.numel() >= (T - 1) * ld + E else _rows(where, device, logits, kind, T, ld, E)
+    e = experts.data_ptr() if experts.dtype is _I32 and experts.get_device() == device and experts.is_contiguous() and experts.numel() >= pairs \
+        else _ints(where, device, experts, pairs)
+    g = gates.data_ptr() if gates.dtype is _F32 and gates.get_device() == device and gates.is_contiguous() and gates.numel() >= pairs \
+        else _f32(where, device, pairs, gates)[0]
+    f = offsets.data_ptr() if offsets.dtype is _I32 and offsets.get_device() == device and offsets.is_contiguous() and offsets.numel() > E \
+        else _ints(where, device, offsets, E + 1)
+    o = order.data_ptr() if order.dtype is _I32 and order.get_device() == device and order.is_contiguous() and order.numel() >= pairs \
+        else _ints(where, device, order, pairs)
+    s = slots.data_ptr() if slots.dtype is _I32 and slots.get_device() == device and slots.is_contiguous() and slots.numel() >= pairs \
+        else _ints(where, device, slots, pairs)
+    ws, ws_bytes = (None, 0) if workspace is None else _ws(where, device, workspace)
+    rc = (_lib or lib()).qesgd_route(x, dtype, ld, T, E, k, gate_kind, e, g, f, o, s, ws, ws_bytes, stream)
     if rc:
         raise QesgdError(rc, where)
 
 
 def qesgd_route_backward(logits, ld, T, E, k, gate_kind, experts, gates, dgates, dlogits, ld_d, stream=None):
-    where = "qesgd_route_backward"
+    where, kind, pairs = "qesgd_route_backward", dlogits.dtype, T * k
     dtype = _dtype(dlogits, where)
     device, stream = _here(where, stream, dlogits)
-    x = None if logits is None else _rows(where, device, logits, dtype, T, ld, E)
-    g, dg = _f32(where, device, T * k, gates, dgates)
-    rc = (_lib or lib()).qesgd_route_backward(x, dtype, ld, T, E, k, gate_kind, _i32(where, device, experts, T * k), g, dg,
-                                              _rows(where, device, dlogits, dtype, T, ld_d, E), ld_d, stream)
+    x = None if logits is None else _rows(where, device, logits, kind, T, ld, E)
+    g, dg = _f32(where, device, pairs, gates, dgates)
+    rc = (_lib or lib()).qesgd_route_backward(x, dtype, ld, T, E, k, gate_kind, _ints(where, device, experts, pairs), g, dg,
+                                              _rows(where, device, dlogits, kind, T, ld_d, E), ld_d, stream)
     if rc:
         raise QesgdError(rc, where)
 
 
 def qesgd_combine(rows, ld, R, slots, gates, T, k, N, out, ld_out, stream=None):
-    where = "qesgd_combine"
+    where, kind, pairs = "qesgd_combine", out.dtype, T * k
     dtype = _dtype(out, where)
     device, stream = _here(where, stream, out)
-    s = None if slots is None else _i32(where, device, slots, T * k)
-    g, = _f32(where, device, T * k, gates)
-    rc = (_lib or lib()).qesgd_combine(_rows(where, device, rows, dtype, R, ld, N), dtype, ld, R, s, g, T, k, N,
-                                       _rows(where, device, out, dtype, T, ld_out, N), ld_out, stream)
+    x = rows.data_ptr() if rows.dtype is kind and rows.get_device() == device and rows.is_contiguous() and rows.numel() >= (R - 1) * ld + N \
+        else _rows(where, device, rows, kind, R, ld, N)
+    y = out.data_ptr() if out.is_contiguous() and out.numel() >= (T - 1) * ld_out + N else _rows(where, device, out, kind, T, ld_out, N)
+    s = None if slots is None else slots.data_ptr() if slots.dtype is _I32 and slots.get_device() == device and slots.is_contiguous() and \
+        slots.numel() >= pairs else _ints(where, device, slots, pairs)
+    g = None if gates is None else gates.data_ptr() if gates.dtype is _F32 and gates.get_device() == device and gates.is_contiguous() and \
+        gates.numel() >= pairs else _f32(where, device, pairs, gates)[0]
+    rc = (_lib or lib()).qesgd_combine(x, dtype, ld, R, s, g, T, k, N, y, ld_out, stream)
     if rc:
         raise QesgdError(rc, where)
 
 
 def qesgd_combine_backward(dy, ld_dy, rows, ld, R, slots, gates, T, k, N, drows, ld_d, dgates, stream=None):
-    where = "qesgd_combine_backward"
+    where, kind, pairs = "qesgd_combine_backward", dy.dtype, T * k
     dtype = _dtype(dy, where)
     device, stream = _here(where, stream, dy)
-    s = None if slots is None else _i32(where, device, slots, T * k)
-    g, dg = _f32(where, device, T * k, gates, dgates)
-    x = None if rows is None else _rows(where, device, rows, dtype, R, ld, N)
-    d = None if drows is None else _rows(where, device, drows, dtype, R, ld_d, N)
-    rc = (_lib or lib()).qesgd_combine_backward(_rows(where, device, dy, dtype, T, ld_dy, N), dtype, ld_dy, x, ld, R, s, g, T, k, N, d, ld_d, dg, stream)
+    d = dy.data_ptr() if dy.is_contiguous() and dy.numel() >= (T - 1) * ld_dy + N else _rows(where, device, dy, kind, T, ld_dy, N)
+    x = None if rows is None else _rows(where, device, rows, kind, R, ld, N)
+    dr = None if drows is None else _rows(where, device, drows, kind, R, ld_d, N)
+    s = None if slots is None else slots.data_ptr() if slots.dtype is _I32 and slots.get_device() == device and slots.is_contiguous() and \
+        slots.numel() >= pairs else _ints(where, device, slots, pairs)
+    g, dg = _f32(where, device, pairs, gates, dgates)
+    rc = (_lib or lib()).qesgd_combine_backward(d, dtype, ld_dy, x, ld, R, s, g, T, k, N, dr, ld_d, dg, stream)
     if rc:
         raise QesgdError(rc, where)
 
@@ -571,14 +585,17 @@ def qesgd_mx4_grouped_columns(R: int, E: int) -> int:
 
 
 def qesgd_mx4_quantize_groups(x, ld, T, order, per, offsets, E, R, cols, mode, seed, rnd, packed, packed_t=None, worker=0, stream=None):
-    where = "qesgd_mx4_quantize_groups"
+    where, kind = "qesgd_mx4_quantize_groups", x.dtype
     dtype = _dtype(x, where)
     device, stream = _here(where, stream, x)
+    a = x.data_ptr() if x.is_contiguous() and x.numel() >= (T - 1) * ld + cols else _rows(where, device, x, kind, T, ld, cols)
+    o = None if order is None else order.data_ptr() if order.dtype is _I32 and order.get_device() == device and order.is_contiguous() and \
+        order.numel() >= R else _ints(where, device, order, R)
+    f = offsets.data_ptr() if offsets.dtype is _I32 and offsets.get_device() == device and offsets.is_contiguous() and offsets.numel() > E \
+        else _ints(where, device, offsets, E + 1)
     p = None if packed is None else _packed(where, device, packed, R, cols)
     pt = None if packed_t is None else _packed(where, device, packed_t, cols, (R + 127 * min(E, R)) // 128 * 128)
-    rc = (_lib or lib()).qesgd_mx4_quantize_groups(_rows(where, device, x, dtype, T, ld, cols), dtype, ld, T,
-                                                   None if order is None else _i32(where, device, order, R), per,
-                                                   _i32(where, device, offsets, E + 1), E, R, cols, mode, seed, rnd, worker, p, pt, stream)
+    rc = (_lib or lib()).qesgd_mx4_quantize_groups(a, dtype, ld, T, o, per, f, E, R, cols, mode, seed, rnd, worker, p, pt, stream)
     if rc:
         raise QesgdError(rc, where)
 
@@ -588,13 +605,15 @@ def qesgd_mx4_grouped_product_workspace_bytes(R: int, N: int, K: int, E: int) ->
 
 
 def qesgd_mx4_grouped_product(a_packed, b_slab, b_stride, offsets, E, R, N, K, c, ldc, workspace=None, stream=None):
-    where = "qesgd_mx4_grouped_product"
+    where, kind = "qesgd_mx4_grouped_product", c.dtype
     dtype = _dtype(c, where)
     device, stream = _here(where, stream, c)
-    ws, ws_bytes = _ws(where, device, workspace)
-    rc = (_lib or lib()).qesgd_mx4_grouped_product(_packed(where, device, a_packed, R, K), _packed(where, device, b_slab, N, K, E, b_stride), b_stride,
-                                                   _i32(where, device, offsets, E + 1), E, R, N, K, _rows(where, device, c, dtype, R, ldc, N), dtype,
-                                                   ldc, ws, ws_bytes, stream)
+    y = c.data_ptr() if c.is_contiguous() and c.numel() >= (R - 1) * ldc + N else _rows(where, device, c, kind, R, ldc, N)
+    f = offsets.data_ptr() if offsets.dtype is _I32 and offsets.get_device() == device and offsets.is_contiguous() and offsets.numel() > E \
+        else _ints(where, device, offsets, E + 1)
+    ws, ws_bytes = (None, 0) if workspace is None else _ws(where, device, workspace)
+    rc = (_lib or lib()).qesgd_mx4_grouped_product(_packed(where, device, a_packed, R, K), _packed(where, device, b_slab, N, K, E, b_stride), b_stride, f, E, R, N,
+                                                   K, y, dtype, ldc, ws, ws_bytes, stream)
     if rc:
         raise QesgdError(rc, where)
 
@@ -604,14 +623,14 @@ def qesgd_mx4_grouped_gradient_workspace_bytes(R: int, N: int, K: int, E: int) -
 
 
 def qesgd_mx4_grouped_gradient(a_packed_t, b_packed_t, offsets, E, R, N, K, d, workspace=None, stream=None):
-    where = "qesgd_mx4_grouped_gradient"
+    where, kind = "qesgd_mx4_grouped_gradient", d.dtype
     dtype = _dtype(d, where)
     device, stream = _here(where, stream, d)
     columns = (R + 127 * min(E, R)) // 128 * 128
-    ws, ws_bytes = _ws(where, device, workspace)
+    y = d.data_ptr() if d.is_contiguous() and d.numel() >= E * N * K else _rows(where, device, d, kind, E, N * K, N * K)
+    ws, ws_bytes = (None, 0) if workspace is None else _ws(where, device, workspace)
     rc = (_lib or lib()).qesgd_mx4_grouped_gradient(_packed(where, device, a_packed_t, N, columns), _packed(where, device, b_packed_t, K, columns),
-                                                    _i32(where, device, offsets, E + 1), E, R, N, K, _rows(where, device, d, dtype, E, N * K, N * K),
-                                                    dtype, ws, ws_bytes, stream)
+                                                    _ints(where, device, offsets, E + 1), E, R, N, K, y, dtype, ws, ws_bytes, stream)
     if rc:
         raise QesgdError(rc, where)
 
@@ -621,15 +640,19 @@ def qesgd_mx4_vector_product_workspace_bytes(R: int, N: int, K: int, E: int) -> 
 
 
 def qesgd_mx4_vector_product(x, ld, T, order, per, w_slab, w_stride, offsets, E, R, N, K, y, ldy, workspace=None, stream=None):
-    where = "qesgd_mx4_vector_product"
+    where, kind = "qesgd_mx4_vector_product", y.dtype
     dtype = _dtype(y, where)
     device, stream = _here(where, stream, y)
-    ws, ws_bytes = _ws(where, device, workspace)
-    rc = (_lib or lib()).qesgd_mx4_vector_product(_rows(where, device, x, dtype, T, ld, K), dtype, ld, T,
-                                                  None if order is None else _i32(where, device, order, R), per,
-                                                  _packed(where, device, w_slab, N, K, E, w_stride), w_stride,
-                                                  None if offsets is None else _i32(where, device, offsets, E + 1), E, R, N, K,
-                                                  _rows(where, device, y, dtype, R, ldy, N), ldy, ws, ws_bytes, stream)
+    a = x.data_ptr() if x.dtype is kind and x.get_device() == device and x.is_contiguous() and x.numel() >= (T - 1) * ld + K \
+        else _rows(where, device, x, kind, T, ld, K)
+    c = y.data_ptr() if y.is_contiguous() and y.numel() >= (R - 1) * ldy + N else _rows(where, device, y, kind, R, ldy, N)
+    o = None if order is None else order.data_ptr() if order.dtype is _I32 and order.get_device() == device and order.is_contiguous() and \
+        order.numel() >= R else _ints(where, device, order, R)
+    f = None if offsets is None else offsets.data_ptr() if offsets.dtype is _I32 and offsets.get_device() == device and offsets.is_contiguous() and \
+        offsets.numel() > E else _ints(where, device, offsets, E + 1)
+    ws, ws_bytes = (None, 0) if workspace is None else _ws(where, device, workspace)
+    rc = (_lib or lib()).qesgd_mx4_vector_product(a, dtype, ld, T, o, per, _packed(where, device, w_slab, N, K, E, w_stride), w_stride, f, E, R, N, K, c, ldy, ws,
+                                                  ws_bytes, stream)
     if rc:
         raise QesgdError(rc, where)
 
