@@ -26,6 +26,9 @@ struct PParams {
     uint32_t row_codes, row_scales;       // of either operand
     uint32_t tiles_m, tiles_n;            // of one expert's D; tiles_n of C
     bool stream;                          // C or D in whole lines that nothing finds in a cache again
+    uint32_t pieces;                      // of the contraction; with more than one the sums go to partial [pieces, all of C or D]
+    float* partial;
+    uint64_t sums;                        // of a piece
 };
 
 // Non-temporal stores where the result is larger than what the memory-side cache keeps for its reader, and made of whole lines (parts of
@@ -62,6 +65,13 @@ __device__ __forceinline__ void store_tile(const Mx4Ops<S>& ops, void* c, uint64
         }
 }
 
+// Steps first .. first + count of `steps`, piece number `piece` of them: an even first one, because scales come in pairs.  A short contraction leaves some pieces
+// without any.
+__device__ __forceinline__ void piece_of(const PParams& p, uint32_t piece, uint32_t steps, uint32_t& first, uint32_t& count) {
+    first = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)piece * steps / p.pieces)) & ~1u;
+    count = (piece + 1u == p.pieces ? steps : __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)(piece + 1u) * steps / p.pieces)) & ~1u) - first;
+}
+
 template <class S>
 __device__ __forceinline__ void multiply_tile(Mx4Ops<S>& ops, uint32_t steps, unsigned char* lds0, unsigned char* lds1, unsigned char* lds2, unsigned char* lds3) {
 #pragma unroll
@@ -90,8 +100,14 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_product(const PParam
     const uint32_t wm = wave / S::WN, wn = wave % S::WN;
     // the workgroups that have a tile are dealt to the XCDs among themselves: those behind the last tile come last of all
     const uint32_t all = all_tiles(p.offsets, p.E, p.R, lg) * p.tiles_n;
-    if (blockIdx.x >= all) return;
-    const uint32_t t = tile_of_workgroup(blockIdx.x, all);
+    if (blockIdx.x >= all * p.pieces) return;
+    uint32_t t = tile_of_workgroup(blockIdx.x, all * p.pieces), piece = 0, first = 0, steps = (p.row_codes + kStepBytes - 1u) / kStepBytes;
+    const uint32_t all_steps = steps;
+    if (p.pieces > 1) {
+        piece = __builtin_amdgcn_readfirstlane(t / all);
+        t -= piece * all;
+        piece_of(p, piece, all_steps, first, steps);
+    }
     Group g;
     if (!group_of_tile(p.offsets, p.E, p.R, lg, p.tiles_n, t, g)) return;
     uint32_t tm, tn;
@@ -101,21 +117,23 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_product(const PParam
     const uint32_t m0 = g.lo + tm * S::BM, n0 = tn * S::BN;
     const unsigned char* b = p.b + g.e * p.b_stride;
     Mx4Ops<S> ops;
-    ops.a = p.a + (uint64_t)m0 * p.row_codes;
-    ops.b = b + (uint64_t)n0 * p.row_codes;
+    ops.a = p.a + (uint64_t)m0 * p.row_codes + (uint64_t)first * kStepBytes;
+    ops.b = b + (uint64_t)n0 * p.row_codes + (uint64_t)first * kStepBytes;
     ops.la.init(p.row_codes, g.hi - m0);
     ops.lb.init(p.row_codes, p.N - n0);
     ops.scales = scales;
-    ops.init_scales(p.a + p.a_scales + (uint64_t)m0 * p.row_scales, b + p.b_scales + (uint64_t)n0 * p.row_scales, g.hi - m0, p.N - n0,
-                    p.row_scales, p.row_scales, wm, wn);
+    ops.init_scales(p.a + p.a_scales + (uint64_t)m0 * p.row_scales + first * 8u, b + p.b_scales + (uint64_t)n0 * p.row_scales + first * 8u, g.hi - m0, p.N - n0,
+                    p.row_scales, p.row_scales - first * 8u, wm, wn);
     ops.at_a = wm * S::FM * 32 * kStepBytes + lane_place(lane);
     ops.at_b = (S::BM + wn * S::FN * 32) * kStepBytes + lane_place(lane);
-    ops.steps = (p.row_codes + kStepBytes - 1u) / kStepBytes;
-    ops.half = p.row_codes % kStepBytes != 0;
+    ops.steps = steps;
+    ops.half = p.row_codes % kStepBytes != 0 && first + steps == all_steps;
     ops.h = h;
-    multiply_tile(ops, ops.steps, lds0, lds1, lds2, lds3);
+    multiply_tile(ops, steps, lds0, lds1, lds2, lds3);
 
-    store_tile<S, DT>(ops, p.c, p.ldc, g.hi, p.N, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= g.hi && n0 + S::BN <= p.N, p.stream);
+    // pieces are of fp32, as DT is for them
+    void* c = p.pieces > 1 ? (void*)(p.partial + piece * p.sums) : p.c;
+    store_tile<S, DT>(ops, c, p.pieces > 1 ? p.N : p.ldc, g.hi, p.N, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= g.hi && n0 + S::BN <= p.N, p.stream);
 }
 
 template <class S, uint32_t DT>
@@ -128,7 +146,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
     const uint32_t wm = wave / S::WN, wn = wave % S::WN;
     // experts differ in rows, so every XCD gets its share of each one's tiles, a run of them: 8 experts of 4096 x 4096, 16384 rows 357 -> 266 us
-    const uint32_t tiles = p.tiles_m * p.tiles_n, e = __builtin_amdgcn_readfirstlane(blockIdx.x / tiles);
+    const uint32_t tiles = p.tiles_m * p.tiles_n, e = __builtin_amdgcn_readfirstlane(blockIdx.x / tiles), piece = blockIdx.y;
     uint32_t tm, tn;
     banded_tile(tile_of_workgroup(blockIdx.x - e * tiles, tiles), p.tiles_m, p.tiles_n, tm, tn);
     tm = __builtin_amdgcn_readfirstlane(tm);
@@ -137,29 +155,71 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
     // bytes of a row's codes before the group and of the group, as far as the rows go
     const uint32_t begin = __builtin_amdgcn_readfirstlane(min(g.first * 64u, p.row_codes));
     const uint32_t bytes = __builtin_amdgcn_readfirstlane(min(((g.hi - g.lo + 127u) >> 7) * 64u, p.row_codes - begin));
-    const uint32_t m0 = tm * S::BM, n0 = tn * S::BN;
+    const uint32_t all_steps = (bytes + kStepBytes - 1u) / kStepBytes;
+    uint32_t first = 0, steps = all_steps;
+    if (p.pieces > 1) piece_of(p, piece, all_steps, first, steps);
+    const uint32_t m0 = tm * S::BM, n0 = tn * S::BN, from = begin + first * kStepBytes;
     Mx4Ops<S> ops;
 #pragma unroll
     for (int i = 0; i < S::FM; ++i)
 #pragma unroll
         for (int j = 0; j < S::FN; ++j) ops.acc[i][j] = acc16{};
-    if (bytes) {
-        ops.a = p.a + (uint64_t)m0 * p.row_codes + begin;
-        ops.b = p.b + (uint64_t)n0 * p.row_codes + begin;
+    if (steps) {
+        ops.a = p.a + (uint64_t)m0 * p.row_codes + from;
+        ops.b = p.b + (uint64_t)n0 * p.row_codes + from;
         ops.la.init(p.row_codes, p.N - m0);
         ops.lb.init(p.row_codes, p.K - n0);
         ops.scales = scales;
-        ops.init_scales(p.a + p.a_scales + (uint64_t)m0 * p.row_scales + begin / 16u, p.b + p.b_scales + (uint64_t)n0 * p.row_scales + begin / 16u,
-                        p.N - m0, p.K - n0, p.row_scales, bytes / 16u, wm, wn);
+        ops.init_scales(p.a + p.a_scales + (uint64_t)m0 * p.row_scales + from / 16u, p.b + p.b_scales + (uint64_t)n0 * p.row_scales + from / 16u,
+                        p.N - m0, p.K - n0, p.row_scales, (bytes - first * kStepBytes) / 16u, wm, wn);
         ops.at_a = wm * S::FM * 32 * kStepBytes + lane_place(lane);
         ops.at_b = (S::BM + wn * S::FN * 32) * kStepBytes + lane_place(lane);
-        ops.steps = (bytes + kStepBytes - 1u) / kStepBytes;
-        ops.half = bytes % kStepBytes != 0;
+        ops.steps = steps;
+        ops.half = bytes % kStepBytes != 0 && first + steps == all_steps;
         ops.h = h;
-        multiply_tile(ops, ops.steps, lds0, lds1, lds2, lds3);
+        multiply_tile(ops, steps, lds0, lds1, lds2, lds3);
     }
-    void* d = (unsigned char*)p.c + (uint64_t)e * p.N * p.K * (DT == QESGD_F32 ? 4u : 2u);
+    const uint64_t of_expert = (uint64_t)e * p.N * p.K;
+    void* d = p.pieces > 1 ? (void*)(p.partial + piece * p.sums + of_expert) : (void*)((unsigned char*)p.c + of_expert * (DT == QESGD_F32 ? 4u : 2u));
     store_tile<S, DT>(ops, d, p.K, p.N, p.K, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= p.N && n0 + S::BN <= p.K, p.stream);
+}
+
+// C or D from the sums of the pieces, added in order: rows of `cols` numbers; offsets: the groups whose rows count, or null for all.  Four numbers a lane where rows
+// allow it, eight pieces on their way: the sums come from the memory-side cache and are few, so it is a launch and a latency.
+template <uint32_t DT>
+__global__ void __launch_bounds__(256) k_mx4_grouped_sum(const PParams p, const int32_t* offsets, uint32_t cols) {
+    const uint64_t i = ((uint64_t)blockIdx.x * 256u + threadIdx.x) * 4u;
+    if (i >= p.sums) return;
+    uint64_t lo = 0, hi = ~0ull;
+    if (offsets) {
+        lo = held(offsets[0], p.R);
+        hi = held(offsets[p.E], p.R);
+    }
+    uint64_t row = i / cols;
+    uint32_t col = (uint32_t)(i - row * cols);
+    if (row >= hi || row + 3u < lo) return;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if ((p.sums & 3u) == 0) {
+        for (uint32_t k0 = 0; k0 < p.pieces; k0 += 8) {
+            float x[8][4];
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) *(float4*)x[k] = *(const float4*)(p.partial + min(k0 + k, p.pieces - 1u) * p.sums + i);
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += k0 + k < p.pieces ? x[k][e] : 0.0f;
+        }
+    } else {
+        for (uint32_t k = 0; k < p.pieces; ++k)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+                if (i + e < p.sums) v[e] += p.partial[k * p.sums + i + e];
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+        if (i + e < p.sums && row >= lo && row < hi) put<DT>(p.c, row * p.ldc + col, v[e]);
+        if (++col == cols) { col = 0; ++row; }
+    }
 }
 
 // ---- large tiles, one after the other ------------------------------------------
@@ -406,32 +466,54 @@ uint64_t group_tiles(const GroupProduct& a, uint64_t edge) {
     return tiles > groups ? tiles : groups;
 }
 
-// The edge of the tiles from how long they take on 256 CUs (tile_us), the larger one where it hardly matters.  Measured, us, with 64 / 128 / 256:
+// The edge of the tiles, and the pieces of the contraction, from how long they take on 256 CUs (tile_us), the larger edge where it hardly matters.  A piece has at least
+// four steps; the sums of the pieces cost a launch, and are written and read at about 4 TB/s.  Measured, us, with 64 / 128 / 256:
 //   products   16 experts, 32768 rows, N = K = 4096 655 / 402 / 339;  13, 9003, 1000, 2049 33 / 25.9 / 22.7;  8, 2048, 2048, 2048 15.5 / 13.7 / 18.1;
 //              64, 1024, 1024, 1024 11.5 / 9.2 / 12.5;  8, 256, 4096, 4096 17.8 / 16.3 / 27.2;  64, 16384, 2048, 1024 70 / 46 / 46
 //   gradients  8, 16384, 4096, 4096 759 / 344 / 266;  64, 4096, 1024, 1024 109 / 65 / 59;  16, 1024, 512, 512 8.9 / 8.3 / 9.7
+struct Cut { uint32_t edge, pieces; };
+constexpr uint32_t kMostPieces = 16;
 template <class F>
-uint32_t choose_edge(F&& tiles, double steps) {
-    uint32_t best = 64;
+Cut choose_cut(F&& tiles, double steps, double around, uint64_t sums) {
+    Cut best{64, 1};
     double least = 1e300;
     for (uint32_t edge : {64u, 128u, 256u}) {
-        const double us = tile_us(tiles(edge), edge, steps);
-        if (us <= least * 1.02) {
-            least = us;
-            best = edge;
+        const uint64_t n = tiles(edge);
+        for (uint32_t pieces = 1; pieces <= kMostPieces && (pieces == 1 || (pieces * 4.0 <= steps && n * pieces <= 1024)); ++pieces) {
+            const double us = tile_us(n * pieces, edge, steps / pieces + around) + (pieces == 1 ? 0.0 : 2.0 + (double)pieces * (double)sums * 2e-6);
+            if (us <= least * (pieces == 1 ? 1.02 : 1.0)) {
+                least = us;
+                best = Cut{edge, pieces};
+            }
         }
     }
     return best;
+}
+Cut product_cut(const GroupProduct& a) {
+    return choose_cut([&](uint64_t edge) { return group_tiles(a, edge) * ((a.N + edge - 1) / edge); }, (double)((a.K + 255) / 256), 0.0, a.R * a.N);
+}
+// The contraction of a group of the mean size, and as much as two steps for the beginning and the end of a tile.
+Cut gradient_cut(const GroupProduct& a) {
+    return choose_cut([&](uint64_t edge) { return a.E * ((a.N + edge - 1) / edge) * ((a.K + edge - 1) / edge); }, 0.5 + (double)a.R / (double)a.E / 256.0, 2.0,
+                      a.E * a.N * a.K);
+}
+
+int launch_sum(const GroupProduct& a, const PParams& p, const int32_t* offsets, uint32_t cols) {
+    const uint64_t groups = (p.sums + 1023) / 1024;
+    if (!grid_ok(groups, 256)) return QESGD_ERR_DIM;
+    by_type(a.dtype, [&](auto t) { k_mx4_grouped_sum<t.value><<<(uint32_t)groups, 256, 0, a.stream>>>(p, offsets, cols); });
+    return launched();
 }
 
 template <class S>
 int launch_product_tiles(const GroupProduct& a, PParams& p) {
     p.tiles_n = (p.N + S::BN - 1) / S::BN;
     // the most tiles that R rows in E groups make
-    const uint64_t groups = a.E < a.R ? a.E : a.R, tiles_m = (a.R + (S::BM - 1) * groups) / S::BM;
-    if (!grid_ok(tiles_m * p.tiles_n, S::threads)) return QESGD_ERR_DIM;
-    by_type(a.dtype, [&](auto t) { k_mx4_grouped_product<S, t.value><<<(uint32_t)(tiles_m * p.tiles_n), S::threads, 0, a.stream>>>(p); });
-    return launched();
+    const uint64_t groups = a.E < a.R ? a.E : a.R, tiles_m = (a.R + (S::BM - 1) * groups) / S::BM, tiles = tiles_m * p.tiles_n * p.pieces;
+    if (!grid_ok(tiles, S::threads)) return QESGD_ERR_DIM;
+    by_type(p.pieces > 1 ? QESGD_F32 : a.dtype, [&](auto t) { k_mx4_grouped_product<S, t.value><<<(uint32_t)tiles, S::threads, 0, a.stream>>>(p); });
+    const int rc = launched();
+    return rc != QESGD_OK || p.pieces == 1 ? rc : launch_sum(a, p, p.offsets, p.N);
 }
 
 // One workgroup a CU, as its LDS has room for.  Where it gets three tiles or more; with fewer their search costs more than it saves.  A workgroup a tile / the chain,
@@ -455,15 +537,24 @@ int launch_gradient_tiles(const GroupProduct& a, PParams& p) {
     p.tiles_m = (p.N + S::BM - 1) / S::BM;
     p.tiles_n = (p.K + S::BN - 1) / S::BN;
     const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n * a.E;
-    if (!grid_ok(tiles, S::threads)) return QESGD_ERR_DIM;
-    by_type(a.dtype, [&](auto t) { k_mx4_grouped_gradient<S, t.value><<<(uint32_t)tiles, S::threads, 0, a.stream>>>(p); });
-    return launched();
+    if (!grid_ok(tiles * p.pieces, S::threads)) return QESGD_ERR_DIM;
+    by_type(p.pieces > 1 ? QESGD_F32 : a.dtype, [&](auto t) {
+        k_mx4_grouped_gradient<S, t.value><<<dim3((uint32_t)tiles, p.pieces), S::threads, 0, a.stream>>>(p);
+    });
+    const int rc = launched();
+    return rc != QESGD_OK || p.pieces == 1 ? rc : launch_sum(a, p, nullptr, p.K);
 }
 
 }  // namespace
 
-size_t grouped_product_workspace(const GroupProduct&) { return 0; }
-size_t grouped_gradient_workspace(const GroupProduct&) { return 0; }
+size_t grouped_product_workspace(const GroupProduct& a) {
+    const uint32_t pieces = product_cut(a).pieces;
+    return pieces > 1 ? pieces * a.R * a.N * sizeof(float) : 0;
+}
+size_t grouped_gradient_workspace(const GroupProduct& a) {
+    const uint32_t pieces = gradient_cut(a).pieces;
+    return pieces > 1 ? pieces * a.E * a.N * a.K * sizeof(float) : 0;
+}
 
 int launch_grouped_product(const GroupProduct& a) {
     qesgd_mx4_layout A, B;
@@ -484,15 +575,15 @@ int launch_grouped_product(const GroupProduct& a) {
     p.N = (uint32_t)a.N;
     p.row_codes = (uint32_t)A.row_codes;
     p.row_scales = (uint32_t)A.row_scales;
-    p.stream = streamed(a.c, a.ldc * dtype_bytes(a.dtype), a.R);
-    const uint64_t steps = (a.K + 255) / 256;
-    switch (choose_edge([&](uint64_t edge) { return group_tiles(a, edge) * ((a.N + edge - 1) / edge); }, (double)steps)) {
-        case 64: return launch_product_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
-        case 128: return launch_product_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
-        default: break;
-    }
-    return group_tiles(a, 256) * ((a.N + 255) / 256) > kChainTiles ? launch_chain<TileShape<2, 4, 4, 2, 2>, false>(a, p)
-                                                                  : launch_product_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
+    const Cut cut = product_cut(a);
+    p.pieces = cut.pieces;
+    p.partial = a.workspace;
+    p.sums = a.R * a.N;
+    p.stream = cut.pieces == 1 && streamed(a.c, a.ldc * dtype_bytes(a.dtype), a.R);
+    if (cut.edge == 64) return launch_product_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
+    if (cut.edge == 128) return launch_product_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
+    if (cut.pieces == 1 && group_tiles(a, 256) * ((a.N + 255) / 256) > kChainTiles) return launch_chain<TileShape<2, 4, 4, 2, 2>, false>(a, p);
+    return launch_product_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
 }
 
 int launch_grouped_gradient(const GroupProduct& a) {
@@ -514,16 +605,16 @@ int launch_grouped_gradient(const GroupProduct& a) {
     p.K = (uint32_t)a.K;
     p.row_codes = (uint32_t)A.row_codes;
     p.row_scales = (uint32_t)A.row_scales;
-    p.stream = streamed(a.c, a.K * dtype_bytes(a.dtype), a.E * a.N);
-    // the contraction of a group of the mean size, and as much as two steps for the beginning and the end of a tile
-    const double steps = 2.5 + (double)a.R / (double)a.E / 256.0;
-    switch (choose_edge([&](uint64_t edge) { return a.E * ((a.N + edge - 1) / edge) * ((a.K + edge - 1) / edge); }, steps)) {
-        case 64: return launch_gradient_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
-        case 128: return launch_gradient_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
-        default: break;
-    }
-    return a.E * ((a.N + 255) / 256) * ((a.K + 255) / 256) > kChainTiles ? launch_chain<TileShape<2, 4, 4, 2, 2>, true>(a, p)
-                                                                        : launch_gradient_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
+    p.ldc = a.K;
+    const Cut cut = gradient_cut(a);
+    p.pieces = cut.pieces;
+    p.partial = a.workspace;
+    p.sums = a.E * a.N * a.K;
+    p.stream = cut.pieces == 1 && streamed(a.c, a.K * dtype_bytes(a.dtype), a.E * a.N);
+    if (cut.edge == 64) return launch_gradient_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
+    if (cut.edge == 128) return launch_gradient_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
+    if (cut.pieces == 1 && a.E * ((a.N + 255) / 256) * ((a.K + 255) / 256) > kChainTiles) return launch_chain<TileShape<2, 4, 4, 2, 2>, true>(a, p);
+    return launch_gradient_tiles<TileShape<2, 4, 4, 2, 2>>(a, p);
 }
 
 }  // namespace qesgd

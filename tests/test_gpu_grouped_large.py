@@ -145,3 +145,53 @@ def test_weighted_sum_of_many_rows(B, dtype):
                 touched[at] = True
             assert ((out[p].double() - want).abs() <= (k + 1) * ONE * mag + half * want.abs() * (1 + 2.0 ** -10) + least).all()
         assert (drows[~touched] == 9.0).all()
+
+
+@pytest.mark.parametrize("kind", ["ragged", "even", "one", "none"])
+@pytest.mark.parametrize("n,N,K,E", [(64, 512, 8192, 8), (5, 33, 9000, 2), (300, 64, 4100, 4), (1, 4096, 4096, 1), (90, 131, 12_345, 3), (40, 60, 2900, 30)])
+def test_long_contractions_in_pieces(B, n, N, K, E, kind):
+    need = B.qesgd_mx4_grouped_product_workspace_bytes(n, N, K, E)
+    assert need > 0 and need % (4 * n * N) == 0
+    dtype = list(TYPES.values())[(n + K) % 3]
+    offsets = X.group_sizes(np.random.default_rng(K), E, n, kind)
+    pa, a = packed_noise(B, n, K, 1, n + K)
+    pb, b = packed_noise(B, N, K, E, N + 2 * K)
+    pa, pb, a, ldc = pa[0].cuda(), pb.cuda(), on_gpu(a[0]), N + 3
+    ws = torch.full((need + 256,), 0x7F, dtype=torch.uint8, device="cuda")
+    out = []
+    for _ in range(2):
+        c = torch.full((n, ldc), 3.0, dtype=dtype, device="cuda")
+        B.qesgd_mx4_grouped_product(pa, pb, pb.stride(0), ints(offsets), E, n, N, K, c, ldc, workspace=ws[:need])
+        out.append(c)
+    assert torch.equal(*out) and (ws[need:] == 0x7F).all()
+    assert (c[offsets[-1]:] == 3.0).all() and (c[:offsets[0]] == 3.0).all() and (c[:, N:] == 3.0).all()
+    for e in range(E):
+        lo, hi = int(offsets[e]), int(offsets[e + 1])
+        assert within(c[lo:hi, :N], a[lo:hi], on_gpu(b[e]), dtype), e
+    with pytest.raises(B.QesgdError):
+        B.qesgd_mx4_grouped_product(pa, pb, pb.stride(0), ints(offsets), E, n, N, K, c, ldc, workspace=ws[:need - 1])
+
+
+@pytest.mark.parametrize("kind", ["ragged", "even", "one", "none"])
+@pytest.mark.parametrize("n,N,K,E", [(20_000, 64, 64, 1), (30_000, 100, 41, 2), (60_000, 256, 131, 3), (16_384, 33, 64, 4)])
+def test_gradients_of_long_groups_in_pieces(B, n, N, K, E, kind):
+    need = B.qesgd_mx4_grouped_gradient_workspace_bytes(n, N, K, E)
+    assert need > 0 and need % (4 * E * N * K) == 0
+    dtype = list(TYPES.values())[(n + K) % 3]
+    offsets = X.group_sizes(np.random.default_rng(K), E, n, kind)
+    columns = X.group_columns(n, E)
+    pa, a = packed_noise(B, N, columns, 1, n + K)
+    pb, b = packed_noise(B, K, columns, 1, N + 2 * K)
+    pa, pb, a, b = pa[0].cuda(), pb[0].cuda(), on_gpu(a[0]), on_gpu(b[0])
+    ws = torch.full((need + 256,), 0x7F, dtype=torch.uint8, device="cuda")
+    out = []
+    for _ in range(2):
+        d = torch.full((E * N * K + 64,), 3.0, dtype=dtype, device="cuda")
+        B.qesgd_mx4_grouped_gradient(pa, pb, ints(offsets), E, n, N, K, d, workspace=ws[:need])
+        out.append(d)
+    assert torch.equal(*out) and (d[E * N * K:] == 3.0).all() and (ws[need:] == 0x7F).all()
+    at, got = 0, d[:E * N * K].view(E, N, K)
+    for e in range(E):
+        wide = int(offsets[e + 1] - offsets[e] + 127) // 128 * 128
+        assert within(got[e], a[:, at:at + wide], b[:, at:at + wide], dtype), e
+        at += wide
