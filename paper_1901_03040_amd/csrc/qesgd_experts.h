@@ -98,6 +98,18 @@ int launch_grouped_product(const GroupProduct& a);
 size_t grouped_gradient_workspace(const GroupProduct& a);
 int launch_grouped_gradient(const GroupProduct& a);
 
+// A result in rows of `cols` numbers, ldc apart, from the sums of the pieces of its contraction, [pieces, sums]; offsets: the groups whose rows count, or null for all.
+struct PieceSum {
+    const float* partial;
+    uint32_t pieces;
+    uint64_t sums;
+    const int32_t* offsets;
+    uint32_t E, R, cols;
+    void* c;
+    uint64_t ldc;
+};
+int launch_piece_sum(const PieceSum& p, uint32_t dtype, hipStream_t stream);
+
 struct VectorProduct {
     const void* x;
     uint32_t dtype;

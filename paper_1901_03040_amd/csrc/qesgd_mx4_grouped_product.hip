@@ -184,19 +184,19 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
     store_tile<S, DT>(ops, d, p.K, p.N, p.K, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= p.N && n0 + S::BN <= p.K, p.stream);
 }
 
-// C or D from the sums of the pieces, added in order: rows of `cols` numbers; offsets: the groups whose rows count, or null for all.  Four numbers a lane where rows
+// A result from the sums of the pieces, added in order (see PieceSum).  Four numbers a lane where rows
 // allow it, eight pieces on their way: the sums come from the memory-side cache and are few, so it is a launch and a latency.
 template <uint32_t DT>
-__global__ void __launch_bounds__(256) k_mx4_grouped_sum(const PParams p, const int32_t* offsets, uint32_t cols) {
+__global__ void __launch_bounds__(256) k_mx4_grouped_sum(const PieceSum p) {
     const uint64_t i = ((uint64_t)blockIdx.x * 256u + threadIdx.x) * 4u;
     if (i >= p.sums) return;
     uint64_t lo = 0, hi = ~0ull;
-    if (offsets) {
-        lo = held(offsets[0], p.R);
-        hi = held(offsets[p.E], p.R);
+    if (p.offsets) {
+        lo = held(p.offsets[0], p.R);
+        hi = held(p.offsets[p.E], p.R);
     }
-    uint64_t row = i / cols;
-    uint32_t col = (uint32_t)(i - row * cols);
+    uint64_t row = i / p.cols;
+    uint32_t col = (uint32_t)(i - row * p.cols);
     if (row >= hi || row + 3u < lo) return;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if ((p.sums & 3u) == 0) {
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(256) k_mx4_grouped_sum(const PParams p, const 
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e) {
         if (i + e < p.sums && row >= lo && row < hi) put<DT>(p.c, row * p.ldc + col, v[e]);
-        if (++col == cols) { col = 0; ++row; }
+        if (++col == p.cols) { col = 0; ++row; }
     }
 }
 
@@ -499,10 +499,7 @@ Cut gradient_cut(const GroupProduct& a) {
 }
 
 int launch_sum(const GroupProduct& a, const PParams& p, const int32_t* offsets, uint32_t cols) {
-    const uint64_t groups = (p.sums + 1023) / 1024;
-    if (!grid_ok(groups, 256)) return QESGD_ERR_DIM;
-    by_type(a.dtype, [&](auto t) { k_mx4_grouped_sum<t.value><<<(uint32_t)groups, 256, 0, a.stream>>>(p, offsets, cols); });
-    return launched();
+    return launch_piece_sum(PieceSum{p.partial, p.pieces, p.sums, offsets, p.E, p.R, cols, p.c, p.ldc}, a.dtype, a.stream);
 }
 
 template <class S>
@@ -546,6 +543,13 @@ int launch_gradient_tiles(const GroupProduct& a, PParams& p) {
 }
 
 }  // namespace
+
+int launch_piece_sum(const PieceSum& p, uint32_t dtype, hipStream_t stream) {
+    const uint64_t groups = (p.sums + 1023) / 1024;
+    if (!grid_ok(groups, 256)) return QESGD_ERR_DIM;
+    by_type(dtype, [&](auto t) { k_mx4_grouped_sum<t.value><<<(uint32_t)groups, 256, 0, stream>>>(p); });
+    return launched();
+}
 
 size_t grouped_product_workspace(const GroupProduct& a) {
     const uint32_t pieces = product_cut(a).pieces;

@@ -11,7 +11,7 @@
 // 1411 x 2049 f32 17 us for 45 MB: a workgroup finds its rows by three trips to memory, then waits for 140 KB of W, and a CU has one or two.
 //
 // A wave owns 16 rows of W and takes steps of 128 columns; the waves of a workgroup share the columns among them, and their sums are added
-// in order.  The rows of x go to LDS once, split.
+// in order.  The rows of x go to LDS once, split; long rows of many tokens in pieces, a workgroup each.
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_launch.h"
@@ -38,6 +38,8 @@ struct VParams {
     uint64_t ldy;
     uint32_t splits;                  // waves that share a row's columns: 1 .. kVWaves
     uint32_t part_columns;            // columns of x that lie in LDS at a time, a multiple of 128
+    uint32_t pieces;                  // of the columns, a workgroup each; with more than one the sums go to partial [pieces, R, N]
+    float* partial;
 };
 
 constexpr uint32_t kVBatch = 2;           // pairs of steps whose blocks a wave has on their way at a time, twice
@@ -127,7 +129,8 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
     const uint32_t row = min(n0 + l, p.N - 1u);
     const unsigned char* codes = w + (uint64_t)row * p.row_codes + block * 16u;
     const unsigned char* scales = w + p.scales_off + (uint64_t)row * p.row_scales + block;
-    const uint32_t steps = p.row_codes / 64u, pitch = p.part_columns * 2u + 16u;
+    const uint32_t steps = p.row_codes / 64u, pitch = p.part_columns * 2u + 16u, piece = blockIdx.z;
+    const uint32_t begin = piece * steps / p.pieces * 128u, end = (piece + 1u) * steps / p.pieces * 128u;
     // blocks of the pairs of steps from + s, + 2 splits .. before step `last` of a part: a pair's are a line of memory
     const auto fetch = [&](uvec4 (&c)[2 * kVBatch], uint32_t (&byte)[2 * kVBatch], uint32_t from, uint32_t s, uint32_t last) {
 #pragma unroll
@@ -146,8 +149,8 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
         acc4 acc[TILES];
 #pragma unroll
         for (uint32_t m = 0; m < TILES; ++m) acc[m] = acc4{0.0f, 0.0f, 0.0f, 0.0f};
-        for (uint32_t c0 = 0; c0 < steps * 128u; c0 += p.part_columns) {
-            const uint32_t here = min(p.part_columns, steps * 128u - c0), last = here / 128u;
+        for (uint32_t c0 = begin; c0 < end; c0 += p.part_columns) {
+            const uint32_t here = min(p.part_columns, end - c0), last = here / 128u;
             // the wave's first blocks are on their way while the rows are brought in
             uvec4 c[2 * kVBatch], next_c[2 * kVBatch];
             uint32_t byte[2 * kVBatch], next_byte[2 * kVBatch];
@@ -235,18 +238,70 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
 #pragma unroll
                 for (uint32_t s = 0; s < kVWaves; ++s) v += part[s];
             }
-            put_row<DT>(p.y, (uint64_t)(r0 + r) * p.ldy + n, v);
+            if (p.pieces > 1) p.partial[((uint64_t)piece * p.R + r0 + r) * p.N + n] = v;
+            else put_row<DT>(p.y, (uint64_t)(r0 + r) * p.ldy + n, v);
         }
     }
 }
 
+struct Plan {
+    uint32_t waves, splits, tiles, lds_rows, part_columns, pieces, blocks;
+};
+
+Plan plan_of(const VectorProduct& a, uint32_t dtype) {
+    Plan p{};
+    const uint32_t steps = (uint32_t)((a.K + 127) / 128), parts = parts_of(dtype), across_rows = (uint32_t)((a.N + 15) / 16);
+    const uint32_t hit = a.E < a.R ? a.E : (uint32_t)a.R;
+    // rows that an expert has at a time, of which two in three are in its share twice over
+    const uint32_t rows = (uint32_t)(a.E == 1 ? a.R : (2 * a.R + a.E - 1) / a.E);
+    p.tiles = 1;
+    while (p.tiles < parts && p.tiles * 16 / parts < rows) ++p.tiles;
+    const uint32_t at_a_time = p.tiles * 16 / parts, kept = (rows < at_a_time ? rows : at_a_time) * parts;
+    const uint64_t all_bytes = (uint64_t)kept * steps * 256u;
+    p.lds_rows = parts * (a.R < at_a_time ? (uint32_t)a.R : at_a_time);
+    // Workgroups of 8 waves, two or three on a CU, where there is little to bring into LDS, else of 16, which bring it in faster.  8 / 16 waves, us, graph of 32 calls: one row
+    // x 4096 x 4096 bf16 5.5 / 5.8, f32 6.2 / 8.7, x 512 x 512 f32 3.9 / 6.3; 8 rows bf16 8.7 / 7.1, 16 rows f32 26.6 / 17.4, 4 rows x 4096 x 25088
+    // bf16 28.9 / 21.5.  And as many waves to a row of W as make kVWavesFew or kVWavesMany of them, beyond which each has more steps instead: 12 tokens x 4 of 64
+    // experts 1411 x 2049 with two waves a row 21.3, with one 18.4; one row x 8192 x 8192 bf16 13.1 with 8, 15.9 with 16.
+    constexpr uint32_t kVWavesFew = 2048, kVWavesMany = 4096;
+    p.waves = all_bytes < 32768u ? 8 : 16;
+    p.splits = 1;
+    while (p.splits < p.waves && p.splits * 4 <= steps + 1 && (uint64_t)across_rows * hit * p.splits < (p.waves == 8 ? kVWavesFew : kVWavesMany)) p.splits *= 2;
+    // Rows that do not fit LDS at once, split by every workgroup, are most of the work.  Where waves share the columns anyway, workgroups share them instead, about 96 KB of
+    // split rows to each, and a second launch adds their sums.  One piece / as chosen, us, graph of 32 calls: 16 rows x 4096 x 4096 f32 17.6 / 13.5 (4 pieces), 16 x 8192 x 8192
+    // f32 40 / 28 and bf16 21 / 18 (4), 16 x 1000 x 8192 f32 30 / 18 (8), 4 x 4096 x 25088 bf16 21 / 19 (8).  Rows that fit gain nothing: 16 x 4096 x 4096 bf16 8.9 / 9.8 (2).
+    constexpr uint64_t kVFits = 131072, kVPiece = 98304;
+    p.pieces = 1;
+    while (all_bytes > kVFits && all_bytes > kVPiece * p.pieces && p.splits >= 4) {
+        p.pieces *= 2;
+        p.splits /= 2;
+    }
+    const uint32_t across = 16u * (p.waves / p.splits);
+    p.blocks = ((uint32_t)a.N + across - 1) / across;
+    // the rows whole, where a CU has one workgroup anyway, or else as much of them as leaves room for two
+    const bool alone = (uint64_t)p.blocks * hit * p.pieces <= 256;
+    const uint32_t room = (alone ? 140u : 60u) * 1024u * p.waves / 16u - p.tiles * 1024u * p.waves * (alone ? 1u : 0u);
+    const uint32_t most = (room / p.lds_rows - 16u) / 2u / 128u * 128u, longest = (steps + p.pieces - 1) / p.pieces * 128u;
+    p.part_columns = most < longest ? most : longest;
+    return p;
+}
+
 }  // namespace
 
-size_t vector_product_workspace(const VectorProduct&) { return 0; }
+// The type is not known here: as much as any of them needs.
+size_t vector_product_workspace(const VectorProduct& a) {
+    uint32_t pieces = 1;
+    for (uint32_t t : {QESGD_F32, QESGD_BF16, QESGD_F16}) {
+        const uint32_t n = plan_of(a, t).pieces;
+        if (n > pieces) pieces = n;
+    }
+    return pieces > 1 ? pieces * a.R * a.N * sizeof(float) : 0;
+}
 
 int launch_vector_product(const VectorProduct& a) {
     qesgd_mx4_layout W;
     if (const int rc = make_mx4_layout(a.N, a.K, &W); rc != QESGD_OK) return rc;
+    const Plan plan = plan_of(a, a.dtype);
     VParams p{};
     p.x = a.x;
     p.ld = a.ld;
@@ -266,31 +321,13 @@ int launch_vector_product(const VectorProduct& a) {
     p.row_scales = (uint32_t)W.row_scales;
     p.y = a.y;
     p.ldy = a.ldy;
-    const uint32_t steps = p.row_codes / 64u, parts = parts_of(a.dtype), across_rows = (p.N + 15) / 16;
-    const uint32_t hit = a.E < a.R ? a.E : (uint32_t)a.R;
-    // rows that an expert has at a time, of which two in three are in its share twice over
-    const uint32_t rows = (uint32_t)(a.E == 1 ? a.R : (2 * a.R + a.E - 1) / a.E);
-    uint32_t tiles = 1;
-    while (tiles < parts && tiles * 16 / parts < rows) ++tiles;
-    const uint32_t at_a_time = tiles * 16 / parts;
-    const uint32_t lds_rows = parts * (a.R < at_a_time ? (uint32_t)a.R : at_a_time);
-    // Workgroups of 8 waves, two or three on a CU, where there is little to bring into LDS, else of 16, which bring it in faster.  8 / 16 waves, us, graph of 32 calls: one row
-    // x 4096 x 4096 bf16 5.5 / 5.8, f32 6.2 / 8.7, x 512 x 512 f32 3.9 / 6.3; 8 rows bf16 8.7 / 7.1, 16 rows f32 26.6 / 17.4, 4 rows x 4096 x 25088
-    // bf16 28.9 / 21.5.  And as many waves to a row of W as make kVWavesFew or kVWavesMany of them, beyond which each has more steps instead: 12 tokens x 4 of 64
-    // experts 1411 x 2049 with two waves a row 21.3, with one 18.4; one row x 8192 x 8192 bf16 13.1 with 8, 15.9 with 16.
-    constexpr uint32_t kVWavesFew = 2048, kVWavesMany = 4096;
-    const uint32_t waves = (uint64_t)(rows < at_a_time ? rows : at_a_time) * parts * steps * 256u < 32768u ? 8 : 16;
-    p.splits = 1;
-    while (p.splits < waves && p.splits * 4 <= steps + 1 && (uint64_t)across_rows * hit * p.splits < (waves == 8 ? kVWavesFew : kVWavesMany)) p.splits *= 2;
-    const uint32_t across = 16u * (waves / p.splits), blocks = (p.N + across - 1) / across;
-    // the rows whole, where a CU has one workgroup anyway, or else as much of them as leaves room for two
-    const bool alone = (uint64_t)blocks * hit <= 256;
-    const uint32_t room = (alone ? 140u : 60u) * 1024u * waves / 16u - tiles * 1024u * waves * (alone ? 1u : 0u);
-    const uint32_t most = (room / lds_rows - 16u) / 2u / 128u * 128u;
-    p.part_columns = most < steps * 128u ? most : steps * 128u;
-    const uint32_t bytes = lds_rows * (p.part_columns * 2u + 16u);
-    const dim3 grid(blocks, a.E);
-    if (!grid_ok((uint64_t)blocks * a.E, waves * 64)) return QESGD_ERR_DIM;
+    p.splits = plan.splits;
+    p.part_columns = plan.part_columns;
+    p.pieces = plan.pieces;
+    p.partial = a.workspace;
+    const uint32_t bytes = plan.lds_rows * (p.part_columns * 2u + 16u), tiles = plan.tiles;
+    const dim3 grid(plan.blocks, a.E, plan.pieces);
+    if (!grid_ok((uint64_t)plan.blocks * a.E * plan.pieces, plan.waves * 64)) return QESGD_ERR_DIM;
     by_type(a.dtype, [&](auto t) {
         constexpr uint32_t DT = t.value, PARTS = parts_of(DT);
         const auto go = [&](auto w) {
@@ -299,10 +336,12 @@ int launch_vector_product(const VectorProduct& a) {
             else if (tiles == 2) k_mx4_vector_product<DT, PARTS >= 2 ? 2 : 1, W><<<grid, W * 64, bytes, a.stream>>>(p);
             else k_mx4_vector_product<DT, PARTS >= 3 ? 3 : 1, W><<<grid, W * 64, bytes, a.stream>>>(p);
         };
-        if (waves == 16) go(std::integral_constant<uint32_t, 16>{});
+        if (plan.waves == 16) go(std::integral_constant<uint32_t, 16>{});
         else go(std::integral_constant<uint32_t, 8>{});
     });
-    return launched();
+    const int rc = launched();
+    if (rc != QESGD_OK || plan.pieces == 1) return rc;
+    return launch_piece_sum(PieceSum{a.workspace, plan.pieces, a.R * a.N, a.offsets, a.E, p.R, p.N, a.y, a.ldy}, a.dtype, a.stream);
 }
 
 }  // namespace qesgd

@@ -183,3 +183,36 @@ def test_graph_and_side_stream(B):
         torch.cuda.synchronize()
         assert torch.equal(y, want), i
         assert np.isfinite(torch.randn(1 << 16, device="cuda").sum().item())
+
+
+LONG = [(16, 1000, 8192, 1), (16, 4096, 4096, 1), (40, 70, 9000, 1), (16, 33, 6001, 3), (64, 512, 5000, 2)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n,N,K,E", LONG)
+def test_long_rows_in_pieces(B, n, N, K, E, dtype):
+    """Several workgroups to a row: the same sums in another order, rows of no group left, a workspace that held NaN, every run the same."""
+    t, need = TYPES[dtype], B.qesgd_mx4_vector_product_workspace_bytes(n, N, K, E)
+    assert need >= 2 * 4 * n * N and need % (4 * n * N) == 0
+    pw, w = packed_noise(B, N, K, E, n + N)
+    offsets = [0, n] if E == 1 else [2] + [2 + (n - 3) * (e + 1) // E for e in range(E)]
+    x, pw = rows(n, K, t, 8), pw.cuda()
+    ws, out = torch.full((need // 4,), float("nan"), device="cuda").view(torch.uint8), []
+    for _ in range(2):
+        y = torch.full((n, N + 3), 3.0, dtype=t, device="cuda")
+        B.qesgd_mx4_vector_product(x.cuda(), K, n, None, 1, pw, pw.stride(0), None if E == 1 else ints(offsets), E, n, N, K, y, N + 3, workspace=ws)
+        out.append(y)
+        ws.view(torch.float32).fill_(float("nan"))
+    assert torch.equal(*out)
+    got = host(out[0])
+    assert (got[:, N:] == 3.0).all() and (got[:offsets[0]] == 3.0).all() and (got[offsets[-1]:] == 3.0).all()
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        want = host(x[lo:hi]) @ w[e].T
+        off = np.abs(got[lo:hi, :N] - want) - limit(host(x[lo:hi]), w[e], want, t)
+        assert (off <= 0).all(), (e, np.argwhere(off > 0)[:4])
+    kept = out[0].clone()
+    for short in (None, ws[:need - 16]):
+        with pytest.raises(B.QesgdError):
+            B.qesgd_mx4_vector_product(x.cuda(), K, n, None, 1, pw, pw.stride(0), None if E == 1 else ints(offsets), E, n, N, K, out[0], N + 3, workspace=short)
+    assert torch.equal(out[0], kept)
