@@ -362,7 +362,7 @@ int qesgd_route_backward(const void* logits, uint32_t dtype, uint64_t ld, uint64
 
 /* out[t] = sum_j gates[t*k+j] * rows[slots[t*k+j]], added in order of j in fp32, rounded once; slots outside 0 .. R-1 are left out.
  * rows [R, N] and out [T, N] in dtype.  gates NULL: 1 each (the gradient of tokens that went to k experts).  slots NULL: row t*k+j (then T*k <= R).
- * T, R and N up to 2^28, T * k < 2^31; calls of more than 2^32 pieces of 16 bytes of out are refused (QESGD_ERR_DIM). */
+ * out may not overlap rows.  T, R and N up to 2^28, T * k < 2^31; calls of more than 2^32 pieces of 16 bytes of out are refused (QESGD_ERR_DIM). */
 int qesgd_combine(const void* rows, uint32_t dtype, uint64_t ld, uint64_t R, const int32_t* slots, const float* gates, uint64_t T, uint32_t k,
                   uint64_t N, void* out, uint64_t ld_out, void* stream);
 

@@ -24,7 +24,7 @@ struct PParams {
     uint64_t ldc;
     uint32_t N, K;                        // rows of B_e; columns of D_e
     uint32_t row_codes, row_scales;       // of either operand
-    uint32_t tiles_m, tiles_n;            // of one expert's D; tiles_n of C
+    uint32_t tiles_m, tiles_n;            // of one expert's D; of C, at most: offsets that fall could make more of them than a number holds
     bool stream;                          // C or D in whole lines that nothing finds in a cache again
     uint32_t pieces;                      // of the contraction; with more than one the sums go to partial [pieces, all of C or D]
     float* partial;
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_product(const PParam
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
     const uint32_t wm = wave / S::WN, wn = wave % S::WN;
     // the workgroups that have a tile are dealt to the XCDs among themselves: those behind the last tile come last of all
-    const uint32_t all = all_tiles(p.offsets, p.E, p.R, lg) * p.tiles_n;
+    const uint32_t all = min(all_tiles(p.offsets, p.E, p.R, lg), p.tiles_m) * p.tiles_n;
     if (blockIdx.x >= all * p.pieces) return;
     uint32_t t = tile_of_workgroup(blockIdx.x, all * p.pieces), piece = 0, first = 0, steps = (p.row_codes + kStepBytes - 1u) / kStepBytes;
     const uint32_t all_steps = steps;
@@ -184,10 +184,10 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
     store_tile<S, DT>(ops, d, p.K, p.N, p.K, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= p.N && n0 + S::BN <= p.K, p.stream);
 }
 
-// A result from the sums of the pieces, added in order (see PieceSum).  Four numbers a lane where rows
-// allow it, eight pieces on their way: the sums come from the memory-side cache and are few, so it is a launch and a latency.
+// A result from the sums of the pieces, added in order (see PieceSum).  Four numbers a lane where rows allow it, eight pieces on their way: the sums
+// come from the memory-side cache and are few, so it is a launch and a latency.
 template <uint32_t DT>
-__global__ void __launch_bounds__(256) k_mx4_grouped_sum(const PieceSum p) {
+__global__ void __launch_bounds__(256) k_mx4_piece_sum(const PieceSum p) {
     const uint64_t i = ((uint64_t)blockIdx.x * 256u + threadIdx.x) * 4u;
     if (i >= p.sums) return;
     uint64_t lo = 0, hi = ~0ull;
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_chain(const PParams 
     if (wave == 0) fill_table(table, p.offsets, p.E, p.R, lg);
     __syncthreads();
     const uint32_t tiles = p.tiles_m * p.tiles_n;
-    const uint32_t all = GRADIENT ? tiles * p.E : (uint32_t)__builtin_amdgcn_readfirstlane((int)table.first[p.E]) * p.tiles_n;
+    const uint32_t all = GRADIENT ? tiles * p.E : min((uint32_t)__builtin_amdgcn_readfirstlane((int)table.first[p.E]), p.tiles_m) * p.tiles_n;
     Mx4Chain<S> ops;
     ops.scales = scales;
     ops.h = lane >> 5;
@@ -471,6 +471,10 @@ uint64_t group_tiles(const GroupProduct& a, uint64_t edge) {
 //   products   16 experts, 32768 rows, N = K = 4096 655 / 402 / 339;  13, 9003, 1000, 2049 33 / 25.9 / 22.7;  8, 2048, 2048, 2048 15.5 / 13.7 / 18.1;
 //              64, 1024, 1024, 1024 11.5 / 9.2 / 12.5;  8, 256, 4096, 4096 17.8 / 16.3 / 27.2;  64, 16384, 2048, 1024 70 / 46 / 46
 //   gradients  8, 16384, 4096, 4096 759 / 344 / 266;  64, 4096, 1024, 1024 109 / 65 / 59;  16, 1024, 512, 512 8.9 / 8.3 / 9.7
+// and, one piece / as many as chosen, graph of 8 calls:
+//   products   1 expert, 64 rows, N 1000, K 16384 20.3 / 9.9 (12 pieces);  8, 64, 512, 8192 12.0 / 8.8 (4);  1, 512, 1000, 25088 29.7 / 21.7 (2);
+//              1, 1, 4096, 4096 7.8 / 7.5 (4);  23, 74, 152, 3597 7.6 / 8.0 (3)
+//   gradients  1, 65536, 256, 256 69 / 14.9 (16);  1, 16384, 64, 64 19.6 / 7.5 (16);  4, 65536, 256, 512 39.7 / 27.7 (2)
 struct Cut { uint32_t edge, pieces; };
 constexpr uint32_t kMostPieces = 16;
 template <class F>
@@ -506,7 +510,9 @@ template <class S>
 int launch_product_tiles(const GroupProduct& a, PParams& p) {
     p.tiles_n = (p.N + S::BN - 1) / S::BN;
     // the most tiles that R rows in E groups make
-    const uint64_t groups = a.E < a.R ? a.E : a.R, tiles_m = (a.R + (S::BM - 1) * groups) / S::BM, tiles = tiles_m * p.tiles_n * p.pieces;
+    const uint64_t groups = a.E < a.R ? a.E : a.R;
+    p.tiles_m = (uint32_t)((a.R + (S::BM - 1) * groups) / S::BM);
+    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n * p.pieces;
     if (!grid_ok(tiles, S::threads)) return QESGD_ERR_DIM;
     by_type(p.pieces > 1 ? QESGD_F32 : a.dtype, [&](auto t) { k_mx4_grouped_product<S, t.value><<<(uint32_t)tiles, S::threads, 0, a.stream>>>(p); });
     const int rc = launched();
@@ -520,9 +526,9 @@ constexpr uint64_t kChainTiles = 512;
 template <class S, bool GRADIENT>
 int launch_chain(const GroupProduct& a, PParams& p) {
     const uint64_t groups = a.E < a.R ? a.E : a.R;
-    p.tiles_m = (p.N + S::BM - 1) / S::BM;
+    p.tiles_m = GRADIENT ? (p.N + S::BM - 1) / S::BM : (uint32_t)((a.R + (S::BM - 1) * groups) / S::BM);
     p.tiles_n = ((GRADIENT ? p.K : p.N) + S::BN - 1) / S::BN;
-    const uint64_t tiles = GRADIENT ? (uint64_t)p.tiles_m * p.tiles_n * a.E : (a.R + (S::BM - 1) * groups) / S::BM * p.tiles_n;
+    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n * (GRADIENT ? a.E : 1);
     if (!grid_ok(tiles, S::threads)) return QESGD_ERR_DIM;
     const uint32_t places = tiles < 256 ? (uint32_t)tiles : 256u;
     by_type(a.dtype, [&](auto t) { k_mx4_grouped_chain<S, t.value, GRADIENT><<<places, S::threads, 0, a.stream>>>(p); });
@@ -547,7 +553,7 @@ int launch_gradient_tiles(const GroupProduct& a, PParams& p) {
 int launch_piece_sum(const PieceSum& p, uint32_t dtype, hipStream_t stream) {
     const uint64_t groups = (p.sums + 1023) / 1024;
     if (!grid_ok(groups, 256)) return QESGD_ERR_DIM;
-    by_type(dtype, [&](auto t) { k_mx4_grouped_sum<t.value><<<(uint32_t)groups, 256, 0, stream>>>(p); });
+    by_type(dtype, [&](auto t) { k_mx4_piece_sum<t.value><<<(uint32_t)groups, 256, 0, stream>>>(p); });
     return launched();
 }
 
