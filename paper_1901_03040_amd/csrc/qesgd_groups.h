@@ -30,29 +30,42 @@ struct Group {
     uint32_t first;                  // tiles of the groups before it
 };
 
-// Tiles of `edge` (a power of two, 2^lg) rows of groups base + lane; lo and hi of that group.
-__device__ __forceinline__ uint32_t group_tiles(const int32_t* offsets, uint32_t E, uint32_t R, uint32_t lg, uint32_t i, uint32_t& lo, uint32_t& hi) {
+// How many tiles a number of rows makes: tiles of 2^lg rows, and of N.
+struct Power {
+    uint32_t lg;
+    __device__ __forceinline__ uint32_t tiles(uint32_t rows) const { return (rows + (1u << lg) - 1u) >> lg; }
+};
+template <uint32_t N>
+struct Times {
+    __device__ __forceinline__ uint32_t tiles(uint32_t rows) const { return (rows + N - 1u) / N; }
+};
+
+// Tiles of group i; lo and hi of that group.
+template <class Edge>
+__device__ __forceinline__ uint32_t group_tiles(const int32_t* offsets, uint32_t E, uint32_t R, Edge edge, uint32_t i, uint32_t& lo, uint32_t& hi) {
     const uint32_t at = min(i, E - 1u);
     lo = held(offsets[at], R);
     hi = held(offsets[at + 1u], R);
-    return i < E && hi > lo ? (hi - lo + (1u << lg) - 1u) >> lg : 0u;
+    return i < E && hi > lo ? edge.tiles(hi - lo) : 0u;
 }
 
 // All groups' tiles.
-__device__ __forceinline__ uint32_t all_tiles(const int32_t* offsets, uint32_t E, uint32_t R, uint32_t lg) {
+template <class Edge>
+__device__ __forceinline__ uint32_t all_tiles(const int32_t* offsets, uint32_t E, uint32_t R, Edge edge) {
     const uint32_t lane = threadIdx.x & 63u;
     uint32_t total = 0, lo, hi;
-    for (uint32_t base = 0; base < E; base += 64u) total += group_tiles(offsets, E, R, lg, base + lane, lo, hi);
+    for (uint32_t base = 0; base < E; base += 64u) total += group_tiles(offsets, E, R, edge, base + lane, lo, hi);
     return lane_value(wave_prefix(total), 63u);
 }
 
 // The group of tile `tile` (times `each`: a group's tiles count so many times); false where there are not so many.  Uniform.
-__device__ __forceinline__ bool group_of_tile(const int32_t* offsets, uint32_t E, uint32_t R, uint32_t lg, uint32_t each, uint32_t tile, Group& g) {
+template <class Edge>
+__device__ __forceinline__ bool group_of_tile(const int32_t* offsets, uint32_t E, uint32_t R, Edge edge, uint32_t each, uint32_t tile, Group& g) {
     const uint32_t lane = threadIdx.x & 63u;
     uint32_t before = 0;
     for (uint32_t base = 0; base < E; base += 64u) {
         uint32_t lo, hi;
-        const uint32_t tiles = group_tiles(offsets, E, R, lg, base + lane, lo, hi) * each;
+        const uint32_t tiles = group_tiles(offsets, E, R, edge, base + lane, lo, hi) * each;
         const uint32_t behind = before + wave_prefix(tiles);
         const uint64_t found = __ballot(tile < behind);
         if (found) {
@@ -68,12 +81,13 @@ __device__ __forceinline__ bool group_of_tile(const int32_t* offsets, uint32_t E
     return false;
 }
 
-// Group e; its first counts tiles of 2^lg rows.
-__device__ __forceinline__ Group group_number(const int32_t* offsets, uint32_t E, uint32_t R, uint32_t lg, uint32_t e) {
+// Group e.
+template <class Edge>
+__device__ __forceinline__ Group group_number(const int32_t* offsets, uint32_t E, uint32_t R, Edge edge, uint32_t e) {
     const uint32_t lane = threadIdx.x & 63u;
     uint32_t total = 0, lo, hi;
     for (uint32_t base = 0; base < e; base += 64u) {
-        const uint32_t tiles = group_tiles(offsets, E, R, lg, base + lane, lo, hi);
+        const uint32_t tiles = group_tiles(offsets, E, R, edge, base + lane, lo, hi);
         total += base + lane < e ? tiles : 0u;
     }
     Group g;

@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_product(const PParam
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, h = lane >> 5;
     const uint32_t wm = wave / S::WN, wn = wave % S::WN;
     // the workgroups that have a tile are dealt to the XCDs among themselves: those behind the last tile come last of all
-    const uint32_t all = min(all_tiles(p.offsets, p.E, p.R, lg), p.tiles_m) * p.tiles_n;
+    const uint32_t all = min(all_tiles(p.offsets, p.E, p.R, Power{lg}), p.tiles_m) * p.tiles_n;
     if (blockIdx.x >= all * p.pieces) return;
     uint32_t t = tile_of_workgroup(blockIdx.x, all * p.pieces), piece = 0, first = 0, steps = (p.row_codes + kStepBytes - 1u) / kStepBytes;
     const uint32_t all_steps = steps;
@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_product(const PParam
         piece_of(p, piece, all_steps, first, steps);
     }
     Group g;
-    if (!group_of_tile(p.offsets, p.E, p.R, lg, p.tiles_n, t, g)) return;
+    if (!group_of_tile(p.offsets, p.E, p.R, Power{lg}, p.tiles_n, t, g)) return;
     uint32_t tm, tn;
     banded_tile(t - g.first, (g.hi - g.lo + S::BM - 1u) >> lg, p.tiles_n, tm, tn);
     tm = __builtin_amdgcn_readfirstlane(tm);
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
     banded_tile(tile_of_workgroup(blockIdx.x - e * tiles, tiles), p.tiles_m, p.tiles_n, tm, tn);
     tm = __builtin_amdgcn_readfirstlane(tm);
     tn = __builtin_amdgcn_readfirstlane(tn);
-    const Group g = group_number(p.offsets, p.E, p.R, 7, e);
+    const Group g = group_number(p.offsets, p.E, p.R, Power{7}, e);
     // bytes of a row's codes before the group and of the group, as far as the rows go
     const uint32_t begin = __builtin_amdgcn_readfirstlane(min(g.first * 64u, p.row_codes));
     const uint32_t bytes = __builtin_amdgcn_readfirstlane(min(((g.hi - g.lo + 127u) >> 7) * 64u, p.row_codes - begin));
@@ -239,7 +239,7 @@ __device__ __forceinline__ void fill_table(GroupTable& table, const int32_t* off
     uint32_t before = 0;
     for (uint32_t base = 0; base < E; base += 64u) {
         uint32_t lo, hi;
-        const uint32_t behind = before + wave_prefix(group_tiles(offsets, E, R, lg, base + lane, lo, hi));
+        const uint32_t behind = before + wave_prefix(group_tiles(offsets, E, R, Power{lg}, base + lane, lo, hi));
         if (base + lane < E) {
             table.first[base + lane + 1u] = behind;
             table.row[base + lane] = lo;

@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kBothThreads) k_mx4_group_both(const GParams p
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint32_t tr = blockIdx.x / p.groups, tc = blockIdx.x - tr * p.groups;
     Group g;
-    if (!group_of_tile(p.offsets, p.E, p.R, 7, 1, tr, g)) return;
+    if (!group_of_tile(p.offsets, p.E, p.R, Power{7}, 1, tr, g)) return;
     const uint32_t r0 = g.lo + (tr - g.first) * kTile, c0 = tc * kTile;
     const uint32_t col = (lane & 15u) * 8u;
     const uint32_t n = c0 + col >= p.cols ? 0u : min(p.cols - c0 - col, 8u);

@@ -37,7 +37,7 @@ struct VParams {
     void* y;
     uint64_t ldy;
     uint32_t splits;                  // waves that share a row's columns: 1 .. kVWaves
-    uint32_t part_columns;            // columns of x that lie in LDS at a time, a multiple of 128
+    uint32_t room;                    // bytes of LDS for rows of x
     uint32_t pieces;                  // of the columns, a workgroup each; with more than one the sums go to partial [pieces, R, N]
     float* partial;
 };
@@ -117,19 +117,10 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
     __shared__ __attribute__((aligned(16))) float sums[kVWaves][TILES][4][64];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t l = lane & 15u, block = lane >> 4;
-    const uint32_t e = blockIdx.y;
-    uint32_t lo = 0, hi = p.R;
-    if (p.offsets) {
-        lo = held(p.offsets[e], p.R);
-        hi = held(p.offsets[e + 1u], p.R);
-        if (lo >= hi) return;
-    }
     const uint32_t share = wave % p.splits, n0 = (blockIdx.x * (kVWaves / p.splits) + wave / p.splits) * 16u;
-    const unsigned char* w = p.w + e * p.w_stride;
     const uint32_t row = min(n0 + l, p.N - 1u);
-    const unsigned char* codes = w + (uint64_t)row * p.row_codes + block * 16u;
-    const unsigned char* scales = w + p.scales_off + (uint64_t)row * p.row_scales + block;
-    const uint32_t steps = p.row_codes / 64u, pitch = p.part_columns * 2u + 16u, piece = blockIdx.z;
+    const unsigned char *codes, *scales;
+    const uint32_t steps = p.row_codes / 64u, piece = blockIdx.z;
     const uint32_t begin = piece * steps / p.pieces * 128u, end = (piece + 1u) * steps / p.pieces * 128u;
     // blocks of the pairs of steps from + s, + 2 splits .. before step `last` of a part: a pair's are a line of memory
     const auto fetch = [&](uvec4 (&c)[2 * kVBatch], uint32_t (&byte)[2 * kVBatch], uint32_t from, uint32_t s, uint32_t last) {
@@ -144,13 +135,20 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
             }
         }
     };
-    for (uint32_t r0 = lo; r0 < hi; r0 += ROWS) {
-        const uint32_t rows = min(ROWS, hi - r0);
+    for (uint32_t tile = blockIdx.y;; tile += gridDim.y) {
+        Group g{0, 0, p.R, 0};
+        if (p.offsets ? !group_of_tile(p.offsets, p.E, p.R, Times<ROWS>{}, 1, tile, g) : tile * ROWS >= p.R) break;        // uniform
+        const uint32_t r0 = g.lo + (tile - g.first) * ROWS, rows = min(ROWS, g.hi - r0);
+        // as many columns of x at a time as there is room for, a multiple of 128, and 16 bytes behind each row
+        const uint32_t part_columns = min((p.room / (rows * PARTS) - 16u) / 256u * 128u, end - begin), pitch = part_columns * 2u + 16u;
+        const unsigned char* w = p.w + g.e * p.w_stride;
+        codes = w + (uint64_t)row * p.row_codes + block * 16u;
+        scales = w + p.scales_off + (uint64_t)row * p.row_scales + block;
         acc4 acc[TILES];
 #pragma unroll
         for (uint32_t m = 0; m < TILES; ++m) acc[m] = acc4{0.0f, 0.0f, 0.0f, 0.0f};
-        for (uint32_t c0 = begin; c0 < end; c0 += p.part_columns) {
-            const uint32_t here = min(p.part_columns, end - c0), last = here / 128u;
+        for (uint32_t c0 = begin; c0 < end; c0 += part_columns) {
+            const uint32_t here = min(part_columns, end - c0), last = here / 128u;
             // the wave's first blocks are on their way while the rows are brought in
             uvec4 c[2 * kVBatch], next_c[2 * kVBatch];
             uint32_t byte[2 * kVBatch], next_byte[2 * kVBatch];
@@ -245,13 +243,14 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
 }
 
 struct Plan {
-    uint32_t waves, splits, tiles, lds_rows, part_columns, pieces, blocks;
+    uint32_t waves, splits, tiles, lds_rows, room, pieces, blocks, row_tiles;
 };
+
+constexpr uint64_t kVFits = 131072, kVPiece = 98304;      // bytes of split rows: as many as fit LDS, and a piece's
 
 Plan plan_of(const VectorProduct& a, uint32_t dtype) {
     Plan p{};
     const uint32_t steps = (uint32_t)((a.K + 127) / 128), parts = parts_of(dtype), across_rows = (uint32_t)((a.N + 15) / 16);
-    const uint32_t hit = a.E < a.R ? a.E : (uint32_t)a.R;
     // rows that an expert has at a time, of which two in three are in its share twice over
     const uint32_t rows = (uint32_t)(a.E == 1 ? a.R : (2 * a.R + a.E - 1) / a.E);
     p.tiles = 1;
@@ -259,18 +258,26 @@ Plan plan_of(const VectorProduct& a, uint32_t dtype) {
     const uint32_t at_a_time = p.tiles * 16 / parts, kept = (rows < at_a_time ? rows : at_a_time) * parts;
     const uint64_t all_bytes = (uint64_t)kept * steps * 256u;
     p.lds_rows = parts * (a.R < at_a_time ? (uint32_t)a.R : at_a_time);
+    // tiles of rows that R rows in E groups make at most, and may be taken to make
+    const uint32_t hit = a.E < a.R ? a.E : (uint32_t)a.R;
+    p.row_tiles = (uint32_t)((a.R + (at_a_time - 1) * (uint64_t)hit) / at_a_time);
+    uint32_t busy = p.row_tiles;
+    if (a.E > 1) {
+        const double groups = (double)a.E * -__builtin_expm1(-(double)a.R / (double)a.E), even = (double)a.R / at_a_time + 0.5 * groups;
+        busy = (uint32_t)((groups > even ? groups : even) + 0.5);
+        if (busy == 0) busy = 1;
+    }
     // Workgroups of 8 waves, two or three on a CU, where there is little to bring into LDS, else of 16, which bring it in faster.  8 / 16 waves, us, graph of 32 calls: one row
-    // x 4096 x 4096 bf16 5.5 / 5.8, f32 6.2 / 8.7, x 512 x 512 f32 3.9 / 6.3; 8 rows bf16 8.7 / 7.1, 16 rows f32 26.6 / 17.4, 4 rows x 4096 x 25088
-    // bf16 28.9 / 21.5.  And as many waves to a row of W as make kVWavesFew or kVWavesMany of them, beyond which each has more steps instead: 12 tokens x 4 of 64
-    // experts 1411 x 2049 with two waves a row 21.3, with one 18.4; one row x 8192 x 8192 bf16 13.1 with 8, 15.9 with 16.
-    constexpr uint32_t kVWavesFew = 2048, kVWavesMany = 4096;
-    p.waves = all_bytes < 32768u ? 8 : 16;
+    // x 4096 x 4096 bf16 5.5 / 5.8, f32 6.2 / 8.7, 8 tokens x 2 of 64 experts 1024 x 2048 bf16 20.6 / 25.3; 8 rows x 4096 x 4096 bf16 8.4 / 7.0, 4 rows f32 8.6 / 8.3.
+    // And as many waves to a row of W as make kVWavesFew or kVWavesMany of them, beyond which each has more steps instead: 4 tokens x 2 of 8 experts 4096 x 4096 bf16 19.5
+    // with one, 12.4 with two; 12 x 4 of 64, 1411 x 2049 f32 17.5 with one, 19.2 with two.
+    constexpr uint32_t kVWavesFew = 1536, kVWavesMany = 4096;
+    p.waves = all_bytes < 65536u ? 8 : 16;
     p.splits = 1;
-    while (p.splits < p.waves && p.splits * 4 <= steps + 1 && (uint64_t)across_rows * hit * p.splits < (p.waves == 8 ? kVWavesFew : kVWavesMany)) p.splits *= 2;
+    while (p.splits < p.waves && p.splits * 4 <= steps + 1 && (uint64_t)across_rows * busy * p.splits < (p.waves == 8 ? kVWavesFew : kVWavesMany)) p.splits *= 2;
     // Rows that do not fit LDS at once, split by every workgroup, are most of the work.  Where waves share the columns anyway, workgroups share them instead, about 96 KB of
     // split rows to each, and a second launch adds their sums.  One piece / as chosen, us, graph of 32 calls: 16 rows x 4096 x 4096 f32 17.6 / 13.5 (4 pieces), 16 x 8192 x 8192
     // f32 40 / 28 and bf16 21 / 18 (4), 16 x 1000 x 8192 f32 30 / 18 (8), 4 x 4096 x 25088 bf16 21 / 19 (8).  Rows that fit gain nothing: 16 x 4096 x 4096 bf16 8.9 / 9.8 (2).
-    constexpr uint64_t kVFits = 131072, kVPiece = 98304;
     p.pieces = 1;
     while (all_bytes > kVFits && all_bytes > kVPiece * p.pieces && p.splits >= 4) {
         p.pieces *= 2;
@@ -279,17 +286,21 @@ Plan plan_of(const VectorProduct& a, uint32_t dtype) {
     const uint32_t across = 16u * (p.waves / p.splits);
     p.blocks = ((uint32_t)a.N + across - 1) / across;
     // the rows whole, where a CU has one workgroup anyway, or else as much of them as leaves room for two
-    const bool alone = (uint64_t)p.blocks * hit * p.pieces <= 256;
+    const bool alone = (uint64_t)p.blocks * busy * p.pieces <= 256;
     const uint32_t room = (alone ? 140u : 60u) * 1024u * p.waves / 16u - p.tiles * 1024u * p.waves * (alone ? 1u : 0u);
-    const uint32_t most = (room / p.lds_rows - 16u) / 2u / 128u * 128u, longest = (steps + p.pieces - 1) / p.pieces * 128u;
-    p.part_columns = most < longest ? most : longest;
+    const uint64_t whole = (uint64_t)p.lds_rows * (((steps + p.pieces - 1) / p.pieces) * 256u + 16u);
+    p.room = whole < room ? (uint32_t)whole : room;
+    const uint64_t most_tiles = (1u << 20) / ((uint64_t)p.blocks * p.pieces);        // a workgroup takes several where there are more
+    if (p.row_tiles > most_tiles) p.row_tiles = (uint32_t)most_tiles;
+    if (p.row_tiles > 65535) p.row_tiles = 65535;
     return p;
 }
 
 }  // namespace
 
-// The type is not known here: as much as any of them needs.
+// As much as the type that needs most: the type is not known where it is asked for.
 size_t vector_product_workspace(const VectorProduct& a) {
+    if ((a.R < 16 ? a.R : 16) * 3 * ((a.K + 127) / 128) * 256 <= kVFits) return 0;          // no type has more to bring in
     uint32_t pieces = 1;
     for (uint32_t t : {QESGD_F32, QESGD_BF16, QESGD_F16}) {
         const uint32_t n = plan_of(a, t).pieces;
@@ -322,12 +333,11 @@ int launch_vector_product(const VectorProduct& a) {
     p.y = a.y;
     p.ldy = a.ldy;
     p.splits = plan.splits;
-    p.part_columns = plan.part_columns;
+    p.room = plan.room;
     p.pieces = plan.pieces;
     p.partial = a.workspace;
-    const uint32_t bytes = plan.lds_rows * (p.part_columns * 2u + 16u), tiles = plan.tiles;
-    const dim3 grid(plan.blocks, a.E, plan.pieces);
-    if (!grid_ok((uint64_t)plan.blocks * a.E * plan.pieces, plan.waves * 64)) return QESGD_ERR_DIM;
+    const uint32_t bytes = plan.room, tiles = plan.tiles;
+    const dim3 grid(plan.blocks, plan.row_tiles, plan.pieces);
     by_type(a.dtype, [&](auto t) {
         constexpr uint32_t DT = t.value, PARTS = parts_of(DT);
         const auto go = [&](auto w) {
