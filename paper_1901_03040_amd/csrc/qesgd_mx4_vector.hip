@@ -7,10 +7,14 @@
 // (one for bf16, two for f16's 11 bits, three for f32's 24), each a row of its own for the matrix instruction, whose 16 rows
 // would stand empty otherwise; so all products are exact and a single row of f32 costs no more instructions than one of bf16.
 //
-// Measured in graphs of 32 calls: one row x 4096 x 4096 bf16 5.4 us, of which a launch is 2.3 and the bytes 1.4; 8192 x 8192 13 us = 2.7 TB/s; 12 tokens x 4 of 64 experts of
-// 1411 x 2049 f32 17 us for 45 MB: a workgroup finds its rows by three trips to memory, then waits for 140 KB of W, and a CU has one or two.
+// The rows of the instruction that x leaves empty take other columns: with SHARES of them to a row of x, each multiplies its own share of the columns, and 16 / SHARES rows of W take
+// the instruction's 16 columns, so 16 lanes read 64 bytes of each of four rows (SHARES 4) and not 16 bytes of each of 16: the lines that a load
+// touches bounded the kernel before, 65536 x 4096 35 us and 25 so.
 //
-// A wave owns 16 rows of W and takes steps of 128 columns; the waves of a workgroup share the columns among them, and their sums are added
+// Measured in graphs of 32 calls: one row x 4096 x 4096 bf16 4.8 us, of which a launch is 2.3 and the bytes 1.4; 8192 x 8192 11.3 us, 65536 x 4096 25 us = 5.7 TB/s; 12 tokens x 4 of
+// 64 experts of 1411 x 2049 f32 15.5 us for 45 MB: a workgroup finds its rows by three trips to memory, then waits for 140 KB of W, and a CU has two.
+//
+// A wave owns 16 rows of W and takes units of 256 or 512 columns; the waves of a workgroup share the units among them, and their sums are added
 // in order.  The rows of x go to LDS once, split; long rows of many tokens in pieces, a workgroup each.
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
@@ -42,7 +46,7 @@ struct VParams {
     float* partial;
 };
 
-constexpr uint32_t kVBatch = 2;           // pairs of steps whose blocks a wave has on their way at a time, twice
+constexpr uint32_t kVLoads = 4;           // loads that a wave has on their way at a time, twice
 
 // bf16 numbers that hold an element.
 constexpr uint32_t parts_of(uint32_t dtype) { return dtype == QESGD_F32 ? 3 : dtype == QESGD_F16 ? 2 : 1; }
@@ -109,57 +113,74 @@ __device__ __forceinline__ void block_values(const uvec4& codes, uint32_t byte, 
     }
 }
 
-// TILES of 16 rows at a time.
-template <uint32_t DT, uint32_t TILES, uint32_t kVWaves>
-__global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VParams p) {
-    constexpr uint32_t PARTS = parts_of(DT), ROWS = TILES * 16 / PARTS;
+// TILES of 16 rows of the instruction, SHARES of which are one number of each element of a row of x: ROWS at a time.
+// Four waves on a SIMD: two workgroups of 8 waves on a CU, which the compiler would not have registers for otherwise.
+template <uint32_t DT, uint32_t TILES, uint32_t SHARES, uint32_t kVWaves>
+__global__ void __launch_bounds__(kVWaves * 64, 4) k_mx4_vector_product(const VParams p) {
+    constexpr uint32_t PARTS = parts_of(DT), KEPT = TILES * 16 / SHARES, ROWS = KEPT / PARTS, GROUP = 16 / SHARES;
+    // a unit: 16 rows of W x 256 or 512 columns, in LOADS loads; BATCH units on their way
+    constexpr uint32_t LOADS = SHARES < 2 ? 2 : SHARES, BATCH = kVLoads / LOADS, UNIT = LOADS * 128;
     extern __shared__ __attribute__((aligned(16))) unsigned char rows_lds[];            // rows of part_columns bf16 and 16 bytes
-    __shared__ __attribute__((aligned(16))) float sums[kVWaves][TILES][4][64];
+    __shared__ float sums[kVWaves][KEPT][16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t l = lane & 15u, block = lane >> 4;
+    const uint32_t l = lane & 15u, block = lane >> 4, piece = blockIdx.z;
     const uint32_t share = wave % p.splits, n0 = (blockIdx.x * (kVWaves / p.splits) + wave / p.splits) * 16u;
-    const uint32_t row = min(n0 + l, p.N - 1u);
-    const unsigned char *codes, *scales;
-    const uint32_t steps = p.row_codes / 64u, piece = blockIdx.z;
-    const uint32_t begin = piece * steps / p.pieces * 128u, end = (piece + 1u) * steps / p.pieces * 128u;
-    // blocks of the pairs of steps from + s, + 2 splits .. before step `last` of a part: a pair's are a line of memory
-    const auto fetch = [&](uvec4 (&c)[2 * kVBatch], uint32_t (&byte)[2 * kVBatch], uint32_t from, uint32_t s, uint32_t last) {
+    // the wave's first row of W, and the scales (sixteen bytes of codes each) before the lane's row in load i of a unit
+    const uint32_t row0 = min(n0, p.N - 1u);
+    uint32_t before[SHARES];
 #pragma unroll
-        for (uint32_t q = 0; q < kVBatch; ++q) {
-            if (s + q * 2u * p.splits >= last) break;                  // uniform
-#pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) {
-                const uint32_t step = from + min(s + q * 2u * p.splits + h, last - 1u);
-                c[2 * q + h] = *(const uvec4*)(codes + step * 64u);
-                byte[2 * q + h] = scales[step * 4u];
-            }
-        }
-    };
+    for (uint32_t i = 0; i < SHARES; ++i) before[i] = min(i * GROUP + l / SHARES, p.N - 1u - row0) * p.row_scales;
+    const uint32_t own = block * SHARES + l % SHARES, blocks = p.row_scales;
+    const uint32_t units = (blocks * 32u + UNIT - 1u) / UNIT, begin = piece * units / p.pieces * UNIT, end = (piece + 1u) * units / p.pieces * UNIT;
     for (uint32_t tile = blockIdx.y;; tile += gridDim.y) {
         Group g{0, 0, p.R, 0};
         if (p.offsets ? !group_of_tile(p.offsets, p.E, p.R, Times<ROWS>{}, 1, tile, g) : tile * ROWS >= p.R) break;        // uniform
         const uint32_t r0 = g.lo + (tile - g.first) * ROWS, rows = min(ROWS, g.hi - r0);
-        // as many columns of x at a time as there is room for, a multiple of 128, and 16 bytes behind each row
-        const uint32_t part_columns = min((p.room / (rows * PARTS) - 16u) / 256u * 128u, end - begin), pitch = part_columns * 2u + 16u;
+        // as many columns of x at a time as there is room for, in whole units, and 16 bytes behind each row
+        const uint32_t part_columns = min((p.room / (rows * PARTS) - 16u) / (2u * UNIT) * UNIT, end - begin), pitch = part_columns * 2u + 16u;
         const unsigned char* w = p.w + g.e * p.w_stride;
-        codes = w + (uint64_t)row * p.row_codes + block * 16u;
-        scales = w + p.scales_off + (uint64_t)row * p.row_scales + block;
-        acc4 acc[TILES];
+        const unsigned char *codes = w + (uint64_t)row0 * p.row_codes, *scales = w + p.scales_off + (uint64_t)row0 * p.row_scales;
+        // blocks of units j, j + 1 .. of the wave's in a part of n units from unit `from` on; behind the row's end its last one, for which x has zeros
+        const auto fetch = [&](uvec4 (&c)[kVLoads], uint32_t (&byte)[kVLoads], uint32_t from, uint32_t j, uint32_t n) {
 #pragma unroll
-        for (uint32_t m = 0; m < TILES; ++m) acc[m] = acc4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (uint32_t q = 0; q < BATCH; ++q) {
+                if (share + (j + q) * p.splits >= n) break;                // uniform
+#pragma unroll
+                for (uint32_t i = 0; i < LOADS; ++i) {
+                    const uint32_t at = min((from + share + (j + q) * p.splits) * (UNIT / 32u) + (SHARES < 2 ? i * 4u : 0u) + own, blocks - 1u) + before[SHARES < 2 ? 0 : i];
+                    c[q * LOADS + i] = *(const uvec4*)(codes + at * 16u);
+                    byte[q * LOADS + i] = scales[at];
+                }
+            }
+        };
+        acc4 acc[TILES][SHARES];
+#pragma unroll
+        for (uint32_t m = 0; m < TILES; ++m)
+#pragma unroll
+            for (uint32_t i = 0; i < SHARES; ++i) acc[m][i] = acc4{0.0f, 0.0f, 0.0f, 0.0f};
         for (uint32_t c0 = begin; c0 < end; c0 += part_columns) {
-            const uint32_t here = min(part_columns, end - c0), last = here / 128u;
+            const uint32_t here = min(part_columns, end - c0), n = here / UNIT;
             // the wave's first blocks are on their way while the rows are brought in
-            uvec4 c[2 * kVBatch], next_c[2 * kVBatch];
-            uint32_t byte[2 * kVBatch], next_byte[2 * kVBatch];
-            fetch(c, byte, c0 / 128u, 2u * share, last);
+            uvec4 c[kVLoads], next_c[kVLoads];
+            uint32_t byte[kVLoads], next_byte[kVLoads];
+            fetch(c, byte, c0 / UNIT, 0u, n);
             __syncthreads();
-            // whole pieces of eight, some of a thread's on their way at a time, and then the elements that are left and zeros behind them
+            // whole pieces of eight, some of a thread's on their way at a time, and by the last threads what is left of the rows and zeros behind them
             const uint32_t filled = p.K > c0 ? min(here, p.K - c0) : 0u, whole = filled / 8u;
             const auto source = [&](uint32_t r) {
                 const int32_t pair = p.order ? p.order[r0 + r] : (int32_t)(r0 + r);
                 return pair < 0 ? p.T : p.per == 1u ? (uint32_t)pair : __umulhi((uint32_t)pair, p.per_factor) >> p.per_shift;
             };
+            const uint32_t behind = here / 8u - whole;
+            for (uint32_t i = kVWaves * 64u - 1u - threadIdx.x; i < rows * behind; i += kVWaves * 64u) {
+                const uint32_t r = i / behind, col = (whole + i - r * behind) * 8u, s = source(r), there = s < p.T && col < filled ? filled - col : 0u;
+                Eight<DT> v;
+                uvec4 parts[PARTS];
+                v.load(p.x, there ? s * p.ld + c0 + col : 0u, there);
+                split<DT, PARTS>(v, parts);
+#pragma unroll
+                for (uint32_t h = 0; h < PARTS; ++h) *(uvec4*)(rows_lds + (r * PARTS + h) * pitch + col * 2u) = parts[h];
+            }
             constexpr uint32_t kPieces = kVWaves == 8 ? 1 : DT == QESGD_BF16 ? 4 : 2;
             for (uint32_t i0 = threadIdx.x; i0 < rows * whole; i0 += kPieces * kVWaves * 64u) {
                 Eight<DT> v[kPieces];
@@ -181,46 +202,57 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
                     for (uint32_t h = 0; h < PARTS; ++h) *(uvec4*)(rows_lds + to[q] + h * pitch) = parts[h];
                 }
             }
-            const uint32_t rest = here - whole * 8u;
-            for (uint32_t i = threadIdx.x; i < rows * rest; i += kVWaves * 64u) {
-                const uint32_t r = i / rest, col = whole * 8u + i - r * rest, s = source(r);
-                uint32_t part[PARTS];
-                split_one<DT, PARTS>(col < filled && s < p.T ? element_at<DT>(p.x, s * p.ld + c0 + col) : 0.0f, part);
-#pragma unroll
-                for (uint32_t h = 0; h < PARTS; ++h) *(unsigned short*)(rows_lds + (r * PARTS + h) * pitch + col * 2u) = (unsigned short)(part[h] >> 16);
-            }
             __syncthreads();
             // rows of the instruction beyond those there are read the last one: what comes of them is not stored
             const unsigned char* x[TILES];
 #pragma unroll
-            for (uint32_t m = 0; m < TILES; ++m) x[m] = rows_lds + min(m * 16u + l, rows * PARTS - 1u) * pitch + block * 64u;
-            for (uint32_t s = 2u * share; s < last; s += 2u * kVBatch * p.splits) {
-                fetch(next_c, next_byte, c0 / 128u, s + 2u * kVBatch * p.splits, last);
+            for (uint32_t m = 0; m < TILES; ++m) x[m] = rows_lds + min(m * GROUP + l / SHARES, rows * PARTS - 1u) * pitch + own * 64u;
+            for (uint32_t j = 0; share + j * p.splits < n; j += BATCH) {
+                fetch(next_c, next_byte, c0 / UNIT, j + BATCH, n);
 #pragma unroll
-                for (uint32_t q = 0; q < 2 * kVBatch; ++q) {
-                    const uint32_t step = s + (q >> 1) * 2u * p.splits + (q & 1u);
-                    if (step >= last) break;                           // uniform
-                    bf16x8 b[4];
-                    block_values(c[q], byte[q], b);
+                for (uint32_t q = 0; q < BATCH; ++q) {
+                    const uint32_t unit = share + (j + q) * p.splits;
+                    if (unit >= n) break;                              // uniform
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (uint32_t h = 0; h < (SHARES < 2 ? LOADS : 1u); ++h) {
+                        bf16x8 a[TILES][4];
 #pragma unroll
                         for (uint32_t m = 0; m < TILES; ++m)
-                            acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)(x[m] + step * 256u + i * 16u), b[i], acc[m], 0, 0, 0);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) a[m][i] = *(const bf16x8*)(x[m] + unit * (UNIT * 2u) + h * 256u + i * 16u);
+#pragma unroll
+                        for (uint32_t s = 0; s < SHARES; ++s) {
+                            bf16x8 b[4];
+                            block_values(c[q * LOADS + (SHARES < 2 ? h : s)], byte[q * LOADS + (SHARES < 2 ? h : s)], b);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                                for (uint32_t m = 0; m < TILES; ++m) acc[m][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[m][i], b[i], acc[m][s], 0, 0, 0);
+                        }
+                    }
                 }
 #pragma unroll
-                for (uint32_t q = 0; q < 2 * kVBatch; ++q) {
+                for (uint32_t q = 0; q < kVLoads; ++q) {
                     c[q] = next_c[q];
                     byte[q] = next_byte[q];
                 }
             }
         }
+        // A lane holds column l and rows 4 block + i of a result, and counts where both have the same share of the columns.
 #pragma unroll
         for (uint32_t m = 0; m < TILES; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sums[wave][m][i][lane] = acc[m][i];
+            for (uint32_t s = 0; s < SHARES; ++s)
+#pragma unroll
+                for (uint32_t i = 0; i < 4; i += SHARES) {
+                    float v = acc[m][s][i];
+#pragma unroll
+                    for (uint32_t k = 1; k < SHARES; ++k) v = l % SHARES == k ? acc[m][s][i + k] : v;
+                    if (SHARES >= 2) v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0xB1, 0xF, 0xF, false));
+                    if (SHARES >= 4) v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x4E, 0xF, 0xF, false));
+                    if (l % SHARES == 0) sums[wave][m * GROUP + (4u * block + i) / SHARES][s * GROUP + l / SHARES] = v;
+                }
         __syncthreads();
-        // sums[wave][m][i][lane]: row 16 m + 4 (lane / 16) + i of the instructions, column lane % 16
         for (uint32_t i = threadIdx.x; i < (kVWaves / p.splits) * 16u * rows; i += kVWaves * 64u) {
             const uint32_t col = i & 15u, r = (i >> 4) % rows, set = (i >> 4) / rows;
             const uint32_t n = (blockIdx.x * (kVWaves / p.splits) + set) * 16u + col;
@@ -228,11 +260,10 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
             float v = 0.0f;
 #pragma unroll
             for (int q = PARTS - 1; q >= 0; --q) {
-                const uint32_t m = r * PARTS + q;
-                const float* from = &sums[set * p.splits][m >> 4][m & 3u][(m >> 2 & 3u) * 16u + col];
+                const float* from = &sums[set * p.splits][r * PARTS + q][col];
                 float part[kVWaves];
 #pragma unroll
-                for (uint32_t s = 0; s < kVWaves; ++s) part[s] = s < p.splits ? from[s * (TILES * 256u)] : 0.0f;
+                for (uint32_t s = 0; s < kVWaves; ++s) part[s] = s < p.splits ? from[s * (KEPT * 16u)] : 0.0f;
 #pragma unroll
                 for (uint32_t s = 0; s < kVWaves; ++s) v += part[s];
             }
@@ -243,7 +274,7 @@ __global__ void __launch_bounds__(kVWaves * 64) k_mx4_vector_product(const VPara
 }
 
 struct Plan {
-    uint32_t waves, splits, tiles, lds_rows, room, pieces, blocks, row_tiles;
+    uint32_t waves, splits, tiles, lds_rows, room, pieces, blocks, row_tiles, shares;
 };
 
 constexpr uint64_t kVFits = 131072, kVPiece = 98304;      // bytes of split rows: as many as fit LDS, and a piece's
@@ -251,22 +282,30 @@ constexpr uint64_t kVFits = 131072, kVPiece = 98304;      // bytes of split rows
 Plan plan_of(const VectorProduct& a, uint32_t dtype) {
     Plan p{};
     const uint32_t steps = (uint32_t)((a.K + 127) / 128), parts = parts_of(dtype), across_rows = (uint32_t)((a.N + 15) / 16);
+    // experts that may be taken to have rows, and tiles of `at` rows that they may be taken to make
+    const double groups = a.E > 1 ? (double)a.E * -__builtin_expm1(-(double)a.R / (double)a.E) : 1.0;
+    const auto tiles_of = [&](uint32_t at) {
+        if (a.E == 1) return (uint32_t)((a.R + at - 1) / at);
+        const double even = (double)a.R / at + 0.5 * groups, n = (groups > even ? groups : even) + 0.5;
+        return n < 1.0 ? 1u : (uint32_t)n;
+    };
+    // Four rows of the instruction to a row of x, unless tiles of so few rows are so many that reading W once for each is most of the work; then two, while the rows of an
+    // expert fit into one tile so, or else one.  Us with 4 / 2 / 1, graph of 16 calls: one row x 4096 x 4096 bf16 5.0 / 5.4 / 5.7, 16 rows 7.4 / 8.5 / 8.9, 4 rows f32 7.1 / 8.3
+    // / 8.3; 8 tokens x 8 of 128 experts 512 x 2048 bf16 8.2 / 10.5 / 12.1; but 12 x 4 of 64, 1411 x 2049 f32 19.6 / 15.3 / 16.9, 16 rows x 8192 x 8192 f32 48 / 50 / 25 and bf16
+    // 20.7 / - / 18.4, 16 x 2 of 8, 4096 x 4096 f32 34 / 41 / 26.
+    constexpr uint64_t kVWork = 80 << 10;               // 16 rows of W x 128 columns each
+    p.tiles = 1;
+    p.shares = 4;
+    if ((uint64_t)across_rows * tiles_of(parts > 2 ? 1 : 4 / parts) * ((steps + 3) / 4 * 4) > kVWork) p.shares = (double)a.R * parts <= 8.5 * groups ? 2 : 1;
     // rows that an expert has at a time, of which two in three are in its share twice over
     const uint32_t rows = (uint32_t)(a.E == 1 ? a.R : (2 * a.R + a.E - 1) / a.E);
-    p.tiles = 1;
-    while (p.tiles < parts && p.tiles * 16 / parts < rows) ++p.tiles;
-    const uint32_t at_a_time = p.tiles * 16 / parts, kept = (rows < at_a_time ? rows : at_a_time) * parts;
+    while (p.shares == 1 && p.tiles < parts && p.tiles * 16 / parts < rows) ++p.tiles;
+    const uint32_t at_a_time = p.tiles * (16 / p.shares) / parts, kept = (rows < at_a_time ? rows : at_a_time) * parts;
     const uint64_t all_bytes = (uint64_t)kept * steps * 256u;
     p.lds_rows = parts * (a.R < at_a_time ? (uint32_t)a.R : at_a_time);
-    // tiles of rows that R rows in E groups make at most, and may be taken to make
-    const uint32_t hit = a.E < a.R ? a.E : (uint32_t)a.R;
+    // at most
+    const uint32_t hit = a.E < a.R ? a.E : (uint32_t)a.R, busy = tiles_of(at_a_time);
     p.row_tiles = (uint32_t)((a.R + (at_a_time - 1) * (uint64_t)hit) / at_a_time);
-    uint32_t busy = p.row_tiles;
-    if (a.E > 1) {
-        const double groups = (double)a.E * -__builtin_expm1(-(double)a.R / (double)a.E), even = (double)a.R / at_a_time + 0.5 * groups;
-        busy = (uint32_t)((groups > even ? groups : even) + 0.5);
-        if (busy == 0) busy = 1;
-    }
     // Workgroups of 8 waves, two or three on a CU, where there is little to bring into LDS, else of 16, which bring it in faster.  8 / 16 waves, us, graph of 32 calls: one row
     // x 4096 x 4096 bf16 5.5 / 5.8, f32 6.2 / 8.7, 8 tokens x 2 of 64 experts 1024 x 2048 bf16 20.6 / 25.3; 8 rows x 4096 x 4096 bf16 8.4 / 7.0, 4 rows f32 8.6 / 8.3.
     // And as many waves to a row of W as make kVWavesFew or kVWavesMany of them, beyond which each has more steps instead: 4 tokens x 2 of 8 experts 4096 x 4096 bf16 19.5
@@ -274,7 +313,7 @@ Plan plan_of(const VectorProduct& a, uint32_t dtype) {
     constexpr uint32_t kVWavesFew = 1536, kVWavesMany = 4096;
     p.waves = all_bytes < 65536u ? 8 : 16;
     p.splits = 1;
-    while (p.splits < p.waves && p.splits * 4 <= steps + 1 && (uint64_t)across_rows * busy * p.splits < (p.waves == 8 ? kVWavesFew : kVWavesMany)) p.splits *= 2;
+    while (p.splits < p.waves && p.splits * (p.shares == 4 ? 8 : 4) <= steps + 1 && (uint64_t)across_rows * busy * p.splits < (p.waves == 8 ? kVWavesFew : kVWavesMany)) p.splits *= 2;
     // Rows that do not fit LDS at once, split by every workgroup, are most of the work.  Where waves share the columns anyway, workgroups share them instead, about 96 KB of
     // split rows to each, and a second launch adds their sums.  One piece / as chosen, us, graph of 32 calls: 16 rows x 4096 x 4096 f32 17.6 / 13.5 (4 pieces), 16 x 8192 x 8192
     // f32 40 / 28 and bf16 21 / 18 (4), 16 x 1000 x 8192 f32 30 / 18 (8), 4 x 4096 x 25088 bf16 21 / 19 (8).  Rows that fit gain nothing: 16 x 4096 x 4096 bf16 8.9 / 9.8 (2).
@@ -287,8 +326,9 @@ Plan plan_of(const VectorProduct& a, uint32_t dtype) {
     p.blocks = ((uint32_t)a.N + across - 1) / across;
     // the rows whole, where a CU has one workgroup anyway, or else as much of them as leaves room for two
     const bool alone = (uint64_t)p.blocks * busy * p.pieces <= 256;
-    const uint32_t room = (alone ? 140u : 60u) * 1024u * p.waves / 16u - p.tiles * 1024u * p.waves * (alone ? 1u : 0u);
-    const uint64_t whole = (uint64_t)p.lds_rows * (((steps + p.pieces - 1) / p.pieces) * 256u + 16u);
+    const uint32_t room = (alone ? 140u : 60u) * 1024u * p.waves / 16u - (alone ? p.tiles * 1024u / p.shares * p.waves : 0u);
+    const uint32_t unit = p.shares == 4 ? 4 : 2, units = (steps + unit - 1) / unit;
+    const uint64_t whole = (uint64_t)p.lds_rows * ((units + p.pieces - 1) / p.pieces * unit * 256u + 16u);
     p.room = whole < room ? (uint32_t)whole : room;
     const uint64_t most_tiles = (1u << 20) / ((uint64_t)p.blocks * p.pieces);        // a workgroup takes several where there are more
     if (p.row_tiles > most_tiles) p.row_tiles = (uint32_t)most_tiles;
@@ -339,15 +379,20 @@ int launch_vector_product(const VectorProduct& a) {
     const uint32_t bytes = plan.room, tiles = plan.tiles;
     const dim3 grid(plan.blocks, plan.row_tiles, plan.pieces);
     by_type(a.dtype, [&](auto t) {
-        constexpr uint32_t DT = t.value, PARTS = parts_of(DT);
-        const auto go = [&](auto w) {
-            constexpr uint32_t W = w.value;
-            if (tiles == 1) k_mx4_vector_product<DT, 1, W><<<grid, W * 64, bytes, a.stream>>>(p);
-            else if (tiles == 2) k_mx4_vector_product<DT, PARTS >= 2 ? 2 : 1, W><<<grid, W * 64, bytes, a.stream>>>(p);
-            else k_mx4_vector_product<DT, PARTS >= 3 ? 3 : 1, W><<<grid, W * 64, bytes, a.stream>>>(p);
+        using std::integral_constant;
+        constexpr uint32_t DT = t.value;
+        const auto go = [&](auto m, auto s) {
+            if (plan.waves == 16) k_mx4_vector_product<DT, m.value, s.value, 16><<<grid, 16 * 64, bytes, a.stream>>>(p);
+            else k_mx4_vector_product<DT, m.value, s.value, 8><<<grid, 8 * 64, bytes, a.stream>>>(p);
         };
-        if (plan.waves == 16) go(std::integral_constant<uint32_t, 16>{});
-        else go(std::integral_constant<uint32_t, 8>{});
+        const integral_constant<uint32_t, 1> one{};
+        const integral_constant<uint32_t, 2> two{};
+        const integral_constant<uint32_t, 4> four{};
+        if (plan.shares == 4) go(one, four);
+        else if (plan.shares == 2) go(one, two);
+        else if (tiles == 1) go(one, one);
+        else if (tiles == 2) go(integral_constant<uint32_t, parts_of(DT) >= 2 ? 2 : 1>{}, one);
+        else go(integral_constant<uint32_t, parts_of(DT) >= 3 ? 3 : 1>{}, one);
     });
     const int rc = launched();
     if (rc != QESGD_OK || plan.pieces == 1) return rc;

@@ -185,7 +185,15 @@ def test_graph_and_side_stream(B):
         assert np.isfinite(torch.randn(1 << 16, device="cuda").sum().item())
 
 
-LONG = [(16, 1000, 8192, 1), (16, 4096, 4096, 1), (40, 70, 9000, 1), (16, 33, 6001, 3), (64, 512, 5000, 2)]
+LONG = [(16, 1000, 8192, 1), (16, 4096, 4096, 1), (40, 70, 9000, 1), (16, 33, 6001, 3), (64, 512, 5000, 2),
+        (16, 4100, 5000, 1), (2, 30, 50_001, 1), (33, 5000, 9000, 1), (4, 20, 40_000, 2), (7, 100, 70_000, 3), (64, 4096, 4096, 1)]
+PIECES = LONG[5:]
+
+
+@pytest.mark.parametrize("n,N,K,E", PIECES)
+def test_long_rows_need_room_for_their_pieces(B, n, N, K, E):
+    need = B.qesgd_mx4_vector_product_workspace_bytes(n, N, K, E)
+    assert need >= 2 * 4 * n * N and need % (4 * n * N) == 0
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
@@ -193,11 +201,10 @@ LONG = [(16, 1000, 8192, 1), (16, 4096, 4096, 1), (40, 70, 9000, 1), (16, 33, 60
 def test_long_rows_in_pieces(B, n, N, K, E, dtype):
     """Several workgroups to a row: the same sums in another order, rows of no group left, a workspace that held NaN, every run the same."""
     t, need = TYPES[dtype], B.qesgd_mx4_vector_product_workspace_bytes(n, N, K, E)
-    assert need >= 2 * 4 * n * N and need % (4 * n * N) == 0
     pw, w = packed_noise(B, N, K, E, n + N)
     offsets = [0, n] if E == 1 else [2] + [2 + (n - 3) * (e + 1) // E for e in range(E)]
     x, pw = rows(n, K, t, 8), pw.cuda()
-    ws, out = torch.full((need // 4,), float("nan"), device="cuda").view(torch.uint8), []
+    ws, out = torch.full((max(need // 4, 1),), float("nan"), device="cuda").view(torch.uint8), []
     for _ in range(2):
         y = torch.full((n, N + 3), 3.0, dtype=t, device="cuda")
         B.qesgd_mx4_vector_product(x.cuda(), K, n, None, 1, pw, pw.stride(0), None if E == 1 else ints(offsets), E, n, N, K, y, N + 3, workspace=ws)
@@ -212,7 +219,38 @@ def test_long_rows_in_pieces(B, n, N, K, E, dtype):
         off = np.abs(got[lo:hi, :N] - want) - limit(host(x[lo:hi]), w[e], want, t)
         assert (off <= 0).all(), (e, np.argwhere(off > 0)[:4])
     kept = out[0].clone()
-    for short in (None, ws[:need - 16]):
+    for short in (None, ws[:need - 16]) if need else ():
         with pytest.raises(B.QesgdError):
             B.qesgd_mx4_vector_product(x.cuda(), K, n, None, 1, pw, pw.stride(0), None if E == 1 else ints(offsets), E, n, N, K, out[0], N + 3, workspace=short)
     assert torch.equal(out[0], kept)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_few_rows_of_many_experts(B, dtype):
+    """As many experts as make the kernel take its rows in larger tiles, the reference on the GPU in 64 bits, an expert at a time."""
+    t, E, n, N, K = TYPES[dtype], 300, 600, 230, 2100
+    rng = np.random.default_rng(4)
+    sizes = rng.multinomial(n - 5, rng.dirichlet(np.full(E, 2.0)))
+    offsets, order = np.concatenate(([3], 3 + np.cumsum(sizes))), rng.permutation(n)
+    lay = B.qesgd_mx4_layout_query(N, K)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    slab = torch.randint(0, 256, (E, lay.bytes), dtype=torch.uint8, device="cuda", generator=g)
+    codes, scales = slab[:, :N * lay.row_codes].view(E, N, -1), slab[:, lay.scales_off:lay.scales_off + N * lay.row_scales].view(E, N, -1)
+    scales.copy_(120 + scales % 14)
+    grid = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, 0, -.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device="cuda")
+    x = rows(n // 2, K, t, 5).cuda()
+    y = torch.full((n, N), 3.0, dtype=t, device="cuda")
+    B.qesgd_mx4_vector_product(x, K, n // 2, ints(order), 2, slab, slab.stride(0), ints(offsets), E, n, N, K, y, N,
+                               workspace=B.alloc_workspace(B.qesgd_mx4_vector_product_workspace_bytes(n, N, K, E)))
+    got, picked = host(y), host(x)[order // 2]
+    assert (got[:3] == 3.0).all() and (got[offsets[-1]:] == 3.0).all()
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        if lo == hi:
+            continue
+        c = codes[e].long()
+        w = grid[torch.stack((c & 15, c >> 4), -1).view(N, -1)] * torch.exp2(scales[e].double() - 127).repeat_interleave(32, 1)
+        w = w[:, :K].cpu().numpy()
+        want = picked[lo:hi] @ w.T
+        off = np.abs(got[lo:hi] - want) - limit(picked[lo:hi], w, want, t)
+        assert (off <= 0).all(), (e, np.argwhere(off > 0)[:4])
