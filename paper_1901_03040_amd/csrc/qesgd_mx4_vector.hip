@@ -286,17 +286,18 @@ Plan plan_of(const VectorProduct& a, uint32_t dtype) {
     const double groups = a.E > 1 ? (double)a.E * -__builtin_expm1(-(double)a.R / (double)a.E) : 1.0;
     const auto tiles_of = [&](uint32_t at) {
         if (a.E == 1) return (uint32_t)((a.R + at - 1) / at);
-        const double even = (double)a.R / at + 0.5 * groups, n = (groups > even ? groups : even) + 0.5;
+        const double even = ((double)a.R + 0.5 * (at - 1) * groups) / at, n = (groups > even ? groups : even) + 0.5;
         return n < 1.0 ? 1u : (uint32_t)n;
     };
-    // Four rows of the instruction to a row of x, unless tiles of so few rows are so many that reading W once for each is most of the work; then two, while the rows of an
-    // expert fit into one tile so, or else one.  Us with 4 / 2 / 1, graph of 16 calls: one row x 4096 x 4096 bf16 5.0 / 5.4 / 5.7, 16 rows 7.4 / 8.5 / 8.9, 4 rows f32 7.1 / 8.3
-    // / 8.3; 8 tokens x 8 of 128 experts 512 x 2048 bf16 8.2 / 10.5 / 12.1; but 12 x 4 of 64, 1411 x 2049 f32 19.6 / 15.3 / 16.9, 16 rows x 8192 x 8192 f32 48 / 50 / 25 and bf16
-    // 20.7 / - / 18.4, 16 x 2 of 8, 4096 x 4096 f32 34 / 41 / 26.
-    constexpr uint64_t kVWork = 80 << 10;               // 16 rows of W x 128 columns each
+    // Four rows of the instruction to a row of x, unless tiles of so few rows make more workgroups than the CUs have places, or reading W once for each is most of the work;
+    // then two, while the rows of an expert fit into one tile so, or else one.  Us with 4 / 2 / 1, graph of 16 calls: one row x 4096 x 4096 bf16 5.0 / 5.4 / 5.7, 16 rows
+    // 7.4 / 8.5 / 8.9, 4 rows f32 7.1 / 8.3 / 8.3; 8 tokens x 8 of 128 experts 512 x 2048 bf16 8.2 / 10.5 / 12.1; 4 x 2 of 8, 4096 x 4096 f32 12.7 / 16.9 / 19; but 12 x 4 of 64,
+    // 1411 x 2049 f32 19.0 / 15.3 / 16.9, 16 rows x 8192 x 8192 f32 48 / 50 / 25 and bf16 20.7 / - / 18.4, 64 x 4 of 64, 1411 x 2049 bf16 36 / 32 / 39.
+    constexpr uint64_t kVPlaces = 4096, kVWork = 128 << 10;               // waves, and units of 16 rows of W x 128 columns
     p.tiles = 1;
     p.shares = 4;
-    if ((uint64_t)across_rows * tiles_of(parts > 2 ? 1 : 4 / parts) * ((steps + 3) / 4 * 4) > kVWork) p.shares = (double)a.R * parts <= 8.5 * groups ? 2 : 1;
+    const uint64_t few = (uint64_t)across_rows * tiles_of(parts > 2 ? 1 : 4 / parts);
+    if (few > kVPlaces || few * ((steps + 3) / 4 * 4) >= kVWork) p.shares = (double)a.R * parts <= 8.5 * groups ? 2 : 1;
     // rows that an expert has at a time, of which two in three are in its share twice over
     const uint32_t rows = (uint32_t)(a.E == 1 ? a.R : (2 * a.R + a.E - 1) / a.E);
     while (p.shares == 1 && p.tiles < parts && p.tiles * 16 / parts < rows) ++p.tiles;

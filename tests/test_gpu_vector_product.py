@@ -228,7 +228,7 @@ def test_long_rows_in_pieces(B, n, N, K, E, dtype):
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_few_rows_of_many_experts(B, dtype):
     """As many experts as make the kernel take its rows in larger tiles, the reference on the GPU in 64 bits, an expert at a time."""
-    t, E, n, N, K = TYPES[dtype], 300, 600, 230, 2100
+    t, E, n, N, K = TYPES[dtype], 300, 600, 270, 2100
     rng = np.random.default_rng(4)
     sizes = rng.multinomial(n - 5, rng.dirichlet(np.full(E, 2.0)))
     offsets, order = np.concatenate(([3], 3 + np.cumsum(sizes))), rng.permutation(n)
