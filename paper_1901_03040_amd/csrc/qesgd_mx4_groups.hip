@@ -4,11 +4,12 @@
 // codes, of four scales), so the product walks whole blocks and no block holds rows of two experts.
 //
 // A row goes to k experts and is read k times, from the memory-side cache where x fits it.  16384 tokens x 2 x 4096 bf16 along the rows 47 us (54 beside other work)
-// = 340 MB at 7.2 TB/s; 8192 x 2, both forms, 36 us nearest and 73 stochastic, which is its arithmetic (two Philox calls for 8 elements).
+// = 340 MB at 7.2 TB/s; 8192 x 2, both forms, 34 us nearest and 69 stochastic, which is its arithmetic (two Philox calls for 8 elements).
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_launch.h"
 #include "qesgd_mx4_codes.h"
+#include "qesgd_tile_product.h"
 
 namespace qesgd {
 namespace {
@@ -46,7 +47,7 @@ __device__ __forceinline__ void sources(const GParams& p, const uint32_t (&row)[
 }
 
 // Along the rows: a lane owns 8 consecutive slots of the padded matrix, a quad a block, a wave kGChunks chunks of 512.
-// One, two and four chunks a wave: 52 / 47 / 49 us there, stochastic 90 / 80 / 77.
+// One, two and four chunks a wave: 52 / 47 / 49 us there; stochastic 74 with two.
 constexpr uint32_t kGWaves = 4, kGChunks = 2;
 
 template <uint32_t DT, bool STOCHASTIC>
@@ -108,7 +109,12 @@ __global__ void __launch_bounds__(kBothThreads) k_mx4_group_both(const GParams p
     constexpr uint32_t kRoom = 64 / sizeof(elem);
     __shared__ __attribute__((aligned(16))) elem tile[kTile * kTile + 4 * kRoom];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint32_t tr = blockIdx.x / p.groups, tc = blockIdx.x - tr * p.groups;
+    // An XCD takes all tiles of some columns, one below the other: its L2 joins their 64 bytes of each column's codes and 4 of its scales into lines.  Against the tiles in order,
+    // nearest: 8192 x 2 x 4096 bf16 35.7 -> 34.2 us, 3001 x 3 x 2049 f16 16.1 -> 13.5; in bands of four rows of tiles 35.7, 14.2.
+    const uint32_t high = min(all_tiles(p.offsets, p.E, p.R, Power{7}), p.groups_t);          // no more than the form has room for, whatever the offsets
+    if (blockIdx.x >= high * p.groups) return;
+    const uint32_t t = tile_of_workgroup(blockIdx.x, high * p.groups);
+    const uint32_t tc = __builtin_amdgcn_readfirstlane(t / high), tr = __builtin_amdgcn_readfirstlane(t - tc * high);
     Group g;
     if (!group_of_tile(p.offsets, p.E, p.R, Power{7}, 1, tr, g)) return;
     const uint32_t r0 = g.lo + (tr - g.first) * kTile, c0 = tc * kTile;

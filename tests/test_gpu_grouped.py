@@ -379,3 +379,22 @@ def test_groups_that_do_not_begin_at_the_first_row(B):
         s, c = slice(offsets[e], offsets[e + 1]), slice(begin[e], begin[e] + offsets[e + 1] - offsets[e])
         for out, left, right in ((host(y)[s], a[s], wv[e]), (host(v)[s], x64[s], wv[e]), (host(dw)[e], bt[:, c], at[:, c])):
             assert (np.abs(out - left @ right.T) <= (3 * left.shape[1] + 3) * ONE * (np.abs(left) @ np.abs(right).T)).all()
+
+
+@pytest.mark.parametrize("both", [False, True])
+def test_groups_that_overlap(B, both):
+    """Offsets that rise to the last row again and again: more tiles than the form along the groups has columns for.  What lies behind the form stays."""
+    n, K, N, E = 1000, 300, 40, 8
+    o, columns = ints([0, n] * (E // 2) + [0]), X.group_columns(n, E)
+    lay, lay_t = B.qesgd_mx4_layout_query(n, K), B.qesgd_mx4_layout_query(K, columns)
+    p, pt = (torch.full((x.bytes + (1 << 20),), 0xA5, dtype=torch.uint8, device="cuda") for x in (lay, lay_t))
+    x = tokens(n, K, torch.float32, 1).cuda()
+    for mode in (B.MX4_NEAREST, B.MX4_STOCHASTIC):
+        B.qesgd_mx4_quantize_groups(x, K, n, None, 1, o, E, n, K, mode, 0, 0, p[:lay.bytes] if both else None, packed_t=pt[:lay_t.bytes])
+    assert (p[lay.bytes:] == 0xA5).all() and (pt[lay_t.bytes:] == 0xA5).all()
+    wp, _ = X.packed_weights(np.random.default_rng(0).standard_normal((E, N, K)))
+    px = B.alloc_mx4(lay).zero_()
+    y = torch.full((n + 64, N), 3.0, device="cuda")
+    B.qesgd_mx4_grouped_product(px, wp.cuda(), wp.stride(0), o, E, n, N, K, y[:n], N)
+    B.qesgd_mx4_vector_product(x, K, n, None, 1, wp.cuda(), wp.stride(0), o, E, n, N, K, y[:n], N)
+    assert (y[n:] == 3.0).all()
