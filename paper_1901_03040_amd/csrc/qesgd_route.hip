@@ -9,7 +9,7 @@
 // integers are counted, so the result is the same however the work falls.
 //
 // Measured: one token of 64 experts 3.7 us, 8192 tokens of 64 bf16 7.7 us (choice and places), which is launches and chains of trips to memory; 160001 of 257 f32, six each,
-// 60 (choice: 165 MB, vector instructions, a third of them to find the largest six times) + 12.5 + 14 us, gradient 68 us = 4.8 TB/s.
+// 57 (choice: 165 MB, vector instructions, two thirds of them to find the largest six times) + 12.5 + 14 us, gradient 68 us = 4.8 TB/s.
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_launch.h"
@@ -95,13 +95,33 @@ __device__ __forceinline__ void load_logits(const void* x, uint64_t from, uint32
 template <uint32_t DT, int L, int C>
 __device__ __forceinline__ void choose(const RParams& p, uint64_t t, uint32_t l, int32_t& expert, float& gate) {
     float v[C];
-    float best = -INFINITY;
     load_logits<DT, L, C>(p.logits, t * p.ld, p.E, l, v);
+    // In pairs, the larger first (of equals the lower expert): a choice looks for its expert among the larger ones only, and brings up the other one of the pair. From ten logits a
+    // lane on: 160001 tokens of 257 experts, six each, 77.5 -> 74.6 us, 20001 of 1024, eight, 64 -> 56; 65536 of 128, four, 22.4 -> 22.8.
+    constexpr bool PAIRS = C >= 10;
+    constexpr int P = PAIRS ? (C + 1) / 2 : C;
+    float first[P], second[P];
+    uint32_t swapped = 0;                                      // bit q: the larger one of pair q is the latter
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        best = larger(v[c], best);
+    for (int q = 0; q < P; ++q) {
+        if constexpr (PAIRS) {
+            const float a = v[2 * q], b = 2 * q + 1 < C ? v[2 * q + 1] : -INFINITY;
+            const bool swap = b > a;
+            first[q] = swap ? b : a;
+            second[q] = swap ? a : b;
+            swapped |= swap ? 1u << q : 0u;
+        } else {
+            first[q] = v[q];
+            second[q] = -INFINITY;
+        }
     }
-    float high = most<L>(best);
+    const auto largest = [&] {
+        float best = first[0];
+#pragma unroll
+        for (int q = 1; q < P; ++q) best = larger(first[q], best);
+        return most<L>(best);
+    };
+    float high = largest();
     const float base = high;                                   // of infinity: every gate is NaN, as infinity - infinity is
     float sum = 0.0f;
     if (p.all) {
@@ -114,17 +134,24 @@ __device__ __forceinline__ void choose(const RParams& p, uint64_t t, uint32_t l,
         // the lowest expert among the largest
         uint32_t at = 0xFFFFFFFFu;
 #pragma unroll
-        for (int c = C - 1; c >= 0; --c) at = v[c] == high ? (uint32_t)c * L + l : at;
+        for (int q = P - 1; q >= 0; --q) at = first[q] == high ? (PAIRS ? (uint32_t)q : (uint32_t)q * L + l) : at;
+        if (PAIRS) at = at < 32 ? (2u * at + (swapped >> at & 1u)) * L + l : at;
         const uint32_t e = least<L>(at);
         if (l == j && high > -INFINITY) { mine = high; mine_e = e; }
         if (++j >= p.k) break;
-        best = -INFINITY;
+        if constexpr (PAIRS) {
+            const uint32_t gone = at == e ? e / L / 2u : 32u;  // only in the lane that has it
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            v[c] = (uint32_t)c * L + l == e ? -INFINITY : v[c];
-            best = larger(v[c], best);
+            for (int q = 0; q < P; ++q) {
+                first[q] = gone == (uint32_t)q ? second[q] : first[q];
+                second[q] = gone == (uint32_t)q ? -INFINITY : second[q];
+            }
+            swapped ^= gone < 32 ? 1u << gone : 0u;
+        } else {
+#pragma unroll
+            for (int q = 0; q < P; ++q) first[q] = (uint32_t)q * L + l == e ? -INFINITY : first[q];
         }
-        high = most<L>(best);
+        high = largest();
     }
     const bool open = mine > -INFINITY;
     const float part = open ? exp_below(mine - base) : 0.0f;
@@ -134,12 +161,15 @@ __device__ __forceinline__ void choose(const RParams& p, uint64_t t, uint32_t l,
 }
 
 // Blocks of 64 tokens, all at once where 16 lanes take one; a wave that takes many in turn waits for each one's logits.  With 4 / 8 / 16 waves a block, both launches: 8192
-// tokens of 64 experts 9.0 / 8.0 / 7.7 us, 2048 of 512 29.5 / 20.5 / 17.5, 160001 of 257 76 / 79 / 77.
-constexpr uint32_t kChooseWaves = 16, kBlockTokens = 64;
+// tokens of 64 experts 9.0 / 8.0 / 7.7 us, 160001 of 257 75 / 73 / 75.  From 20 logits a lane on, of whose registers a CU has room for 16 waves of 64 lanes but not for two such
+// blocks: 80001 tokens of 512 experts bf16 64 / 62 / 116 us, 20001 of 1024 f32 63 / 56 / 58.
+constexpr uint32_t kBlockTokens = 64;
+constexpr uint32_t choose_waves(int c) { return c < 20 ? 16 : 8; }
 
 // The choices of a block of tokens and how many pairs each expert has there.
 template <uint32_t DT, int L, int C>
-__global__ void __launch_bounds__(kChooseWaves * 64) k_route_choose(const RParams p) {
+__global__ void __launch_bounds__(choose_waves(C) * 64) k_route_choose(const RParams p) {
+    constexpr uint32_t kChooseWaves = choose_waves(C);
     __shared__ uint32_t count[QESGD_MAX_EXPERTS];
     for (uint32_t e = threadIdx.x; e < p.E; e += kChooseWaves * 64u) count[e] = 0u;
     __syncthreads();
@@ -424,9 +454,10 @@ __global__ void __launch_bounds__(256) k_route_backward(const BParams p) {
 }
 
 // f(lanes of a token, logits of a lane): few lanes, because the exchanges between them cost the same for one token or four, and hardly more logits than
-// there are.
+// there are.  wide: more lanes from 320 experts on, whose loads and stores of 32 bits take whole lines: gradient of 40001 x 512 f32 28.5 us, with 16 lanes 32.9; but 80001 x
+// 512 bf16 73 and 51, and the choice 120 and 62.
 template <class F>
-void by_experts(uint32_t E, F&& f) {
+void by_experts(uint32_t E, bool wide, F&& f) {
     using std::integral_constant;
 #define QESGD_LANES(lanes, each) if (E <= lanes * each) return f(integral_constant<int, lanes>{}, integral_constant<int, each>{})
     QESGD_LANES(8, 1);
@@ -442,11 +473,18 @@ void by_experts(uint32_t E, F&& f) {
     QESGD_LANES(16, 14);
     QESGD_LANES(16, 17);
     QESGD_LANES(16, 20);
-    QESGD_LANES(32, 12);
-    QESGD_LANES(32, 16);
-    QESGD_LANES(64, 10);
-    QESGD_LANES(64, 12);
-    QESGD_LANES(64, 16);
+    if (wide) {
+        QESGD_LANES(32, 12);
+        QESGD_LANES(32, 16);
+        QESGD_LANES(64, 10);
+        QESGD_LANES(64, 12);
+        QESGD_LANES(64, 16);
+    }
+    QESGD_LANES(16, 24);
+    QESGD_LANES(16, 32);
+    QESGD_LANES(32, 20);
+    QESGD_LANES(32, 24);
+    QESGD_LANES(32, 32);
 #undef QESGD_LANES
 }
 
@@ -483,7 +521,7 @@ int launch_route(const Route& a) {
     while ((1u << p.bits) <= a.E) ++p.bits;
     if (route_small(a.T, a.E, a.k)) {
         by_type(a.dtype, [&](auto t) {
-            by_experts(a.E, [&](auto l, auto c) {
+            by_experts(a.E, false, [&](auto l, auto c) {
                 k_route_small<t.value, l.value, c.value><<<1, kSmallWaves * 64, ((kSmallWaves + 1) * a.E + kSmallWaves) * sizeof(uint32_t), a.stream>>>(p);
             });
         });
@@ -493,7 +531,7 @@ int launch_route(const Route& a) {
     p.blocks = (uint32_t)route_blocks(a.T);
     p.totals = p.counts + (uint64_t)p.blocks * a.E;
     by_type(a.dtype, [&](auto t) {
-        by_experts(a.E, [&](auto l, auto c) { k_route_choose<t.value, l.value, c.value><<<p.blocks, kChooseWaves * 64, 0, a.stream>>>(p); });
+        by_experts(a.E, false, [&](auto l, auto c) { k_route_choose<t.value, l.value, c.value><<<p.blocks, choose_waves(c.value) * 64, 0, a.stream>>>(p); });
     });
     if (const int rc = launched(); rc != QESGD_OK) return rc;
     const uint32_t lds = ((kPlaceWaves + 1) * a.E + kPlaceWaves) * sizeof(uint32_t);
@@ -522,7 +560,7 @@ int launch_route_backward(const RouteBackward& a) {
     p.dlogits = a.dlogits;
     int rc = QESGD_OK;
     by_type(a.dtype, [&](auto t) {
-        by_experts(a.E, [&](auto l, auto c) {
+        by_experts(a.E, t.value == QESGD_F32, [&](auto l, auto c) {
             const uint64_t groups = (a.T + 256 / l.value - 1) / (256 / l.value);
             if (!grid_ok(groups, 256)) { rc = QESGD_ERR_DIM; return; }
             k_route_backward<t.value, l.value, c.value><<<(uint32_t)groups, 256, 0, a.stream>>>(p);

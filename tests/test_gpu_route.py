@@ -62,7 +62,8 @@ def check_route(x, k, all_, out):
 
 
 SHAPES = [(1, 1, 1), (1, 8, 8), (1, 64, 2), (3, 5, 2), (2, 16, 16), (7, 9, 1), (63, 33, 4), (65, 64, 2), (129, 65, 3), (500, 17, 16), (300, 130, 8),
-          (257, 257, 6), (40, 600, 5), (20, 1024, 16), (4100, 4, 2), (20_011, 12, 3), (9000, 1000, 2)]
+          (257, 257, 6), (40, 600, 5), (20, 1024, 16), (4100, 4, 2), (20_011, 12, 3), (9000, 1000, 2),
+          (701, 160, 16), (135, 192, 8), (501, 224, 7), (301, 300, 5), (300, 330, 4), (401, 384, 6), (333, 512, 16), (201, 640, 9), (400, 768, 3), (299, 1024, 12)]
 
 
 @pytest.mark.parametrize("all_", [True, False], ids=["all", "chosen"])
@@ -74,7 +75,7 @@ def test_route(B, T, E, k, dtype, all_):
 
 
 @pytest.mark.parametrize("all_", [True, False], ids=["all", "chosen"])
-@pytest.mark.parametrize("T,E,k", [(1, 8, 3), (70, 8, 8), (200, 64, 4), (1000, 257, 6), (5000, 33, 2)])
+@pytest.mark.parametrize("T,E,k", [(1, 8, 3), (70, 8, 8), (200, 64, 4), (1000, 257, 6), (5000, 33, 2), (300, 200, 16), (211, 512, 9), (150, 1024, 5)])
 def test_closed_experts_and_padded_tokens(B, T, E, k, all_):
     x = logits(T, E, torch.float32, 3, closed=0.3).cuda()
     check_route(x, k, all_, run_route(B, x, k, all_))
