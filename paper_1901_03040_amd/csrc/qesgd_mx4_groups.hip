@@ -4,12 +4,11 @@
 // codes, of four scales), so the product walks whole blocks and no block holds rows of two experts.
 //
 // A row goes to k experts and is read k times, from the memory-side cache where x fits it.  16384 tokens x 2 x 4096 bf16 along the rows 47 us (54 beside other work)
-// = 340 MB at 7.2 TB/s; 8192 x 2, both forms, 34 us nearest and 69 stochastic, which is its arithmetic (two Philox calls for 8 elements).
+// = 340 MB at 7.2 TB/s; 8192 x 2, both forms, 36 us nearest and 69 stochastic, which is its arithmetic (two Philox calls for 8 elements).
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_launch.h"
 #include "qesgd_mx4_codes.h"
-#include "qesgd_tile_product.h"
 
 namespace qesgd {
 namespace {
@@ -99,6 +98,7 @@ __global__ void __launch_bounds__(kGWaves * 64) k_mx4_group_rows(const GParams p
 
 // Both forms, or that along the groups alone, of 128 rows of one group x 128 columns.  The rows' form is made while the tile is read; the raw
 // elements go to LDS, and then a lane takes 32 rows of one column.
+// The tiles in order: all of some columns on one XCD, whose L2 would join their 64 bytes of a column into lines, took 34 us for 36 where x lay in a cache and 51 for 49 where it did not.
 constexpr uint32_t kTile = 128, kBothThreads = 512;
 
 template <uint32_t DT, bool STOCHASTIC>
@@ -109,12 +109,7 @@ __global__ void __launch_bounds__(kBothThreads) k_mx4_group_both(const GParams p
     constexpr uint32_t kRoom = 64 / sizeof(elem);
     __shared__ __attribute__((aligned(16))) elem tile[kTile * kTile + 4 * kRoom];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    // An XCD takes all tiles of some columns, one below the other: its L2 joins their 64 bytes of each column's codes and 4 of its scales into lines.  Against the tiles in order,
-    // nearest: 8192 x 2 x 4096 bf16 35.7 -> 34.2 us, 3001 x 3 x 2049 f16 16.1 -> 13.5; in bands of four rows of tiles 35.7, 14.2.
-    const uint32_t high = min(all_tiles(p.offsets, p.E, p.R, Power{7}), p.groups_t);          // no more than the form has room for, whatever the offsets
-    if (blockIdx.x >= high * p.groups) return;
-    const uint32_t t = tile_of_workgroup(blockIdx.x, high * p.groups);
-    const uint32_t tc = __builtin_amdgcn_readfirstlane(t / high), tr = __builtin_amdgcn_readfirstlane(t - tc * high);
+    const uint32_t tr = blockIdx.x / p.groups, tc = blockIdx.x - tr * p.groups;
     Group g;
     if (!group_of_tile(p.offsets, p.E, p.R, Power{7}, 1, tr, g)) return;
     const uint32_t r0 = g.lo + (tr - g.first) * kTile, c0 = tc * kTile;
