@@ -9,6 +9,7 @@
 // the reading of the experts' matrices and by launches.
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
+#include "qesgd_mx4_codes.h"
 #include "qesgd_mx4_tiles.h"
 
 namespace qesgd {
@@ -37,32 +38,85 @@ struct PParams {
 constexpr uint64_t kStreamBytes = 192ull << 20;
 inline bool streamed(const void* c, uint64_t row_bytes, uint64_t rows) { return row_bytes * rows >= kStreamBytes && ((uintptr_t)c | row_bytes) % 128 == 0; }
 
-template <uint32_t DT>
-__device__ __forceinline__ void put_stream(void* c, uint64_t at, float v) {
-    if (DT == QESGD_F32) __builtin_nontemporal_store(v, (float*)c + at);
-    else if (DT == QESGD_F16) __builtin_nontemporal_store((_Float16)v, (_Float16*)c + at);
-    else __builtin_nontemporal_store((__bf16)v, (__bf16*)c + at);
+// Four numbers of a row, whose rows begin at any element.
+template <uint32_t DT, bool STREAM>
+__device__ __forceinline__ void put_four(void* c, uint64_t at, const float (&v)[4]) {
+    if constexpr (DT == QESGD_F32) {
+        vec4_any* to = (vec4_any*)((float*)c + at);
+        const vec4 x = {v[0], v[1], v[2], v[3]};
+        if (STREAM) __builtin_nontemporal_store(x, to);
+        else *to = x;
+    } else {
+        typedef uvec2 __attribute__((aligned(2))) uvec2_any;
+        uvec2 x;
+        if constexpr (DT == QESGD_BF16) x = uvec2{__builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[0], (__bf16)v[1]}), __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2], (__bf16)v[3]})};
+        else x = uvec2{__builtin_bit_cast(uint32_t, f16x2{(_Float16)v[0], (_Float16)v[1]}), __builtin_bit_cast(uint32_t, f16x2{(_Float16)v[2], (_Float16)v[3]})};
+        uvec2_any* to = (uvec2_any*)((unsigned short*)c + at);
+        if (STREAM) __builtin_nontemporal_store(x, to);
+        else *to = x;
+    }
 }
 
-// The wave's fragments to rows and columns from row0 and col0 on, of rows up to M and columns up to N.
+// B's rows in fours where a wave has two fragments side by side.
+template <class S>
+using OrderB = std::conditional_t<S::FN == 2, InFours, Straight>;
+
+// The wave's fragments to rows and columns from row0 and col0 on, of rows up to M and columns up to N.  In fours 16 lanes write a row's 64 columns at once: an element a lane took
+// four times as many stores, and a wave has 63 on their way.
 template <class S, uint32_t DT>
-__device__ __forceinline__ void store_tile(const Mx4Ops<S>& ops, void* c, uint64_t ldc, uint32_t M, uint32_t N, uint32_t row0, uint32_t col0, bool whole, bool stream) {
+__device__ __forceinline__ void store_tile(const Mx4Ops<S>& ops, void* c, uint64_t ldc, uint32_t M, uint32_t N, uint32_t row0, uint32_t col0, bool stream) {
     const uint32_t lane = threadIdx.x & 63u;
+    row0 = __builtin_amdgcn_readfirstlane(row0);
+    col0 = __builtin_amdgcn_readfirstlane(col0);
+    if (row0 >= M || col0 >= N) return;
+    const bool whole = row0 + S::FM * 32u <= M && col0 + S::FN * 32u <= N;
+    if constexpr (S::FN == 2) {
+        const uint32_t row = row0 + 4u * (lane >> 5) + (lane >> 4 & 1u), col = col0 + 4u * (lane & 15u);
+        const uint64_t base = (uint64_t)row * ldc + col;
+        const auto four = [&](int i, int e, float (&v)[4]) {
+            // rows of 16 lanes exchanged: two columns of one matrix row, from either fragment
 #pragma unroll
-    for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-        for (int j = 0; j < S::FN; ++j) {
-            // a lane holds column lane & 31 of a fragment and rows 8 q + 4 h + r
-            const uint32_t row = row0 + i * 32u + 4u * (lane >> 5), col = col0 + j * 32u + (lane & 31u);
-            if (whole && stream) {
-                asm volatile("; streamed");              // keeps the two arms apart, which the compiler would merge into ordinary stores
-                const uint64_t base = (uint64_t)row * ldc + col;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) put_stream<DT>(c, base + (8u * (e >> 2) + (e & 3)) * ldc, ops.acc[i][j][e]);
-            } else {
-                store_fragment<DT>(c, ldc, M, N, row, col, whole, ops.acc[i][j]);
+            for (int j = 0; j < 2; ++j) {
+                const auto two = __builtin_amdgcn_permlane16_swap(__float_as_uint(ops.acc[i][j][e]), __float_as_uint(ops.acc[i][j][e + 1]), false, false);
+                v[2 * j] = __uint_as_float(two[0]);
+                v[2 * j + 1] = __uint_as_float(two[1]);
             }
+        };
+        const auto all = [&](auto put) {
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    float v[4];
+                    four(i, e, v);
+                    put((uint32_t)(i * 32 + 8 * (e >> 2) + (e & 3)), v);
+                }
+        };
+        if (whole && stream) {
+            asm volatile("; streamed");              // keeps the two arms apart, which the compiler would merge into ordinary stores
+            all([&](uint32_t r, const float (&v)[4]) { put_four<DT, true>(c, base + r * ldc, v); });
+        } else if (whole) {
+            all([&](uint32_t r, const float (&v)[4]) { put_four<DT, false>(c, base + r * ldc, v); });
+        } else if (col0 + 64u <= N || (N - col0) % 4u == 0) {
+            all([&](uint32_t r, const float (&v)[4]) {
+                if (col < N && row + r < M) put_four<DT, false>(c, base + r * ldc, v);
+            });
+        } else {
+            // a row's last ones are fewer than four: a number a lane, in the columns that its rows of B are
+#pragma unroll
+            for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    store_fragment<DT>(c, ldc, M, N, row0 + i * 32u + 4u * (lane >> 5), col + 2u * j + (lane >> 4 & 1u), false, ops.acc[i][j]);
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::FN; ++j)
+                // a lane holds column lane & 31 of a fragment and rows 8 q + 4 h + r
+                store_fragment<DT>(c, ldc, M, N, row0 + i * 32u + 4u * (lane >> 5), col0 + j * 32u + (lane & 31u), whole, ops.acc[i][j]);
+    }
 }
 
 // Steps first .. first + count of `steps`, piece number `piece` of them: an even first one, because scales come in pairs.  A short contraction leaves some pieces
@@ -120,10 +174,10 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_product(const PParam
     ops.a = p.a + (uint64_t)m0 * p.row_codes + (uint64_t)first * kStepBytes;
     ops.b = b + (uint64_t)n0 * p.row_codes + (uint64_t)first * kStepBytes;
     ops.la.init(p.row_codes, g.hi - m0);
-    ops.lb.init(p.row_codes, p.N - n0);
+    ops.lb.init(p.row_codes, p.N - n0, OrderB<S>{});
     ops.scales = scales;
     ops.init_scales(p.a + p.a_scales + (uint64_t)m0 * p.row_scales + first * 8u, b + p.b_scales + (uint64_t)n0 * p.row_scales + first * 8u, g.hi - m0, p.N - n0,
-                    p.row_scales, p.row_scales - first * 8u, wm, wn);
+                    p.row_scales, p.row_scales - first * 8u, wm, wn, OrderB<S>{});
     ops.at_a = wm * S::FM * 32 * kStepBytes + lane_place(lane);
     ops.at_b = (S::BM + wn * S::FN * 32) * kStepBytes + lane_place(lane);
     ops.steps = steps;
@@ -133,7 +187,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_product(const PParam
 
     // pieces are of fp32, as DT is for them
     void* c = p.pieces > 1 ? (void*)(p.partial + piece * p.sums) : p.c;
-    store_tile<S, DT>(ops, c, p.pieces > 1 ? p.N : p.ldc, g.hi, p.N, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= g.hi && n0 + S::BN <= p.N, p.stream);
+    store_tile<S, DT>(ops, c, p.pieces > 1 ? p.N : p.ldc, g.hi, p.N, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, p.stream);
 }
 
 template <class S, uint32_t DT>
@@ -168,10 +222,10 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
         ops.a = p.a + (uint64_t)m0 * p.row_codes + from;
         ops.b = p.b + (uint64_t)n0 * p.row_codes + from;
         ops.la.init(p.row_codes, p.N - m0);
-        ops.lb.init(p.row_codes, p.K - n0);
+        ops.lb.init(p.row_codes, p.K - n0, OrderB<S>{});
         ops.scales = scales;
         ops.init_scales(p.a + p.a_scales + (uint64_t)m0 * p.row_scales + from / 16u, p.b + p.b_scales + (uint64_t)n0 * p.row_scales + from / 16u,
-                        p.N - m0, p.K - n0, p.row_scales, (bytes - first * kStepBytes) / 16u, wm, wn);
+                        p.N - m0, p.K - n0, p.row_scales, (bytes - first * kStepBytes) / 16u, wm, wn, OrderB<S>{});
         ops.at_a = wm * S::FM * 32 * kStepBytes + lane_place(lane);
         ops.at_b = (S::BM + wn * S::FN * 32) * kStepBytes + lane_place(lane);
         ops.steps = steps;
@@ -181,7 +235,7 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_gradient(const PPara
     }
     const uint64_t of_expert = (uint64_t)e * p.N * p.K;
     void* d = p.pieces > 1 ? (void*)(p.partial + piece * p.sums + of_expert) : (void*)((unsigned char*)p.c + of_expert * (DT == QESGD_F32 ? 4u : 2u));
-    store_tile<S, DT>(ops, d, p.K, p.N, p.K, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, m0 + S::BM <= p.N && n0 + S::BN <= p.K, p.stream);
+    store_tile<S, DT>(ops, d, p.K, p.N, p.K, m0 + wm * S::FM * 32u, n0 + wn * S::FN * 32u, p.stream);
 }
 
 // A result from the sums of the pieces, added in order (see PieceSum).  Four numbers a lane where rows allow it, eight pieces on their way: the sums
@@ -277,8 +331,8 @@ struct Mx4Chain : Mx4Ops<S> {
         B::a = a;
         B::b = b;
         B::la.init(pitch, t.rows_a);
-        B::lb.init(pitch, t.rows_b);
-        B::init_scales(sa, sb, t.rows_a, t.rows_b, row_scales, bytes / 16u, wm, wn);
+        B::lb.init(pitch, t.rows_b, OrderB<S>{});
+        B::init_scales(sa, sb, t.rows_a, t.rows_b, row_scales, bytes / 16u, wm, wn, OrderB<S>{});
         B::steps = t.steps;
         B::half = t.half;
     }
@@ -425,9 +479,9 @@ __global__ void __launch_bounds__(S::threads) k_mx4_grouped_chain(const PParams 
     const auto finish = [&](const ChainTile& t) {
         if constexpr (GRADIENT) {
             void* d = (unsigned char*)p.c + (uint64_t)t.e * p.N * p.K * (DT == QESGD_F32 ? 4u : 2u);
-            store_tile<S, DT>(ops, d, p.K, p.N, p.K, t.m0 + wm * S::FM * 32u, t.n0 + wn * S::FN * 32u, t.rows_a >= S::BM && t.rows_b >= S::BN, p.stream);
+            store_tile<S, DT>(ops, d, p.K, p.N, p.K, t.m0 + wm * S::FM * 32u, t.n0 + wn * S::FN * 32u, p.stream);
         } else {
-            store_tile<S, DT>(ops, p.c, p.ldc, t.m0 + t.rows_a, p.N, t.m0 + wm * S::FM * 32u, t.n0 + wn * S::FN * 32u, t.rows_a >= S::BM && t.rows_b >= S::BN, p.stream);
+            store_tile<S, DT>(ops, p.c, p.ldc, t.m0 + t.rows_a, p.N, t.m0 + wm * S::FM * 32u, t.n0 + wn * S::FN * 32u, p.stream);
         }
     };
     if constexpr (GRADIENT) {

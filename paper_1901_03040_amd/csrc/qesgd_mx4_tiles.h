@@ -54,15 +54,16 @@ struct Mx4Ops {
 
     // a, b: the first scales of the tile's first rows, of which there are rows_a and rows_b; row_scales: bytes from one row to the next; bytes: of a row's
     // scales from there to the end of the contraction.
+    template <class Order = Straight>
     __device__ __forceinline__ void init_scales(const unsigned char* a, const unsigned char* b, uint32_t rows_a, uint32_t rows_b, uint32_t row_scales,
-                                                uint32_t bytes, uint32_t wm, uint32_t wn) {
+                                                uint32_t bytes, uint32_t wm, uint32_t wn, Order of_b = {}) {
         last_word = bytes - 4u;
         sa = a;
         sb = b;
 #pragma unroll
         for (int i = 0; i < NA; ++i) off_a[i] = min((i * S::threads + threadIdx.x) >> 2, rows_a - 1u) * row_scales;
 #pragma unroll
-        for (int i = 0; i < NB; ++i) off_b[i] = min((i * S::threads + threadIdx.x) >> 2, rows_b - 1u) * row_scales;
+        for (int i = 0; i < NB; ++i) off_b[i] = min(of_b((i * S::threads + threadIdx.x) >> 2), rows_b - 1u) * row_scales;
         scale_at = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * 256u);
         scale_at_a = (wm * S::FM * 32u + (threadIdx.x & 31u)) * 16u;
         scale_at_b = (S::BM + wn * S::FN * 32u + (threadIdx.x & 31u)) * 16u;

@@ -55,6 +55,15 @@ __device__ __forceinline__ uint32_t lds_number(const unsigned char* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)p;
 }
 
+// Which row of an operand lies at row r of its tile: the same one, or, of every 64, rows 0, 4, 8 .. and 1, 5, 9 .. in a fragment and 2, 6 .. and 3, 7 .. in the next, so
+// that four columns of a result come together in a lane once two rows of 16 lanes are exchanged.
+struct Straight {
+    __device__ __forceinline__ uint32_t operator()(uint32_t r) const { return r; }
+};
+struct InFours {
+    __device__ __forceinline__ uint32_t operator()(uint32_t r) const { return (r & ~63u) | (r & 15u) << 2 | (r >> 5 & 1u) << 1 | (r >> 4 & 1u); }
+};
+
 // One step of ROWS rows to LDS.  `off` holds the lane's byte offsets from the tile's first row.
 template <int ROWS, int THREADS>
 struct TileLoader {
@@ -63,13 +72,14 @@ struct TileLoader {
     uint32_t off[N];
     uint32_t wave_at;
 
-    // Row r of the tile is row min(r, rows - 1) of what is there: no row beyond the end is read.
-    __device__ __forceinline__ void init(uint32_t pitch, uint32_t rows) {
+    // Row r of the tile is row min(of(r), rows - 1) of what is there: no row beyond the end is read.
+    template <class Order = Straight>
+    __device__ __forceinline__ void init(uint32_t pitch, uint32_t rows, Order of = {}) {
         wave_at = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * 1024u);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uint32_t at = i * THREADS + threadIdx.x, r = at >> 3, c = (at & 7u) ^ ((r >> 1) & 7u);
-            off[i] = min(r, rows - 1u) * pitch + c * 16u;
+            off[i] = min(of(r), rows - 1u) * pitch + c * 16u;
         }
     }
     // From the byte of the rows that `base` points at.  half: only 64 bytes are left, the chunks of the second half repeat the first.
