@@ -5,8 +5,8 @@
 //
 // Element products are exact, sums are fp32.
 //
-// Bound by the matrix units at the power the card allows them: 16 experts of 4096 x 4096, 32768 rows 304 us = 3.6 PFLOP/s, with operands of zeros 239 us; small groups by
-// the reading of the experts' matrices and by launches.
+// Bound by the matrix units at the power the card allows them: 16 experts of 4096 x 4096, 32768 rows bf16 286 us = 3.8 PFLOP/s; small groups by
+// the reading of the experts' matrices and by launches, short contractions by a tile's beginning and by the writing of the result.
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_mx4_codes.h"
@@ -32,11 +32,13 @@ struct PParams {
     uint64_t sums;                        // of a piece
 };
 
-// Non-temporal stores where the result is larger than what the memory-side cache keeps for its reader, and made of whole lines (parts of
-// lines cost such a store a read): D 537 MB 266 -> 222 us, 64 experts of 2048 x 1024 142 -> 107; C 268 MB in bf16 340 -> 317; 134 MB and less
-// the same; rows of 2049 numbers 38 -> 50.
-constexpr uint64_t kStreamBytes = 192ull << 20;
-inline bool streamed(const void* c, uint64_t row_bytes, uint64_t rows) { return row_bytes * rows >= kStreamBytes && ((uintptr_t)c | row_bytes) % 128 == 0; }
+// Non-temporal stores of results made of whole lines (parts of lines cost such a store a read: rows of 2049 numbers 38 -> 50 us): of products where the result is larger than what the
+// memory-side cache keeps for its reader, of gradients where their writing out at the kernel's end counts.  Us without / with, and in brackets with the call that reads the result:
+// products 16 experts, 32768 rows, N = K = 4096 bf16 312 / 280, 8, 16384, 4096, 4096 134 MB 151 / 151 (181 / 190), 50, 25990, 1024, 576 53 MB 24.8 / 23.2 (39.5 / 41.7), 16,
+// 8192, 1024, 1024 17 MB 14.2 / 12.2 (23.2 / 23.0), 49, 3621, 832, 3142 6 MB 20.9 / 20.7 (25.1 / 25.9); gradients 8, 16384, 4096, 4096 251 / 207, 50, 25990, 576, 1024 118 MB
+// 47.6 / 46.2 (68.6 / 68.8), 16, 4096, 1024, 1024 67 MB 18.2 / 17.4 (32.8 / 31.9), 4, 996, 320, 3136 16 MB 8.4 / 7.6 (17.9 / 16.5), 8, 2048, 512, 512 8 MB 6.3 / 6.3 (12.4 / 12.5).
+constexpr uint64_t kStreamProduct = 192ull << 20, kStreamGradient = 12ull << 20;
+inline bool whole_lines(const void* c, uint64_t row_bytes) { return ((uintptr_t)c | row_bytes) % 128 == 0; }
 
 // Four numbers of a row, whose rows begin at any element.
 template <uint32_t DT, bool STREAM>
@@ -522,9 +524,9 @@ uint64_t group_tiles(const GroupProduct& a, uint64_t edge) {
 
 // The edge of the tiles, and the pieces of the contraction, from how long they take on 256 CUs (tile_us), the larger edge where it hardly matters.  A piece has at least
 // four steps; the sums of the pieces cost a launch, and are written and read at about 4 TB/s.  Measured, us, with 64 / 128 / 256:
-//   products   16 experts, 32768 rows, N = K = 4096 655 / 402 / 339;  13, 9003, 1000, 2049 33 / 25.9 / 22.7;  8, 2048, 2048, 2048 15.5 / 13.7 / 18.1;
-//              64, 1024, 1024, 1024 11.5 / 9.2 / 12.5;  8, 256, 4096, 4096 17.8 / 16.3 / 27.2;  64, 16384, 2048, 1024 70 / 46 / 46
-//   gradients  8, 16384, 4096, 4096 759 / 344 / 266;  64, 4096, 1024, 1024 109 / 65 / 59;  16, 1024, 512, 512 8.9 / 8.3 / 9.7
+//   products   16 experts, 32768 rows, N = K = 4096 660 / 348 / 280;  13, 9003, 1000, 2049 32.9 / 23.9 / 21.6;  8, 2048, 2048, 2048 15.6 / 11.9 / 16.8;
+//              64, 1024, 1024, 1024 12.1 / 8.5 / 12.1;  8, 256, 4096, 4096 17.9 / 15.6 / 26.2;  64, 16384, 2048, 1024 70 / 40 / 35;  50, 25990, 576, 1024 32.5 / 20.0 / 22.3
+//   gradients  8, 16384, 4096, 4096 544 / 256 / 207;  64, 4096, 1024, 1024 96 / 47 / 54;  16, 1024, 512, 512 8.9 / 7.5 / 8.9;  13, 9003, 1000, 2049 59 / 34.0 / 34.7
 // and, one piece / as many as chosen, graph of 8 calls:
 //   products   1 expert, 64 rows, N 1000, K 16384 20.3 / 9.9 (12 pieces);  8, 64, 512, 8192 12.0 / 8.8 (4);  1, 512, 1000, 25088 29.7 / 21.7 (2);
 //              1, 1, 4096, 4096 7.8 / 7.5 (4);  23, 74, 152, 3597 7.6 / 8.0 (3)
@@ -574,8 +576,8 @@ int launch_product_tiles(const GroupProduct& a, PParams& p) {
 }
 
 // One workgroup a CU, as its LDS has room for.  Where it gets three tiles or more; with fewer their search costs more than it saves.  A workgroup a tile / the chain,
-// us: products of 16 experts, 32768 rows, N = K = 4096 317 / 302 (3.7 PFLOP/s), 8, 16384 169 / 163, 64, 16384, 2048, 1024 43.8 / 39.0, but 13, 9003, 1000,
-// 2049 (164 tiles) 22.9 / 25.2; gradients 8, 16384, 4096, 4096 225 / 210, but 13, 9003, 1000, 2049 (468 tiles) 37 / 42.
+// us: products of 16 experts, 32768 rows, N = K = 4096 297 / 280 (3.9 PFLOP/s), 8, 16384 158 / 150, 64, 16384, 2048, 1024 39.6 / 35.3, but 13, 9003, 1000,
+// 2049 (164 tiles) 21.6 / 23.4; gradients 8, 16384, 4096, 4096 217 / 207, but 13, 9003, 1000, 2049 (468 tiles) 34.7 / 39.7.
 constexpr uint64_t kChainTiles = 512;
 template <class S, bool GRADIENT>
 int launch_chain(const GroupProduct& a, PParams& p) {
@@ -643,7 +645,7 @@ int launch_grouped_product(const GroupProduct& a) {
     p.pieces = cut.pieces;
     p.partial = a.workspace;
     p.sums = a.R * a.N;
-    p.stream = cut.pieces == 1 && streamed(a.c, a.ldc * dtype_bytes(a.dtype), a.R);
+    p.stream = cut.pieces == 1 && a.R * a.ldc * dtype_bytes(a.dtype) >= kStreamProduct && whole_lines(a.c, a.ldc * dtype_bytes(a.dtype));
     if (cut.edge == 64) return launch_product_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
     if (cut.edge == 128) return launch_product_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
     if (cut.pieces == 1 && group_tiles(a, 256) * ((a.N + 255) / 256) > kChainTiles) return launch_chain<TileShape<2, 4, 4, 2, 2>, false>(a, p);
@@ -674,7 +676,7 @@ int launch_grouped_gradient(const GroupProduct& a) {
     p.pieces = cut.pieces;
     p.partial = a.workspace;
     p.sums = a.E * a.N * a.K;
-    p.stream = cut.pieces == 1 && streamed(a.c, a.K * dtype_bytes(a.dtype), a.E * a.N);
+    p.stream = cut.pieces == 1 && p.sums * dtype_bytes(a.dtype) >= kStreamGradient && whole_lines(a.c, a.K * dtype_bytes(a.dtype));
     if (cut.edge == 64) return launch_gradient_tiles<TileShape<2, 2, 1, 1, 4>>(a, p);
     if (cut.edge == 128) return launch_gradient_tiles<TileShape<2, 2, 2, 2, 2>>(a, p);
     if (cut.pieces == 1 && a.E * ((a.N + 255) / 256) * ((a.K + 255) / 256) > kChainTiles) return launch_chain<TileShape<2, 4, 4, 2, 2>, true>(a, p);
