@@ -195,3 +195,44 @@ def test_gradients_of_long_groups_in_pieces(B, n, N, K, E, kind):
         wide = int(offsets[e + 1] - offsets[e] + 127) // 128 * 128
         assert within(got[e], a[:, at:at + wide], b[:, at:at + wide], dtype), e
         at += wide
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n,N,K,E", [(3000, 555, 1088, 13), (400, 2300, 1408, 4), (9000, 4100, 960, 3)])
+def test_gradients_in_whole_lines(B, n, N, K, E, dtype):
+    """Results of 12 MB and more whose rows are whole lines, in 64 to 256 rows and columns a tile, the last ones short."""
+    t, offsets, columns = TYPES[dtype], X.group_sizes(np.random.default_rng(K), E, n, "ragged"), X.group_columns(n, E)
+    pa, a = packed_noise(B, N, columns, 1, n + K)
+    pb, b = packed_noise(B, K, columns, 1, N + 2 * K)
+    a, b = on_gpu(a[0]), on_gpu(b[0])
+    ws = B.alloc_workspace(B.qesgd_mx4_grouped_gradient_workspace_bytes(n, N, K, E))
+    d = torch.full((E * N * K + 640,), 3.0, dtype=t, device="cuda")
+    B.qesgd_mx4_grouped_gradient(pa[0].cuda(), pb[0].cuda(), ints(offsets), E, n, N, K, d[:E * N * K], workspace=ws)
+    assert (d[E * N * K:] == 3.0).all()
+    d, at = d[:E * N * K].view(E, N, K), 0
+    for e in range(E):
+        wide = int(offsets[e + 1] - offsets[e] + 127) // 128 * 128
+        assert within(d[e], a[:, at:at + wide], b[:, at:at + wide], t), e
+        at += wide
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N", [63, 65, 126, 130, 253, 254, 255, 1021, 1022, 1025])
+def test_rows_that_do_not_end_with_four_columns(B, N, dtype):
+    """Every rest of four, rows that begin at any element, and what lies between them left as it was; tiles of 64, 128 and 256."""
+    t = TYPES[dtype]
+    for n, K, E in ((150, 200, 3), (1500, 700, 4), (9000, 300, 5)):
+        offsets = X.group_sizes(np.random.default_rng(N), E, n, "ragged")
+        pa, a = packed_noise(B, n, K, 1, n + K)
+        pb, b = packed_noise(B, N, K, E, N + 2 * K)
+        pb, a = pb.cuda(), on_gpu(a[0])
+        ldc = N + 3
+        c = torch.full((n * ldc + 7,), 3.0, dtype=t, device="cuda")
+        ws = B.alloc_workspace(B.qesgd_mx4_grouped_product_workspace_bytes(n, N, K, E))
+        B.qesgd_mx4_grouped_product(pa[0].cuda(), pb, pb.stride(0), ints(offsets), E, n, N, K, c[1:], ldc, workspace=ws)
+        rows = torch.as_strided(c, (n, ldc), (ldc, 1), 1)
+        assert c[0] == 3.0 and (rows[:, N:] == 3.0).all() and (c[n * ldc + 1:] == 3.0).all()
+        assert (rows[offsets[-1]:] == 3.0).all() and (rows[:offsets[0]] == 3.0).all()
+        for e in range(E):
+            lo, hi = int(offsets[e]), int(offsets[e + 1])
+            assert within(rows[lo:hi, :N], a[lo:hi], on_gpu(b[e]), t), (n, e)
