@@ -332,7 +332,7 @@ int qesgd_orthogonal_update(const float* g, uint64_t rows, uint64_t cols, uint32
  * R is the number of rows that the buffers have room for, offsets[E] <= R; rows outside of every group are neither read nor
  * written.  Offsets beyond 0 .. R are taken as the nearest of the two, whatever they hold no call reads or writes outside its buffers.
  * R, N, K and T in [1, 2^20] unless said otherwise, E in [1, QESGD_MAX_EXPERTS], k in [1, min(E, QESGD_MAX_CHOICES)].  Inputs and
- * outputs of 16 and 32 bits are aligned to their elements, their rows ld >= row elements apart.
+ * outputs of 16 and 32 bits are aligned to their elements, their rows ld >= row elements apart.  A workspace serves one call at a time.
  * ------------------------------------------------------------------------- */
 
 #define QESGD_MAX_EXPERTS 1024u
