@@ -236,3 +236,56 @@ def test_rows_that_do_not_end_with_four_columns(B, N, dtype):
         for e in range(E):
             lo, hi = int(offsets[e]), int(offsets[e + 1])
             assert within(rows[lo:hi, :N], a[lo:hi], on_gpu(b[e]), t), (n, e)
+
+
+def test_pieces_in_graphs_and_on_two_streams(B):
+    """Calls of two launches, each with a workspace of its own, captured and run side by side: every replay gives what a call alone gives."""
+    E, n, N, K = 2, 64, 300, 9000
+    o, far = ints([0, 30, n]), ints([0, 7000, 16_384])
+    a, w = packed_noise(B, n, K, 1, 1)[0][0].cuda(), packed_noise(B, N, K, E, 2)[0].cuda()
+    columns = X.group_columns(16_384, E)
+    ga, gb = packed_noise(B, 64, columns, 1, 3)[0][0].cuda(), packed_noise(B, 41, columns, 1, 4)[0][0].cuda()
+    x = torch.randn(n, K, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+
+    def job():
+        out = [torch.zeros(n, N, device="cuda"), torch.zeros(E, 64, 41, device="cuda"), torch.zeros(n, N, dtype=torch.bfloat16, device="cuda")]
+        sizes = [B.qesgd_mx4_grouped_product_workspace_bytes(n, N, K, E), B.qesgd_mx4_grouped_gradient_workspace_bytes(16_384, 64, 41, E),
+                 B.qesgd_mx4_vector_product_workspace_bytes(n, N, K, E)]
+        ws = [B.alloc_workspace(s) for s in sizes]
+
+        def run():
+            B.qesgd_mx4_grouped_product(a, w, w.stride(0), o, E, n, N, K, out[0], N, workspace=ws[0])
+            B.qesgd_mx4_grouped_gradient(ga, gb, far, E, 16_384, 64, 41, out[1], workspace=ws[1])
+            B.qesgd_mx4_vector_product(x, K, n, None, 1, w, w.stride(0), o, E, n, N, K, out[2], N, workspace=ws[2])
+        return out, run, sizes
+
+    jobs = [job() for _ in range(2)]
+    assert jobs[0][2][0] > 0 and jobs[0][2][1] > 0
+    jobs[0][1]()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in jobs[0][0]]
+    assert all(t.any() for t in want)
+    streams, graphs = [torch.cuda.Stream() for _ in jobs], []
+    for (out, run, _), s in zip(jobs, streams):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            run()
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            run()
+        graphs.append(g)
+    for turn in range(5):
+        for out, _, _ in jobs:
+            for t in out:
+                t.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                for _ in range(3):
+                    g.replay()
+        torch.cuda.synchronize()
+        for out, _, _ in jobs:
+            assert all(torch.equal(t, v) for t, v in zip(out, want)), turn
+        jobs[turn % 2][1]()                                    # the program's own calls between the replays
+        assert all(torch.equal(t, v) for t, v in zip(jobs[turn % 2][0], want)), turn
