@@ -374,7 +374,7 @@ int qesgd_combine_backward(const void* dy, uint32_t dtype, uint64_t ld_dy, const
 /* Columns of the form along the groups' rows: every group begins at a multiple of 128, at most R rows in at most E groups.  0 for sizes out of range. */
 uint64_t qesgd_mx4_grouped_columns(uint64_t R, uint32_t E);
 
-/* Packs rows in the groups' order: row r of a group is row order[r] / per of x [T, cols] (order NULL: row r; rows outside x are zeros).
+/* Packs rows in the groups' order: row r of a group is row order[r] / per of x [T, cols] (order NULL: row r, whatever per; rows outside x are zeros).
  *   packed    nullable: layout (R, cols), as qesgd_mx4_quantize_pack of the gathered rows; rows outside of every group are left as they are
  *   packed_t  nullable: layout (cols, qesgd_mx4_grouped_columns(R, E)): each column of x cut into blocks of 32 rows of one group; group e's
  *         rows begin at column sum_{i<e} up(size_i, 128), and zeros follow them to the next multiple of 128.  Equal to quantising that
@@ -398,8 +398,8 @@ size_t qesgd_mx4_grouped_gradient_workspace_bytes(uint64_t R, uint64_t N, uint64
 int qesgd_mx4_grouped_gradient(const void* a_packed_t, const void* b_packed_t, const int32_t* offsets, uint32_t E, uint64_t R, uint64_t N,
                                uint64_t K, void* d, uint32_t dtype, void* workspace, size_t workspace_bytes, void* stream);
 
-/* y[r, n] = sum_k x[row, k] W_e[n, k] for the rows of every group, x not quantised: row = order[r] / per, or r where order is NULL, of x
- * [T, K] in dtype; rows outside x count as zeros.  W_e packed, layout (N, K), w_stride bytes apart.  offsets NULL: one group of all R rows (E = 1).
+/* y[r, n] = sum_k x[row, k] W_e[n, k] for the rows of every group, x not quantised: row = order[r] / per, or r (whatever per) where order is NULL,
+ * of x [T, K] in dtype; rows outside x count as zeros.  W_e packed, layout (N, K), w_stride bytes apart.  offsets NULL: one group of all R rows (E = 1).
  * Products are exact (x as a sum of one, two or three bf16 numbers for bf16, f16 and f32), sums in fp32, y [R, N] in dtype.  Right for any
  * R, made for the next tokens of a few sequences: what it takes is the reading of the matrices that have rows.
  * workspace: qesgd_mx4_vector_product_workspace_bytes(R, N, K, E), 16-byte aligned; may be NULL when that is 0 (all but long rows of many tokens).

@@ -186,7 +186,7 @@ int qesgd_mx4_quantize_groups(const void* x, uint32_t dtype, uint64_t ld, uint64
     a.ld = T > 1 ? ld : cols;
     a.T = T;
     a.order = order;
-    a.per = per;
+    a.per = order ? per : 1;        // row r of x, not one of its pairs
     a.offsets = offsets;
     a.E = E;
     a.R = R;
@@ -280,7 +280,7 @@ int qesgd_mx4_vector_product(const void* x, uint32_t dtype, uint64_t ld, uint64_
     a.ld = T > 1 ? ld : K;
     a.T = T;
     a.order = order;
-    a.per = per;
+    a.per = order ? per : 1;        // row r of x, not one of its pairs
     a.w = (const unsigned char*)w_slab;
     a.w_stride = w_stride;
     a.offsets = offsets;
