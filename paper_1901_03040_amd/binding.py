@@ -31,6 +31,7 @@ MX4_NEAREST, MX4_STOCHASTIC = 0, 1
 MAX_STEPS = 32
 MAX_EXPERTS, MAX_CHOICES = 1024, 16
 GATE_ALL, GATE_CHOSEN = 0, 1
+ROWS_F32 = 0x100
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -553,8 +554,11 @@ def qesgd_combine(rows, ld, R, slots, gates, T, k, N, out, ld_out, stream=None):
     where, kind, pairs = "qesgd_combine", out.dtype, T * k
     dtype = _dtype(out, where)
     device, stream = _here(where, stream, out)
-    x = rows.data_ptr() if rows.dtype is kind and rows.get_device() == device and rows.is_contiguous() and rows.numel() >= (R - 1) * ld + N \
-        else _rows(where, device, rows, kind, R, ld, N)
+    own = kind                                                # the rows' type
+    if rows.dtype is _F32 and kind is not _F32:
+        dtype, own = dtype | ROWS_F32, _F32
+    x = rows.data_ptr() if rows.dtype is own and rows.get_device() == device and rows.is_contiguous() and rows.numel() >= (R - 1) * ld + N \
+        else _rows(where, device, rows, own, R, ld, N)
     y = out.data_ptr() if out.is_contiguous() and out.numel() >= (T - 1) * ld_out + N else _rows(where, device, out, kind, T, ld_out, N)
     s = None if slots is None else slots.data_ptr() if slots.dtype is _I32 and slots.get_device() == device and slots.is_contiguous() and \
         slots.numel() >= pairs else _ints(where, device, slots, pairs)
@@ -570,7 +574,10 @@ def qesgd_combine_backward(dy, ld_dy, rows, ld, R, slots, gates, T, k, N, drows,
     dtype = _dtype(dy, where)
     device, stream = _here(where, stream, dy)
     d = dy.data_ptr() if dy.is_contiguous() and dy.numel() >= (T - 1) * ld_dy + N else _rows(where, device, dy, kind, T, ld_dy, N)
-    x = None if rows is None else _rows(where, device, rows, kind, R, ld, N)
+    own = kind                                                # the rows' type
+    if rows is not None and rows.dtype is _F32 and kind is not _F32:
+        dtype, own = dtype | ROWS_F32, _F32
+    x = None if rows is None else _rows(where, device, rows, own, R, ld, N)
     dr = None if drows is None else _rows(where, device, drows, kind, R, ld_d, N)
     s = None if slots is None else slots.data_ptr() if slots.dtype is _I32 and slots.get_device() == device and slots.is_contiguous() and \
         slots.numel() >= pairs else _ints(where, device, slots, pairs)

@@ -100,8 +100,22 @@ struct Piece {
     }
 };
 
+// As many elements of a row of type RT as sixteen bytes of type DT hold: one piece, or two where the rows are fp32 beside results of 16 bits.
+template <uint32_t DT, uint32_t RT>
+struct RowPiece {
+    static constexpr uint32_t V = Piece<RT>::V, P = Piece<DT>::V / V;
+    Piece<RT> part[P];
+
+    template <bool STREAM>
+    __device__ __forceinline__ void load(const void* x, uint64_t at, uint32_t n) {
+#pragma unroll
+        for (uint32_t i = 0; i < P; ++i) part[i].template load<STREAM>(x, at + i * V, n > i * V ? n - i * V : 0u);
+    }
+    __device__ __forceinline__ float at(uint32_t i) const { return part[i / V].at((int)(i % V)); }
+};
+
 // A thread a piece of a token's row.  STREAM: out is written non-temporally.
-template <uint32_t DT, bool STREAM>
+template <uint32_t DT, uint32_t RT, bool STREAM>
 __global__ void __launch_bounds__(256) k_combine(const CParams p) {
     constexpr uint32_t V = Piece<DT>::V;
     const uint32_t i = blockIdx.x * 256u + threadIdx.x, token = i / p.vectors;         // a launch has fewer than 2^32 threads
@@ -116,7 +130,7 @@ __global__ void __launch_bounds__(256) k_combine(const CParams p) {
         const uint32_t slot = p.slots ? (uint32_t)p.slots[pair] : (uint32_t)pair;
         if (slot >= p.R) continue;
         const float g = p.gates ? p.gates[pair] : 1.0f;
-        Piece<DT> x;
+        RowPiece<DT, RT> x;
         x.template load<false>(p.rows, slot * p.ld + col, n);
 #pragma unroll
         for (uint32_t e = 0; e < V; ++e) sum[e] += g * x.at(e);
@@ -130,7 +144,7 @@ __global__ void __launch_bounds__(256) k_combine(const CParams p) {
 enum { kKept = 0, kStreamOut = 1, kStreamBoth = 2 };
 
 // L lanes a token (256: a workgroup); KM: at least k.
-template <uint32_t DT, uint32_t L, int KM, int POLICY>
+template <uint32_t DT, uint32_t RT, uint32_t L, int KM, int POLICY>
 __global__ void __launch_bounds__(256) k_combine_backward(const CParams p) {
     constexpr uint32_t V = Piece<DT>::V, tokens = 256 / L;
     constexpr bool OUT = POLICY != kKept, IN = POLICY == kStreamBoth;
@@ -154,7 +168,8 @@ __global__ void __launch_bounds__(256) k_combine_backward(const CParams p) {
     if (there) {
         for (uint32_t c = lane; c < p.vectors; c += L) {
             const uint32_t col = c * V, n = p.N - col;
-            Piece<DT> d, x[KM];
+            Piece<DT> d;
+            RowPiece<DT, RT> x[KM];
             d.template load<false>(p.dy, t * p.ld_dy + col, n);
             if (p.dgates) {
 #pragma unroll
@@ -230,14 +245,23 @@ CParams params(const Combine& a) {
 constexpr uint64_t kStreamMoved = 128ull << 20, kStreamRows = 256ull << 20;
 static bool whole_lines(const void* p, uint64_t ld, uint32_t dtype) { return ((uintptr_t)p | ld * dtype_bytes(dtype)) % 128 == 0; }
 
+// f(types of the results and of the rows, as constants): the same, or rows of fp32.
+template <class F>
+static void by_types(const Combine& a, F&& f) {
+    by_type(a.dtype, [&](auto t) {
+        if (a.rows_dtype == t.value) f(t, t);
+        else f(t, std::integral_constant<uint32_t, QESGD_F32>{});
+    });
+}
+
 int launch_combine(const Combine& a) {
     const CParams p = params(a);
-    const uint64_t groups = ((uint64_t)p.T * p.vectors + 255) / 256, moved = a.N * (a.T * a.k + a.T) * dtype_bytes(a.dtype);
+    const uint64_t groups = ((uint64_t)p.T * p.vectors + 255) / 256, moved = a.N * (a.T * a.k * dtype_bytes(a.rows_dtype) + a.T * dtype_bytes(a.dtype));
     if (!grid_ok(groups, 256)) return QESGD_ERR_DIM;
     const bool stream = moved >= kStreamMoved && whole_lines(a.out, a.ld_out, a.dtype);
-    by_type(a.dtype, [&](auto t) {
-        if (stream) k_combine<t.value, true><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
-        else k_combine<t.value, false><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+    by_types(a, [&](auto t, auto r) {
+        if (stream) k_combine<t.value, r.value, true><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+        else k_combine<t.value, r.value, false><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
     });
     return launched();
 }
@@ -246,31 +270,31 @@ int launch_combine_backward(const Combine& a) {
     const CParams p = params(a);
     // lanes of a token: a workgroup for long rows, for short ones no more than have work
     const uint32_t lanes = p.vectors > 128 ? 256 : p.vectors > 16 ? 64 : p.vectors > 8 ? 16 : 8;
-    const uint64_t tokens = 256 / lanes, groups = (p.T + tokens - 1) / tokens, rows = a.N * a.T * a.k * dtype_bytes(a.dtype);
+    const uint64_t tokens = 256 / lanes, groups = (p.T + tokens - 1) / tokens, pairs = a.T * a.k, rows = a.N * pairs * dtype_bytes(a.rows_dtype);
     if (!grid_ok(groups, 256)) return QESGD_ERR_DIM;
-    const bool stream = a.drows && 2 * rows >= kStreamMoved && whole_lines(a.drows, a.ld_d, a.dtype);
-    const auto go = [&](auto t, auto l, auto km) {
-        constexpr uint32_t DT = t.value, L = l.value;
+    const bool stream = a.drows && rows + a.N * pairs * dtype_bytes(a.dtype) >= kStreamMoved && whole_lines(a.drows, a.ld_d, a.dtype);
+    const auto go = [&](auto t, auto r, auto l, auto km) {
+        constexpr uint32_t DT = t.value, RT = r.value, L = l.value;
         constexpr int KM = km.value;
         // rows of up to 256 bytes are not streamed: a call of them has to have a million
-        if (L == 256 && stream && rows >= kStreamRows) k_combine_backward<DT, L, KM, L == 256 ? kStreamBoth : kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
-        else if (L >= 64 && stream) k_combine_backward<DT, L, KM, L >= 64 ? kStreamOut : kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
-        else k_combine_backward<DT, L, KM, kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+        if (L == 256 && stream && rows >= kStreamRows) k_combine_backward<DT, RT, L, KM, L == 256 ? kStreamBoth : kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+        else if (L >= 64 && stream) k_combine_backward<DT, RT, L, KM, L >= 64 ? kStreamOut : kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+        else k_combine_backward<DT, RT, L, KM, kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
     };
-    const auto by_choices = [&](auto t, auto l) {
+    const auto by_choices = [&](auto t, auto r, auto l) {
         using std::integral_constant;
-        if (p.k <= 2) go(t, l, integral_constant<int, 2>{});
-        else if (p.k <= 4) go(t, l, integral_constant<int, 4>{});
-        else if (p.k <= 8) go(t, l, integral_constant<int, 8>{});
-        else go(t, l, integral_constant<int, 16>{});
+        if (p.k <= 2) go(t, r, l, integral_constant<int, 2>{});
+        else if (p.k <= 4) go(t, r, l, integral_constant<int, 4>{});
+        else if (p.k <= 8) go(t, r, l, integral_constant<int, 8>{});
+        else go(t, r, l, integral_constant<int, 16>{});
     };
-    by_type(a.dtype, [&](auto t) {
+    by_types(a, [&](auto t, auto r) {
         using std::integral_constant;
         switch (lanes) {
-            case 8: by_choices(t, integral_constant<uint32_t, 8>{}); break;
-            case 16: by_choices(t, integral_constant<uint32_t, 16>{}); break;
-            case 64: by_choices(t, integral_constant<uint32_t, 64>{}); break;
-            default: by_choices(t, integral_constant<uint32_t, 256>{}); break;
+            case 8: by_choices(t, r, integral_constant<uint32_t, 8>{}); break;
+            case 16: by_choices(t, r, integral_constant<uint32_t, 16>{}); break;
+            case 64: by_choices(t, r, integral_constant<uint32_t, 64>{}); break;
+            default: by_choices(t, r, integral_constant<uint32_t, 256>{}); break;
         }
     });
     return launched();

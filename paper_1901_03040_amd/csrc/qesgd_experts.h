@@ -41,7 +41,7 @@ int launch_route_backward(const RouteBackward& a);
 
 struct Combine {
     const void* rows;
-    uint32_t dtype;
+    uint32_t dtype, rows_dtype;     // of the rest; of rows: the same or fp32
     uint64_t ld, R;
     const int32_t* slots;           // nullable
     const float* gates;             // nullable

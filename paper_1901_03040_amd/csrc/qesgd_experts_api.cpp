@@ -12,6 +12,12 @@ bool dtype_ok(uint32_t t) { return t == QESGD_F32 || t == QESGD_BF16 || t == QES
 bool experts_ok(uint32_t E) { return E != 0 && E <= QESGD_MAX_EXPERTS; }
 bool choices_ok(uint32_t E, uint32_t k) { return experts_ok(E) && k != 0 && k <= E && k <= QESGD_MAX_CHOICES; }
 bool side_ok(uint64_t v) { return v != 0 && v <= kMaxSide; }
+// The type of the experts' rows beside results of dtype; takes the mark off dtype.
+uint32_t rows_type(uint32_t& dtype) {
+    const bool wide = dtype & QESGD_ROWS_F32;
+    dtype &= ~QESGD_ROWS_F32;
+    return wide ? (uint32_t)QESGD_F32 : dtype;
+}
 // rows of `row` elements, ld apart
 bool rows_ok(uint64_t rows, uint64_t row, uint64_t ld) { return rows < 2 || (ld >= row && ld < (1ull << 40) / rows); }
 bool slab_ok(uint64_t E, uint64_t stride, uint64_t bytes) { return E < 2 || (stride >= bytes && stride % 256 == 0 && stride < (1ull << 48)); }
@@ -116,12 +122,14 @@ int qesgd_route_backward(const void* logits, uint32_t dtype, uint64_t ld, uint64
 int qesgd_combine(const void* rows, uint32_t dtype, uint64_t ld, uint64_t R, const int32_t* slots, const float* gates, uint64_t T, uint32_t k,
                   uint64_t N, void* out, uint64_t ld_out, void* stream) {
     if (!rows || !out) return QESGD_ERR_NULL;
+    const uint32_t rows_dtype = rows_type(dtype);
     if (const int rc = combine_check(dtype, R, slots, T, k, N); rc != QESGD_OK) return rc;
-    if (!aligned(rows, dtype_bytes(dtype)) || !aligned(out, dtype_bytes(dtype)) || !aligned(slots, 4) || !aligned(gates, 4)) return QESGD_ERR_ALIGN;
+    if (!aligned(rows, dtype_bytes(rows_dtype)) || !aligned(out, dtype_bytes(dtype)) || !aligned(slots, 4) || !aligned(gates, 4)) return QESGD_ERR_ALIGN;
     if (!rows_ok(R, N, ld) || !rows_ok(T, N, ld_out)) return QESGD_ERR_STRIDE;
     Combine a{};
     a.rows = rows;
     a.dtype = dtype;
+    a.rows_dtype = rows_dtype;
     a.ld = R > 1 ? ld : N;
     a.R = R;
     a.slots = slots;
@@ -138,14 +146,17 @@ int qesgd_combine(const void* rows, uint32_t dtype, uint64_t ld, uint64_t R, con
 int qesgd_combine_backward(const void* dy, uint32_t dtype, uint64_t ld_dy, const void* rows, uint64_t ld, uint64_t R, const int32_t* slots,
                            const float* gates, uint64_t T, uint32_t k, uint64_t N, void* drows, uint64_t ld_d, float* dgates, void* stream) {
     if (!dy || (!drows && !dgates) || (dgates && !rows) || (drows && !gates)) return QESGD_ERR_NULL;
+    const uint32_t given = rows_type(dtype), rows_dtype = dgates ? given : dtype;      // without dgates nothing is read of the rows
     if (const int rc = combine_check(dtype, R, slots, T, k, N); rc != QESGD_OK) return rc;
-    if (!aligned(dy, dtype_bytes(dtype)) || !aligned(rows, dtype_bytes(dtype)) || !aligned(drows, dtype_bytes(dtype)) || !aligned(slots, 4) ||
+    if (dgates && drows == rows && rows_dtype != dtype) return QESGD_ERR_DTYPE;
+    if (!aligned(dy, dtype_bytes(dtype)) || !aligned(rows, dtype_bytes(rows_dtype)) || !aligned(drows, dtype_bytes(dtype)) || !aligned(slots, 4) ||
         !aligned(gates, 4) || !aligned(dgates, 4))
         return QESGD_ERR_ALIGN;
     if (!rows_ok(T, N, ld_dy) || (dgates && !rows_ok(R, N, ld)) || (drows && !rows_ok(R, N, ld_d))) return QESGD_ERR_STRIDE;
     Combine a{};
     a.rows = rows;
     a.dtype = dtype;
+    a.rows_dtype = rows_dtype;
     a.ld = R > 1 ? ld : N;
     a.R = R;
     a.slots = slots;
