@@ -403,8 +403,8 @@ int qesgd_mx4_grouped_gradient(const void* a_packed_t, const void* b_packed_t, c
 
 /* y[r, n] = sum_k x[row, k] W_e[n, k] for the rows of every group, x not quantised: row = order[r] / per, or r (whatever per) where order is NULL,
  * of x [T, K] in dtype; rows outside x count as zeros.  W_e packed, layout (N, K), w_stride bytes apart.  offsets NULL: one group of all R rows (E = 1).
- * Products are exact (x as a sum of one, two or three bf16 numbers for bf16, f16 and f32), sums in fp32, y [R, N] in dtype.  Right for any
- * R, made for the next tokens of a few sequences: what it takes is the reading of the matrices that have rows.
+ * Products are exact (x as a sum of one, two or three bf16 numbers for bf16, f16 and f32), sums in fp32, y [R, N] in dtype, in fp32 with
+ * dtype | QESGD_ROWS_F32.  Right for any R, made for the next tokens of a few sequences: what it takes is the reading of the matrices that have rows.
  * workspace: qesgd_mx4_vector_product_workspace_bytes(R, N, K, E), 16-byte aligned; may be NULL when that is 0 (all but long rows of many tokens).
  * Scale bytes of the format (up to 252, and 255); elements of W below 2^-126 may count as 0; an element of x in f32 keeps 2^-24 of itself down to 2^-102, smaller ones may lose digits. */
 size_t qesgd_mx4_vector_product_workspace_bytes(uint64_t R, uint64_t N, uint64_t K, uint32_t E);

@@ -647,12 +647,15 @@ def qesgd_mx4_vector_product_workspace_bytes(R: int, N: int, K: int, E: int) -> 
 
 
 def qesgd_mx4_vector_product(x, ld, T, order, per, w_slab, w_stride, offsets, E, R, N, K, y, ldy, workspace=None, stream=None):
-    where, kind = "qesgd_mx4_vector_product", y.dtype
-    dtype = _dtype(y, where)
+    where, kind = "qesgd_mx4_vector_product", x.dtype
+    dtype = _dtype(x, where)
     device, stream = _here(where, stream, y)
-    a = x.data_ptr() if x.dtype is kind and x.get_device() == device and x.is_contiguous() and x.numel() >= (T - 1) * ld + K \
+    own = kind                                                # y's type
+    if y.dtype is _F32 and kind is not _F32:
+        dtype, own = dtype | ROWS_F32, _F32
+    a = x.data_ptr() if x.get_device() == device and x.is_contiguous() and x.numel() >= (T - 1) * ld + K \
         else _rows(where, device, x, kind, T, ld, K)
-    c = y.data_ptr() if y.is_contiguous() and y.numel() >= (R - 1) * ldy + N else _rows(where, device, y, kind, R, ldy, N)
+    c = y.data_ptr() if y.dtype is own and y.is_contiguous() and y.numel() >= (R - 1) * ldy + N else _rows(where, device, y, own, R, ldy, N)
     o = None if order is None else order.data_ptr() if order.dtype is _I32 and order.get_device() == device and order.is_contiguous() and \
         order.numel() >= R else _ints(where, device, order, R)
     f = None if offsets is None else offsets.data_ptr() if offsets.dtype is _I32 and offsets.get_device() == device and offsets.is_contiguous() and \

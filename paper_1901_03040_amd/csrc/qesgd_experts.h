@@ -112,7 +112,7 @@ int launch_piece_sum(const PieceSum& p, uint32_t dtype, hipStream_t stream);
 
 struct VectorProduct {
     const void* x;
-    uint32_t dtype;
+    uint32_t dtype, rows_dtype;     // of x; of y: the same or fp32
     uint64_t ld, T;
     const int32_t* order;           // nullable
     uint32_t per;

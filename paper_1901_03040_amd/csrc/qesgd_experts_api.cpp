@@ -278,8 +278,9 @@ int qesgd_mx4_vector_product(const void* x, uint32_t dtype, uint64_t ld, uint64_
     if (!x || !w_slab || !y || (!offsets && E > 1)) return QESGD_ERR_NULL;
     if (!experts_ok(E)) return QESGD_ERR_EXPERTS;
     if (!vector_sizes_ok(R, N, K, E) || !side_ok(T) || !side_ok(per)) return QESGD_ERR_DIM;
+    const uint32_t rows_dtype = rows_type(dtype);
     if (!dtype_ok(dtype)) return QESGD_ERR_DTYPE;
-    if (!aligned(x, dtype_bytes(dtype)) || !aligned(y, dtype_bytes(dtype)) || !aligned(order, 4) || !aligned(offsets, 4) || !aligned(w_slab, 256) ||
+    if (!aligned(x, dtype_bytes(dtype)) || !aligned(y, dtype_bytes(rows_dtype)) || !aligned(order, 4) || !aligned(offsets, 4) || !aligned(w_slab, 256) ||
         !aligned(workspace, 16))
         return QESGD_ERR_ALIGN;
     qesgd_mx4_layout W;
@@ -288,6 +289,7 @@ int qesgd_mx4_vector_product(const void* x, uint32_t dtype, uint64_t ld, uint64_
     VectorProduct a{};
     a.x = x;
     a.dtype = dtype;
+    a.rows_dtype = rows_dtype;
     a.ld = T > 1 ? ld : K;
     a.T = T;
     a.order = order;

@@ -40,6 +40,7 @@ struct VParams {
     uint32_t row_codes, row_scales;
     void* y;
     uint64_t ldy;
+    bool wide;                        // y is fp32, whatever x is
     uint32_t splits;                  // waves that share a row's columns: 1 .. kVWaves
     uint32_t room;                    // bytes of LDS for rows of x
     uint32_t pieces;                  // of the columns, a workgroup each; with more than one the sums go to partial [pieces, R, N]
@@ -268,6 +269,7 @@ __global__ void __launch_bounds__(kVWaves * 64, 4) k_mx4_vector_product(const VP
                 for (uint32_t s = 0; s < kVWaves; ++s) v += part[s];
             }
             if (p.pieces > 1) p.partial[((uint64_t)piece * p.R + r0 + r) * p.N + n] = v;
+            else if (DT != QESGD_F32 && p.wide) ((float*)p.y)[(uint64_t)(r0 + r) * p.ldy + n] = v;
             else put_row<DT>(p.y, (uint64_t)(r0 + r) * p.ldy + n, v);
         }
     }
@@ -373,6 +375,7 @@ int launch_vector_product(const VectorProduct& a) {
     p.row_scales = (uint32_t)W.row_scales;
     p.y = a.y;
     p.ldy = a.ldy;
+    p.wide = a.rows_dtype == QESGD_F32;
     p.splits = plan.splits;
     p.room = plan.room;
     p.pieces = plan.pieces;
@@ -397,7 +400,7 @@ int launch_vector_product(const VectorProduct& a) {
     });
     const int rc = launched();
     if (rc != QESGD_OK || plan.pieces == 1) return rc;
-    return launch_piece_sum(PieceSum{a.workspace, plan.pieces, a.R * a.N, a.offsets, a.E, p.R, p.N, a.y, a.ldy}, a.dtype, a.stream);
+    return launch_piece_sum(PieceSum{a.workspace, plan.pieces, a.R * a.N, a.offsets, a.E, p.R, p.N, a.y, a.ldy}, a.rows_dtype, a.stream);
 }
 
 }  // namespace qesgd
