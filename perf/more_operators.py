@@ -428,23 +428,23 @@ def run(state):
             B.qesgd_mx4_vector_product(x, K, T, order, k, w, w.stride(0), offsets, E, R, N, K, state["rows"], N, workspace=kept["ws"])
         return state["rows"]
     if kind == "layer":
-        if not kept:
-            kept["ws"] = B.alloc_workspace(B.qesgd_mx4_grouped_product_workspace_bytes(R, N, K, E), DEV)
+        if not kept:                                         # the rows that are added up are fp32: the result is rounded once
+            kept.update(ws=B.alloc_workspace(B.qesgd_mx4_grouped_product_workspace_bytes(R, N, K, E), DEV), rows=torch.empty((R, N), device=DEV))
         B.qesgd_mx4_quantize_groups(x, K, T, order, k, offsets, E, R, K, B.MX4_NEAREST, 0, 0, state["px"])
-        B.qesgd_mx4_grouped_product(state["px"], w, w.stride(0), offsets, E, R, N, K, state["rows"], N, workspace=kept["ws"])
-        B.qesgd_combine(state["rows"], N, R, slots, gates, T, k, N, state["y"], N)
+        B.qesgd_mx4_grouped_product(state["px"], w, w.stride(0), offsets, E, R, N, K, kept["rows"], N, workspace=kept["ws"])
+        B.qesgd_combine(kept["rows"], N, R, slots, gates, T, k, N, state["y"], N)
         return state["y"]
     mode, wt = B.MX4_STOCHASTIC if case["mode"] == "stochastic" else B.MX4_NEAREST, state["wt"]
     if not kept:
         need = max(B.qesgd_mx4_grouped_product_workspace_bytes(R, N, K, E), B.qesgd_mx4_grouped_product_workspace_bytes(R, K, N, E),
                    B.qesgd_mx4_grouped_gradient_workspace_bytes(R, N, K, E))
-        kept["ws"] = B.alloc_workspace(need, DEV)
+        kept.update(ws=B.alloc_workspace(need, DEV), dxrows=torch.empty((R, K), device=DEV))
     B.qesgd_mx4_quantize_groups(x, K, T, order, k, offsets, E, R, K, B.MX4_NEAREST, 0, 0, state["px"], packed_t=state["pxt"])
     B.qesgd_mx4_grouped_product(state["px"], w, w.stride(0), offsets, E, R, N, K, state["rows"], N, workspace=kept["ws"])
     B.qesgd_mx4_quantize_groups(state["drows"], N, R, None, 1, offsets, E, R, N, mode, seed, 5, state["pd"], packed_t=state["pdt"])
-    B.qesgd_mx4_grouped_product(state["pd"], wt, wt.stride(0), offsets, E, R, K, N, state["dxrows"], K, workspace=kept["ws"])
+    B.qesgd_mx4_grouped_product(state["pd"], wt, wt.stride(0), offsets, E, R, K, N, kept["dxrows"], K, workspace=kept["ws"])
     B.qesgd_mx4_grouped_gradient(state["pdt"], state["pxt"], offsets, E, R, N, K, state["dw"], workspace=kept["ws"])
-    B.qesgd_combine(state["dxrows"], K, R, slots, None, T, k, K, state["dx"], K)
+    B.qesgd_combine(kept["dxrows"], K, R, slots, None, T, k, K, state["dx"], K)
     return [state["rows"], state["dx"], state["dw"]]
 
 
