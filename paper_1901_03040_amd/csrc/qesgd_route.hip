@@ -71,10 +71,7 @@ __device__ __forceinline__ float total(float v) {
     return __uint_as_float(over_lanes<L>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 
-// exp(x) for x <= 0 (a NaN: NaN), 0 below 2^-126.  By x log2(e), whose rounding moves the result by |x| 2^-24 of itself: for the terms of a sum, where
-// those that count have a small |x|.
-__device__ __forceinline__ float exp_of_sum(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
-// The same with the product's rest: right to two steps whatever x.
+// exp(x) for x <= 0 (a NaN: NaN), 0 below 2^-126: by x log2(e) and that product's rest, right to two steps whatever x.
 __device__ __forceinline__ float exp_below(float x) {
     const float high = x * 1.44269504f;
     const float rest = __builtin_fmaf(x, 1.925963033e-8f, __builtin_fmaf(x, 1.44269504f, -high));
@@ -126,7 +123,7 @@ __device__ __forceinline__ void choose(const RParams& p, uint64_t t, uint32_t l,
     float sum = 0.0f;
     if (p.all) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) sum += exp_of_sum(v[c] - base);
+        for (int c = 0; c < C; ++c) sum += exp_below(v[c] - base);
     }
     float mine = -INFINITY;
     uint32_t mine_e = 0xFFFFFFFFu;
