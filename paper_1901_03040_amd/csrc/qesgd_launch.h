@@ -26,4 +26,15 @@ void by_type(uint32_t dtype, F&& f) {
     }
 }
 
+// f(first, count) for all of `groups` workgroups of `threads`, as many at a time as one launch may number threads for: fewer than 2^32.
+template <class F>
+int by_launches(uint64_t groups, uint32_t threads, F&& f) {
+    const uint64_t most = (1ull << 31) / threads;
+    for (uint64_t first = 0; first < groups; first += most) {
+        f((uint32_t)first, (uint32_t)(groups - first < most ? groups - first : most));
+        if (const int rc = launched(); rc != QESGD_OK) return rc;
+    }
+    return QESGD_OK;
+}
+
 }  // namespace qesgd

@@ -29,6 +29,7 @@ struct RParams {
     uint32_t* counts;                 // [blocks, E]
     uint32_t* totals;                 // [E], behind them
     uint32_t blocks;
+    uint32_t block0;                  // of the launch, where the choice takes several
     uint32_t bits;                    // of E: those that an expert's number can have, and of -1 as E
 };
 
@@ -171,7 +172,7 @@ __global__ void __launch_bounds__(choose_waves(C) * 64) k_route_choose(const RPa
     for (uint32_t e = threadIdx.x; e < p.E; e += kChooseWaves * 64u) count[e] = 0u;
     __syncthreads();
     const uint32_t l = threadIdx.x & (L - 1u), part = threadIdx.x / L;
-    const uint32_t first = blockIdx.x * kBlockTokens, n = min(kBlockTokens, p.T - first);
+    const uint32_t block = p.block0 + blockIdx.x, first = block * kBlockTokens, n = min(kBlockTokens, p.T - first);
     // every part of a wave makes as many turns: the exchanges between lanes are the whole wave's
     for (uint32_t i = part; i < ((n + 64u / L - 1u) & ~(64u / L - 1u)); i += kChooseWaves * 64u / L) {
         const uint64_t t = first + min(i, n - 1u);
@@ -185,7 +186,7 @@ __global__ void __launch_bounds__(choose_waves(C) * 64) k_route_choose(const RPa
         }
     }
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < p.E; e += kChooseWaves * 64u) p.counts[(uint64_t)blockIdx.x * p.E + e] = count[e];
+    for (uint32_t e = threadIdx.x; e < p.E; e += kChooseWaves * 64u) p.counts[(uint64_t)block * p.E + e] = count[e];
 }
 
 // Many blocks: counts[block, e] becomes the pairs of e in the blocks before, totals[e] those of all.  A workgroup has four experts, a thread a stretch
@@ -527,14 +528,21 @@ int launch_route(const Route& a) {
     p.counts = a.workspace;
     p.blocks = (uint32_t)route_blocks(a.T);
     p.totals = p.counts + (uint64_t)p.blocks * a.E;
+    int rc = QESGD_OK;
     by_type(a.dtype, [&](auto t) {
-        by_experts(a.E, false, [&](auto l, auto c) { k_route_choose<t.value, l.value, c.value><<<p.blocks, choose_waves(c.value) * 64, 0, a.stream>>>(p); });
+        by_experts(a.E, false, [&](auto l, auto c) {
+            constexpr uint32_t threads = choose_waves(c.value) * 64;
+            rc = by_launches(p.blocks, threads, [&](uint32_t first, uint32_t count) {
+                p.block0 = first;
+                k_route_choose<t.value, l.value, c.value><<<count, threads, 0, a.stream>>>(p);
+            });
+        });
     });
-    if (const int rc = launched(); rc != QESGD_OK) return rc;
+    if (rc != QESGD_OK) return rc;
     const uint32_t lds = ((kPlaceWaves + 1) * a.E + kPlaceWaves) * sizeof(uint32_t);
     if (route_scanned(p.blocks, a.E)) {
         k_route_scan<<<(a.E + kScanExperts - 1) / kScanExperts, kScanExperts * kScanParts, 0, a.stream>>>(p);
-        if (const int rc = launched(); rc != QESGD_OK) return rc;
+        if (rc = launched(); rc != QESGD_OK) return rc;
         k_route_place<true><<<p.blocks, kPlaceWaves * 64, lds, a.stream>>>(p);
     } else {
         k_route_place<false><<<p.blocks, kPlaceWaves * 64, lds, a.stream>>>(p);

@@ -1,0 +1,38 @@
+"""Layers of experts at the ends of the ranges that the header states: as many tokens as it allows, which are more than one launch numbers threads for."""
+import pytest
+import torch
+
+from expert_reference import ONE
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1901_03040_amd import binding
+    assert torch.cuda.is_available()
+    binding.lib()
+    yield binding
+    torch.cuda.empty_cache()
+
+
+def test_choices_of_2_28_tokens(B):
+    """Blocks of 64 tokens, 1024 threads each, are 2^32 threads."""
+    T, E, part = 1 << 28, 9, 1 << 24
+    x = torch.empty(T, E, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    experts, order, slots = (torch.full((T,), -7, dtype=torch.int32, device="cuda") for _ in range(3))
+    gates, offsets = torch.zeros(T, device="cuda"), torch.empty(E + 1, dtype=torch.int32, device="cuda")
+    B.qesgd_route(x, E, T, E, 1, B.GATE_CHOSEN, experts, gates, offsets, order, slots, workspace=B.alloc_workspace(B.qesgd_route_workspace_bytes(T, E, 1)))
+    assert (gates == 1.0).all()                                 # of one choice
+    numbers, counts = torch.arange(E, device="cuda"), torch.zeros(E, dtype=torch.int64, device="cuda")
+    for lo in range(0, T, part):
+        v = x[lo:lo + part]
+        first = torch.where(v == v.amax(1, keepdim=True), numbers, E).amin(1)      # ties: the lower one
+        assert torch.equal(experts[lo:lo + part].long(), first), lo
+        counts += torch.bincount(first, minlength=E)
+        # a pair's place holds the pair
+        assert torch.equal(order[slots[lo:lo + part].long()].long(), torch.arange(lo, lo + part, device="cuda")), lo
+    assert offsets[0] == 0 and torch.equal(offsets[1:].long(), counts.cumsum(0))
+    for e in range(E):                                          # places: by expert, those of one in the tokens' order
+        own = order[offsets[e]:offsets[e + 1]]
+        assert bool((own[1:] > own[:-1]).all()) and bool((experts[own.long()] == e).all()), e
