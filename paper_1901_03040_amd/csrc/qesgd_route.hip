@@ -395,12 +395,13 @@ struct BParams {
     const float* gates;
     const float* dgates;
     void* dlogits;
+    uint32_t block0;                  // of the launch, where there are several
 };
 
 template <uint32_t DT, int L, int C>
 __global__ void __launch_bounds__(256) k_route_backward(const BParams p) {
     const uint32_t l = threadIdx.x & (L - 1u);
-    const uint64_t i = (uint64_t)blockIdx.x * (256u / L) + threadIdx.x / L;
+    const uint64_t i = (uint64_t)(p.block0 + blockIdx.x) * (256u / L) + threadIdx.x / L;
     const uint64_t t = min(i, (uint64_t)p.T - 1u);
     int32_t expert = -1;
     float g = 0.0f, d = 0.0f;
@@ -566,12 +567,13 @@ int launch_route_backward(const RouteBackward& a) {
     int rc = QESGD_OK;
     by_type(a.dtype, [&](auto t) {
         by_experts(a.E, t.value == QESGD_F32, [&](auto l, auto c) {
-            const uint64_t groups = (a.T + 256 / l.value - 1) / (256 / l.value);
-            if (!grid_ok(groups, 256)) { rc = QESGD_ERR_DIM; return; }
-            k_route_backward<t.value, l.value, c.value><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+            rc = by_launches((a.T + 256 / l.value - 1) / (256 / l.value), 256, [&](uint32_t first, uint32_t count) {
+                p.block0 = first;
+                k_route_backward<t.value, l.value, c.value><<<count, 256, 0, a.stream>>>(p);
+            });
         });
     });
-    return rc != QESGD_OK ? rc : launched();
+    return rc;
 }
 
 }  // namespace qesgd

@@ -36,3 +36,19 @@ def test_choices_of_2_28_tokens(B):
     for e in range(E):                                          # places: by expert, those of one in the tokens' order
         own = order[offsets[e]:offsets[e + 1]]
         assert bool((own[1:] > own[:-1]).all()) and bool((experts[own.long()] == e).all()), e
+
+
+def test_gradient_of_the_logits_of_2_28_tokens(B):
+    """16 lanes to a token are 2^32 threads.  In the logits' place, so that a token worked out twice, or not at all, shows."""
+    T, E = 1 << 28, 9
+    x = torch.empty(T, E, dtype=torch.bfloat16, device="cuda").fill_(7.0)
+    experts = torch.arange(T, dtype=torch.int32, device="cuda") % E
+    gates, dgates = torch.full((T,), 0.5, device="cuda"), experts.float()
+    B.qesgd_route_backward(None, E, T, E, 1, B.GATE_CHOSEN, experts, gates, dgates, x, E)
+    # one choice: s = g d, and dlogits = g (d - g d) = d / 4 at the chosen one: exact in bf16
+    for lo in range(0, T, 1 << 24):
+        part = x[lo:lo + (1 << 24)]
+        want = torch.zeros_like(part)
+        e = experts[lo:lo + (1 << 24)].long()
+        want.scatter_(1, e[:, None], (e.float() / 4).to(torch.bfloat16)[:, None])
+        assert torch.equal(part, want), lo
