@@ -26,6 +26,7 @@ struct CParams {
     void* drows;
     uint64_t ld_d;
     float* dgates;
+    uint32_t block0;                  // of the launch, where the gradients take several
 };
 
 // Sixteen bytes of a row, or the n elements that are left of it.
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(256) k_combine_backward(const CParams p) {
     constexpr bool OUT = POLICY != kKept, IN = POLICY == kStreamBoth;
     __shared__ float sums[4][KM];
     const uint32_t lane = threadIdx.x % L;
-    const uint64_t t = (uint64_t)blockIdx.x * tokens + threadIdx.x / L;
+    const uint64_t t = (uint64_t)(p.block0 + blockIdx.x) * tokens + threadIdx.x / L;
     const bool there = t < p.T;
     float dot[KM], gate[KM];
     uint32_t slot[KM];
@@ -267,19 +268,25 @@ int launch_combine(const Combine& a) {
 }
 
 int launch_combine_backward(const Combine& a) {
-    const CParams p = params(a);
+    CParams p = params(a);
     // lanes of a token: a workgroup for long rows, for short ones no more than have work
     const uint32_t lanes = p.vectors > 128 ? 256 : p.vectors > 16 ? 64 : p.vectors > 8 ? 16 : 8;
     const uint64_t tokens = 256 / lanes, groups = (p.T + tokens - 1) / tokens, pairs = a.T * a.k, rows = a.N * pairs * dtype_bytes(a.rows_dtype);
-    if (!grid_ok(groups, 256)) return QESGD_ERR_DIM;
     const bool stream = a.drows && rows + a.N * pairs * dtype_bytes(a.dtype) >= kStreamMoved && whole_lines(a.drows, a.ld_d, a.dtype);
+    int rc = QESGD_OK;
     const auto go = [&](auto t, auto r, auto l, auto km) {
         constexpr uint32_t DT = t.value, RT = r.value, L = l.value;
         constexpr int KM = km.value;
+        const auto launch = [&](auto policy) {
+            rc = by_launches(groups, 256, [&](uint32_t first, uint32_t count) {
+                p.block0 = first;
+                k_combine_backward<DT, RT, L, KM, policy.value><<<count, 256, 0, a.stream>>>(p);
+            });
+        };
         // rows of up to 256 bytes are not streamed: a call of them has to have a million
-        if (L == 256 && stream && rows >= kStreamRows) k_combine_backward<DT, RT, L, KM, L == 256 ? kStreamBoth : kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
-        else if (L >= 64 && stream) k_combine_backward<DT, RT, L, KM, L >= 64 ? kStreamOut : kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
-        else k_combine_backward<DT, RT, L, KM, kKept><<<(uint32_t)groups, 256, 0, a.stream>>>(p);
+        if (L == 256 && stream && rows >= kStreamRows) launch(std::integral_constant<int, L == 256 ? kStreamBoth : kKept>{});
+        else if (L >= 64 && stream) launch(std::integral_constant<int, L >= 64 ? kStreamOut : kKept>{});
+        else launch(std::integral_constant<int, kKept>{});
     };
     const auto by_choices = [&](auto t, auto r, auto l) {
         using std::integral_constant;
@@ -297,7 +304,7 @@ int launch_combine_backward(const Combine& a) {
             default: by_choices(t, r, integral_constant<uint32_t, 256>{}); break;
         }
     });
-    return launched();
+    return rc;
 }
 
 }  // namespace qesgd

@@ -52,3 +52,27 @@ def test_gradient_of_the_logits_of_2_28_tokens(B):
         e = experts[lo:lo + (1 << 24)].long()
         want.scatter_(1, e[:, None], (e.float() / 4).to(torch.bfloat16)[:, None])
         assert torch.equal(part, want), lo
+
+
+def test_gradient_of_the_gates_of_2_24_long_rows(B):
+    """A workgroup to a token of 129 pieces of 16 bytes is 2^32 threads."""
+    T, N, R = (1 << 24) + 5, 1032, 6
+    dy = torch.empty(T, N, dtype=torch.bfloat16, device="cuda")
+    dy.copy_((torch.arange(T, device="cuda") % 3 - 1).to(torch.bfloat16)[:, None].expand(T, N))
+    rows = torch.randn(R, N, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(torch.bfloat16)
+    slots = (torch.arange(T, dtype=torch.int32, device="cuda") % (R + 1)) - 1
+    dgates = torch.full((T,), 9.0, device="cuda")
+    B.qesgd_combine_backward(dy, N, rows, N, R, slots, None, T, 1, N, None, 0, dgates)
+    sums, size = rows.double().sum(1), rows.double().abs().sum(1)
+    pad = torch.zeros(1, dtype=torch.float64, device="cuda")
+    want = torch.cat((pad, sums))[slots.long() + 1] * (torch.arange(T, device="cuda") % 3 - 1)
+    assert bool(((dgates.double() - want).abs() <= (N + 1) * ONE * torch.cat((pad, size))[slots.long() + 1]).all())
+    # and the rows' gradients: rows that a few tokens at either end name
+    named = {0: 0, 1: 1, (1 << 23) + 7: 2, (1 << 24) - 2: 3, 1 << 24: 4, T - 1: 5}
+    slots.fill_(-1)
+    for t, s in named.items():
+        slots[t] = s
+    gates, drows = torch.full((T,), 2.0, device="cuda"), torch.full((R, N), 9.0, dtype=torch.bfloat16, device="cuda")
+    B.qesgd_combine_backward(dy, N, None, 0, R, slots, gates, T, 1, N, drows, N, None)
+    for t, s in named.items():
+        assert torch.equal(drows[s], 2 * dy[t])
