@@ -69,21 +69,25 @@ enum {
     QESGD_ERR_NULL = -1,       /* a required pointer is NULL                          */
     QESGD_ERR_DIM = -2,        /* d == 0 or d >= 2^40, or the launch would need 2^31
                                   workgroups or more (one per 1024..65536 coordinates
-                                  and worker: e.g. d = 2^38 with K = 64)              */
+                                  and worker: e.g. d = 2^38 with K = 64); a matrix's
+                                  side or a number of rows or tokens out of its range  */
     QESGD_ERR_LEVELS = -3,     /* s not 2,4,8,16,32,64,128,256 or 65536                */
     QESGD_ERR_BUCKET = -4,     /* bucket == 0, or bucket < d and bucket % 32 != 0      */
     QESGD_ERR_WORKERS = -5,    /* K == 0 or K > QESGD_MAX_WORKERS                      */
     QESGD_ERR_NORM_KIND = -6,  /* norm_kind not QESGD_NORM_L2 / QESGD_NORM_MAX         */
     QESGD_ERR_ALIGN = -7,      /* a pointer is not aligned as required                 */
-    QESGD_ERR_STRIDE = -8,     /* a slab stride is too small or not a 16-byte multiple */
-    QESGD_ERR_WORKSPACE = -9,  /* workspace NULL or smaller than qesgd_workspace_bytes */
+    QESGD_ERR_STRIDE = -8,     /* a slab stride is too small or not a 16-byte multiple,
+                                  or rows lie less than a row apart                    */
+    QESGD_ERR_WORKSPACE = -9,  /* workspace NULL or smaller than the call's
+                                  .._workspace_bytes                                   */
     QESGD_ERR_HIP = -10,       /* a launch failed; see qesgd_last_hip_error()          */
     QESGD_ERR_BITS = -11,      /* b not in {2,4,8,16}                                  */
     QESGD_ERR_DELTA = -12,     /* delta not a positive finite number                   */
     QESGD_ERR_ROUNDS = -13,    /* rounds == 0                                          */
     QESGD_ERR_SCRATCH = -14,   /* the shape needs more than QESGD_NOALLOC_SCRATCH_BYTES */
     QESGD_ERR_DTYPE = -15,     /* dtype not QESGD_F32, QESGD_BF16 or QESGD_F16         */
-    QESGD_ERR_MODE = -16,      /* mode not QESGD_MX4_NEAREST or QESGD_MX4_STOCHASTIC   */
+    QESGD_ERR_MODE = -16,      /* mode not QESGD_MX4_NEAREST or QESGD_MX4_STOCHASTIC,
+                                  gate_kind not QESGD_GATE_ALL or QESGD_GATE_CHOSEN    */
     QESGD_ERR_STEPS = -17,     /* steps == 0 or steps > QESGD_MAX_STEPS                */
     QESGD_ERR_COEFF = -18,     /* a coefficient, eps, alpha or mu not finite, eps < 0  */
     QESGD_ERR_EXPERTS = -19    /* E not in [1, QESGD_MAX_EXPERTS], or k not in [1, min(E, QESGD_MAX_CHOICES)] */
@@ -370,7 +374,7 @@ int qesgd_combine(const void* rows, uint32_t dtype, uint64_t ld, uint64_t R, con
 
 /* drows[slots[t*k+j]] = gates[t*k+j] * dy[t] in dtype; dgates[t*k+j] = <dy[t], rows[slots[t*k+j]]> in fp32, 0 for a slot outside 0 .. R-1.
  * rows are fp32 with dtype | QESGD_ROWS_F32.  drows and dgates may each be NULL, but not both; rows that no slot names are left as they are, and a row
- * that several pairs name has pieces of any of theirs.  drows may be rows itself where both are of one type (QESGD_ERR_DTYPE otherwise).  T, R, N and k
+ * that several pairs name has pieces of any of theirs.  drows may be rows itself where both are of one type (QESGD_ERR_DTYPE otherwise) and no row is named twice.  T, R, N and k
  * as in qesgd_combine, however many pieces that is. */
 int qesgd_combine_backward(const void* dy, uint32_t dtype, uint64_t ld_dy, const void* rows, uint64_t ld, uint64_t R, const int32_t* slots,
                            const float* gates, uint64_t T, uint32_t k, uint64_t N, void* drows, uint64_t ld_d, float* dgates, void* stream);

@@ -301,21 +301,21 @@ const char* qesgd_strerror(int code) {
     switch (code) {
         case QESGD_OK: return "ok";
         case QESGD_ERR_NULL: return "a required pointer is NULL";
-        case QESGD_ERR_DIM: return "d must be in [1, 2^40)";
+        case QESGD_ERR_DIM: return "a size is out of its range: d in [1, 2^40), a matrix's sides and numbers of rows and tokens as their call says";
         case QESGD_ERR_LEVELS: return "s must be one of 2, 4, 8, 16, 32, 64, 128, 256, 65536";
         case QESGD_ERR_BUCKET: return "bucket must be > 0 and, when smaller than d, a multiple of 32";
         case QESGD_ERR_WORKERS: return "K must be in [1, 64]";
         case QESGD_ERR_NORM_KIND: return "norm_kind must be 0 (L2) or 1 (max)";
-        case QESGD_ERR_ALIGN: return "pointer alignment: 16 bytes for vectors, 256 for packed blocks";
-        case QESGD_ERR_STRIDE: return "slab stride too small or not a multiple of 16 bytes (packed: 256)";
-        case QESGD_ERR_WORKSPACE: return "workspace missing or smaller than qesgd_workspace_bytes()";
+        case QESGD_ERR_ALIGN: return "pointer alignment: 16 bytes for vectors, 256 for packed blocks, an element for matrices and tokens' rows";
+        case QESGD_ERR_STRIDE: return "slab stride too small or not a multiple of 16 bytes (packed: 256), or rows less than a row apart";
+        case QESGD_ERR_WORKSPACE: return "workspace missing or smaller than the call's .._workspace_bytes()";
         case QESGD_ERR_HIP: return "kernel launch failed (see qesgd_last_hip_error)";
         case QESGD_ERR_BITS: return "b must be one of 2, 4, 8, 16";
         case QESGD_ERR_DELTA: return "delta must be a positive finite number";
         case QESGD_ERR_ROUNDS: return "rounds must be at least 1";
         case QESGD_ERR_SCRATCH: return "shape needs more scratch than the no-allocation entry point holds (4 MiB)";
         case QESGD_ERR_DTYPE: return "dtype must be 0 (f32), 1 (bf16) or 2 (f16)";
-        case QESGD_ERR_MODE: return "mode must be 0 (nearest) or 1 (stochastic)";
+        case QESGD_ERR_MODE: return "mode must be 0 (nearest) or 1 (stochastic), gate_kind 0 (softmax over all) or 1 (over the chosen)";
         case QESGD_ERR_STEPS: return "steps must be in [1, 32]";
         case QESGD_ERR_COEFF: return "coefficients, eps, alpha and mu must be finite, eps not negative";
         case QESGD_ERR_EXPERTS: return "E must be in [1, 1024], k in [1, min(E, 16)]";
