@@ -1,4 +1,4 @@
-// What every launch on the host side needs (not installed).
+// What every launch on the host side needs, and the element types in a kernel (not installed).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -24,6 +24,14 @@ void by_type(uint32_t dtype, F&& f) {
         case QESGD_BF16: f(std::integral_constant<uint32_t, QESGD_BF16>{}); break;
         default: f(std::integral_constant<uint32_t, QESGD_F16>{}); break;
     }
+}
+
+// Element number `at` of type DT becomes v, rounded to it.
+template <uint32_t DT>
+__device__ __forceinline__ void put(void* c, uint64_t at, float v) {
+    if (DT == QESGD_F32) ((float*)c)[at] = v;
+    else if (DT == QESGD_F16) ((_Float16*)c)[at] = (_Float16)v;
+    else ((__bf16*)c)[at] = (__bf16)v;
 }
 
 // f(first, count) for all of `groups` workgroups of `threads`, as many at a time as one launch may number threads for: fewer than 2^32.

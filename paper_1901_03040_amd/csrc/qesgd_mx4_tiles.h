@@ -8,13 +8,6 @@
 
 namespace qesgd {
 
-template <uint32_t DT>
-__device__ __forceinline__ void put(void* c, uint64_t at, float v) {
-    if (DT == QESGD_F32) ((float*)c)[at] = v;
-    else if (DT == QESGD_F16) ((_Float16*)c)[at] = (_Float16)v;
-    else ((__bf16*)c)[at] = (__bf16)v;
-}
-
 // A fragment whose lane holds column `col` and rows row + 8 q + r, r = 0..3.
 template <uint32_t DT>
 __device__ __forceinline__ void store_fragment(void* c, uint64_t ldc, uint32_t M, uint32_t N, uint32_t row, uint32_t col, bool whole, const acc16& acc) {

@@ -52,13 +52,6 @@ constexpr uint32_t kVLoads = 4;           // loads that a wave has on their way 
 // bf16 numbers that hold an element.
 constexpr uint32_t parts_of(uint32_t dtype) { return dtype == QESGD_F32 ? 3 : dtype == QESGD_F16 ? 2 : 1; }
 
-template <uint32_t DT>
-__device__ __forceinline__ void put_row(void* y, uint64_t at, float v) {
-    if (DT == QESGD_F32) ((float*)y)[at] = v;
-    else if (DT == QESGD_F16) ((_Float16*)y)[at] = (_Float16)v;
-    else ((__bf16*)y)[at] = (__bf16)v;
-}
-
 // The upper 16 bits of v: a bf16 number no larger than v, so that nothing overflows.
 __device__ __forceinline__ uint32_t upper(float v) { return __float_as_uint(v) & 0xFFFF0000u; }
 
@@ -77,12 +70,6 @@ __device__ __forceinline__ void split_one(float x, uint32_t (&part)[PARTS]) {
         }
         part[0] = x != x ? 0x7FC00000u : part[0];
     }
-}
-template <uint32_t DT>
-__device__ __forceinline__ float element_at(const void* x, uint64_t at) {
-    if (DT == QESGD_F32) return ((const float*)x)[at];
-    if (DT == QESGD_BF16) return __uint_as_float((uint32_t)((const unsigned short*)x)[at] << 16);
-    return (float)((const _Float16*)x)[at];
 }
 
 // Eight elements as PARTS times eight bf16 numbers.
@@ -270,7 +257,7 @@ __global__ void __launch_bounds__(kVWaves * 64, 4) k_mx4_vector_product(const VP
             }
             if (p.pieces > 1) p.partial[((uint64_t)piece * p.R + r0 + r) * p.N + n] = v;
             else if (DT != QESGD_F32 && p.wide) ((float*)p.y)[(uint64_t)(r0 + r) * p.ldy + n] = v;
-            else put_row<DT>(p.y, (uint64_t)(r0 + r) * p.ldy + n, v);
+            else put<DT>(p.y, (uint64_t)(r0 + r) * p.ldy + n, v);
         }
     }
 }

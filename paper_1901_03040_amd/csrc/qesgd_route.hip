@@ -39,12 +39,6 @@ __device__ __forceinline__ float element(const void* x, uint64_t at) {
     if (DT == QESGD_BF16) return __uint_as_float((uint32_t)((const unsigned short*)x)[at] << 16);
     return (float)((const _Float16*)x)[at];
 }
-template <uint32_t DT>
-__device__ __forceinline__ void put_element(void* x, uint64_t at, float v) {
-    if (DT == QESGD_F32) ((float*)x)[at] = v;
-    else if (DT == QESGD_F16) ((_Float16*)x)[at] = (_Float16)v;
-    else ((__bf16*)x)[at] = (__bf16)v;
-}
 
 // A logit as the choice compares it: a NaN as infinity.
 __device__ __forceinline__ float compared(float v) { return __builtin_fminf(v, INFINITY); }
@@ -448,7 +442,7 @@ __global__ void __launch_bounds__(256) k_route_backward(const BParams p) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const uint32_t e = (uint32_t)c * L + l;
-        if (e < p.E) put_element<DT>(p.dlogits, t * p.ld_d + e, add[c]);
+        if (e < p.E) put<DT>(p.dlogits, t * p.ld_d + e, add[c]);
     }
 }
 
