@@ -2,8 +2,9 @@
 //
 //   out[t] = sum_j gates[t, j] rows[slot(t, j)];  drows[slot(t, j)] = gates[t, j] dy[t];  dgates[t, j] = <dy[t], rows[slot(t, j)]>
 //
-// Sums in fp32, in order of j and, for the products with dy, lane by lane and then over the lanes, always in the same order.  Bound by the bytes: 16384 tokens x
-// 2 rows x 4096 bf16, sum 58 us = 6.9 TB/s, gradients 104 us = 6.4 TB/s; a call of 517 x 3 x 1001 is a launch and three trips to memory, 5 us.
+// Sums in fp32, in order of j and, for the products with dy, lane by lane and then over the lanes, always in the same order.  Rows in fp32 beside results of 16 bits, which are then
+// rounded once, or of the results' type.  Bound by the bytes: 16384 tokens x 2 rows x 4096 bf16, two sets in turn, sum 75 us = 5.4 TB/s (the same rows again 61), gradients 102 us =
+// 6.6 TB/s; with rows of fp32 113 = 5.9 and 158 = 6.0.  A call of 517 x 3 x 1001 is a launch and three trips to memory, 5 us.
 #include "qesgd_experts.h"
 #include "qesgd_launch.h"
 #include "qesgd_mx4_codes.h"

@@ -3,8 +3,8 @@
 // The form along a group's rows is what a contraction over the group needs: group e's columns begin at a multiple of 128 (of 64 bytes of
 // codes, of four scales), so the product walks whole blocks and no block holds rows of two experts.
 //
-// A row goes to k experts and is read k times, from the memory-side cache where x fits it.  16384 tokens x 2 x 4096 bf16 along the rows 47 us (54 beside other work)
-// = 340 MB at 7.2 TB/s; 8192 x 2, both forms, 36 us nearest and 69 stochastic, which is its arithmetic (two Philox calls for 8 elements).
+// A row goes to k experts and is read k times, from the memory-side cache where x fits it.  16384 tokens x 2 x 4096 bf16 along the rows 48 us = 340 MB at 7.1 TB/s, 54 where x is another
+// one each time; 8192 x 2, both forms, 37 (47) us nearest and 70 (72) stochastic, which is its arithmetic (two Philox calls for 8 elements).
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_launch.h"

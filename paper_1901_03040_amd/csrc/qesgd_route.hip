@@ -8,8 +8,8 @@
 // first places, and inside a block a pair finds the earlier ones of its expert by comparing the bits of the experts' numbers across the wave.  Only
 // integers are counted, so the result is the same however the work falls.
 //
-// Measured: one token of 64 experts 3.7 us, 8192 tokens of 64 bf16 7.7 us (choice and places), which is launches and chains of trips to memory; 160001 of 257 f32, six each,
-// 57 (choice: 165 MB, vector instructions, two thirds of them to find the largest six times) + 12.5 + 14 us, gradient 68 us = 4.8 TB/s.
+// Measured, kernels by the trace: one token of 64 experts 3.8 us, 8192 tokens of 64 bf16 3.4 + 5.0 us (choice and places), which is launches and chains of trips to memory; 160001 of
+// 257 f32, six each, softmax over all, 56 (choice: 165 MB, vector instructions, two thirds of them to find the largest six times) + 12.5 + 14 us, in a graph 76 together; gradient 66 us = 5.0 TB/s.
 #include "qesgd_experts.h"
 #include "qesgd_groups.h"
 #include "qesgd_launch.h"
