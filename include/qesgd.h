@@ -361,7 +361,7 @@ int qesgd_route(const void* logits, uint32_t dtype, uint64_t ld, uint64_t T, uin
 /* Gradient of the gates with respect to the logits: s = sum_j gates_j dgates_j;
  *   QESGD_GATE_ALL: dlogits_e = sum_{j: experts_j = e} gates_j dgates_j - p_e s, p the softmax over all;
  *   QESGD_GATE_CHOSEN: dlogits_e = sum_{j: experts_j = e} gates_j (dgates_j - s), 0 elsewhere.
- * 0 for closed experts.  logits, experts and gates as in (and from) qesgd_route; logits may be NULL for QESGD_GATE_CHOSEN.  dlogits [T, E] in
+ * 0 for closed experts; where a token's gates are NaN, so are these at its open experts (QESGD_GATE_CHOSEN: the chosen ones).  logits, experts and gates as in (and from) qesgd_route; logits may be NULL for QESGD_GATE_CHOSEN.  dlogits [T, E] in
  * dtype, rows ld_d apart, may be logits itself where ld_d = ld; choices outside 0 .. E-1 are left out. */
 int qesgd_route_backward(const void* logits, uint32_t dtype, uint64_t ld, uint64_t T, uint32_t E, uint32_t k, uint32_t gate_kind,
                          const int32_t* experts, const float* gates, const float* dgates, void* dlogits, uint64_t ld_d, void* stream);

@@ -429,14 +429,14 @@ __global__ void __launch_bounds__(256) k_route_backward(const BParams p) {
         float sum = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            // closed is 0, also where all are
-            x[c] = x[c] == -INFINITY ? 0.0f : exp_below(x[c] - high);
+            // closed is 0, also where all are, and marked by its sign: an open one may be 0 too, and has a NaN where the token's gates are
+            x[c] = x[c] == -INFINITY ? -0.0f : exp_below(x[c] - high);
             sum += x[c];
         }
         sum = total<L>(sum);
         const float part = s / sum;
 #pragma unroll
-        for (int c = 0; c < C; ++c) add[c] -= x[c] == 0.0f ? 0.0f : x[c] * part;
+        for (int c = 0; c < C; ++c) add[c] -= __float_as_uint(x[c]) == 0x80000000u ? 0.0f : x[c] * part;
     }
     if (i >= p.T) return;
 #pragma unroll
