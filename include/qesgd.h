@@ -361,21 +361,23 @@ int qesgd_route(const void* logits, uint32_t dtype, uint64_t ld, uint64_t T, uin
 /* Gradient of the gates with respect to the logits: s = sum_j gates_j dgates_j;
  *   QESGD_GATE_ALL: dlogits_e = sum_{j: experts_j = e} gates_j dgates_j - p_e s, p the softmax over all;
  *   QESGD_GATE_CHOSEN: dlogits_e = sum_{j: experts_j = e} gates_j (dgates_j - s), 0 elsewhere.
- * 0 for closed experts; where a token's gates are NaN, so are these at its open experts (QESGD_GATE_CHOSEN: the chosen ones).  logits, experts and gates as in (and from) qesgd_route; logits may be NULL for QESGD_GATE_CHOSEN.  dlogits [T, E] in
- * dtype, rows ld_d apart, may be logits itself where ld_d = ld; choices outside 0 .. E-1 are left out. */
+ * 0 for closed experts; where a token's gates are NaN, so are these at its open experts (QESGD_GATE_CHOSEN: the chosen ones).
+ * logits, experts and gates as in (and from) qesgd_route; logits may be NULL for QESGD_GATE_CHOSEN.  dlogits [T, E] in dtype, rows
+ * ld_d apart, may be logits itself where ld_d = ld; choices outside 0 .. E-1 are left out. */
 int qesgd_route_backward(const void* logits, uint32_t dtype, uint64_t ld, uint64_t T, uint32_t E, uint32_t k, uint32_t gate_kind,
                          const int32_t* experts, const float* gates, const float* dgates, void* dlogits, uint64_t ld_d, void* stream);
 
 /* out[t] = sum_j gates[t*k+j] * rows[slots[t*k+j]], added in order of j in fp32, rounded once; slots outside 0 .. R-1 are left out.
- * rows [R, N] and out [T, N] in dtype, rows in fp32 with dtype | QESGD_ROWS_F32.  gates NULL: 1 each (the gradient of tokens that went to k experts).  slots NULL: row t*k+j (then T*k <= R).
+ * rows [R, N] and out [T, N] in dtype, rows in fp32 with dtype | QESGD_ROWS_F32.  gates NULL: 1 each (the gradient of tokens that went to
+ * k experts).  slots NULL: row t*k+j (then T*k <= R).
  * out may not overlap rows.  T, R and N up to 2^28, T * k < 2^31, T * N up to 2^38; calls of 2^32 pieces of 16 bytes of out and more are refused (QESGD_ERR_DIM). */
 int qesgd_combine(const void* rows, uint32_t dtype, uint64_t ld, uint64_t R, const int32_t* slots, const float* gates, uint64_t T, uint32_t k,
                   uint64_t N, void* out, uint64_t ld_out, void* stream);
 
 /* drows[slots[t*k+j]] = gates[t*k+j] * dy[t] in dtype; dgates[t*k+j] = <dy[t], rows[slots[t*k+j]]> in fp32, 0 for a slot outside 0 .. R-1.
  * rows are fp32 with dtype | QESGD_ROWS_F32.  drows and dgates may each be NULL, but not both; rows that no slot names are left as they are, and a row
- * that several pairs name has pieces of any of theirs.  drows may be rows itself where both are of one type (QESGD_ERR_DTYPE otherwise) and no row is named twice.  T, R, N and k
- * as in qesgd_combine, however many pieces that is. */
+ * that several pairs name has pieces of any of theirs.  drows may be rows itself where both are of one type (QESGD_ERR_DTYPE otherwise) and no row
+ * is named twice.  T, R, N and k as in qesgd_combine, however many pieces that is. */
 int qesgd_combine_backward(const void* dy, uint32_t dtype, uint64_t ld_dy, const void* rows, uint64_t ld, uint64_t R, const int32_t* slots,
                            const float* gates, uint64_t T, uint32_t k, uint64_t N, void* drows, uint64_t ld_d, float* dgates, void* stream);
 
